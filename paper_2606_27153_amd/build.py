@@ -1,6 +1,6 @@
-"""Builds libmuon_mi355x.so (the optimizer) and libmuon_diag.so (a matrix-core
-ceiling probe the bench reports as context) for gfx950 with hipcc, in-tree,
-no JIT cache.
+"""Builds libmuon_mi355x.so (the optimizer), libmuon_layers.so (the layer
+operators) and libmuon_diag.so (a matrix-core ceiling probe the bench reports as
+context) for gfx950 with hipcc, in-tree, no JIT cache.
 
 Usage: python -m paper_2606_27153_amd.build [-v]
 """
@@ -25,6 +25,8 @@ ARCH = "gfx950"
 SOURCES = ["api.cpp", "plan.cpp", "ew_kernels.hip", "ns_gemm.hip", "ns_gemm_t256_bf16_bx.hip",
            "ns_gemm_t256_bf16_sq.hip", "ns_gemm_t256_f16_bx.hip", "ns_gemm_t256_f16_sq.hip", "ns_tile_bf16.hip",
            "ns_tile_f16.hip", "ns_tile_f32.hip", "static_ws.hip"]
+LAYER_SOURCES = ["layers/layers_api.cpp", "layers/mm_simple.hip", "layers/act_grad.hip", "layers/layer_norm.hip"]
+LAYER_LIB_PATH = os.path.join(PKG, "libmuon_layers.so")
 DIAG_SOURCES = ["diag/mfma_ceiling.hip"]
 DIAG_LIB_PATH = os.path.join(PKG, "libmuon_diag.so")
 
@@ -70,11 +72,12 @@ def _link(objs, path: str, verbose: bool) -> None:
 
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
-    srcs = SOURCES + DIAG_SOURCES
+    parts = ((SOURCES, LIB_PATH), (LAYER_SOURCES, LAYER_LIB_PATH), (DIAG_SOURCES, DIAG_LIB_PATH))
+    srcs = [s for sources, _ in parts for s in sources]
     with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 4)) as ex:
-        objs = list(ex.map(lambda s: _compile(s, verbose), srcs))
-    _link(objs[:len(SOURCES)], LIB_PATH, verbose)
-    _link(objs[len(SOURCES):], DIAG_LIB_PATH, verbose)
+        objs = dict(zip(srcs, ex.map(lambda s: _compile(s, verbose), srcs)))
+    for sources, path in parts:
+        _link([objs[s] for s in sources], path, verbose)
     return LIB_PATH
 
 

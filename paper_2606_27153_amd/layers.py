@@ -1,0 +1,496 @@
+"""Layer operators around the matrices the Muon step updates: a matrix product
+with a fused epilogue (``linear``), the same grouped by expert
+(``grouped_linear``) and ``layer_norm``, each with its backward pass.
+
+Each operator comes as a function torch's autograd sees (``linear``,
+``grouped_linear``, ``layer_norm``) and as its two passes (``*_forward``,
+``*_backward``), which only enqueue HIP kernels on torch's current stream of the
+tensors' device: no host synchronisation, no copies, nothing cached between
+calls.  Weights are [in, out] like the optimizer's workloads; the transposed
+view of an [out, in] weight is taken as it lies.  Weight gradients come in the
+weight's own memory layout, so that ``Muon`` steps them without a copy.
+
+Tensors are fp32 or bf16 (one dtype per call; layer norm's weight and bias may be
+fp32 next to bf16 activations), sums are fp32.  Rows may be strided (a slice of
+wider rows), their elements may not.  A bad argument raises ValueError or
+TypeError before anything is launched.
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Sequence, Union
+
+import torch
+
+from . import _layers_lib as LL
+from ._lib import MUON_BF16, MUON_F32
+
+_DTYPES = {torch.float32: MUON_F32, torch.bfloat16: MUON_BF16}
+_lib = None
+
+
+def _load():
+    global _lib
+    if _lib is None:
+        _lib = LL.load()
+    return _lib
+
+
+def _dtype_code(t: torch.Tensor) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {t.dtype}; use float32 or bfloat16")
+    return code
+
+
+def _rows(t: torch.Tensor, name: str, like: torch.Tensor, rows: Optional[int], cols: int):
+    """(pointer, leading dimension) of a 2-D tensor whose rows are contiguous."""
+    if t.dim() != 2 or t.size(1) != cols or (rows is not None and t.size(0) != rows):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({'rows' if rows is None else rows}, {cols})")
+    _same(t, name, like)
+    ld, step = t.stride()
+    if step != 1 and cols != 1:
+        raise ValueError(f"{name}'s rows are not contiguous (stride {t.stride()})")
+    if ld < cols:
+        if t.size(0) > 1:
+            raise ValueError(f"{name}'s rows overlap (stride {t.stride()})")
+        ld = cols
+    return t.data_ptr(), ld
+
+
+def _same(t: torch.Tensor, name: str, like: torch.Tensor) -> None:
+    if t.dtype != like.dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {like.dtype}")
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+
+
+def _vector(t: Optional[torch.Tensor], name: str, like: torch.Tensor, n: int):
+    if t is None:
+        return None
+    if t.dim() != 1 or t.size(0) != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous vector of {n} elements")
+    _same(t, name, like)
+    return t.data_ptr()
+
+
+def _weight(w: torch.Tensor, like: torch.Tensor, inner: int):
+    """(pointer, leading dimension, transposed, outer) of a weight [inner, outer]
+    kept by rows, or by columns (the transposed view of an [outer, inner] one)."""
+    if w.dim() != 2 or w.size(0) != inner:
+        raise ValueError(f"weight has shape {tuple(w.shape)}, expected ({inner}, out)")
+    _same(w, "weight", like)
+    outer = w.size(1)
+    ld, step = w.stride()
+    if (step == 1 or outer == 1) and (ld >= outer or inner == 1):
+        return w.data_ptr(), max(ld, outer), 0, outer
+    if (ld == 1 or inner == 1) and (step >= inner or outer == 1):
+        return w.data_ptr(), max(step, inner), 1, outer
+    raise ValueError(f"neither the rows nor the columns of the weight are contiguous (stride {w.stride()})")
+
+
+def _input(x: torch.Tensor, name: str = "x") -> None:
+    if x.dim() != 2:
+        raise ValueError(f"{name} must be 2-D [rows, features], got shape {tuple(x.shape)}")
+    if not x.is_cuda:
+        raise ValueError(f"{name} is not on a GPU")
+    if x.size(1) == 0:
+        raise ValueError(f"{name} has no features")
+
+
+def _activation(name: str) -> int:
+    code = LL.ACTIVATIONS.get(name)
+    if code is None:
+        raise ValueError(f"unknown activation {name!r}; choose from {tuple(LL.ACTIVATIONS)}")
+    return code
+
+
+class _On:
+    """Makes the tensors' device current for a call, if it is not already, and
+    names torch's current stream there."""
+
+    def __init__(self, device):
+        self.index = device.index
+        self.before = None
+
+    def __enter__(self):
+        now = torch.cuda.current_device()
+        if now != self.index:
+            self.before = now
+            torch.cuda.set_device(self.index)
+        return torch._C._cuda_getCurrentRawStream(self.index)
+
+    def __exit__(self, *exc):
+        if self.before is not None:
+            torch.cuda.set_device(self.before)
+        return False
+
+
+def _bytes(fn, *args) -> int:
+    n = ctypes.c_size_t()
+    LL.check(fn(*args, ctypes.byref(n)))
+    return n.value
+
+
+def _workspace(n: int, like: torch.Tensor):
+    """A workspace from torch's allocator: it belongs to the current stream, and
+    goes back to it when the call that enqueued its use returns."""
+    return torch.empty(n, dtype=torch.uint8, device=like.device) if n else None
+
+
+# ------------------------------------------------------------------- linear
+
+def linear_forward(x: torch.Tensor, weight: torch.Tensor, *, bias: Optional[torch.Tensor] = None,
+                   residual: Optional[torch.Tensor] = None, activation: str = "none",
+                   keep_preactivation: bool = False):
+    """``act(x @ weight + bias) + residual`` for x [rows, in], weight [in, out].
+
+    With ``keep_preactivation`` returns ``(y, z)``, z = x @ weight + bias being
+    what ``linear_backward`` reads (None without an activation)."""
+    lib = _load()
+    _input(x)
+    act = _activation(activation)
+    code = _dtype_code(x)
+    rows, inner = x.shape
+    xp, ldx = _rows(x, "x", x, rows, inner)
+    wp, ldw, wt, outer = _weight(weight, x, inner)
+    if outer == 0:
+        raise ValueError("weight has no output features")
+    bp = _vector(bias, "bias", x, outer)
+    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", x, rows, outer)
+    with _On(x.device) as stream:
+        y = torch.empty(rows, outer, dtype=x.dtype, device=x.device)
+        z = torch.empty_like(y) if keep_preactivation and act else None
+        need = _bytes(lib.muon_linear_workspace_bytes, rows, inner, outer, code, act, 0)
+        ws = _workspace(need, x)
+        LL.check(lib.muon_linear_forward(xp, ldx, wp, ldw, wt, bp, rp, ldr, y.data_ptr(), outer,
+                                         None if z is None else z.data_ptr(), outer, rows, inner, outer, code, act,
+                                         None if ws is None else ws.data_ptr(), need, stream))
+    return (y, z) if keep_preactivation else y
+
+
+def _like_weight(weight: torch.Tensor, transposed: int) -> torch.Tensor:
+    """An uninitialised gradient in the weight's own layout, dense."""
+    if transposed:
+        return torch.empty(weight.size(1), weight.size(0), dtype=weight.dtype, device=weight.device).t()
+    return torch.empty(weight.size(0), weight.size(1), dtype=weight.dtype, device=weight.device)
+
+
+def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, *,
+                    preactivation: Optional[torch.Tensor] = None, activation: str = "none", bias_grad: bool = False,
+                    input_grad: bool = True, weight_grad: bool = True):
+    """Gradients ``(dx, dweight, dbias)`` of ``linear_forward`` for the output
+    gradient dy (the residual's gradient is dy); those not asked for are None.
+    dweight is kept like the weight (by rows or by columns)."""
+    lib = _load()
+    _input(x)
+    act = _activation(activation)
+    code = _dtype_code(x)
+    rows, inner = x.shape
+    xp, ldx = _rows(x, "x", x, rows, inner)
+    wp, ldw, wt, outer = _weight(weight, x, inner)
+    if outer == 0:
+        raise ValueError("weight has no output features")
+    gp, ldg = _rows(dy, "dy", x, rows, outer)
+    zp, ldz = None, 0
+    if act:
+        if preactivation is None:
+            raise ValueError(f"the backward pass of {activation!r} needs the forward pass's preactivation")
+        zp, ldz = _rows(preactivation, "preactivation", x, rows, outer)
+    with _On(x.device) as stream:
+        dx = torch.empty(rows, inner, dtype=x.dtype, device=x.device) if input_grad else None
+        dw = _like_weight(weight, wt) if weight_grad else None
+        db = torch.empty(outer, dtype=x.dtype, device=x.device) if bias_grad else None
+        need = _bytes(lib.muon_linear_workspace_bytes, rows, inner, outer, code, act, 1)
+        ws = _workspace(need, x)
+        LL.check(lib.muon_linear_backward(gp, ldg, xp, ldx, wp, ldw, wt, zp, ldz,
+                                          None if dx is None else dx.data_ptr(), inner,
+                                          None if dw is None else dw.data_ptr(), inner if wt else outer,
+                                          None if db is None else db.data_ptr(), rows, inner, outer, code, act,
+                                          None if ws is None else ws.data_ptr(), need, stream))
+    return dx, dw, db
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, activation):
+        need = any(ctx.needs_input_grad[:3])
+        y, z = linear_forward(x, weight, bias=bias, residual=residual, activation=activation,
+                              keep_preactivation=True) if need else \
+            (linear_forward(x, weight, bias=bias, residual=residual, activation=activation), None)
+        ctx.activation = activation
+        ctx.save_for_backward(x, weight, z)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, z = ctx.saved_tensors
+        nx, nw, nb, nr = ctx.needs_input_grad[:4]
+        dx = dw = db = None
+        if nx or nw or nb:
+            dx, dw, db = linear_backward(dy.contiguous(), x, weight, preactivation=z, activation=ctx.activation,
+                                         bias_grad=nb, input_grad=nx, weight_grad=nw)
+        return dx, dw, db, dy if nr else None, None
+
+
+def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, *,
+           activation: str = "none", residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``act(x @ weight + bias) + residual`` over the last dimension of x,
+    differentiable once.  weight is [in, out] (or the transposed view of an
+    [out, in] one); activation is "none", "relu", "gelu", "gelu_tanh" or "silu"."""
+    lead = x.shape[:-1]
+    x2 = x.reshape(-1, x.shape[-1]) if x.dim() != 2 else x
+    r2 = residual
+    if residual is not None and residual.dim() != 2:
+        r2 = residual.reshape(-1, residual.shape[-1])
+    y = _Linear.apply(_dense(x2), weight, bias, None if r2 is None else _dense(r2), activation)
+    return y if x.dim() == 2 else y.view(*lead, y.shape[-1])
+
+
+def _dense(t: torch.Tensor) -> torch.Tensor:
+    """t, copied if its rows are not contiguous or overlap."""
+    if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.size(1):
+        return t
+    return t.contiguous()
+
+
+# ----------------------------------------------------------- grouped linear
+
+Weights = Union[torch.Tensor, Sequence[torch.Tensor]]
+
+
+def _experts(weights: Weights, like: torch.Tensor, inner: int):
+    """(pointers, leading dimension, transposed, outer, count) of the experts'
+    weights: one [experts, in, out] tensor or a sequence of [in, out] ones."""
+    if isinstance(weights, torch.Tensor):
+        if weights.dim() != 3:
+            raise ValueError(f"weights must be [experts, in, out], got shape {tuple(weights.shape)}")
+        n = weights.size(0)
+        if n < 1 or n > LL.MUON_GROUPED_MAX_EXPERTS:
+            raise ValueError(f"{n} experts; 1 to {LL.MUON_GROUPED_MAX_EXPERTS} are supported")
+        p, ld, t, outer = _weight(weights[0], like, inner)
+        step = weights.stride(0) * weights.element_size()
+        return [p + i * step for i in range(n)], ld, t, outer, n
+    n = len(weights)
+    if n < 1 or n > LL.MUON_GROUPED_MAX_EXPERTS:
+        raise ValueError(f"{n} experts; 1 to {LL.MUON_GROUPED_MAX_EXPERTS} are supported")
+    p, ld, t, outer = _weight(weights[0], like, inner)
+    first = weights[0]
+    ptrs = [p]
+    for i in range(1, n):
+        w = weights[i]
+        if w.shape != first.shape or w.stride() != first.stride():
+            raise ValueError(f"weight {i} has shape {tuple(w.shape)} and stride {w.stride()}, the first one "
+                             f"{tuple(first.shape)} and {first.stride()}")
+        _same(w, f"weight {i}", like)
+        ptrs.append(w.data_ptr())
+    return ptrs, ld, t, outer, n
+
+
+def _offsets(offsets: torch.Tensor, n: int, like: torch.Tensor) -> int:
+    if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.size(0) != n + 1 or offsets.stride(0) != 1:
+        raise ValueError(f"offsets must be a contiguous int32 vector of {n + 1} elements")
+    if offsets.device != like.device:
+        raise ValueError(f"offsets is on {offsets.device}, expected {like.device}")
+    return offsets.data_ptr()
+
+
+def grouped_linear_forward(x: torch.Tensor, weights: Weights, offsets: torch.Tensor) -> torch.Tensor:
+    """``y[t] = x[t] @ weights[e]`` for offsets[e] <= t < offsets[e + 1]: rows
+    sorted by expert, int32 offsets on the GPU (the host never reads them).
+    Rows outside every expert's range get 0."""
+    lib = _load()
+    _input(x)
+    code = _dtype_code(x)
+    rows, inner = x.shape
+    xp, ldx = _rows(x, "x", x, rows, inner)
+    ptrs, ldw, wt, outer, n = _experts(weights, x, inner)
+    if outer == 0:
+        raise ValueError("the weights have no output features")
+    op = _offsets(offsets, n, x)
+    with _On(x.device) as stream:
+        y = torch.empty(rows, outer, dtype=x.dtype, device=x.device)
+        need = _bytes(lib.muon_grouped_linear_workspace_bytes, rows, inner, outer, n, code, 0)
+        ws = _workspace(need, x)
+        LL.check(lib.muon_grouped_linear_forward(xp, ldx, (ctypes.c_void_p * n)(*ptrs), ldw, wt, op, n, y.data_ptr(),
+                                                 outer, rows, inner, outer, code,
+                                                 None if ws is None else ws.data_ptr(), need, stream))
+    return y
+
+
+def grouped_linear_backward(dy: torch.Tensor, x: torch.Tensor, weights: Weights, offsets: torch.Tensor, *,
+                            input_grad: bool = True, weight_grad: Union[bool, Sequence[bool]] = True):
+    """Gradients ``(dx, dweights)`` of ``grouped_linear_forward``.  dweights is
+    one [experts, in, out] tensor, or a list of its slices if the weights came
+    as a sequence; an expert without rows gets zeros.  ``weight_grad`` may name
+    per expert whether its gradient is wanted (None in the list if not)."""
+    lib = _load()
+    _input(x)
+    code = _dtype_code(x)
+    rows, inner = x.shape
+    xp, ldx = _rows(x, "x", x, rows, inner)
+    ptrs, ldw, wt, outer, n = _experts(weights, x, inner)
+    if outer == 0:
+        raise ValueError("the weights have no output features")
+    gp, ldg = _rows(dy, "dy", x, rows, outer)
+    op = _offsets(offsets, n, x)
+    want = None
+    if not isinstance(weight_grad, bool):
+        want = [bool(v) for v in weight_grad]
+        if len(want) != n:
+            raise ValueError(f"weight_grad names {len(want)} experts, there are {n}")
+        weight_grad = any(want)
+    with _On(x.device) as stream:
+        dx = torch.empty(rows, inner, dtype=x.dtype, device=x.device) if input_grad else None
+        dw = dptrs = None
+        if weight_grad:
+            a, b = (outer, inner) if wt else (inner, outer)
+            dw = torch.empty(n, a, b, dtype=x.dtype, device=x.device)
+            step = a * b * dw.element_size()
+            base = dw.data_ptr()
+            dptrs = (ctypes.c_void_p * n)(*[base + i * step if want is None or want[i] else None for i in range(n)])
+            if wt:
+                dw = dw.transpose(1, 2)
+        need = _bytes(lib.muon_grouped_linear_workspace_bytes, rows, inner, outer, n, code, 1)
+        ws = _workspace(need, x)
+        LL.check(lib.muon_grouped_linear_backward(gp, ldg, xp, ldx, (ctypes.c_void_p * n)(*ptrs), ldw, wt, op, n,
+                                                  None if dx is None else dx.data_ptr(), inner, dptrs,
+                                                  inner if wt else outer, rows, inner, outer, code,
+                                                  None if ws is None else ws.data_ptr(), need, stream))
+    if dw is not None and (want is not None or not isinstance(weights, torch.Tensor)):
+        dw = [dw[i] if want is None or want[i] else None for i in range(n)]
+    return dx, dw
+
+
+class _GroupedLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, offsets, *weights):
+        ctx.stacked = len(weights) == 1 and weights[0].dim() == 3
+        ctx.save_for_backward(x, offsets, *weights)
+        return grouped_linear_forward(x, weights[0] if ctx.stacked else weights, offsets)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, offsets, *weights = ctx.saved_tensors
+        nx, _, *nw = ctx.needs_input_grad
+        if not (nx or any(nw)):
+            return (None, None) + (None,) * len(weights)
+        dx, dw = grouped_linear_backward(_dense(dy), x, weights[0] if ctx.stacked else weights, offsets,
+                                         input_grad=nx, weight_grad=nw[0] if ctx.stacked else nw)
+        if ctx.stacked:
+            return dx, None, dw
+        return (dx, None, *(dw if dw is not None else (None,) * len(weights)))
+
+
+def grouped_linear(x: torch.Tensor, weights: Weights, offsets: torch.Tensor) -> torch.Tensor:
+    """``y[t] = x[t] @ weights[e]`` for the rows offsets[e] <= t < offsets[e + 1]
+    of x [rows, in], differentiable once.  weights: one [experts, in, out]
+    tensor, or the experts' own [in, out] parameters (which ``Muon`` steps)."""
+    ws = (weights,) if isinstance(weights, torch.Tensor) else tuple(weights)
+    return _GroupedLinear.apply(_dense(x), offsets, *ws)
+
+
+# --------------------------------------------------------------- layer norm
+
+def _norm_vectors(x: torch.Tensor, vectors, cols: int):
+    """Pointers of the weight and bias, and the dtype code they share."""
+    code, ptrs = None, []
+    for name, t in vectors:
+        if t is None:
+            ptrs.append(None)
+            continue
+        if t.dim() != 1 or t.size(0) != cols or (cols > 1 and t.stride(0) != 1):
+            raise ValueError(f"{name} must be a contiguous vector of {cols} elements")
+        if t.device != x.device:
+            raise ValueError(f"{name} is on {t.device}, expected {x.device}")
+        if t.dtype not in (torch.float32, x.dtype):
+            raise ValueError(f"{name} has dtype {t.dtype}, expected float32 or {x.dtype}")
+        c = _DTYPES[t.dtype]
+        if code is not None and c != code:
+            raise ValueError("weight and bias have different dtypes")
+        code = c
+        ptrs.append(t.data_ptr())
+    return (*ptrs, _DTYPES[x.dtype] if code is None else code)
+
+
+def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
+                       eps: float = 1e-5, keep_stats: bool = False):
+    """Layer norm over the columns of x [rows, cols].  With ``keep_stats``
+    returns ``(y, mean, rstd)``, the fp32 statistics its backward pass reads."""
+    lib = _load()
+    _input(x)
+    code = _dtype_code(x)
+    rows, cols = x.shape
+    xp, ldx = _rows(x, "x", x, rows, cols)
+    wp, bp, wcode = _norm_vectors(x, (("weight", weight), ("bias", bias)), cols)
+    with _On(x.device) as stream:
+        y = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
+        mean = rstd = None
+        if keep_stats:
+            mean, rstd = torch.empty(2, rows, dtype=torch.float32, device=x.device).unbind(0)
+        LL.check(lib.muon_layer_norm_forward(xp, ldx, wp, bp, y.data_ptr(), cols,
+                                             None if mean is None else mean.data_ptr(),
+                                             None if rstd is None else rstd.data_ptr(), rows, cols, eps, code, wcode,
+                                             stream))
+    return (y, mean, rstd) if keep_stats else y
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor,
+                        rstd: torch.Tensor, *, input_grad: bool = True, weight_grad: bool = True,
+                        bias_grad: bool = True):
+    """Gradients ``(dx, dweight, dbias)`` of ``layer_norm_forward``; those not
+    asked for are None.  dweight and dbias have the weight's dtype (x's without
+    a weight)."""
+    lib = _load()
+    _input(x)
+    code = _dtype_code(x)
+    rows, cols = x.shape
+    xp, ldx = _rows(x, "x", x, rows, cols)
+    gp, ldg = _rows(dy, "dy", x, rows, cols)
+    wp, _, wcode = _norm_vectors(x, (("weight", weight), ("bias", None)), cols)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t.dtype != torch.float32 or t.dim() != 1 or t.size(0) != rows or (rows > 1 and t.stride(0) != 1):
+            raise ValueError(f"{name} must be a contiguous float32 vector of {rows} elements")
+        if t.device != x.device:
+            raise ValueError(f"{name} is on {t.device}, expected {x.device}")
+    with _On(x.device) as stream:
+        dx = torch.empty(rows, cols, dtype=x.dtype, device=x.device) if input_grad else None
+        wdt = torch.float32 if wcode == MUON_F32 else x.dtype
+        dw = torch.empty(cols, dtype=wdt, device=x.device) if weight_grad else None
+        db = torch.empty(cols, dtype=wdt, device=x.device) if bias_grad else None
+        need = _bytes(lib.muon_layer_norm_workspace_bytes, rows, cols) if weight_grad or bias_grad else 0
+        ws = _workspace(need, x)
+        LL.check(lib.muon_layer_norm_backward(gp, ldg, xp, ldx, wp, mean.data_ptr(), rstd.data_ptr(),
+                                              None if dx is None else dx.data_ptr(), cols,
+                                              None if dw is None else dw.data_ptr(),
+                                              None if db is None else db.data_ptr(), rows, cols, code, wcode,
+                                              None if ws is None else ws.data_ptr(), need, stream))
+    return dx, dw, db
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, mean, rstd = layer_norm_forward(x, weight, bias, eps=eps, keep_stats=True)
+        ctx.bias_dtype = None if bias is None else bias.dtype
+        ctx.save_for_backward(x, weight, mean, rstd)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, mean, rstd = ctx.saved_tensors
+        nx, nw, nb = ctx.needs_input_grad[:3]
+        dx, dw, db = layer_norm_backward(_dense(dy), x, weight, mean, rstd, input_grad=nx, weight_grad=nw,
+                                         bias_grad=nb)
+        return dx, dw, db if db is None else db.to(ctx.bias_dtype), None
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
+               eps: float = 1e-5) -> torch.Tensor:
+    """Layer norm over the last dimension of x, differentiable once."""
+    x2 = x.reshape(-1, x.shape[-1]) if x.dim() != 2 else x
+    y = _LayerNorm.apply(_dense(x2), weight, bias, float(eps))
+    return y if x.dim() == 2 else y.view(x.shape)
