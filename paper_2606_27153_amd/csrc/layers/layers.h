@@ -82,6 +82,12 @@ struct ActGradArgs {
 // Launchers: enqueue and return hipGetLastError's answer.
 hipError_t launch_simple(bool bf16, int form, int group, const Product& p, const Table* t, hipStream_t st);
 
+// Matrix-core kernels on tiles of 256 x 256 (bf16) and 128 x 128; the operands
+// must suit them (tile_fits).
+hipError_t launch_tile256_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st);
+hipError_t launch_tile128_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st);
+hipError_t launch_tile128_f32(int form, int group, const Product& p, const Table* t, hipStream_t st);
+
 hipError_t launch_act_grad(bool bf16, const ActGradArgs& a, hipStream_t st);
 int act_grad_chunks(int64_t rows, int64_t N);   // rows of `part`
 

@@ -78,9 +78,33 @@ muon_status check_workspace(const void* ws, size_t have, size_t need) {
     if (try_st != MUON_OK) return try_st;      \
   } while (0)
 
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// Whether the tile kernels can fetch the operands: 16-byte chunks that lie on
+// 16-byte addresses and do not straddle the end of a row, and 32-bit byte
+// offsets within a tile of 256 rows.
+bool tile_fits(bool bf16, int form, int group, const Product& p, const Table* t) {
+  const int64_t epc = bf16 ? 8 : 4, es = bf16 ? 2 : 4;
+  const bool atr = form == FORM_TT, btr = form != FORM_RR;
+  if (p.lda % epc || p.ldb % epc) return false;
+  if (p.lda * es * 256 >= (int64_t(1) << 31) || p.ldb * es * 256 >= (int64_t(1) << 31)) return false;
+  if ((atr ? p.M : p.K) % epc || (btr ? p.N : p.K) % epc) return false;
+  if (!aligned16(p.a)) return false;
+  if (group == GROUP_ROWS) {
+    for (int32_t e = 0; e < p.experts; ++e)
+      if (!aligned16(t->p[e])) return false;
+    return true;
+  }
+  return aligned16(p.b);
+}
+
 // One matrix product: the kernel that suits it.
-hipError_t product(bool bf16, int form, int group, const Product& p, const Table* t, hipStream_t st) {
-  return launch_simple(bf16, form, group, p, t, st);
+hipError_t product(bool bf16, int form, int group, Product p, const Table* t, hipStream_t st) {
+  p.splits = 1;
+  if (!tile_fits(bf16, form, group, p, t)) return launch_simple(bf16, form, group, p, t, st);
+  if (!bf16) return launch_tile128_f32(form, group, p, t, st);
+  const int64_t big = ((p.M + 255) / 256) * ((p.N + 255) / 256) * int64_t(group == GROUP_SUM ? p.experts : 1);
+  return big >= 256 ? launch_tile256_bf16(form, group, p, t, st) : launch_tile128_bf16(form, group, p, t, st);
 }
 
 // Workspace of muon_linear_backward: dz and the partial column sums.
