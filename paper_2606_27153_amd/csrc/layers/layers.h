@@ -24,6 +24,8 @@ enum Form {
   FORM_TT = 2   // A tr, B tr:   x^T dz (or dz^T x, when W is transposed)
 };
 
+constexpr int kCUs = 256;   // of an MI355X
+
 enum Group {
   GROUP_NONE = 0,
   GROUP_ROWS = 1,  // row ranges of A and C belong to experts; B is the expert's
@@ -82,11 +84,19 @@ struct ActGradArgs {
 // Launchers: enqueue and return hipGetLastError's answer.
 hipError_t launch_simple(bool bf16, int form, int group, const Product& p, const Table* t, hipStream_t st);
 
-// Matrix-core kernels on tiles of 256 x 256 (bf16) and 128 x 128; the operands
-// must suit them (tile_fits).
+// Matrix-core kernels on tiles of 256 x 256 (bf16 only), 128 x 128 and 64 x 64;
+// the operands must suit them (tile_fits in layers_api.cpp).
 hipError_t launch_tile256_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st);
 hipError_t launch_tile128_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st);
 hipError_t launch_tile128_f32(int form, int group, const Product& p, const Table* t, hipStream_t st);
+hipError_t launch_tile64_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st);
+hipError_t launch_tile64_f32(int form, int group, const Product& p, const Table* t, hipStream_t st);
+
+// Few rows: tiles of 16 mt rows (mt 1, 2 or 4), forms RT and RR, any alignment,
+// at least 16 bytes of columns.
+hipError_t launch_skinny(bool bf16, int form, int group, int mt, const Product& p, const Table* t, hipStream_t st);
+// Adds p.splits partial results and applies the epilogue.
+hipError_t launch_reduce(bool bf16, const Product& p, hipStream_t st);
 
 hipError_t launch_act_grad(bool bf16, const ActGradArgs& a, hipStream_t st);
 int act_grad_chunks(int64_t rows, int64_t N);   // rows of `part`

@@ -98,24 +98,135 @@ bool tile_fits(bool bf16, int form, int group, const Product& p, const Table* t)
   return aligned16(p.b);
 }
 
-// One matrix product: the kernel that suits it.
-hipError_t product(bool bf16, int form, int group, Product p, const Table* t, hipStream_t st) {
-  p.splits = 1;
-  if (!tile_fits(bf16, form, group, p, t)) return launch_simple(bf16, form, group, p, t, st);
-  if (!bf16) return launch_tile128_f32(form, group, p, t, st);
-  const int64_t big = ((p.M + 255) / 256) * ((p.N + 255) / 256) * int64_t(group == GROUP_SUM ? p.experts : 1);
-  return big >= 256 ? launch_tile256_bf16(form, group, p, t, st) : launch_tile128_bf16(form, group, p, t, st);
+// Which kernel runs a product, and into how many ranges it cuts the summed
+// dimension (plain products only: each range leaves an fp32 partial result).
+struct Choice {
+  enum Kernel { SIMPLE, SKINNY, TILE64, TILE128, TILE256 } kernel = SIMPLE;
+  int mt = 0;       // SKINNY: 16-row tiles per block
+  int splits = 1;
+};
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Expected time of a tile kernel in us, from the measured time of a slab (64 K
+// in bf16, 32 in fp32) and of everything else of a tile (first loads, epilogue),
+// with the chip full and with a CU holding a single block.  Measured (bf16, us a
+// slab, full / alone): 256: 1.4 / 1.15, 128: 1.0 / 0.53 for the two blocks of a
+// CU, 64: 0.42 / 0.29; the rest 6, 4.5 and 3 us.  fp32's MFMAs are what a slab
+// takes: 1.8 us of the 128 tile, 0.45 of the 64 tile, twice that for two blocks.
+double tile_us(bool bf16, int tile, double blocks, double slabs) {
+  const double full = bf16 ? (tile == 256 ? 1.4 : tile == 128 ? 1.0 : 0.42) : tile == 128 ? 3.6 : 0.9;
+  const double alone = bf16 ? (tile == 256 ? 1.15 : tile == 128 ? 0.53 : 0.29) : tile == 128 ? 1.8 : 0.45;
+  const double rest = tile == 256 ? 6 : tile == 128 ? 4.5 : 3;
+  const double slots = tile == 256 ? kCUs : 2 * kCUs;
+  if (blocks <= kCUs) return slabs * alone + rest;
+  if (tile == 256) {
+    const double rounds = std::floor(blocks / slots), left = blocks - rounds * slots;
+    return rounds * (slabs * full + rest) + (left > 0 ? slabs * alone + rest : 0);
+  }
+  if (blocks <= slots) return slabs * (alone + (full - alone) * (blocks / kCUs - 1)) + rest;
+  return blocks / slots * (slabs * full + rest);
 }
 
-// Workspace of muon_linear_backward: dz and the partial column sums.
+// Partial results are written and read once in fp32 (4 bytes a pass at about
+// 4 TB/s); the kernel that adds them costs a launch.
+double reduce_us(int64_t M, int64_t N, int splits) {
+  return splits > 1 ? 3.0 + double(splits) * M * N * 8 / 4e6 : 0.0;
+}
+
+Choice choose(bool bf16, int form, int group, int64_t M, int64_t N, int64_t K, int64_t experts, bool fits) {
+  Choice c;
+  const int64_t epc = bf16 ? 8 : 4;
+  // Few rows: the weight's bytes are all that counts, which the skinny kernel
+  // streams without LDS.  From 65 rows on (17 per expert) the tile kernels win.
+  const double per_expert = group == GROUP_ROWS ? double(M) / experts : double(M);
+  if (form != FORM_TT && N >= epc && per_expert <= (group == GROUP_ROWS ? 16 : 64)) {
+    c.kernel = Choice::SKINNY;
+    c.mt = group == GROUP_ROWS || M <= 16 ? 1 : M <= 32 ? 2 : 4;
+    if (group == GROUP_NONE) {
+      // 512 blocks (two per CU) keep enough loads in flight; at least 4 K steps per wave
+      const int64_t blocks = ceil_div(N, 16 * epc), steps = ceil_div(K, 4 * epc);
+      int64_t s = 512 / blocks;
+      s = s < steps / 16 ? s : steps / 16;
+      c.splits = int(s < 1 ? 1 : s);
+    }
+    return c;
+  }
+  if (!fits) return c;
+  const int64_t bk = bf16 ? 64 : 32;
+  double best = 0;
+  for (int tile : {256, 128, 64}) {
+    if (tile == 256 && !bf16) continue;
+    const int64_t nt = ceil_div(N, tile);
+    double blocks = double(ceil_div(M, tile) * nt), slabs = double(ceil_div(K, bk));
+    if (group == GROUP_ROWS) blocks = (double(M) / tile + 0.5 * (experts < M ? experts : M)) * nt;
+    if (group == GROUP_SUM) {
+      blocks *= experts;
+      slabs = double(K) / experts / bk + 0.5;
+    }
+    for (int s = 1; s <= 16; ++s) {
+      if (s > 1 && (group != GROUP_NONE || slabs < 4 * s)) break;
+      const double us = tile_us(bf16, tile, blocks * s, std::ceil(slabs / s)) + reduce_us(M, N, s);
+      if (best == 0 || us < best) {
+        best = us;
+        c.kernel = tile == 256 ? Choice::TILE256 : tile == 128 ? Choice::TILE128 : Choice::TILE64;
+        c.splits = s;
+      }
+    }
+  }
+  return c;
+}
+
+size_t part_bytes(const Choice& c, int64_t M, int64_t N) {
+  return c.splits > 1 ? padded(size_t(c.splits) * size_t(M) * size_t(N) * 4) : 0;
+}
+
+// One matrix product: the kernel that suits it.  part: part_bytes of the choice
+// that takes the operands to be aligned (no other needs more).
+hipError_t product(bool bf16, int form, int group, Product p, const Table* t, void* part, hipStream_t st) {
+  const Choice c =
+      choose(bf16, form, group, p.M, p.N, p.K, p.experts, tile_fits(bf16, form, group, p, t));
+  p.splits = c.splits;
+  p.part = static_cast<float*>(part);
+  hipError_t e = hipSuccess;
+  switch (c.kernel) {
+    case Choice::SIMPLE: e = launch_simple(bf16, form, group, p, t, st); break;
+    case Choice::SKINNY: e = launch_skinny(bf16, form, group, c.mt, p, t, st); break;
+    case Choice::TILE64: e = bf16 ? launch_tile64_bf16(form, group, p, t, st) : launch_tile64_f32(form, group, p, t, st); break;
+    case Choice::TILE128:
+      e = bf16 ? launch_tile128_bf16(form, group, p, t, st) : launch_tile128_f32(form, group, p, t, st);
+      break;
+    case Choice::TILE256: e = launch_tile256_bf16(form, group, p, t, st); break;
+  }
+  return e == hipSuccess && c.splits > 1 ? launch_reduce(bf16, p, st) : e;
+}
+size_t product_bytes(bool bf16, int form, int64_t M, int64_t N, int64_t K) {
+  if (M == 0 || K == 0) return 0;
+  return part_bytes(choose(bf16, form, GROUP_NONE, M, N, K, 0, true), M, N);
+}
+
+// Workspace of muon_linear_backward: dz, the partial column sums and the
+// partial results of the two products (one after the other, in one place).  The
+// weight may come either way round.
 struct BackwardLayout {
-  size_t dz = 0, part = 0, total = 0;
+  size_t dz = 0, sums = 0, part = 0, total = 0;
 };
-BackwardLayout backward_layout(int64_t rows, int64_t outer, int32_t dtype, int32_t act) {
+BackwardLayout backward_layout(int64_t rows, int64_t inner, int64_t outer, int32_t dtype, int32_t act) {
+  const bool bf16 = dtype == MUON_BF16;
   BackwardLayout l;
-  if (act != MUON_ACT_NONE) l.part = padded(size_t(rows) * size_t(outer) * size_of(dtype));
-  l.total = l.part + padded(size_t(act_grad_chunks(rows, outer)) * size_t(outer) * 4);
+  if (act != MUON_ACT_NONE) l.sums = padded(size_t(rows) * size_t(outer) * size_of(dtype));
+  l.part = l.sums + padded(size_t(act_grad_chunks(rows, outer)) * size_t(outer) * 4);
+  size_t most = 0;
+  const size_t all[] = {product_bytes(bf16, FORM_RR, rows, inner, outer), product_bytes(bf16, FORM_RT, rows, inner, outer),
+                   product_bytes(bf16, FORM_TT, inner, outer, rows), product_bytes(bf16, FORM_TT, outer, inner, rows)};
+  for (size_t b : all) most = b > most ? b : most;
+  l.total = l.part + most;
   return l;
+}
+size_t forward_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype) {
+  const size_t a = product_bytes(dtype == MUON_BF16, FORM_RT, rows, outer, inner);
+  const size_t b = product_bytes(dtype == MUON_BF16, FORM_RR, rows, outer, inner);
+  return a > b ? a : b;
 }
 
 muon_status fill_table(const char* name, const void* const* p, int32_t n, bool may_be_null, size_t esize, Table& t) {
@@ -149,7 +260,8 @@ MUON_API muon_status muon_linear_workspace_bytes(int64_t rows, int64_t inner, in
   if (!bytes) return fail(MUON_ERR_INVALID_ARG, "bytes is NULL");
   TRY(check_sizes(rows, inner, outer, dtype));
   TRY(check_activation(activation));
-  *bytes = backward ? backward_layout(rows, outer, dtype, activation).total : 0;
+  *bytes = backward ? backward_layout(rows, inner, outer, dtype, activation).total
+                    : forward_bytes(rows, inner, outer, dtype);
   return done(hipSuccess, "");
 }
 
@@ -168,9 +280,7 @@ MUON_API muon_status muon_linear_forward(const void* x, int64_t ldx, const void*
   if (residual) TRY(check_matrix("residual", residual, ldr, outer, es));
   if (preact) TRY(check_matrix("preact", preact, ldz, outer, es));
   TRY(check_vector("bias", bias, es));
-  size_t need = 0;
-  TRY(muon_linear_workspace_bytes(rows, inner, outer, dtype, activation, 0, &need));
-  TRY(check_workspace(workspace, workspace_bytes, need));
+  TRY(check_workspace(workspace, workspace_bytes, forward_bytes(rows, inner, outer, dtype)));
   Product p{};
   p.a = x; p.lda = ldx;
   p.b = w; p.ldb = ldw;
@@ -181,7 +291,7 @@ MUON_API muon_status muon_linear_forward(const void* x, int64_t ldx, const void*
   p.M = int32_t(rows); p.N = int32_t(outer); p.K = int32_t(inner);
   p.act = activation;
   return done(product(dtype == MUON_BF16, w_transposed ? FORM_RR : FORM_RT, GROUP_NONE, p, nullptr,
-                      hipStream_t(hip_stream)),
+                      workspace, hipStream_t(hip_stream)),
               "linear forward");
 }
 
@@ -203,7 +313,7 @@ MUON_API muon_status muon_linear_backward(const void* dy, int64_t lddy, const vo
   }
   if (dw) TRY(check_matrix("dw", dw, lddw, w_transposed ? inner : outer, es));
   TRY(check_vector("dbias", dbias, es));
-  const BackwardLayout l = backward_layout(rows, outer, dtype, activation);
+  const BackwardLayout l = backward_layout(rows, inner, outer, dtype, activation);
   TRY(check_workspace(workspace, workspace_bytes, l.total));
   const hipStream_t st = hipStream_t(hip_stream);
   char* ws = static_cast<char*>(workspace);
@@ -215,7 +325,7 @@ MUON_API muon_status muon_linear_backward(const void* dy, int64_t lddy, const vo
     a.z = act ? preact : nullptr; a.ldz = ldz;
     a.dz = act ? ws + l.dz : nullptr; a.lddz = outer;
     a.dbias = dbias;
-    a.part = reinterpret_cast<float*>(ws + l.part);
+    a.part = reinterpret_cast<float*>(ws + l.sums);
     a.rows = int32_t(rows); a.N = int32_t(outer); a.act = activation;
     TRY(done(launch_act_grad(bf16, a, st), "activation gradient"));
     if (act) {
@@ -229,7 +339,7 @@ MUON_API muon_status muon_linear_backward(const void* dy, int64_t lddy, const vo
     p.b = w; p.ldb = ldw;
     p.c = dx; p.ldc = lddx;
     p.M = int32_t(rows); p.N = int32_t(inner); p.K = int32_t(outer);
-    TRY(done(product(bf16, w_transposed ? FORM_RT : FORM_RR, GROUP_NONE, p, nullptr, st), "linear input gradient"));
+    TRY(done(product(bf16, w_transposed ? FORM_RT : FORM_RR, GROUP_NONE, p, nullptr, ws + l.part, st), "linear input gradient"));
   }
   if (dw) {
     Product p{};
@@ -239,7 +349,7 @@ MUON_API muon_status muon_linear_backward(const void* dy, int64_t lddy, const vo
     p.a = w_transposed ? dz : x; p.lda = w_transposed ? lddz : ldx;
     p.b = w_transposed ? x : dz; p.ldb = w_transposed ? ldx : lddz;
     p.M = int32_t(w_transposed ? outer : inner); p.N = int32_t(w_transposed ? inner : outer);
-    TRY(done(product(bf16, FORM_TT, GROUP_NONE, p, nullptr, st), "linear weight gradient"));
+    TRY(done(product(bf16, FORM_TT, GROUP_NONE, p, nullptr, ws + l.part, st), "linear weight gradient"));
   }
   return done(hipSuccess, "");
 }
@@ -279,7 +389,7 @@ MUON_API muon_status muon_grouped_linear_forward(const void* x, int64_t ldx, con
   p.experts = experts;
   p.M = int32_t(rows); p.N = int32_t(outer); p.K = int32_t(inner);
   return done(product(dtype == MUON_BF16, w_transposed ? FORM_RR : FORM_RT, GROUP_ROWS, p, &t,
-                      hipStream_t(hip_stream)),
+                      nullptr, hipStream_t(hip_stream)),
               "grouped linear forward");
 }
 
@@ -319,7 +429,7 @@ MUON_API muon_status muon_grouped_linear_backward(const void* dy, int64_t lddy, 
     p.ldb = ldw;
     p.c = dx; p.ldc = lddx;
     p.M = int32_t(rows); p.N = int32_t(inner); p.K = int32_t(outer);
-    TRY(done(product(bf16, w_transposed ? FORM_RT : FORM_RR, GROUP_ROWS, p, &tw, st), "grouped input gradient"));
+    TRY(done(product(bf16, w_transposed ? FORM_RT : FORM_RR, GROUP_ROWS, p, &tw, nullptr, st), "grouped input gradient"));
   }
   if (dw) {
     p.c = nullptr; p.ldc = lddw;
@@ -327,7 +437,7 @@ MUON_API muon_status muon_grouped_linear_backward(const void* dy, int64_t lddy, 
     p.a = w_transposed ? dy : x; p.lda = w_transposed ? lddy : ldx;
     p.b = w_transposed ? x : dy; p.ldb = w_transposed ? ldx : lddy;
     p.M = int32_t(w_transposed ? outer : inner); p.N = int32_t(w_transposed ? inner : outer);
-    TRY(done(product(bf16, FORM_TT, GROUP_SUM, p, &td, st), "grouped weight gradients"));
+    TRY(done(product(bf16, FORM_TT, GROUP_SUM, p, &td, nullptr, st), "grouped weight gradients"));
   }
   return done(hipSuccess, "");
 }

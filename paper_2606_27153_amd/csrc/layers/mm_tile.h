@@ -1,20 +1,24 @@
-// Matrix products on the matrix cores, one block of four waves per TM x TN
-// tile of C.
+// Matrix products on the matrix cores, one block of four waves per T x T tile
+// of C.
 //
-// K advances in slabs of 128 bytes of a K-contiguous row (64 bf16, 32 fp32),
-// which go straight from global memory into two LDS stages (16 bytes per lane
-// and instruction).  A "row" operand's slab holds its rows, 128 bytes each; a
-// "tr" operand's slab holds BK rows of TM (TN) elements as they lie in memory,
-// and the fragment reads transpose: ds_read_b64_tr_b16 for bf16, single words
-// for fp32.  16-byte chunks (32-byte segments) are XOR-swizzled with the row so
-// that the fragment reads are free of bank conflicts.
+// K advances in slabs of 128 bytes of a K-contiguous row (64 bf16, 32 fp32).  An
+// operand's slab is a unit of the LDS ring, filled straight from global memory
+// (16 bytes per lane and instruction).  A "row" operand's unit holds its rows,
+// 128 bytes each; a "tr" operand's holds BK rows of T elements as they lie in
+// memory, and the fragment reads transpose: ds_read_b64_tr_b16 for bf16, single
+// words for fp32.  16-byte chunks (32-byte segments) are XOR-swizzled with the
+// row so that the fragment reads are free of bank conflicts.
 //
-// Each wave owns a (TM / 2) x (TN / 2) piece of 32 x 32 MFMA blocks.  A slab is
+// Each wave owns a (T / 2) x (T / 2) piece of 32 x 32 MFMA blocks.  A slab is
 // four K steps; the fragments of the next step are read while the current
-// step's MFMAs run, one memory instruction per MFMA or so.  The last step of a
-// slab starts with the slab's only barrier (every wave has read the slab, the
-// next one has landed) and also issues the loads of the slab after next into
-// the stage just read, which leaves them a whole slab's time to arrive.
+// step's MFMAs run, one memory instruction per MFMA or so.  The ring has U
+// units, A's and B's slabs in turn; before the last step of a slab comes the
+// slab's only barrier (every wave has read the slab, the next one has landed),
+// which frees two units.  The loads of the first go out during that step, those
+// of the second over the next two: the path from the caches to LDS moves 64
+// bytes a cycle, half of which the 256 tile needs, so a burst of all of them
+// would hold up the MFMAs behind it.  5 units of the 256 tile (two blocks of
+// the 128 tile) fill the 160 KB.
 //
 // The MFMAs take B as their first operand, so a lane holds 4 consecutive
 // columns of a row of C; exchanging halves of the wave between two such groups
@@ -34,15 +38,15 @@ namespace muon {
 namespace layers {
 namespace {
 
-template <typename E, int TM_, int TN_>
+template <typename E, int T_, int U_>
 struct Tile {
-  static constexpr int TM = TM_, TN = TN_;
+  static constexpr int T = T_;                      // C's tile is T x T
+  static constexpr int U = U_;                      // units of the LDS ring
   static constexpr int EPC = 16 / int(sizeof(E));   // elements of a 16-byte chunk
   static constexpr int BK = 8 * EPC;                // K elements of a slab
-  static constexpr int WTM = TM / 2, WTN = TN / 2;  // wave piece
-  static constexpr int NBM = WTM / 32, NBN = WTN / 32;
-  static constexpr int ABYTES = TM * 128, BBYTES = TN * 128;
-  static constexpr int STAGE = ABYTES + BBYTES;
+  static constexpr int WT = T / 2;                  // wave piece: WT x WT
+  static constexpr int NB = WT / 32;
+  static constexpr int UNIT = T * 128;              // bytes of one operand's slab
 };
 
 __device__ const float4 kZeros[4] = {};
@@ -69,12 +73,14 @@ struct Loader {
   int64_t step;          // bytes from slab to slab
   uint32_t off[TR ? 1 : N];  // this lane's offsets; a tr operand's differ by `stride` from load to load
   uint32_t stride;
+  int left;              // K elements from the slab's first one on
   int k;                 // this lane's K element (row operand) or K row (tr operand) in its first chunk
 
   // op: the tile's corner (row or column 0, the first K); ld in elements;
   // valid: rows or columns of the tile that exist (>= 1).
-  __device__ __forceinline__ void init(const E* op, int64_t ld, int valid, int wid, int lane) {
+  __device__ __forceinline__ void init(const E* op, int64_t ld, int valid, int K, int wid, int lane) {
     base = reinterpret_cast<const char*>(op);
+    left = K;
     if constexpr (TR) {
       const int row = wid * RPC + lane / LPR, slot = lane % LPR;
       int chunk = slot;
@@ -94,14 +100,17 @@ struct Loader {
       stride = 0;
     }
   }
-  // Load i of the slab that starts kleft elements before the end of K (kleft
-  // <= 0: past it; the slab is never read, the loads only keep the count).
-  __device__ __forceinline__ void load(int i, uint32_t lds, int wid, int kleft) const {
-    const bool in = k + (TR ? 4 * RPC * i : 0) < kleft;
+  // Load i of the slab (past the end of K: zeros, which nothing reads; they
+  // only keep the count of loads).
+  __device__ __forceinline__ void load(int i, uint32_t lds, int wid) const {
+    const bool in = k + (TR ? 4 * RPC * i : 0) < left;
     const char* from = base + (TR ? off[0] + i * stride : off[i]);
     dma16_to(in ? from : reinterpret_cast<const char*>(kZeros), lds + (wid + 4 * i) * 1024);
   }
-  __device__ __forceinline__ void next() { base += step; }
+  __device__ __forceinline__ void next() {
+    base += step;
+    left -= BK;
+  }
 };
 
 // One operand's fragment reads.  NB 32-row blocks from row (column) w0 of the slab.
@@ -111,7 +120,9 @@ struct Reader {
   static constexpr bool F32 = sizeof(E) == 4;
   static constexpr int READS = !TR ? NB : F32 ? 4 * NB : 2 * NB;   // LDS instructions per K step
   typedef typename Frag<E>::T F;
-  int at[TR ? (F32 ? 1 : 2 * NB) : 4];
+  static constexpr int ADDRS = TR ? (F32 ? 1 : 2 * NB) : 4;
+  int at[ADDRS];    // within a unit
+  int cur[ADDRS];   // in the current one
 
   __device__ __forceinline__ void init(int w0, int lane) {
     if constexpr (!TR) {
@@ -131,21 +142,18 @@ struct Reader {
         }
     }
   }
-  // The other stage's addresses (the stages differ in one address bit).
-  template <int STAGE>
-  __device__ __forceinline__ void flip() {
+  __device__ __forceinline__ void unit(int offset) {
 #pragma unroll
-    for (int i = 0; i < int(sizeof(at) / sizeof(at[0])); ++i) at[i] ^= STAGE;
+    for (int i = 0; i < ADDRS; ++i) cur[i] = at[i] + offset;
   }
   // LDS instruction r (0 .. READS - 1) of K step s.
-  // (st: the slab's place in LDS; at[] holds the stage.)
   __device__ __forceinline__ void read(const char* st, int s, int r, F (&f)[NB]) const {
     if constexpr (!TR) {
-      f[r] = *reinterpret_cast<const F*>(st + at[s] + r * 4096);
+      f[r] = *reinterpret_cast<const F*>(st + cur[s] + r * 4096);
     } else if constexpr (F32) {
-      f[r / 4][r % 4] = *reinterpret_cast<const float*>(st + at[0] + (8 * s + r % 4) * ROWB + (r / 4) * 128);
+      f[r / 4][r % 4] = *reinterpret_cast<const float*>(st + cur[0] + (8 * s + r % 4) * ROWB + (r / 4) * 128);
     } else {
-      const i16x4 v = lds_tr16(st + at[r] + s * 16 * ROWB);
+      const i16x4 v = lds_tr16(st + cur[r] + s * 16 * ROWB);
       i16x8 x = __builtin_bit_cast(i16x8, f[r / 2]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[4 * (r & 1) + e] = v[e];
@@ -154,42 +162,20 @@ struct Reader {
   }
 };
 
+template <bool FIRST, class A, class B>
+__device__ __forceinline__ auto& pick(A& a, B& b) {
+  if constexpr (FIRST)
+    return a;
+  else
+    return b;
+}
+
 template <typename E>
 __device__ __forceinline__ f32x16 mfma(const typename Frag<E>::T& a, const typename Frag<E>::T& b, f32x16 c, int q) {
   if constexpr (sizeof(E) == 2)
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_32x32x2f32(a[q], b[q], c, 0, 0, 0);
-}
-
-// 8 (or the first n < 8) consecutive elements at any alignment.
-template <typename E>
-struct __attribute__((packed, aligned(sizeof(E)))) Packed8 {
-  E v[8];
-};
-template <typename E>
-__device__ __forceinline__ void load8(const E* p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    const Packed8<E> x = *reinterpret_cast<const Packed8<E>*>(p);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = float(x.v[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n ? float(p[e]) : 0.f;
-  }
-}
-template <typename E>
-__device__ __forceinline__ void store8(E* p, int n, const float (&v)[8]) {
-  if (n >= 8) {
-    Packed8<E> x;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x.v[e] = E(v[e]);
-    *reinterpret_cast<Packed8<E>*>(p) = x;
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < n) p[e] = E(v[e]);
-  }
 }
 
 // Where a block works: its tile's corner and extent in C, its operands, its K range.
@@ -216,29 +202,19 @@ __device__ __forceinline__ int xcd_runs(int pid, int run) {
   return (round * 8 + (r & 7)) * run + (r >> 3);
 }
 
-// A plain product takes no table.
-struct NoTable {};
-template <int GROUP>
-struct TableOf {
-  typedef Table T;
-};
-template <>
-struct TableOf<GROUP_NONE> {
-  typedef NoTable T;
-};
-
-template <typename E, int TM, int TN, int FORM, int GROUP>
-__device__ __forceinline__ bool locate(const Product& p, const typename TableOf<GROUP>::T& tab, int run, int lane, Work<E>& w) {
-  const int nt = (p.N + TN - 1) / TN, mt = (p.M + TM - 1) / TM;
+template <typename E, int T, int U, int FORM, int GROUP>
+__device__ __forceinline__ bool locate(const Product& p, const typename TableOf<GROUP>::T& tab, int pid, int run, int lane,
+                                       Work<E>& w) {
+  const int nt = (p.N + T - 1) / T, mt = (p.M + T - 1) / T;
   const E* a = static_cast<const E*>(p.a);
   const E* b = static_cast<const E*>(p.b);
   w.c = static_cast<E*>(p.c);
   int k0 = 0, k1 = p.K;
   int ni;
   if constexpr (GROUP == GROUP_ROWS) {
-    const int id = xcd_runs(blockIdx.x, run);
+    const int id = xcd_runs(pid, run);
     RowTile t;
-    if (!find_row_tile<TM>(p.offsets, p.experts, p.M, id / nt, lane, t)) return false;
+    if (!find_row_tile<T>(p.offsets, p.experts, p.M, id / nt, lane, t)) return false;
     ni = id % nt;
     w.m0 = t.row0;
     w.rows = t.rows;
@@ -247,7 +223,7 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
   } else {
     int id, mi;
     if constexpr (GROUP == GROUP_SUM) {
-      id = xcd_runs(blockIdx.x, run);
+      id = xcd_runs(pid, run);
       const int e = id / (mt * nt);
       if (e >= p.experts) return false;
       id -= e * (mt * nt);
@@ -255,9 +231,9 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
       if (!w.c) return false;
       expert_range(p.offsets, e, p.K, lane, k0, k1);
     } else {
-      id = xcd_order(blockIdx.x, mt * nt);
-      const int slabs = (p.K + Tile<E, TM, TN>::BK - 1) / Tile<E, TM, TN>::BK;
-      const int per = (slabs + p.splits - 1) / p.splits * Tile<E, TM, TN>::BK;
+      id = xcd_order(pid, mt * nt);
+      const int slabs = (p.K + Tile<E, T, U>::BK - 1) / Tile<E, T, U>::BK;
+      const int per = (slabs + p.splits - 1) / p.splits * Tile<E, T, U>::BK;
       k0 = min(p.K, int(blockIdx.y) * per);
       k1 = min(p.K, k0 + per);
     }
@@ -265,178 +241,229 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
     const int band = id / (8 * nt), in = id - band * 8 * nt, h = min(8, mt - band * 8);
     ni = in / h;
     mi = band * 8 + in - ni * h;
-    w.m0 = int64_t(mi) * TM;
-    w.rows = min(TM, p.M - int(w.m0));
+    w.m0 = int64_t(mi) * T;
+    w.rows = min(T, p.M - int(w.m0));
   }
-  w.n0 = int64_t(ni) * TN;
-  w.cols = min(TN, p.N - int(w.n0));
+  w.n0 = int64_t(ni) * T;
+  w.cols = min(T, p.N - int(w.n0));
   w.K = k1 - k0;
   w.a = FORM == FORM_TT ? a + k0 * p.lda + w.m0 : a + w.m0 * p.lda + k0;
   w.b = FORM == FORM_RR ? b + w.n0 * p.ldb + k0 : b + k0 * p.ldb + w.n0;
   return true;
 }
 
-template <typename E, int TM, int TN, int FORM, int GROUP>
-__global__ __launch_bounds__(256, TM* TN >= 256 * 256 ? 1 : 2) void mm_tile_kernel(
-    Product p, typename TableOf<GROUP>::T tab, int run) {
-  using C = Tile<E, TM, TN>;
+template <typename E, int T, int U, int FORM, int GROUP>
+__global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
+    Product p, typename TableOf<GROUP>::T tab, int run, int blocks) {
+  using C = Tile<E, T, U>;
   constexpr bool ATR = FORM == FORM_TT, BTR = FORM != FORM_RR;
-  __shared__ __attribute__((aligned(2 * C::STAGE))) char lds[2 * C::STAGE];
+  __shared__ __attribute__((aligned(1024))) char lds[U * C::UNIT];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // The block's tiles: blockIdx.x and every gridDim.x-th after it that exists.
+  auto find = [&](int& pid, Work<E>& at) {
+    for (; pid < blocks; pid += gridDim.x)
+      if (locate<E, T, U, FORM, GROUP>(p, tab, pid, run, lane, at)) return true;
+    return false;
+  };
   Work<E> w;
-  if (!locate<E, TM, TN, FORM, GROUP>(p, tab, run, lane, w)) return;
-  const int wm = (wid >> 1) * C::WTM, wn = (wid & 1) * C::WTN;
+  int pid = blockIdx.x;
+  if (!find(pid, w)) return;
+  const int wm = (wid >> 1) * C::WT, wn = (wid & 1) * C::WT;
 
-  using LA = Loader<E, TM, ATR>;
-  using LB = Loader<E, TN, BTR>;
-  using RA = Reader<E, TM, C::NBM, ATR>;
-  using RB = Reader<E, TN, C::NBN, BTR>;
+  using LA = Loader<E, T, ATR>;
+  using LB = Loader<E, T, BTR>;
+  using RA = Reader<E, T, C::NB, ATR>;
+  using RB = Reader<E, T, C::NB, BTR>;
   typedef typename Frag<E>::T F;
   LA la;
   LB lb;
   RA ra;
   RB rb;
-  la.init(w.a, p.lda, w.rows, wid, lane);
-  lb.init(w.b, p.ldb, w.cols, wid, lane);
   ra.init(wm, lane);
   rb.init(wn, lane);
+  const uint32_t base = lds_addr(lds);
+  // The first U units of a tile's slabs.
+  auto fill = [&]() {
+    la.init(w.a, p.lda, w.rows, w.K, wid, lane);
+    lb.init(w.b, p.ldb, w.cols, w.K, wid, lane);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int i = 0; i < LA::N; ++i) {
+        if (u & 1)
+          lb.load(i, base + u * C::UNIT, wid);
+        else
+          la.load(i, base + u * C::UNIT, wid);
+      }
+      if (u & 1)
+        lb.next();
+      else
+        la.next();
+    }
+  };
+  fill();
 
-  f32x16 acc[C::NBM][C::NBN];
+  for (;;) {
+  f32x16 acc[C::NB][C::NB];
 #pragma unroll
-  for (int i = 0; i < C::NBM; ++i)
+  for (int i = 0; i < C::NB; ++i)
 #pragma unroll
-    for (int j = 0; j < C::NBN; ++j)
+    for (int j = 0; j < C::NB; ++j)
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+  // the next tile is looked up while this one's first loads arrive
+  Work<E> next;
+  pid += gridDim.x;
+  const bool more = find(pid, next);
 
   const int nk = (w.K + C::BK - 1) / C::BK;
-  int kleft = w.K;   // K elements from the next slab to load on
-  constexpr int LOADS = LA::N + LB::N;
-  // load number i of the next slab (A's, then B's)
-  auto load_one = [&](int i, uint32_t to) {
-    if (i < LA::N)
-      la.load(i, to, wid, kleft);
-    else
-      lb.load(i - LA::N, to + C::ABYTES, wid, kleft);
-  };
-  auto loaded = [&]() {
-    la.next();
-    lb.next();
-    kleft -= C::BK;
-  };
-
-  F fa[2][C::NBM], fb[2][C::NBN];
+  constexpr int LOADS = LA::N;                            // of a unit
+  F fa[2][C::NB], fb[2][C::NB];
   constexpr int READS = RA::READS + RB::READS;
   constexpr int Q = sizeof(E) == 2 ? 1 : 4;               // MFMAs per block and K step
-  constexpr int MFMAS = C::NBM * C::NBN * Q;
+  constexpr int MFMAS = C::NB * C::NB * Q;
   auto read_one = [&](int s, int r, int buf) {
     if (r < RB::READS)
-      rb.read(lds + C::ABYTES, s, r, fb[buf]);
+      rb.read(lds, s, r, fb[buf]);
     else
       ra.read(lds, s, r - RB::READS, fa[buf]);
   };
-  // MFMAs of a K step (fragments buf) with the reads of step rs and, with
-  // LOAD, the loads of a slab spread over them.  No branch surrounds an MFMA:
-  // the accumulators would be copied where the paths meet.
-  auto k_step = [&](auto load_tag, int rs, int buf, uint32_t to) {
-    constexpr bool LOAD = decltype(load_tag)::value;
+  // MFMAs of a K step (fragments buf) with the reads of step rs spread over the
+  // first SPAN of them and the loads l0 .. l1 - 1 of a unit of operand L over
+  // all; `mid` runs after MID of them.  No branch surrounds an MFMA: the
+  // accumulators would be copied where the paths meet.
+  constexpr int SPAN = MFMAS >= 4 ? MFMAS * 3 / 4 : MFMAS, MID = SPAN;
+  auto k_step = [&](const auto& L, int l0, int l1, int rs, int buf, uint32_t to, int span, auto mid) {
 #pragma unroll
     for (int t = 0; t < MFMAS; ++t) {
 #pragma unroll
       for (int r = 0; r < READS; ++r)
-        if (r * MFMAS / READS == t) read_one(rs, r, buf ^ 1);
-      if constexpr (LOAD) {
+        if (r * span / READS == t) read_one(rs, r, buf ^ 1);
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-          if (i * MFMAS / LOADS == t) load_one(i, to);
-      }
-      const int q = t / (C::NBM * C::NBN), ij = t % (C::NBM * C::NBN), i = ij / C::NBN, j = ij % C::NBN;
+      for (int i = l0; i < l1; ++i)
+        if ((i - l0) * MFMAS / (l1 - l0) == t) L.load(i, to, wid);
+      const int q = t / (C::NB * C::NB), ij = t % (C::NB * C::NB), i = ij / C::NB, j = ij % C::NB;
       acc[i][j] = mfma<E>(fb[buf][j], fa[buf][i], acc[i][j], q);
       __builtin_amdgcn_sched_barrier(0);
+      if (t + 1 == MID) mid();
     }
   };
+  auto nothing = []() {};
 
   if (nk > 0) {
-    uint32_t to = lds_addr(lds);
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) load_one(i, to);
-    loaded();
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) load_one(i, to + C::STAGE);
-    loaded();
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"(LOADS) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"((U - 2) * LOADS) : "memory");
     __builtin_amdgcn_sched_barrier(0);
+    int ua = 0, ub = C::UNIT;   // the current slab's units
+    uint32_t free1 = 0;         // the unit whose loads go out in steps 0 and 1
+    ra.unit(ua);
+    rb.unit(ub);
 #pragma unroll
     for (int r = 0; r < READS; ++r) read_one(0, r, 0);
-    for (int kt = 0; kt < nk; ++kt) {
-      k_step(BoolTag<false>{}, 1, 0, 0);
-      k_step(BoolTag<false>{}, 2, 1, 0);
-      k_step(BoolTag<false>{}, 3, 0, 0);
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    // The loads that step 3 starts go first, and are A's where U is even.
+    auto& first = pick<(U & 1) == 0>(la, lb);
+    auto& second = pick<(U & 1) != 0>(la, lb);
+    constexpr int L1 = LOADS / 2;
+    auto wrap = [](int v) { return v >= U * C::UNIT ? v - U * C::UNIT : v; };
+    // Step 2 reads the slab's last fragments early and meets the other waves
+    // before its own last MFMAs: this slab is read, the next one has landed;
+    // U - 4 units may be in flight.
+    constexpr int EARLY = MFMAS >= 4 ? MFMAS / 2 : MFMAS;
+    auto publish = [&]() {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"((U - 4) * LOADS) : "memory");
       __builtin_amdgcn_sched_barrier(0);
-      ra.template flip<C::STAGE>();
-      rb.template flip<C::STAGE>();
-      k_step(BoolTag<true>{}, 0, 1, to);
-      loaded();
-      to ^= C::STAGE;
+    };
+    auto last_step = [&]() {
+      const uint32_t free0 = base + ua;
+      free1 = base + ub;
+      ua = wrap(ua + 2 * C::UNIT);
+      ub = wrap(ub + 2 * C::UNIT);
+      ra.unit(ua);
+      rb.unit(ub);
+      k_step(first, 0, LOADS, 0, 1, free0, SPAN, nothing);
+      first.next();
+    };
+    // The first slab's steps load nothing: every unit of the ring is taken.
+    k_step(la, 0, 0, 1, 0, 0, SPAN, nothing);
+    k_step(la, 0, 0, 2, 1, 0, SPAN, nothing);
+    k_step(la, 0, 0, 3, 0, 0, EARLY, publish);
+    last_step();
+    for (int kt = 1; kt < nk; ++kt) {
+      k_step(second, 0, L1, 1, 0, free1, SPAN, nothing);
+      k_step(second, L1, LOADS, 2, 1, free1, SPAN, nothing);
+      second.next();
+      k_step(second, 0, 0, 3, 0, 0, EARLY, publish);
+      last_step();
     }
-    // the last slabs' loads (past K) and reads end before the block does
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  }
+  // The last slabs' loads (past K) and every wave's reads end here, and the ring
+  // takes the next tile's first slabs while this one is stored.
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  const Work<E> o = w;
+  if (more) {
+    w = next;
+    fill();
   }
 
   // ---------------------------------------------------------------- epilogue
   // Element q of block (i, j): row 32 i + lane % 32, column 32 j + 8 (q / 4) +
   // 4 (lane / 32) + q % 4.
   const int h = lane >> 5;
-  const E* bias = static_cast<const E*>(p.bias);
-  const E* res = static_cast<const E*>(p.res);
-  E* z = static_cast<E*>(p.z);
-  with_act(p.act, [&](auto act_tag) {
+  // (only the layers' own products have anything to add)
+  constexpr bool EPI = GROUP == GROUP_NONE && FORM != FORM_TT;
+  const E* bias = EPI ? static_cast<const E*>(p.bias) : nullptr;
+  const E* res = EPI ? static_cast<const E*>(p.res) : nullptr;
+  E* z = EPI ? static_cast<E*>(p.z) : nullptr;
+  with_act<EPI>(p.act, [&](auto act_tag) {
     constexpr int ACT = decltype(act_tag)::value;
+    static_for<2 * C::NB>([&](auto jg) {
+      constexpr int j = decltype(jg)::value / 2, g = decltype(jg)::value % 2 * 2;
+      const int col = wn + 32 * j + 8 * g + 8 * h;
+      const int n = o.cols - col;
+      float bv[8] = {};
+      if (bias && n > 0) load8(bias + o.n0 + col, n, bv);
+      static_for<C::NB>([&](auto it) {
+        constexpr int i = decltype(it)::value;
+        const int row = wm + 32 * i + (lane & 31);
+        float v[8];
 #pragma unroll
-    for (int j = 0; j < C::NBN; ++j)
-#pragma unroll
-      for (int g = 0; g < 4; g += 2) {
-        const int col = wn + 32 * j + 8 * g + 8 * h;
-        const int n = w.cols - col;
-        float bv[8] = {};
-        if (bias && n > 0) load8(bias + w.n0 + col, n, bv);
-#pragma unroll
-        for (int i = 0; i < C::NBM; ++i) {
-          const int row = wm + 32 * i + (lane & 31);
-          float v[8];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            // the upper half of group g against the lower half of group g + 1
-            // (values of their own: a bit cast of a vector's element takes element 0)
-            const float lo = acc[i][j][4 * g + e], hi = acc[i][j][4 * g + 4 + e];
-            const auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, lo),
-                                                            __builtin_bit_cast(uint32_t, hi), false, false);
-            const uint32_t s0 = s[0], s1 = s[1];
-            v[e] = __builtin_bit_cast(float, s0);
-            v[4 + e] = __builtin_bit_cast(float, s1);
-          }
-          if (row >= w.rows || n <= 0) continue;
-          const int64_t m = w.m0 + row, c = w.n0 + col;
+        for (int e = 0; e < 4; ++e) {
+          // the upper half of group g against the lower half of group g + 1
+          // (values of their own: a bit cast of a vector's element takes element
+          // 0; and in place: the exchanges of all activations' code are the
+          // same, and done ahead of the choice they would not fit the registers)
+          float lo = acc[i][j][4 * g + e], hi = acc[i][j][4 * g + 4 + e];
+          asm volatile("" : "+v"(lo), "+v"(hi));
+          const auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, lo),
+                                                          __builtin_bit_cast(uint32_t, hi), false, false);
+          const uint32_t s0 = s[0], s1 = s[1];
+          v[e] = __builtin_bit_cast(float, s0);
+          v[4 + e] = __builtin_bit_cast(float, s1);
+        }
+        if (row < o.rows && n > 0) {
+          const int64_t m = o.m0 + row, c = o.n0 + col;
           if (p.splits > 1) {
             store8(p.part + (int64_t(blockIdx.y) * p.M + m) * p.N + c, n, v);
-            continue;
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += bv[e];
+            if (z) store8(z + m * p.ldz + c, n, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = act_one<ACT>(v[e]);
+            if (res) {
+              float rv[8];
+              load8(res + m * p.ldr + c, n, rv);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] += rv[e];
+            }
+            store8(o.c + m * p.ldc + c, n, v);
           }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] += bv[e];
-          if (z) store8(z + m * p.ldz + c, n, v);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = act_one<ACT>(v[e]);
-          if (res) {
-            float rv[8];
-            load8(res + m * p.ldr + c, n, rv);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += rv[e];
-          }
-          store8(w.c + m * p.ldc + c, n, v);
         }
-      }
+        __builtin_amdgcn_sched_barrier(0);   // (loads gathered further ahead would not fit the registers)
+      });
+    });
   });
+  if (!more) break;
+  }
 }
 
 // Tiles in a row that one XCD takes of a grouped product (xcd_runs).
@@ -445,12 +472,12 @@ int run_length(int64_t mt, int64_t nt) {
   return int(GROUP == GROUP_ROWS ? 2 * nt : mt * nt);
 }
 
-template <typename E, int TM, int TN, int FORM, int GROUP>
+template <typename E, int T, int U, int FORM, int GROUP>
 hipError_t launch_one(const Product& p, const Table* t, hipStream_t st) {
-  const int64_t nt = (int64_t(p.N) + TN - 1) / TN, mt = (int64_t(p.M) + TM - 1) / TM;
+  const int64_t nt = (int64_t(p.N) + T - 1) / T, mt = (int64_t(p.M) + T - 1) / T;
   int64_t blocks = nt * mt;
   int run = 1;
-  if constexpr (GROUP == GROUP_ROWS) blocks = nt * row_tiles_bound(p.M, p.experts, TM);
+  if constexpr (GROUP == GROUP_ROWS) blocks = nt * row_tiles_bound(p.M, p.experts, T);
   if constexpr (GROUP == GROUP_SUM) blocks *= p.experts;
   if constexpr (GROUP != GROUP_NONE) {
     const int64_t want = run_length<GROUP>(mt, nt), most = (blocks + 7) / 8;
@@ -460,24 +487,29 @@ hipError_t launch_one(const Product& p, const Table* t, hipStream_t st) {
   }
   if (blocks >= (int64_t(1) << 24)) return hipErrorInvalidConfiguration;
   if (!blocks) return hipSuccess;
-  const dim3 g{unsigned(blocks), unsigned(p.splits)}, b{256};
+  // A block of the 256 tile has its CU to itself: no more of them than CUs, each
+  // with several tiles, so that a tile's first loads hide behind the stores of
+  // the one before.  The smaller tiles' blocks share a CU and hide each other's.
+  int64_t grid = blocks;
+  if (T == 256 && grid > kCUs / p.splits) grid = kCUs / p.splits;
+  const dim3 g{unsigned(grid), unsigned(p.splits)}, b{256};
   if constexpr (GROUP == GROUP_NONE)
-    hipLaunchKernelGGL((mm_tile_kernel<E, TM, TN, FORM, GROUP>), g, b, 0, st, p, NoTable{}, run);
+    hipLaunchKernelGGL((mm_tile_kernel<E, T, U, FORM, GROUP>), g, b, 0, st, p, NoTable{}, run, int(blocks));
   else
-    hipLaunchKernelGGL((mm_tile_kernel<E, TM, TN, FORM, GROUP>), g, b, 0, st, p, *t, run);
+    hipLaunchKernelGGL((mm_tile_kernel<E, T, U, FORM, GROUP>), g, b, 0, st, p, *t, run, int(blocks));
   return hipGetLastError();
 }
 
 // The forms and groupings the layers use.
-template <typename E, int TM, int TN>
+template <typename E, int T, int U>
 hipError_t launch_form(int form, int group, const Product& p, const Table* t, hipStream_t st) {
-  if (group == GROUP_SUM) return launch_one<E, TM, TN, FORM_TT, GROUP_SUM>(p, t, st);
+  if (group == GROUP_SUM) return launch_one<E, T, U, FORM_TT, GROUP_SUM>(p, t, st);
   if (group == GROUP_ROWS)
-    return form == FORM_RT ? launch_one<E, TM, TN, FORM_RT, GROUP_ROWS>(p, t, st)
-                           : launch_one<E, TM, TN, FORM_RR, GROUP_ROWS>(p, t, st);
-  if (form == FORM_RT) return launch_one<E, TM, TN, FORM_RT, GROUP_NONE>(p, t, st);
-  if (form == FORM_RR) return launch_one<E, TM, TN, FORM_RR, GROUP_NONE>(p, t, st);
-  return launch_one<E, TM, TN, FORM_TT, GROUP_NONE>(p, t, st);
+    return form == FORM_RT ? launch_one<E, T, U, FORM_RT, GROUP_ROWS>(p, t, st)
+                           : launch_one<E, T, U, FORM_RR, GROUP_ROWS>(p, t, st);
+  if (form == FORM_RT) return launch_one<E, T, U, FORM_RT, GROUP_NONE>(p, t, st);
+  if (form == FORM_RR) return launch_one<E, T, U, FORM_RR, GROUP_NONE>(p, t, st);
+  return launch_one<E, T, U, FORM_TT, GROUP_NONE>(p, t, st);
 }
 
 }  // namespace
