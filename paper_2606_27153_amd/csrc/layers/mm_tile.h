@@ -20,10 +20,8 @@
 // would hold up the MFMAs behind it.  5 units of the 256 tile (two blocks of
 // the 128 tile) fill the 160 KB.
 //
-// The MFMAs take B as their first operand, so a lane holds 4 consecutive
-// columns of a row of C; exchanging halves of the wave between two such groups
-// gives it 8, and the epilogue (bias, activation, residual) and its stores
-// work on 16 bytes of bf16 without passing through LDS.
+// The MFMAs take B as their first operand, so a lane holds 4 consecutive columns
+// of a row of C, and the epilogue needs no LDS (store_tile).
 //
 // Rows and columns past the edge of C read the last valid ones again; their
 // sums are never stored.  Where K ends inside a slab, the chunks past it come
@@ -121,8 +119,7 @@ struct Reader {
   static constexpr int READS = !TR ? NB : F32 ? 4 * NB : 2 * NB;   // LDS instructions per K step
   typedef typename Frag<E>::T F;
   static constexpr int ADDRS = TR ? (F32 ? 1 : 2 * NB) : 4;
-  int at[ADDRS];    // within a unit
-  int cur[ADDRS];   // in the current one
+  int at[ADDRS];   // in the current unit
 
   __device__ __forceinline__ void init(int w0, int lane) {
     if constexpr (!TR) {
@@ -142,18 +139,19 @@ struct Reader {
         }
     }
   }
-  __device__ __forceinline__ void unit(int offset) {
+  // On to the unit `bytes` further in the ring.
+  __device__ __forceinline__ void move(int bytes) {
 #pragma unroll
-    for (int i = 0; i < ADDRS; ++i) cur[i] = at[i] + offset;
+    for (int i = 0; i < ADDRS; ++i) at[i] += bytes;
   }
   // LDS instruction r (0 .. READS - 1) of K step s.
   __device__ __forceinline__ void read(const char* st, int s, int r, F (&f)[NB]) const {
     if constexpr (!TR) {
-      f[r] = *reinterpret_cast<const F*>(st + cur[s] + r * 4096);
+      f[r] = *reinterpret_cast<const F*>(st + at[s] + r * 4096);
     } else if constexpr (F32) {
-      f[r / 4][r % 4] = *reinterpret_cast<const float*>(st + cur[0] + (8 * s + r % 4) * ROWB + (r / 4) * 128);
+      f[r / 4][r % 4] = *reinterpret_cast<const float*>(st + at[0] + (8 * s + r % 4) * ROWB + (r / 4) * 128);
     } else {
-      const i16x4 v = lds_tr16(st + cur[r] + s * 16 * ROWB);
+      const i16x4 v = lds_tr16(st + at[r] + s * 16 * ROWB);
       i16x8 x = __builtin_bit_cast(i16x8, f[r / 2]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[4 * (r & 1) + e] = v[e];
@@ -252,6 +250,179 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
   return true;
 }
 
+// The epilogue of a wave's piece.  Element q of block (i, j) is row 32 i +
+// lane % 32, column 32 j + 8 (q / 4) + 4 (lane / 32) + q % 4: four consecutive
+// columns per lane and group of q, which bias, activation and residual work on.
+// The results are rounded and exchanged between the wave's halves, so that a
+// lane stores 8 consecutive columns.  A lane's vector instructions are what this
+// costs -- with one wave per SIMD nothing else runs meanwhile -- so rows and
+// columns past the edge are masked per store, an address is a uniform pointer
+// plus one 32-bit lane offset, and only products that have an epilogue (EPI) get
+// its code.
+template <typename O>
+__device__ __forceinline__ void exchange(const float (&v)[2][4], O (&out)[8]) {
+  if constexpr (sizeof(O) == 2) {
+    uint32_t u[2][2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        bf16x2 x;
+        x[0] = __bf16(v[s][2 * k]);
+        x[1] = __bf16(v[s][2 * k + 1]);
+        u[s][k] = __builtin_bit_cast(uint32_t, x);
+      }
+    uint32_t r[4];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      // the upper half of the first group against the lower half of the second
+      const auto x = __builtin_amdgcn_permlane32_swap(u[0][k], u[1][k], false, false);
+      r[k] = x[0];
+      r[2 + k] = x[1];
+    }
+    __builtin_memcpy(out, r, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const auto x = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v[0][e]),
+                                                      __builtin_bit_cast(uint32_t, v[1][e]), false, false);
+      const uint32_t x0 = x[0], x1 = x[1];
+      out[e] = __builtin_bit_cast(float, x0);
+      out[4 + e] = __builtin_bit_cast(float, x1);
+    }
+  }
+}
+template <typename O>
+__device__ __forceinline__ void put8(O* base, uint32_t off, const O (&v)[8]) {
+  Packed8<O> x;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x.v[e] = v[e];
+  *reinterpret_cast<Packed8<O>*>(reinterpret_cast<char*>(base) + off) = x;
+}
+template <typename E>
+struct __attribute__((packed, aligned(sizeof(E)))) Packed4 {
+  E v[4];
+};
+
+// OUT: the type stored (E, or float for partial results, which get no epilogue).
+template <class C, typename E, typename OUT, int ACT, bool EPI>
+__device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ldc, const Work<E>& o,
+                                            const f32x16 (&acc)[C::NB][C::NB], int wm, int wn, int lane) {
+  const int h = lane >> 5, r = lane & 31;
+  const E* bias = EPI ? static_cast<const E*>(p.bias) : nullptr;
+  const E* res = EPI ? static_cast<const E*>(p.res) : nullptr;
+  E* z = EPI ? static_cast<E*>(p.z) : nullptr;
+  const int64_t m = o.m0 + wm, n = o.n0 + wn;
+  const uint32_t at = uint32_t(r) * uint32_t(ldc) * uint32_t(sizeof(OUT)) + 8 * h * uint32_t(sizeof(OUT));
+  const uint32_t zat = uint32_t(r) * uint32_t(p.ldz) * uint32_t(sizeof(E)) + 8 * h * uint32_t(sizeof(E));
+  const uint32_t rat = uint32_t(r) * uint32_t(p.ldr) * uint32_t(sizeof(E)) + 4 * h * uint32_t(sizeof(E));
+  static_for<2 * C::NB>([&](auto jg) {
+    constexpr int j = decltype(jg)::value / 2, g = decltype(jg)::value % 2 * 2, col = 32 * j + 8 * g;
+    const bool cols = wn + col + 8 * h < o.cols;      // (whole groups of 8: the columns' number is a multiple)
+    float bv[2][4] = {};
+    if (bias) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int at4 = min(wn + col + 8 * s + 4 * h, o.cols - 4);
+        const Packed4<E> x = *reinterpret_cast<const Packed4<E>*>(bias + o.n0 + at4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bv[s][e] = float(x.v[e]);
+      }
+    }
+    static_for<C::NB>([&](auto it) {
+      constexpr int i = decltype(it)::value;
+      const bool in = cols && wm + 32 * i + r < o.rows;
+      float v[2][4];
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[s][e] = acc[i][j][4 * (g + s) + e];
+          // (in place: what the activations' code has in common, done ahead of
+          // the choice of one, would not fit the registers)
+          asm volatile("" : "+v"(v[s][e]));
+          if (EPI) v[s][e] += bv[s][e];
+        }
+      OUT out[8];
+      if constexpr (EPI) {
+        if (z) {
+          E zo[8];
+          exchange(v, zo);
+          if (in) put8(z + (m + 32 * i) * p.ldz + n + col, zat, zo);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[s][e] = act_one<ACT>(v[s][e]);
+        if (res) {
+          const char* rp = reinterpret_cast<const char*>(res + (m + 32 * i) * p.ldr + n + col);
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+            if (wm + 32 * i + r < o.rows && wn + col + 8 * s < o.cols) {
+              const Packed4<E> x = *reinterpret_cast<const Packed4<E>*>(rp + rat + 8 * s * sizeof(E));
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[s][e] += float(x.v[e]);
+            }
+        }
+      }
+      exchange(v, out);
+      if (in) put8(c + (m + 32 * i) * ldc + n + col, at, out);
+      __builtin_amdgcn_sched_barrier(0);   // (loads gathered further ahead would not fit the registers)
+    });
+  });
+}
+
+// Any number of columns, any leading dimension: element by element.
+template <class C, typename E, bool EPI>
+__device__ __forceinline__ void store_elements(const Product& p, const Work<E>& o, const f32x16 (&acc)[C::NB][C::NB],
+                                               int wm, int wn, int lane) {
+  static_for<C::NB>([&](auto jt) {
+    static_for<C::NB>([&](auto it) {
+      constexpr int i = decltype(it)::value, j = decltype(jt)::value;
+      const int row = wm + 32 * i + (lane & 31);
+      // (a loop over a copy in registers of its own would be one over memory)
+      static_for<16>([&](auto qt) {
+        constexpr int q = decltype(qt)::value;
+        const int col = wn + 32 * j + 8 * (q / 4) + 4 * (lane >> 5) + q % 4;
+        float v = acc[i][j][q];
+        asm volatile("" : "+v"(v));
+        if (row < o.rows && col < o.cols) {
+          const int64_t m = o.m0 + row, n = o.n0 + col;
+          if (p.splits > 1) {
+            p.part[(int64_t(blockIdx.y) * p.M + m) * p.N + n] = v;
+          } else {
+            if constexpr (EPI) {
+              if (p.bias) v += float(static_cast<const E*>(p.bias)[n]);
+              if (p.z) static_cast<E*>(p.z)[m * p.ldz + n] = E(v);
+              v = act_of(p.act, v);
+              if (p.res) v += float(static_cast<const E*>(p.res)[m * p.ldr + n]);
+            }
+            o.c[m * p.ldc + n] = E(v);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    });
+  });
+}
+
+template <class C, typename E, bool EPI>
+__device__ __forceinline__ void store_tile(const Product& p, const Work<E>& o, const f32x16 (&acc)[C::NB][C::NB],
+                                           int wm, int wn, int lane) {
+  constexpr int64_t kFar = int64_t(1) << 24;   // 31 rows of as many fp32 elements: below 2^32 bytes
+  if (p.N % 8 || p.ldc >= kFar || (EPI && (p.ldr >= kFar || p.ldz >= kFar))) {
+    store_elements<C, E, EPI>(p, o, acc, wm, wn, lane);
+  } else if (p.splits > 1) {
+    store_piece<C, E, float, MUON_ACT_NONE, false>(p, p.part + int64_t(blockIdx.y) * p.M * p.N, p.N, o, acc, wm, wn,
+                                                   lane);
+  } else {
+    with_act<EPI>(p.act, [&](auto act) {
+      store_piece<C, E, E, decltype(act)::value, EPI>(p, o.c, p.ldc, o, acc, wm, wn, lane);
+    });
+  }
+}
+
 template <typename E, int T, int U, int FORM, int GROUP>
 __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
     Product p, typename TableOf<GROUP>::T tab, int run, int blocks) {
@@ -281,6 +452,7 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
   RB rb;
   ra.init(wm, lane);
   rb.init(wn, lane);
+  rb.move(C::UNIT);
   const uint32_t base = lds_addr(lds);
   // The first U units of a tile's slabs.
   auto fill = [&]() {
@@ -350,13 +522,11 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
   };
   auto nothing = []() {};
 
+  int ua = 0, ub = C::UNIT;   // the current slab's units
   if (nk > 0) {
     asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"((U - 2) * LOADS) : "memory");
     __builtin_amdgcn_sched_barrier(0);
-    int ua = 0, ub = C::UNIT;   // the current slab's units
     uint32_t free1 = 0;         // the unit whose loads go out in steps 0 and 1
-    ra.unit(ua);
-    rb.unit(ub);
 #pragma unroll
     for (int r = 0; r < READS; ++r) read_one(0, r, 0);
     // The loads that step 3 starts go first, and are A's where U is even.
@@ -375,10 +545,11 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
     auto last_step = [&]() {
       const uint32_t free0 = base + ua;
       free1 = base + ub;
-      ua = wrap(ua + 2 * C::UNIT);
-      ub = wrap(ub + 2 * C::UNIT);
-      ra.unit(ua);
-      rb.unit(ub);
+      const int na = wrap(ua + 2 * C::UNIT), nb = wrap(ub + 2 * C::UNIT);
+      ra.move(na - ua);
+      rb.move(nb - ub);
+      ua = na;
+      ub = nb;
       k_step(first, 0, LOADS, 0, 1, free0, SPAN, nothing);
       first.next();
     };
@@ -395,6 +566,8 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
       last_step();
     }
   }
+  ra.move(-ua);
+  rb.move(C::UNIT - ub);
   // The last slabs' loads (past K) and every wave's reads end here, and the ring
   // takes the next tile's first slabs while this one is stored.
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -404,64 +577,7 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
     fill();
   }
 
-  // ---------------------------------------------------------------- epilogue
-  // Element q of block (i, j): row 32 i + lane % 32, column 32 j + 8 (q / 4) +
-  // 4 (lane / 32) + q % 4.
-  const int h = lane >> 5;
-  // (only the layers' own products have anything to add)
-  constexpr bool EPI = GROUP == GROUP_NONE && FORM != FORM_TT;
-  const E* bias = EPI ? static_cast<const E*>(p.bias) : nullptr;
-  const E* res = EPI ? static_cast<const E*>(p.res) : nullptr;
-  E* z = EPI ? static_cast<E*>(p.z) : nullptr;
-  with_act<EPI>(p.act, [&](auto act_tag) {
-    constexpr int ACT = decltype(act_tag)::value;
-    static_for<2 * C::NB>([&](auto jg) {
-      constexpr int j = decltype(jg)::value / 2, g = decltype(jg)::value % 2 * 2;
-      const int col = wn + 32 * j + 8 * g + 8 * h;
-      const int n = o.cols - col;
-      float bv[8] = {};
-      if (bias && n > 0) load8(bias + o.n0 + col, n, bv);
-      static_for<C::NB>([&](auto it) {
-        constexpr int i = decltype(it)::value;
-        const int row = wm + 32 * i + (lane & 31);
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          // the upper half of group g against the lower half of group g + 1
-          // (values of their own: a bit cast of a vector's element takes element
-          // 0; and in place: the exchanges of all activations' code are the
-          // same, and done ahead of the choice they would not fit the registers)
-          float lo = acc[i][j][4 * g + e], hi = acc[i][j][4 * g + 4 + e];
-          asm volatile("" : "+v"(lo), "+v"(hi));
-          const auto s = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, lo),
-                                                          __builtin_bit_cast(uint32_t, hi), false, false);
-          const uint32_t s0 = s[0], s1 = s[1];
-          v[e] = __builtin_bit_cast(float, s0);
-          v[4 + e] = __builtin_bit_cast(float, s1);
-        }
-        if (row < o.rows && n > 0) {
-          const int64_t m = o.m0 + row, c = o.n0 + col;
-          if (p.splits > 1) {
-            store8(p.part + (int64_t(blockIdx.y) * p.M + m) * p.N + c, n, v);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += bv[e];
-            if (z) store8(z + m * p.ldz + c, n, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = act_one<ACT>(v[e]);
-            if (res) {
-              float rv[8];
-              load8(res + m * p.ldr + c, n, rv);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] += rv[e];
-            }
-            store8(o.c + m * p.ldc + c, n, v);
-          }
-        }
-        __builtin_amdgcn_sched_barrier(0);   // (loads gathered further ahead would not fit the registers)
-      });
-    });
-  });
+  store_tile<C, E, GROUP == GROUP_NONE && FORM != FORM_TT>(p, o, acc, wm, wn, lane);
   if (!more) break;
   }
 }
