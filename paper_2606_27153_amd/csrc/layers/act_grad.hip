@@ -56,19 +56,25 @@ __global__ __launch_bounds__(256) void act_grad_kernel(ActGradArgs a, int chunk)
   }
 }
 
-// Adds `chunks` rows of fp32 partial sums: a wave per 64 columns of a block,
-// the block's 4 waves every fourth row, then their sums in order.
+// Adds `chunks` rows of fp32 partial sums: 64 columns per block, its 16 waves
+// every 16th row, then their sums in order.
 template <typename E>
-__global__ __launch_bounds__(256) void column_sum_kernel(const float* part, int chunks, int N, E* out) {
-  __shared__ float red[4][64];
+__global__ __launch_bounds__(1024) void column_sum_kernel(const float* part, int chunks, int N, E* out) {
+  __shared__ float red[16][64];
   const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
   const int col = blockIdx.x * 64 + lane;
   float s = 0.f;
-  if (col < N)
-    for (int r = wid; r < chunks; r += 4) s += part[int64_t(r) * N + col];
+  if (col < N) {
+#pragma unroll 8
+    for (int r = wid; r < chunks; r += 16) s += part[int64_t(r) * N + col];
+  }
   red[wid][lane] = s;
   __syncthreads();
-  if (wid == 0 && col < N) out[col] = E(red[0][lane] + red[1][lane] + red[2][lane] + red[3][lane]);
+  if (wid || col >= N) return;
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s += red[i][lane];
+  out[col] = E(s);
 }
 
 // Chunks of rows: enough blocks to fill the chip a few times over, at least 16
@@ -119,7 +125,7 @@ hipError_t launch(const ActGradArgs& a, hipStream_t st) {
     if (e != hipSuccess) return e;
   }
   if (a.dbias)
-    hipLaunchKernelGGL((column_sum_kernel<E>), dim3(unsigned((int64_t(a.N) + 63) / 64)), dim3(256), 0, st, a.part,
+    hipLaunchKernelGGL((column_sum_kernel<E>), dim3(unsigned((int64_t(a.N) + 63) / 64)), dim3(1024), 0, st, a.part,
                        chunks, a.N, static_cast<E*>(a.dbias));
   return hipGetLastError();
 }

@@ -37,149 +37,194 @@ __device__ __forceinline__ float weight_at(const void* w, int, int64_t i, const 
 }
 
 // Rows that fit the registers of T threads stay there: one read of x (and dy),
-// one write.  T is 64 -- a wave per row, four rows per block, no barrier -- for
-// short rows, then a block of 256 or 1024 threads per row.  Loads and stores are 16 bytes at any alignment;
-// a row's last, partial chunk is moved element by element.
+// one write.  T is 64 -- a wave per row, no barrier -- for short rows, then 256
+// or 1024 threads.  A block holds a few rows at a time and takes every
+// gridDim.x-th group of them; the next group's loads are issued before the
+// current one is reduced, so that the memory never waits for the reductions.
+// Loads and stores are 16 bytes at any alignment, and no load sits in a branch
+// (which would end in a wait for it).
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <typename E>
 struct __attribute__((packed, aligned(sizeof(E)))) Chunk {
   E v[16 / sizeof(E)];
 };
 template <typename E>
-__device__ __forceinline__ Chunk<E> load_chunk(const E* p, int n) {   // n: elements that exist
-  constexpr int V = 16 / sizeof(E);
-  Chunk<E> c;
-  if (n >= V) {
-    c = *reinterpret_cast<const Chunk<E>*>(p);
-  } else {
-#pragma unroll
-    for (int e = 0; e < V; ++e) c.v[e] = e < n ? p[e] : E(0.f);
-  }
-  return c;
+__device__ __forceinline__ Chunk<E> load_chunk(const E* p) {
+  return *reinterpret_cast<const Chunk<E>*>(p);
 }
-template <typename E>
-__device__ __forceinline__ void store_chunk(E* p, int n, const Chunk<E>& c) {
-  constexpr int V = 16 / sizeof(E);
-  if (n >= V) {
-    *reinterpret_cast<Chunk<E>*>(p) = c;
-  } else {
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      if (e < n) p[e] = c.v[e];
-  }
+// Thread t's chunk j of a row of n >= V columns: its first column, moved back
+// where it would pass the row's end, and how many of its elements are then the
+// chunk before's (V: all; they hold the same values, and count as 0 in sums).
+struct Place {
+  int col, dup;
+};
+template <int V, int T>
+__device__ __forceinline__ Place place(int t, int j, int n) {
+  const int want = (t + j * T) * V, col = min(want, n - V);
+  return Place{col, want - col};
 }
-// V weights from column c on, as fp32 (1 or 0 where there are none).
+// V weights from column c on, as fp32 (`none` where there are none).
 template <typename E>
-__device__ __forceinline__ void load_weights(const void* w, int wf32, int c, int n, float none,
+__device__ __forceinline__ void load_weights(const void* w, int wf32, int c, float none,
                                              float (&v)[16 / sizeof(E)]) {
   constexpr int V = 16 / sizeof(E);
+  if (!w) {
 #pragma unroll
-  for (int e = 0; e < V; ++e) v[e] = none;
-  if (!w || n <= 0) return;
-  if (wf32) {
+    for (int e = 0; e < V; ++e) v[e] = none;
+  } else if (wf32) {
 #pragma unroll
     for (int q = 0; q < V; q += 4) {
-      const Chunk<float> x = load_chunk(static_cast<const float*>(w) + c + q, n - q);
+      const Chunk<float> x = load_chunk(static_cast<const float*>(w) + c + q);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[q + e] = x.v[e];
     }
   } else {
-    const Chunk<E> x = load_chunk(static_cast<const E*>(w) + c, n);
+    const Chunk<E> x = load_chunk(static_cast<const E*>(w) + c);
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = float(x.v[e]);
   }
 }
 
-template <typename E, int NV, int T>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_forward_kernel(NormArgs a) {
-  constexpr int V = 16 / int(sizeof(E));
-  __shared__ float red[T / 64];
-  const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x;
-  const int64_t r = T == 64 ? int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6) : blockIdx.x;
-  if (r >= a.rows) return;
-  const E* x = static_cast<const E*>(a.x) + r * a.ldx;
-  Chunk<E> c[NV];
+// Rows a block holds at a time, and its threads.
+template <int T>
+struct Shape {
+  static constexpr int ROWS = T == 64 ? 4 : 1;
+  static constexpr int THREADS = T * ROWS;
+  static constexpr int WAVES = T / 64;   // of a row
+};
+
+// Sums of N values over the T threads of a row, the same for all of them.  buf:
+// LDS for the waves' sums, N x THREADS / 64 floats that no wave may still read
+// from an earlier sum (two buffers in turn: a barrier lies between their uses).
+template <int T, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float* buf) {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int col = (t + j * T) * V;
-    c[j] = load_chunk(x + col, a.cols - col);
-  }
-  float s = 0.f;
+  for (int i = 0; i < N; ++i)
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
+    for (int d = 32; d; d >>= 1) v[i] += __shfl_xor(v[i], d);
+  if constexpr (T > 64) {
+    constexpr int W = Shape<T>::WAVES;
+    const int wid = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) s += float(c[j].v[e]);
-  const float mean = block_sum<T>(s, red) / float(a.cols);
-  s = 0.f;
-#pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const float d = (t + j * T) * V + e < a.cols ? float(c[j].v[e]) - mean : 0.f;
-      s = fmaf(d, d, s);
+      for (int i = 0; i < N; ++i) buf[wid * N + i] = v[i];
     }
-  const float rstd = 1.f / sqrtf(block_sum<T>(s, red) / float(a.cols) + a.eps);
-  if (t == 0) {
-    if (a.mean) a.mean[r] = mean;
-    if (a.rstd) a.rstd[r] = rstd;
-  }
-  E* y = static_cast<E*>(a.y) + r * a.ldy;
+    __syncthreads();
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int col = (t + j * T) * V, n = a.cols - col;
-    float w[V], b[V];
-    load_weights<E>(a.weight, a.wf32, col, n, 1.f, w);
-    load_weights<E>(a.bias, a.wf32, col, n, 0.f, b);
-    Chunk<E> o;
+    for (int i = 0; i < N; ++i) v[i] = 0.f;
 #pragma unroll
-    for (int e = 0; e < V; ++e) o.v[e] = E(fmaf((float(c[j].v[e]) - mean) * rstd, w[e], b[e]));
-    store_chunk(y + col, n, o);
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += buf[(wid / W * W + w) * N + i];
   }
 }
 
-// A block (T 64: each of its four waves) takes every gridDim.x-th (4
-// gridDim.x-th) row and keeps its columns' sums over those rows in registers;
-// they go to the block's rows of part at the end (T 64: the waves' sums added in
-// order through LDS).  SUMS: whether dw and db are wanted.  The next row's loads
-// are issued before the current row is reduced, and the weights stay in
-// registers, except with 1024 threads, which have 128 registers each.
-template <typename E, int NV, int T, bool SUMS>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_backward_kernel(NormArgs a) {
+template <typename E, int NV, int T>
+__global__ __launch_bounds__(Shape<T>::THREADS) void norm_forward_kernel(NormArgs a) {
+  using S = Shape<T>;
   constexpr int V = 16 / int(sizeof(E));
-  constexpr int ROWS = T == 64 ? 4 : 1;
-  __shared__ float red[2][T / 64];
-  __shared__ float sums[SUMS && T == 64 ? 64 * NV * V : 1];
-  const int t = T == 64 ? threadIdx.x & 63 : threadIdx.x, wid = threadIdx.x >> 6;
-  const int64_t r0 = int64_t(blockIdx.x) * ROWS + (T == 64 ? wid : 0), step = int64_t(gridDim.x) * ROWS;
-  constexpr bool AHEAD = T < 1024;
-  float w[AHEAD ? NV : 1][V], pw[NV][V], pb[NV][V];
-  auto weights = [&](int j, float (&v)[V]) {
-    const int col = (t + j * T) * V;
-    load_weights<E>(a.weight, a.wf32, col, a.cols - col, 1.f, v);
-  };
+  __shared__ float red[2][S::THREADS / 64];
+  const int t = threadIdx.x % T;
+  const int64_t step = int64_t(gridDim.x) * S::ROWS;
+  float w[NV][V], b[NV][V];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    if constexpr (AHEAD) weights(j, w[j]);
+    const int col = place<V, T>(t, j, a.cols).col;
+    load_weights<E>(a.weight, a.wf32, col, 1.f, w[j]);
+    load_weights<E>(a.bias, a.wf32, col, 0.f, b[j]);
+  }
+  Chunk<E> next[NV];
+  auto load = [&](int64_t r) {
+    const E* x = static_cast<const E*>(a.x) + min(r, int64_t(a.rows) - 1) * a.ldx;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) next[j] = load_chunk(x + place<V, T>(t, j, a.cols).col);
+  };
+  // (rows past the last read it again)
+  int64_t r = int64_t(blockIdx.x) * S::ROWS + threadIdx.x / T;
+  load(r);
+  for (int64_t first = int64_t(blockIdx.x) * S::ROWS; first < a.rows; first += step, r += step) {
+    Chunk<E> c[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) c[j] = next[j];
+    load(r + step);
+    float s[1] = {0.f};
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int dup = place<V, T>(t, j, a.cols).dup;
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[0] += e >= dup ? float(c[j].v[e]) : 0.f;
+    }
+    row_sums<T>(s, red[0]);
+    const float mean = s[0] / float(a.cols);
+    s[0] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int dup = place<V, T>(t, j, a.cols).dup;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float d = e >= dup ? float(c[j].v[e]) - mean : 0.f;
+        s[0] = fmaf(d, d, s[0]);
+      }
+    }
+    row_sums<T>(s, red[1]);
+    const float rstd = 1.f / sqrtf(s[0] / float(a.cols) + a.eps);
+    if (r >= a.rows) continue;
+    if (t == 0) {
+      if (a.mean) a.mean[r] = mean;
+      if (a.rstd) a.rstd[r] = rstd;
+    }
+    E* y = static_cast<E*>(a.y) + r * a.ldy;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const Place at = place<V, T>(t, j, a.cols);
+      Chunk<E> o;
+#pragma unroll
+      for (int e = 0; e < V; ++e) o.v[e] = E(fmaf((float(c[j].v[e]) - mean) * rstd, w[j][e], b[j][e]));
+      if (at.dup < V) *reinterpret_cast<Chunk<E>*>(y + at.col) = o;
+    }
+  }
+}
+
+// The columns' sums over a block's rows stay in registers; at the end its rows'
+// threads add theirs in order through LDS, into the block's rows of part.  SUMS:
+// whether dw and db are wanted.  The weights are read again for each row (from
+// the caches): the registers they would take are worth another wave.
+template <typename E, int NV, int T, bool SUMS>
+__global__ __launch_bounds__(Shape<T>::THREADS, T < 1024 && NV * 16 / sizeof(E) <= 16 ? 3 : 1) void
+norm_backward_kernel(NormArgs a) {
+  using S = Shape<T>;
+  constexpr int V = 16 / int(sizeof(E));
+  __shared__ float red[2][2 * S::THREADS / 64];
+  __shared__ float sums[SUMS && S::ROWS > 1 ? S::ROWS : 1][SUMS && S::ROWS > 1 ? T * NV * V : 1];
+  const int t = threadIdx.x % T, row = threadIdx.x / T;
+  const int64_t step = int64_t(gridDim.x) * S::ROWS;
+  float pw[NV][V], pb[NV][V];
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
 #pragma unroll
     for (int e = 0; e < V; ++e) pw[j][e] = pb[j][e] = 0.f;
-  }
+  // (with 1024 threads the registers hold one row only)
+  constexpr bool AHEAD = T < 1024;
   Chunk<E> x[NV], d[NV];
   float mean = 0.f, rstd = 0.f;
   auto load = [&](int64_t r) {
-    if (r >= a.rows) return;
+    const int64_t at = min(r, int64_t(a.rows) - 1);
+    const E* xp = static_cast<const E*>(a.x) + at * a.ldx;
+    const E* dp = static_cast<const E*>(a.dy) + at * a.lddy;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int col = (t + j * T) * V;
-      x[j] = load_chunk(static_cast<const E*>(a.x) + r * a.ldx + col, a.cols - col);
-      d[j] = load_chunk(static_cast<const E*>(a.dy) + r * a.lddy + col, a.cols - col);
+      const int col = place<V, T>(t, j, a.cols).col;
+      x[j] = load_chunk(xp + col);
+      d[j] = load_chunk(dp + col);
     }
-    mean = a.mean[r];
-    rstd = a.rstd[r];
+    mean = a.mean[at];
+    rstd = a.rstd[at];
   };
-  if constexpr (AHEAD) load(r0);
-  for (int64_t r = r0; r < a.rows; r += step) {
+  int64_t r = int64_t(blockIdx.x) * S::ROWS + row;
+  if constexpr (AHEAD) load(r);
+  int turn = 0;
+  for (int64_t first = int64_t(blockIdx.x) * S::ROWS; first < a.rows; first += step, r += step, turn ^= 1) {
     if constexpr (!AHEAD) load(r);
-    float s1 = 0.f, s2 = 0.f;
     Chunk<E> xr[NV], dr[NV];
     const float m = mean, rs = rstd;
 #pragma unroll
@@ -188,73 +233,80 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_backward_kernel(NormAr
       dr[j] = d[j];
     }
     if constexpr (AHEAD) load(r + step);
+    // (a pointer of this row's own, so that its loads are not kept in registers)
+    const void* weight = a.weight;
+    asm volatile("" : "+s"(weight));
+    float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      float(&wj)[V] = w[AHEAD ? j : 0];
-      if constexpr (!AHEAD) weights(j, wj);
+      float w[V];
+      const Place at = place<V, T>(t, j, a.cols);
+      load_weights<E>(weight, a.wf32, at.col, 1.f, w);
+      const int from = r < a.rows ? at.dup : V;   // (nothing of rows past the last)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        // (past the last column dy is 0)
-        const float h = (float(xr[j].v[e]) - m) * rs, dd = float(dr[j].v[e]), g = dd * wj[e];
-        s1 += g;
-        s2 = fmaf(g, h, s2);
+        const float h = (float(xr[j].v[e]) - m) * rs, dd = float(dr[j].v[e]);
+        if (e < from) continue;
+        const float g = dd * w[e];
+        s[0] += g;
+        s[1] = fmaf(g, h, s[1]);
         if constexpr (SUMS) {
           pw[j][e] = fmaf(dd, h, pw[j][e]);
           pb[j][e] += dd;
         }
       }
     }
-    s1 = block_sum<T>(s1, red[0]) / float(a.cols);
-    s2 = block_sum<T>(s2, red[1]) / float(a.cols);
-    if (a.dx) {
+    row_sums<T>(s, red[turn]);
+    asm volatile("" : "+s"(weight));
+    const float s1 = s[0] / float(a.cols), s2 = s[1] / float(a.cols);
+    if (a.dx && r < a.rows) {
       E* dx = static_cast<E*>(a.dx) + r * a.lddx;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const int col = (t + j * T) * V;
-        float(&wj)[V] = w[AHEAD ? j : 0];
-        if constexpr (!AHEAD) weights(j, wj);
+        float w[V];
+        const Place at = place<V, T>(t, j, a.cols);
+        load_weights<E>(weight, a.wf32, at.col, 1.f, w);
         Chunk<E> o;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           const float h = (float(xr[j].v[e]) - m) * rs;
-          o.v[e] = E(rs * (float(dr[j].v[e]) * wj[e] - s1 - h * s2));
+          o.v[e] = E(rs * (float(dr[j].v[e]) * w[e] - s1 - h * s2));
         }
-        store_chunk(dx + col, a.cols - col, o);
+        if (at.dup < V) *reinterpret_cast<Chunk<E>*>(dx + at.col) = o;
       }
     }
   }
   if constexpr (SUMS) {
     for (int k = 0; k < 2; ++k) {
       float* part = a.part + (int64_t(blockIdx.x) * 2 + k) * a.cols;
-      if constexpr (T == 64) {
-        for (int q = 0; q < 4; ++q) {
-          if (wid == q) {
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
+      for (int j = 0; j < NV; ++j) {
+        const Place at = place<V, T>(t, j, a.cols);
 #pragma unroll
-              for (int e = 0; e < V; ++e) {
-                float& at = sums[(t + j * T) * V + e];
-                at = (q ? at : 0.f) + (k ? pb[j][e] : pw[j][e]);
-              }
-          }
-          __syncthreads();
+        for (int e = 0; e < V; ++e) {
+          const float v = k ? pb[j][e] : pw[j][e];
+          if (e < at.dup) continue;
+          if constexpr (S::ROWS > 1)
+            sums[row][at.col + e] = v;
+          else
+            part[at.col + e] = v;
         }
-        for (int c = threadIdx.x; c < a.cols; c += 256) part[c] = sums[c];
+      }
+      if constexpr (S::ROWS > 1) {
         __syncthreads();
-      } else {
+        for (int c = threadIdx.x; c < a.cols; c += S::THREADS) {
+          float v = 0.f;
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const int col = (t + j * T) * V + e;
-            if (col < a.cols) part[col] = k ? pb[j][e] : pw[j][e];
-          }
+          for (int q = 0; q < S::ROWS; ++q) v += sums[q][c];
+          part[c] = v;
+        }
+        __syncthreads();
       }
     }
   }
 }
 
-// Longer rows: read again for each sum.
+// Other rows: read again for each sum.
 template <typename E>
 __global__ __launch_bounds__(256) void norm_forward_loop_kernel(NormArgs a) {
   __shared__ float red[4];
@@ -345,11 +397,11 @@ __global__ __launch_bounds__(1024) void norm_column_sum_kernel(NormArgs a, int b
     static_cast<E*>(out)[col] = E(s);
 }
 
-// Threads per row, so that a thread holds at most 32 elements forward, 24 (16
-// with 1024 threads) backward, where the sums take registers too.  0: the row
-// does not fit.
-int forward_threads(int64_t cols) { return cols <= 2048 ? 64 : cols <= 8192 ? 256 : cols <= 32768 ? 1024 : 0; }
-int backward_threads(int64_t cols) { return cols <= 1536 ? 64 : cols <= 6144 ? 256 : cols <= 16384 ? 1024 : 0; }
+// Threads per row, so that a thread holds at most 32 elements (16 with 1024
+// threads) forward, 24 (8) backward, where the sums take registers too.  0: the row
+// does not fit, or is shorter than a chunk.
+int forward_threads(int64_t cols) { return cols < 8 ? 0 : cols <= 2048 ? 64 : cols <= 8192 ? 256 : cols <= 16384 ? 1024 : 0; }
+int backward_threads(int64_t cols) { return cols < 8 ? 0 : cols <= 1536 ? 64 : cols <= 6144 ? 256 : cols <= 8192 ? 1024 : 0; }
 
 // f(chunks per thread tag, threads tag) for rows of `cols` on t threads: the
 // smallest chunk count that covers them, in quarters of 32 elements.
@@ -375,9 +427,15 @@ hipError_t forward(const NormArgs& a, hipStream_t st) {
   if (!t) {
     hipLaunchKernelGGL((norm_forward_loop_kernel<E>), dim3(unsigned(a.rows)), dim3(256), 0, st, a);
   } else {
-    const dim3 g{unsigned(t == 64 ? (a.rows + 3) / 4 : a.rows)}, b{unsigned(t == 64 ? 256 : t)};
     with_shape<E>(a.cols, t, [&](auto nv, auto tt) {
-      hipLaunchKernelGGL((norm_forward_kernel<E, decltype(nv)::value, decltype(tt)::value>), g, b, 0, st, a);
+      using S = Shape<decltype(tt)::value>;
+      // as many blocks as the chip holds at once, 2048 threads per CU
+      const int64_t groups = (int64_t(a.rows) + S::ROWS - 1) / S::ROWS, most = int64_t(kCUs) * 2048 / S::THREADS;
+      const dim3 g{unsigned(groups < most ? groups : most)}, b{S::THREADS};
+      // (1024 threads hold 16 elements each: forward_threads)
+      constexpr int NV = decltype(nv)::value;
+      if constexpr (S::WAVES < 16 || NV * 16 / int(sizeof(E)) <= 16)
+        hipLaunchKernelGGL((norm_forward_kernel<E, NV, decltype(tt)::value>), g, b, 0, st, a);
     });
   }
   return hipGetLastError();
@@ -391,14 +449,16 @@ hipError_t backward(const NormArgs& a, hipStream_t st) {
     if (!t) {
       hipLaunchKernelGGL((norm_backward_loop_kernel<E>), dim3(unsigned(blocks)), dim3(256), 0, st, a);
     } else {
-      const dim3 g{unsigned(blocks)}, b{unsigned(t == 64 ? 256 : t)};
       with_shape<E>(a.cols, t, [&](auto nv, auto tt) {
         constexpr int NV = decltype(nv)::value, TT = decltype(tt)::value;
-        if constexpr (NV * 16 / int(sizeof(E)) > (TT == 1024 ? 16 : 24)) return;   // (never: backward_threads)
-        else if (a.dweight || a.dbias)
-          hipLaunchKernelGGL((norm_backward_kernel<E, NV, TT, true>), g, b, 0, st, a);
-        else
-          hipLaunchKernelGGL((norm_backward_kernel<E, NV, TT, false>), g, b, 0, st, a);
+        const dim3 g{unsigned(blocks)}, b{Shape<TT>::THREADS};
+        // (a thread holds no more: backward_threads)
+        if constexpr (NV * 16 / int(sizeof(E)) <= (TT == 1024 ? 8 : 24)) {
+          if (a.dweight || a.dbias)
+            hipLaunchKernelGGL((norm_backward_kernel<E, NV, TT, true>), g, b, 0, st, a);
+          else
+            hipLaunchKernelGGL((norm_backward_kernel<E, NV, TT, false>), g, b, 0, st, a);
+        }
       });
     }
     const hipError_t e = hipGetLastError();
@@ -412,12 +472,13 @@ hipError_t backward(const NormArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Blocks of the backward pass: two to four rows per wave at least, no more
-// blocks than keep the chip full (their partial sums are written and read too).
+// Blocks of the backward pass: what the chip holds at once (3 of 256 threads, 1
+// of 1024 per CU), and at least two rows per thread group, so that their partial
+// sums stay few.
 int norm_blocks(int64_t rows, int64_t cols) {
   const int t = backward_threads(cols);
-  const int64_t per = t == 64 ? 8 : 4, most = t == 64 ? 1024 : t == 1024 ? 256 : 512;
-  const int64_t n = (rows + per - 1) / per;
+  const int64_t group = t == 64 ? 4 : 1, most = kCUs * (t == 1024 ? 1 : 3);
+  const int64_t n = (rows + 2 * group - 1) / (2 * group);
   return int(n < 1 ? 1 : n < most ? n : most);
 }
 
