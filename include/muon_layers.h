@@ -20,8 +20,8 @@
  *
  *  - A matrix is a pointer and a leading dimension in elements (row i starts
  *    at data + i * ld, ld >= its columns); rows need the alignment of their
- *    element type only, 16-byte aligned rows of a multiple of 16 bytes run
- *    faster.
+ *    element type only; rows of whole, aligned 16-byte chunks are read where
+ *    they lie, others copied first (MUON_LAYERS_UNALIGNED).
  *  - w_transposed != 0: W is kept as outer x inner (element (k, n) at
  *    w + n * ldw + k), and so is dW.
  *  - dtype is that of every matrix and of the bias: MUON_F32 or MUON_BF16.
@@ -79,10 +79,17 @@ MUON_API muon_status muon_linear_backward(const void* dy, int64_t lddy, const vo
                                           int64_t inner, int64_t outer, int32_t dtype, int32_t activation,
                                           void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* Workspace bytes of muon_linear_forward (backward == 0) or
- * muon_linear_backward with any choice of outputs. */
+/* Flags of the workspace functions. */
+#define MUON_LAYERS_BACKWARD 1   /* the backward pass's workspace, not the forward pass's */
+#define MUON_LAYERS_UNALIGNED 2  /* room for copies of operands whose rows are not 16-byte aligned
+                                    or not a multiple of 16 bytes long; without it the call still
+                                    works, on a kernel that reads them as they lie and is many
+                                    times slower on large products */
+
+/* Workspace bytes of muon_linear_forward or muon_linear_backward (with any
+ * choice of outputs). */
 MUON_API muon_status muon_linear_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype,
-                                                 int32_t activation, int32_t backward, size_t* bytes);
+                                                 int32_t activation, int32_t flags, size_t* bytes);
 
 /* y_t = x_t W_e for the rows t of expert e.  w: a host array of `experts`
  * device pointers, all with leading dimension ldw; it is read during the call
@@ -107,9 +114,9 @@ MUON_API muon_status muon_grouped_linear_backward(const void* dy, int64_t lddy, 
                                                   int64_t outer, int32_t dtype, void* workspace, size_t workspace_bytes,
                                                   void* hip_stream);
 
-/* Workspace bytes of muon_grouped_linear_forward (backward == 0) or _backward. */
+/* Workspace bytes of muon_grouped_linear_forward or _backward. */
 MUON_API muon_status muon_grouped_linear_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t experts,
-                                                         int32_t dtype, int32_t backward, size_t* bytes);
+                                                         int32_t dtype, int32_t flags, size_t* bytes);
 
 /* Layer norm over the columns.  weight and bias (cols elements of
  * weight_dtype, MUON_F32 or dtype) may be NULL (1 and 0).  mean and rstd, rows

@@ -28,7 +28,7 @@ SOURCES = ["api.cpp", "plan.cpp", "ew_kernels.hip", "ns_gemm.hip", "ns_gemm_t256
 LAYER_SOURCES = ["layers/layers_api.cpp", "layers/mm_simple.hip", "layers/mm_tile_256_bf16.hip",
                  "layers/mm_tile_128_bf16.hip", "layers/mm_tile_128_f32.hip",
                  "layers/mm_tile_64_bf16.hip", "layers/mm_tile_64_f32.hip", "layers/mm_skinny.hip",
-                 "layers/act_grad.hip", "layers/layer_norm.hip"]
+                 "layers/pack.hip", "layers/act_grad.hip", "layers/layer_norm.hip"]
 LAYER_LIB_PATH = os.path.join(PKG, "libmuon_layers.so")
 DIAG_SOURCES = ["diag/mfma_ceiling.hip"]
 DIAG_LIB_PATH = os.path.join(PKG, "libmuon_diag.so")

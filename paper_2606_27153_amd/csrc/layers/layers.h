@@ -53,6 +53,18 @@ struct Table {
   const void* p[MUON_GROUPED_MAX_EXPERTS];
 };
 
+// An operand's copy: rows x cols of leading dimension ld_src to rows of ld_dst
+// elements (a multiple of 16 bytes), zeros after the last column.  dst NULL: none.
+struct PackOne {
+  const void* src;
+  void* dst;
+  int64_t rows, cols, ld_src, ld_dst;
+};
+struct PackArgs {
+  PackOne a, b;
+  int32_t experts;   // > 0: b is copied from every pointer of the table, one after the other
+};
+
 struct NormArgs {
   const void* x;
   const void* dy;
@@ -97,6 +109,8 @@ hipError_t launch_tile64_f32(int form, int group, const Product& p, const Table*
 hipError_t launch_skinny(bool bf16, int form, int group, int mt, const Product& p, const Table* t, hipStream_t st);
 // Adds p.splits partial results and applies the epilogue.
 hipError_t launch_reduce(bool bf16, const Product& p, hipStream_t st);
+
+hipError_t launch_pack(bool bf16, const PackArgs& a, const Table& t, hipStream_t st);
 
 hipError_t launch_act_grad(bool bf16, const ActGradArgs& a, hipStream_t st);
 int act_grad_chunks(int64_t rows, int64_t N);   // rows of `part`

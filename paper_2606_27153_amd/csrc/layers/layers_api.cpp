@@ -48,6 +48,11 @@ muon_status check_activation(int32_t a) {
   return MUON_OK;
 }
 
+muon_status check_flags(int32_t f) {
+  if (f & ~(MUON_LAYERS_BACKWARD | MUON_LAYERS_UNALIGNED)) return fail(MUON_ERR_INVALID_ARG, "unknown flags %d", f);
+  return MUON_OK;
+}
+
 // A matrix operand: a pointer aligned to its element and a leading dimension of
 // at least its columns.
 muon_status check_matrix(const char* name, const void* p, int64_t ld, int64_t cols, size_t esize) {
@@ -80,22 +85,44 @@ muon_status check_workspace(const void* ws, size_t have, size_t need) {
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
-// Whether the tile kernels can fetch the operands: 16-byte chunks that lie on
-// 16-byte addresses and do not straddle the end of a row, and 32-bit byte
-// offsets within a tile of 256 rows.
-bool tile_fits(bool bf16, int form, int group, const Product& p, const Table* t) {
-  const int64_t epc = bf16 ? 8 : 4, es = bf16 ? 2 : 4;
-  const bool atr = form == FORM_TT, btr = form != FORM_RR;
-  if (p.lda % epc || p.ldb % epc) return false;
-  if (p.lda * es * 256 >= (int64_t(1) << 31) || p.ldb * es * 256 >= (int64_t(1) << 31)) return false;
-  if ((atr ? p.M : p.K) % epc || (btr ? p.N : p.K) % epc) return false;
-  if (!aligned16(p.a)) return false;
+// Whether the tile kernels can fetch an operand of rows of `cols` elements:
+// 16-byte chunks that lie on 16-byte addresses and do not straddle the end of a
+// row, and 32-bit byte offsets within a tile of 256 rows.
+bool rows_fit(const void* ptr, int64_t ld, int64_t cols, int64_t epc) {
+  return aligned16(ptr) && ld % epc == 0 && cols % epc == 0 && ld * 16 / epc * 256 < (int64_t(1) << 31);
+}
+struct Fits {
+  bool a, b;
+};
+Fits tile_fits(bool bf16, int form, int group, const Product& p, const Table* t) {
+  const int64_t epc = bf16 ? 8 : 4;
+  Fits f;
+  f.a = rows_fit(p.a, p.lda, form == FORM_TT ? p.M : p.K, epc);
+  const int64_t cols = form == FORM_RR ? p.K : p.N;
+  f.b = group != GROUP_ROWS && rows_fit(p.b, p.ldb, cols, epc);
   if (group == GROUP_ROWS) {
-    for (int32_t e = 0; e < p.experts; ++e)
-      if (!aligned16(t->p[e])) return false;
-    return true;
+    f.b = true;
+    for (int32_t e = 0; e < p.experts && f.b; ++e) f.b = rows_fit(t->p[e], p.ldb, cols, epc);
   }
-  return aligned16(p.b);
+  return f;
+}
+
+// Shapes of the operands' copies (pack.hip): rows of whole chunks.
+PackOne copy_shape(int64_t rows, int64_t cols, int64_t epc) {
+  PackOne o{};
+  o.rows = rows;
+  o.cols = cols;
+  o.ld_dst = (cols + epc - 1) / epc * epc;
+  return o;
+}
+PackOne copy_of_a(int form, int64_t M, int64_t K, int64_t epc) {
+  return form == FORM_TT ? copy_shape(K, M, epc) : copy_shape(M, K, epc);
+}
+PackOne copy_of_b(int form, int64_t N, int64_t K, int64_t epc) {
+  return form == FORM_RR ? copy_shape(N, K, epc) : copy_shape(K, N, epc);
+}
+size_t copy_bytes(const PackOne& o, int64_t epc, int64_t copies) {
+  return padded(size_t(o.rows) * size_t(o.ld_dst) * size_t(16 / epc) * size_t(copies));
 }
 
 // Which kernel runs a product, and into how many ranges it cuts the summed
@@ -114,10 +141,11 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // slab, full / alone): 256: 1.4 / 1.15, 128: 1.0 / 0.53 for the two blocks of a
 // CU, 64: 0.42 / 0.29; the rest 6, 4.5 and 3 us.  fp32's MFMAs are what a slab
 // takes: 1.8 us of the 128 tile, 0.45 of the 64 tile, twice that for two blocks.
-double tile_us(bool bf16, int tile, double blocks, double slabs) {
+// An activation costs the 256 tile, which has nothing to run beside it, 8 us more.
+double tile_us(bool bf16, int tile, double blocks, double slabs, bool act) {
   const double full = bf16 ? (tile == 256 ? 1.4 : tile == 128 ? 1.0 : 0.42) : tile == 128 ? 3.6 : 0.9;
   const double alone = bf16 ? (tile == 256 ? 1.15 : tile == 128 ? 0.53 : 0.29) : tile == 128 ? 1.8 : 0.45;
-  const double rest = tile == 256 ? 6 : tile == 128 ? 4.5 : 3;
+  const double rest = (tile == 256 ? 6 : tile == 128 ? 4.5 : 3) + (act && tile == 256 ? 8 : 0);
   const double slots = tile == 256 ? kCUs : 2 * kCUs;
   if (blocks <= kCUs) return slabs * alone + rest;
   if (tile == 256) {
@@ -134,7 +162,8 @@ double reduce_us(int64_t M, int64_t N, int splits) {
   return splits > 1 ? 3.0 + double(splits) * M * N * 8 / 4e6 : 0.0;
 }
 
-Choice choose(bool bf16, int form, int group, int64_t M, int64_t N, int64_t K, int64_t experts, bool fits) {
+Choice choose(bool bf16, int form, int group, int64_t M, int64_t N, int64_t K, int64_t experts,
+              bool act) {
   Choice c;
   const int64_t epc = bf16 ? 8 : 4;
   // Few rows: the weight's bytes are all that counts, which the skinny kernel
@@ -152,7 +181,6 @@ Choice choose(bool bf16, int form, int group, int64_t M, int64_t N, int64_t K, i
     }
     return c;
   }
-  if (!fits) return c;
   const int64_t bk = bf16 ? 64 : 32;
   double best = 0;
   for (int tile : {256, 128, 64}) {
@@ -166,7 +194,7 @@ Choice choose(bool bf16, int form, int group, int64_t M, int64_t N, int64_t K, i
     }
     for (int s = 1; s <= 16; ++s) {
       if (s > 1 && (group != GROUP_NONE || slabs < 4 * s)) break;
-      const double us = tile_us(bf16, tile, blocks * s, std::ceil(slabs / s)) + reduce_us(M, N, s);
+      const double us = tile_us(bf16, tile, blocks * s, std::ceil(slabs / s), act) + reduce_us(M, N, s);
       if (best == 0 || us < best) {
         best = us;
         c.kernel = tile == 256 ? Choice::TILE256 : tile == 128 ? Choice::TILE128 : Choice::TILE64;
@@ -181,14 +209,68 @@ size_t part_bytes(const Choice& c, int64_t M, int64_t N) {
   return c.splits > 1 ? padded(size_t(c.splits) * size_t(M) * size_t(N) * 4) : 0;
 }
 
-// One matrix product: the kernel that suits it.  part: part_bytes of the choice
-// that takes the operands to be aligned (no other needs more).
-hipError_t product(bool bf16, int form, int group, Product p, const Table* t, void* part, hipStream_t st) {
-  const Choice c =
-      choose(bf16, form, group, p.M, p.N, p.K, p.experts, tile_fits(bf16, form, group, p, t));
-  p.splits = c.splits;
-  p.part = static_cast<float*>(part);
+// Scratch memory of a product, and what it can use: partial results, and copies
+// of operands the tile kernels cannot fetch.
+struct Scratch {
+  char* p;
+  size_t bytes;
+};
+
+// One matrix product: the kernel that suits it.  Operands off 16-byte rows are
+// copied first if the scratch memory holds the copies; else the simple kernel
+// takes them as they lie.
+hipError_t product(bool bf16, int form, int group, Product p, const Table* t, Scratch ws, hipStream_t st) {
+  const int64_t epc = bf16 ? 8 : 4;
+  Choice c = choose(bf16, form, group, p.M, p.N, p.K, p.experts, p.act != MUON_ACT_NONE);
   hipError_t e = hipSuccess;
+  Table copies;
+  if (c.kernel != Choice::SKINNY) {
+    const Fits f = tile_fits(bf16, form, group, p, t);
+    if (!f.a || !f.b) {
+      PackArgs k{};
+      const int64_t n = group == GROUP_ROWS ? p.experts : 1;
+      size_t used = part_bytes(c, p.M, p.N);
+      if (!f.a) {
+        k.a = copy_of_a(form, p.M, p.K, epc);
+        k.a.src = p.a;
+        k.a.ld_src = p.lda;
+        k.a.dst = ws.p + used;
+        used += copy_bytes(k.a, epc, 1);
+      }
+      if (!f.b) {
+        k.b = copy_of_b(form, p.N, p.K, epc);
+        k.b.src = p.b;
+        k.b.ld_src = p.ldb;
+        k.b.dst = ws.p + used;
+        k.experts = group == GROUP_ROWS ? p.experts : 0;
+        used += copy_bytes(k.b, epc, n);
+      }
+      // (the tile kernels' 32-bit offsets hold for the copies too)
+      const bool near = k.a.ld_dst * 16 / epc * 256 < (int64_t(1) << 31) && k.b.ld_dst * 16 / epc * 256 < (int64_t(1) << 31);
+      if (ws.p && used <= ws.bytes && near && p.K > 0) {
+        static const Table none{};
+        e = launch_pack(bf16, k, group == GROUP_ROWS ? *t : none, st);
+        if (e != hipSuccess) return e;
+        if (!f.a) {
+          p.a = k.a.dst;
+          p.lda = k.a.ld_dst;
+        }
+        if (!f.b) {
+          p.b = k.b.dst;
+          p.ldb = k.b.ld_dst;
+          if (group == GROUP_ROWS) {
+            for (int32_t i = 0; i < p.experts; ++i)
+              copies.p[i] = static_cast<char*>(k.b.dst) + size_t(i) * size_t(k.b.rows) * size_t(k.b.ld_dst) * size_t(16 / epc);
+            t = &copies;
+          }
+        }
+      } else {
+        c = Choice{};
+      }
+    }
+  }
+  p.splits = c.splits;
+  p.part = reinterpret_cast<float*>(ws.p);
   switch (c.kernel) {
     case Choice::SIMPLE: e = launch_simple(bf16, form, group, p, t, st); break;
     case Choice::SKINNY: e = launch_skinny(bf16, form, group, c.mt, p, t, st); break;
@@ -200,33 +282,48 @@ hipError_t product(bool bf16, int form, int group, Product p, const Table* t, vo
   }
   return e == hipSuccess && c.splits > 1 ? launch_reduce(bf16, p, st) : e;
 }
-size_t product_bytes(bool bf16, int form, int64_t M, int64_t N, int64_t K) {
+// What product() can use.  copies: for operands at any alignment.
+size_t product_bytes(bool bf16, int form, int group, int64_t M, int64_t N, int64_t K, int64_t experts, bool act,
+                     bool copies) {
   if (M == 0 || K == 0) return 0;
-  return part_bytes(choose(bf16, form, GROUP_NONE, M, N, K, 0, true), M, N);
+  const int64_t epc = bf16 ? 8 : 4;
+  const Choice c = choose(bf16, form, group, M, N, K, experts, act);
+  size_t b = part_bytes(c, M, N);
+  if (copies && c.kernel != Choice::SKINNY)
+    b += copy_bytes(copy_of_a(form, M, K, epc), epc, 1) +
+         copy_bytes(copy_of_b(form, N, K, epc), epc, group == GROUP_ROWS ? experts : 1);
+  return b;
+}
+// Most of a layer's products, in either layout of the weight.
+size_t forward_bytes(int group, int64_t rows, int64_t inner, int64_t outer, int64_t experts, int32_t dtype,
+                     bool act, bool copies) {
+  const bool bf16 = dtype == MUON_BF16;
+  const size_t a = product_bytes(bf16, FORM_RT, group, rows, outer, inner, experts, act, copies);
+  const size_t b = product_bytes(bf16, FORM_RR, group, rows, outer, inner, experts, act, copies);
+  return a > b ? a : b;
+}
+size_t gradient_bytes(int group, int64_t rows, int64_t inner, int64_t outer, int64_t experts, int32_t dtype,
+                      bool copies) {
+  const bool bf16 = dtype == MUON_BF16;
+  const int sums = group == GROUP_ROWS ? GROUP_SUM : GROUP_NONE;
+  const size_t dx = forward_bytes(group, rows, outer, inner, experts, dtype, false, copies);
+  const size_t d1 = product_bytes(bf16, FORM_TT, sums, inner, outer, rows, experts, false, copies);
+  const size_t d2 = product_bytes(bf16, FORM_TT, sums, outer, inner, rows, experts, false, copies);
+  const size_t dw = d1 > d2 ? d1 : d2;
+  return dx > dw ? dx : dw;
 }
 
-// Workspace of muon_linear_backward: dz, the partial column sums and the
-// partial results of the two products (one after the other, in one place).  The
-// weight may come either way round.
+// Workspace of muon_linear_backward: dz, the partial column sums and the two
+// products' scratch memory (one after the other, in one place).
 struct BackwardLayout {
-  size_t dz = 0, sums = 0, part = 0, total = 0;
+  size_t dz = 0, sums = 0, scratch = 0, total = 0;
 };
-BackwardLayout backward_layout(int64_t rows, int64_t inner, int64_t outer, int32_t dtype, int32_t act) {
-  const bool bf16 = dtype == MUON_BF16;
+BackwardLayout backward_layout(int64_t rows, int64_t inner, int64_t outer, int32_t dtype, int32_t act, bool copies) {
   BackwardLayout l;
   if (act != MUON_ACT_NONE) l.sums = padded(size_t(rows) * size_t(outer) * size_of(dtype));
-  l.part = l.sums + padded(size_t(act_grad_chunks(rows, outer)) * size_t(outer) * 4);
-  size_t most = 0;
-  const size_t all[] = {product_bytes(bf16, FORM_RR, rows, inner, outer), product_bytes(bf16, FORM_RT, rows, inner, outer),
-                   product_bytes(bf16, FORM_TT, inner, outer, rows), product_bytes(bf16, FORM_TT, outer, inner, rows)};
-  for (size_t b : all) most = b > most ? b : most;
-  l.total = l.part + most;
+  l.scratch = l.sums + padded(size_t(act_grad_chunks(rows, outer)) * size_t(outer) * 4);
+  l.total = l.scratch + gradient_bytes(GROUP_NONE, rows, inner, outer, 0, dtype, copies);
   return l;
-}
-size_t forward_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype) {
-  const size_t a = product_bytes(dtype == MUON_BF16, FORM_RT, rows, outer, inner);
-  const size_t b = product_bytes(dtype == MUON_BF16, FORM_RR, rows, outer, inner);
-  return a > b ? a : b;
 }
 
 muon_status fill_table(const char* name, const void* const* p, int32_t n, bool may_be_null, size_t esize, Table& t) {
@@ -256,12 +353,14 @@ extern "C" {
 MUON_API const char* muon_layers_last_error(void) { return g_error; }
 
 MUON_API muon_status muon_linear_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype,
-                                                 int32_t activation, int32_t backward, size_t* bytes) {
+                                                 int32_t activation, int32_t flags, size_t* bytes) {
   if (!bytes) return fail(MUON_ERR_INVALID_ARG, "bytes is NULL");
   TRY(check_sizes(rows, inner, outer, dtype));
   TRY(check_activation(activation));
-  *bytes = backward ? backward_layout(rows, inner, outer, dtype, activation).total
-                    : forward_bytes(rows, inner, outer, dtype);
+  TRY(check_flags(flags));
+  const bool copies = flags & MUON_LAYERS_UNALIGNED;
+  *bytes = flags & MUON_LAYERS_BACKWARD ? backward_layout(rows, inner, outer, dtype, activation, copies).total
+                                        : forward_bytes(GROUP_NONE, rows, inner, outer, 0, dtype, activation != MUON_ACT_NONE, copies);
   return done(hipSuccess, "");
 }
 
@@ -280,7 +379,7 @@ MUON_API muon_status muon_linear_forward(const void* x, int64_t ldx, const void*
   if (residual) TRY(check_matrix("residual", residual, ldr, outer, es));
   if (preact) TRY(check_matrix("preact", preact, ldz, outer, es));
   TRY(check_vector("bias", bias, es));
-  TRY(check_workspace(workspace, workspace_bytes, forward_bytes(rows, inner, outer, dtype)));
+  TRY(check_workspace(workspace, workspace_bytes, forward_bytes(GROUP_NONE, rows, inner, outer, 0, dtype, activation != MUON_ACT_NONE, false)));
   Product p{};
   p.a = x; p.lda = ldx;
   p.b = w; p.ldb = ldw;
@@ -291,7 +390,7 @@ MUON_API muon_status muon_linear_forward(const void* x, int64_t ldx, const void*
   p.M = int32_t(rows); p.N = int32_t(outer); p.K = int32_t(inner);
   p.act = activation;
   return done(product(dtype == MUON_BF16, w_transposed ? FORM_RR : FORM_RT, GROUP_NONE, p, nullptr,
-                      workspace, hipStream_t(hip_stream)),
+                      Scratch{static_cast<char*>(workspace), workspace_bytes}, hipStream_t(hip_stream)),
               "linear forward");
 }
 
@@ -313,10 +412,11 @@ MUON_API muon_status muon_linear_backward(const void* dy, int64_t lddy, const vo
   }
   if (dw) TRY(check_matrix("dw", dw, lddw, w_transposed ? inner : outer, es));
   TRY(check_vector("dbias", dbias, es));
-  const BackwardLayout l = backward_layout(rows, inner, outer, dtype, activation);
+  const BackwardLayout l = backward_layout(rows, inner, outer, dtype, activation, false);
   TRY(check_workspace(workspace, workspace_bytes, l.total));
   const hipStream_t st = hipStream_t(hip_stream);
   char* ws = static_cast<char*>(workspace);
+  const Scratch scratch{ws ? ws + l.scratch : nullptr, workspace_bytes > l.scratch ? workspace_bytes - l.scratch : 0};
   const void* dz = dy;
   int64_t lddz = lddy;
   if ((act && rows) || dbias) {
@@ -339,7 +439,7 @@ MUON_API muon_status muon_linear_backward(const void* dy, int64_t lddy, const vo
     p.b = w; p.ldb = ldw;
     p.c = dx; p.ldc = lddx;
     p.M = int32_t(rows); p.N = int32_t(inner); p.K = int32_t(outer);
-    TRY(done(product(bf16, w_transposed ? FORM_RT : FORM_RR, GROUP_NONE, p, nullptr, ws + l.part, st), "linear input gradient"));
+    TRY(done(product(bf16, w_transposed ? FORM_RT : FORM_RR, GROUP_NONE, p, nullptr, scratch, st), "linear input gradient"));
   }
   if (dw) {
     Product p{};
@@ -349,19 +449,21 @@ MUON_API muon_status muon_linear_backward(const void* dy, int64_t lddy, const vo
     p.a = w_transposed ? dz : x; p.lda = w_transposed ? lddz : ldx;
     p.b = w_transposed ? x : dz; p.ldb = w_transposed ? ldx : lddz;
     p.M = int32_t(w_transposed ? outer : inner); p.N = int32_t(w_transposed ? inner : outer);
-    TRY(done(product(bf16, FORM_TT, GROUP_NONE, p, nullptr, ws + l.part, st), "linear weight gradient"));
+    TRY(done(product(bf16, FORM_TT, GROUP_NONE, p, nullptr, scratch, st), "linear weight gradient"));
   }
   return done(hipSuccess, "");
 }
 
 MUON_API muon_status muon_grouped_linear_workspace_bytes(int64_t rows, int64_t inner, int64_t outer, int32_t experts,
-                                                         int32_t dtype, int32_t backward, size_t* bytes) {
+                                                         int32_t dtype, int32_t flags, size_t* bytes) {
   if (!bytes) return fail(MUON_ERR_INVALID_ARG, "bytes is NULL");
   TRY(check_sizes(rows, inner, outer, dtype));
   if (experts < 1 || experts > MUON_GROUPED_MAX_EXPERTS)
     return fail(MUON_ERR_INVALID_ARG, "experts %d out of [1, %d]", experts, MUON_GROUPED_MAX_EXPERTS);
-  (void)backward;
-  *bytes = 0;
+  TRY(check_flags(flags));
+  const bool copies = flags & MUON_LAYERS_UNALIGNED;
+  *bytes = flags & MUON_LAYERS_BACKWARD ? gradient_bytes(GROUP_ROWS, rows, inner, outer, experts, dtype, copies)
+                                        : forward_bytes(GROUP_ROWS, rows, inner, outer, experts, dtype, false, copies);
   return done(hipSuccess, "");
 }
 
@@ -389,7 +491,7 @@ MUON_API muon_status muon_grouped_linear_forward(const void* x, int64_t ldx, con
   p.experts = experts;
   p.M = int32_t(rows); p.N = int32_t(outer); p.K = int32_t(inner);
   return done(product(dtype == MUON_BF16, w_transposed ? FORM_RR : FORM_RT, GROUP_ROWS, p, &t,
-                      nullptr, hipStream_t(hip_stream)),
+                      Scratch{static_cast<char*>(workspace), workspace_bytes}, hipStream_t(hip_stream)),
               "grouped linear forward");
 }
 
@@ -418,9 +520,10 @@ MUON_API muon_status muon_grouped_linear_backward(const void* dy, int64_t lddy, 
                   (long long)(w_transposed ? inner : outer));
   }
   size_t need = 0;
-  TRY(muon_grouped_linear_workspace_bytes(rows, inner, outer, experts, dtype, 1, &need));
+  TRY(muon_grouped_linear_workspace_bytes(rows, inner, outer, experts, dtype, MUON_LAYERS_BACKWARD, &need));
   TRY(check_workspace(workspace, workspace_bytes, need));
   const hipStream_t st = hipStream_t(hip_stream);
+  const Scratch scratch{static_cast<char*>(workspace), workspace_bytes};
   Product p{};
   p.offsets = offsets;
   p.experts = experts;
@@ -429,7 +532,7 @@ MUON_API muon_status muon_grouped_linear_backward(const void* dy, int64_t lddy, 
     p.ldb = ldw;
     p.c = dx; p.ldc = lddx;
     p.M = int32_t(rows); p.N = int32_t(inner); p.K = int32_t(outer);
-    TRY(done(product(bf16, w_transposed ? FORM_RT : FORM_RR, GROUP_ROWS, p, &tw, nullptr, st), "grouped input gradient"));
+    TRY(done(product(bf16, w_transposed ? FORM_RT : FORM_RR, GROUP_ROWS, p, &tw, scratch, st), "grouped input gradient"));
   }
   if (dw) {
     p.c = nullptr; p.ldc = lddw;
@@ -437,7 +540,7 @@ MUON_API muon_status muon_grouped_linear_backward(const void* dy, int64_t lddy, 
     p.a = w_transposed ? dy : x; p.lda = w_transposed ? lddy : ldx;
     p.b = w_transposed ? x : dy; p.ldb = w_transposed ? ldx : lddy;
     p.M = int32_t(w_transposed ? outer : inner); p.N = int32_t(w_transposed ? inner : outer);
-    TRY(done(product(bf16, FORM_TT, GROUP_SUM, p, &td, nullptr, st), "grouped weight gradients"));
+    TRY(done(product(bf16, FORM_TT, GROUP_SUM, p, &td, scratch, st), "grouped weight gradients"));
   }
   return done(hipSuccess, "");
 }

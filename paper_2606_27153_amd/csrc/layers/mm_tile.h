@@ -83,7 +83,7 @@ struct Loader {
       const int row = wid * RPC + lane / LPR, slot = lane % LPR;
       int chunk = slot;
       if constexpr (sizeof(E) == 2) chunk = (((slot >> 1) ^ seg_swz<ROWB>(row)) << 1) | (slot & 1);
-      const int col = min(chunk * EPC, valid - EPC);
+      const int col = min(chunk * EPC, (valid + EPC - 1) / EPC * EPC - EPC);   // (rows are whole chunks)
       step = BK * ld * int64_t(sizeof(E));
       off[0] = uint32_t(row * ld * int64_t(sizeof(E)) + col * int64_t(sizeof(E)));
       stride = uint32_t(4 * RPC * ld * int64_t(sizeof(E)));

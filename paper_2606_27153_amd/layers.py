@@ -126,6 +126,17 @@ class _On:
         return False
 
 
+def _flags(backward: int, x: torch.Tensor, outer: int, *addresses: int) -> int:
+    """Flags of the workspace functions: whether the pass is the backward one, and
+    whether an operand's rows are off 16-byte chunks (addresses: pointers, and
+    leading dimensions in bytes)."""
+    size = x.element_size()
+    bits = (x.size(1) * size) | (outer * size)
+    for a in addresses:
+        bits |= a
+    return backward | (2 if bits & 15 else 0)
+
+
 def _bytes(fn, *args) -> int:
     n = ctypes.c_size_t()
     LL.check(fn(*args, ctypes.byref(n)))
@@ -161,7 +172,9 @@ def linear_forward(x: torch.Tensor, weight: torch.Tensor, *, bias: Optional[torc
     with _On(x.device) as stream:
         y = torch.empty(rows, outer, dtype=x.dtype, device=x.device)
         z = torch.empty_like(y) if keep_preactivation and act else None
-        need = _bytes(lib.muon_linear_workspace_bytes, rows, inner, outer, code, act, 0)
+        size = x.element_size()
+        need = _bytes(lib.muon_linear_workspace_bytes, rows, inner, outer, code, act,
+                      _flags(0, x, outer, xp, ldx * size, wp, ldw * size))
         ws = _workspace(need, x)
         LL.check(lib.muon_linear_forward(xp, ldx, wp, ldw, wt, bp, rp, ldr, y.data_ptr(), outer,
                                          None if z is None else z.data_ptr(), outer, rows, inner, outer, code, act,
@@ -201,7 +214,9 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, *,
         dx = torch.empty(rows, inner, dtype=x.dtype, device=x.device) if input_grad else None
         dw = _like_weight(weight, wt) if weight_grad else None
         db = torch.empty(outer, dtype=x.dtype, device=x.device) if bias_grad else None
-        need = _bytes(lib.muon_linear_workspace_bytes, rows, inner, outer, code, act, 1)
+        size = x.element_size()
+        need = _bytes(lib.muon_linear_workspace_bytes, rows, inner, outer, code, act,
+                      _flags(1, x, outer, xp, ldx * size, wp, ldw * size, gp, ldg * size))
         ws = _workspace(need, x)
         LL.check(lib.muon_linear_backward(gp, ldg, xp, ldx, wp, ldw, wt, zp, ldz,
                                           None if dx is None else dx.data_ptr(), inner,
@@ -311,7 +326,9 @@ def grouped_linear_forward(x: torch.Tensor, weights: Weights, offsets: torch.Ten
     op = _offsets(offsets, n, x)
     with _On(x.device) as stream:
         y = torch.empty(rows, outer, dtype=x.dtype, device=x.device)
-        need = _bytes(lib.muon_grouped_linear_workspace_bytes, rows, inner, outer, n, code, 0)
+        size = x.element_size()
+        need = _bytes(lib.muon_grouped_linear_workspace_bytes, rows, inner, outer, n, code,
+                      _flags(0, x, outer, xp, ldx * size, ldw * size, *ptrs))
         ws = _workspace(need, x)
         LL.check(lib.muon_grouped_linear_forward(xp, ldx, (ctypes.c_void_p * n)(*ptrs), ldw, wt, op, n, y.data_ptr(),
                                                  outer, rows, inner, outer, code,
@@ -352,7 +369,9 @@ def grouped_linear_backward(dy: torch.Tensor, x: torch.Tensor, weights: Weights,
             dptrs = (ctypes.c_void_p * n)(*[base + i * step if want is None or want[i] else None for i in range(n)])
             if wt:
                 dw = dw.transpose(1, 2)
-        need = _bytes(lib.muon_grouped_linear_workspace_bytes, rows, inner, outer, n, code, 1)
+        size = x.element_size()
+        need = _bytes(lib.muon_grouped_linear_workspace_bytes, rows, inner, outer, n, code,
+                      _flags(1, x, outer, xp, ldx * size, ldw * size, gp, ldg * size, *ptrs))
         ws = _workspace(need, x)
         LL.check(lib.muon_grouped_linear_backward(gp, ldg, xp, ldx, (ctypes.c_void_p * n)(*ptrs), ldw, wt, op, n,
                                                   None if dx is None else dx.data_ptr(), inner, dptrs,
