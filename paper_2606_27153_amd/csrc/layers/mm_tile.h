@@ -251,129 +251,78 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
 }
 
 // The epilogue of a wave's piece.  Element q of block (i, j) is row 32 i +
-// lane % 32, column 32 j + 8 (q / 4) + 4 (lane / 32) + q % 4: four consecutive
-// columns per lane and group of q, which bias, activation and residual work on.
-// The results are rounded and exchanged between the wave's halves, so that a
-// lane stores 8 consecutive columns.  A lane's vector instructions are what this
-// costs -- with one wave per SIMD nothing else runs meanwhile -- so rows and
-// columns past the edge are masked per store, an address is a uniform pointer
-// plus one 32-bit lane offset, and only products that have an epilogue (EPI) get
-// its code.
-template <typename O>
-__device__ __forceinline__ void exchange(const float (&v)[2][4], O (&out)[8]) {
-  if constexpr (sizeof(O) == 2) {
-    uint32_t u[2][2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-        bf16x2 x;
-        x[0] = __bf16(v[s][2 * k]);
-        x[1] = __bf16(v[s][2 * k + 1]);
-        u[s][k] = __builtin_bit_cast(uint32_t, x);
-      }
-    uint32_t r[4];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      // the upper half of the first group against the lower half of the second
-      const auto x = __builtin_amdgcn_permlane32_swap(u[0][k], u[1][k], false, false);
-      r[k] = x[0];
-      r[2 + k] = x[1];
-    }
-    __builtin_memcpy(out, r, 16);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const auto x = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v[0][e]),
-                                                      __builtin_bit_cast(uint32_t, v[1][e]), false, false);
-      const uint32_t x0 = x[0], x1 = x[1];
-      out[e] = __builtin_bit_cast(float, x0);
-      out[4 + e] = __builtin_bit_cast(float, x1);
-    }
-  }
-}
-template <typename O>
-__device__ __forceinline__ void put8(O* base, uint32_t off, const O (&v)[8]) {
-  Packed8<O> x;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x.v[e] = v[e];
-  *reinterpret_cast<Packed8<O>*>(reinterpret_cast<char*>(base) + off) = x;
-}
-template <typename E>
-struct __attribute__((packed, aligned(sizeof(E)))) Packed4 {
-  E v[4];
+// lane % 32, column 32 j + 8 (q / 4) + 4 (lane / 32) + q % 4.  32 rows at a time
+// pass through the wave's own part of the ring (free by then) in fp32, so that a
+// lane then has 8 consecutive columns of a row, the same columns every time, and
+// every access to C, the residual and z is of whole lines.  (Stored from the
+// registers in pieces of 32 bytes a row, the weight gradients of 64 experts of
+// 1408 x 2048 took 224 us, 75 of them for the stores.)  A lane's vector
+// instructions count: with one wave per SIMD nothing else runs meanwhile.  OUT:
+// the type stored (E, or float for partial results, which get no epilogue).
+template <class C>
+struct Staging {
+  static constexpr int LD = C::WT + 4;                 // floats of a row: rows 4 banks apart
+  static constexpr int BYTES = 32 * LD * 4;            // of a wave
+  static constexpr int LPR = C::WT / 8, RPI = 64 / LPR;  // lanes of a row, rows of a store instruction
 };
-
-// OUT: the type stored (E, or float for partial results, which get no epilogue).
 template <class C, typename E, typename OUT, int ACT, bool EPI>
 __device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ldc, const Work<E>& o,
-                                            const f32x16 (&acc)[C::NB][C::NB], int wm, int wn, int lane) {
-  const int h = lane >> 5, r = lane & 31;
+                                            const f32x16 (&acc)[C::NB][C::NB], float* region, int wm, int wn,
+                                            int lane) {
+  using S = Staging<C>;
   const E* bias = EPI ? static_cast<const E*>(p.bias) : nullptr;
   const E* res = EPI ? static_cast<const E*>(p.res) : nullptr;
   E* z = EPI ? static_cast<E*>(p.z) : nullptr;
-  const int64_t m = o.m0 + wm, n = o.n0 + wn;
-  const uint32_t at = uint32_t(r) * uint32_t(ldc) * uint32_t(sizeof(OUT)) + 8 * h * uint32_t(sizeof(OUT));
-  const uint32_t zat = uint32_t(r) * uint32_t(p.ldz) * uint32_t(sizeof(E)) + 8 * h * uint32_t(sizeof(E));
-  const uint32_t rat = uint32_t(r) * uint32_t(p.ldr) * uint32_t(sizeof(E)) + 4 * h * uint32_t(sizeof(E));
-  static_for<2 * C::NB>([&](auto jg) {
-    constexpr int j = decltype(jg)::value / 2, g = decltype(jg)::value % 2 * 2, col = 32 * j + 8 * g;
-    const bool cols = wn + col + 8 * h < o.cols;      // (whole groups of 8: the columns' number is a multiple)
-    float bv[2][4] = {};
-    if (bias) {
+  const int r0 = lane / S::LPR, col = wn + lane % S::LPR * 8;   // this lane's first row of a pass, its columns
+  const bool in = col < o.cols;                                 // (whole groups of 8: N is a multiple)
+  float bv[8] = {};
+  if (bias && in) load8(bias + o.n0 + col, 8, bv);
+  const float* from = region + r0 * S::LD + lane % S::LPR * 8;
+  float* to = region + (lane & 31) * S::LD + 4 * (lane >> 5);
+  const int64_t m = o.m0 + wm + r0, n = o.n0 + col;
+  OUT* cp = c + m * ldc + n;
+  const E* rp = res + m * p.ldr + n;
+  E* zp = z + m * p.ldz + n;
+  int left = in ? o.rows - wm - r0 : 0;                         // rows from this lane's on
+  static_for<C::NB>([&](auto it) {
+    constexpr int i = decltype(it)::value;
+    static_for<4 * C::NB>([&](auto jg) {
+      constexpr int j = decltype(jg)::value / 4, g = decltype(jg)::value % 4;
+      *reinterpret_cast<f32x4*>(to + 32 * j + 8 * g) =
+          f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+    });
+#pragma unroll 2
+    for (int k = 0; k < 32 / S::RPI; ++k) {
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(from + k * S::RPI * S::LD);
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(from + k * S::RPI * S::LD + 4);
+      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      if (left > 0) {
+        if constexpr (EPI) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const int at4 = min(wn + col + 8 * s + 4 * h, o.cols - 4);
-        const Packed4<E> x = *reinterpret_cast<const Packed4<E>*>(bias + o.n0 + at4);
+          for (int e = 0; e < 8; ++e) v[e] += bv[e];
+          if (z) store8(zp, 8, v);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) bv[s][e] = float(x.v[e]);
+          for (int e = 0; e < 8; ++e) v[e] = act_one<ACT>(v[e]);
+          if (res) {
+            float rv[8];
+            load8(rp, 8, rv);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += rv[e];
+          }
+        }
+        store8(cp, 8, v);
+      }
+      left -= S::RPI;
+      cp += S::RPI * ldc;
+      if constexpr (EPI) {
+        rp += S::RPI * p.ldr;
+        zp += S::RPI * p.ldz;
       }
     }
-    static_for<C::NB>([&](auto it) {
-      constexpr int i = decltype(it)::value;
-      const bool in = cols && wm + 32 * i + r < o.rows;
-      float v[2][4];
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[s][e] = acc[i][j][4 * (g + s) + e];
-          // (in place: what the activations' code has in common, done ahead of
-          // the choice of one, would not fit the registers)
-          asm volatile("" : "+v"(v[s][e]));
-          if (EPI) v[s][e] += bv[s][e];
-        }
-      OUT out[8];
-      if constexpr (EPI) {
-        if (z) {
-          E zo[8];
-          exchange(v, zo);
-          if (in) put8(z + (m + 32 * i) * p.ldz + n + col, zat, zo);
-        }
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[s][e] = act_one<ACT>(v[s][e]);
-        if (res) {
-          const char* rp = reinterpret_cast<const char*>(res + (m + 32 * i) * p.ldr + n + col);
-#pragma unroll
-          for (int s = 0; s < 2; ++s)
-            if (wm + 32 * i + r < o.rows && wn + col + 8 * s < o.cols) {
-              const Packed4<E> x = *reinterpret_cast<const Packed4<E>*>(rp + rat + 8 * s * sizeof(E));
-#pragma unroll
-              for (int e = 0; e < 4; ++e) v[s][e] += float(x.v[e]);
-            }
-        }
-      }
-      exchange(v, out);
-      if (in) put8(c + (m + 32 * i) * ldc + n + col, at, out);
-      __builtin_amdgcn_sched_barrier(0);   // (loads gathered further ahead would not fit the registers)
-    });
   });
 }
 
-// Any number of columns, any leading dimension: element by element.
+// Any number of columns: element by element.
 template <class C, typename E, bool EPI>
 __device__ __forceinline__ void store_elements(const Product& p, const Work<E>& o, const f32x16 (&acc)[C::NB][C::NB],
                                                int wm, int wn, int lane) {
@@ -409,16 +358,15 @@ __device__ __forceinline__ void store_elements(const Product& p, const Work<E>& 
 
 template <class C, typename E, bool EPI>
 __device__ __forceinline__ void store_tile(const Product& p, const Work<E>& o, const f32x16 (&acc)[C::NB][C::NB],
-                                           int wm, int wn, int lane) {
-  constexpr int64_t kFar = int64_t(1) << 24;   // 31 rows of as many fp32 elements: below 2^32 bytes
-  if (p.N % 8 || p.ldc >= kFar || (EPI && (p.ldr >= kFar || p.ldz >= kFar))) {
+                                           float* region, int wm, int wn, int lane) {
+  if (p.N % 8) {
     store_elements<C, E, EPI>(p, o, acc, wm, wn, lane);
   } else if (p.splits > 1) {
-    store_piece<C, E, float, MUON_ACT_NONE, false>(p, p.part + int64_t(blockIdx.y) * p.M * p.N, p.N, o, acc, wm, wn,
-                                                   lane);
+    store_piece<C, E, float, MUON_ACT_NONE, false>(p, p.part + int64_t(blockIdx.y) * p.M * p.N, p.N, o, acc, region,
+                                                   wm, wn, lane);
   } else {
     with_act<EPI>(p.act, [&](auto act) {
-      store_piece<C, E, E, decltype(act)::value, EPI>(p, o.c, p.ldc, o, acc, wm, wn, lane);
+      store_piece<C, E, E, decltype(act)::value, EPI>(p, o.c, p.ldc, o, acc, region, wm, wn, lane);
     });
   }
 }
@@ -568,17 +516,16 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
   }
   ra.move(-ua);
   rb.move(C::UNIT - ub);
-  // The last slabs' loads (past K) and every wave's reads end here, and the ring
-  // takes the next tile's first slabs while this one is stored.
+  // the last slabs' loads (past K) and every wave's reads end here
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  const Work<E> o = w;
-  if (more) {
-    w = next;
-    fill();
-  }
-
-  store_tile<C, E, GROUP == GROUP_NONE && FORM != FORM_TT>(p, o, acc, wm, wn, lane);
+  static_assert(4 * Staging<C>::BYTES <= U * C::UNIT, "the waves' parts of the ring");
+  store_tile<C, E, GROUP == GROUP_NONE && FORM != FORM_TT>(
+      p, w, acc, reinterpret_cast<float*>(lds + wid * Staging<C>::BYTES), wm, wn, lane);
   if (!more) break;
+  // every wave's part is free again for the next tile's first slabs
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  w = next;
+  fill();
   }
 }
 
