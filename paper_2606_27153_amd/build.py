@@ -26,7 +26,7 @@ SOURCES = ["api.cpp", "plan.cpp", "ew_kernels.hip", "ns_gemm.hip", "ns_gemm_t256
            "ns_gemm_t256_bf16_sq.hip", "ns_gemm_t256_f16_bx.hip", "ns_gemm_t256_f16_sq.hip", "ns_tile_bf16.hip",
            "ns_tile_f16.hip", "ns_tile_f32.hip", "static_ws.hip"]
 LAYER_SOURCES = ["layers/layers_api.cpp", "layers/mm_simple.hip", "layers/mm_tile_256_bf16.hip",
-                 "layers/mm_tile_128_bf16.hip", "layers/mm_tile_128_f32.hip",
+                 "layers/mm_tile_128x256_bf16.hip", "layers/mm_tile_128_bf16.hip", "layers/mm_tile_128_f32.hip",
                  "layers/mm_tile_64_bf16.hip", "layers/mm_tile_64_f32.hip", "layers/mm_skinny.hip",
                  "layers/pack.hip", "layers/act_grad.hip", "layers/layer_norm.hip"]
 LAYER_LIB_PATH = os.path.join(PKG, "libmuon_layers.so")

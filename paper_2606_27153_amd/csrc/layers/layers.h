@@ -96,9 +96,11 @@ struct ActGradArgs {
 // Launchers: enqueue and return hipGetLastError's answer.
 hipError_t launch_simple(bool bf16, int form, int group, const Product& p, const Table* t, hipStream_t st);
 
-// Matrix-core kernels on tiles of 256 x 256 (bf16 only), 128 x 128 and 64 x 64;
+// Matrix-core kernels on tiles of 256 x 256 and 128 x 256 (bf16 only), 128 x 128
+// and 64 x 64;
 // the operands must suit them (tile_fits in layers_api.cpp).
 hipError_t launch_tile256_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st);
+hipError_t launch_tile128x256_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st);
 hipError_t launch_tile128_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st);
 hipError_t launch_tile128_f32(int form, int group, const Product& p, const Table* t, hipStream_t st);
 hipError_t launch_tile64_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st);

@@ -128,32 +128,40 @@ size_t copy_bytes(const PackOne& o, int64_t epc, int64_t copies) {
 // Which kernel runs a product, and into how many ranges it cuts the summed
 // dimension (plain products only: each range leaves an fp32 partial result).
 struct Choice {
-  enum Kernel { SIMPLE, SKINNY, TILE64, TILE128, TILE256 } kernel = SIMPLE;
+  enum Kernel { SIMPLE, SKINNY, TILE64, TILE128, TILE128X256, TILE256 } kernel = SIMPLE;
   int mt = 0;       // SKINNY: 16-row tiles per block
   int splits = 1;
 };
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Expected time of a tile kernel in us, from the measured time of a slab (64 K
-// in bf16, 32 in fp32) and of everything else of a tile (first loads, epilogue),
-// with the chip full and with a CU holding a single block.  Measured (bf16, us a
-// slab, full / alone): 256: 1.4 / 1.15, 128: 1.0 / 0.53 for the two blocks of a
-// CU, 64: 0.42 / 0.29; the rest 6, 4.5 and 3 us.  fp32's MFMAs are what a slab
-// takes: 1.8 us of the 128 tile, 0.45 of the 64 tile, twice that for two blocks.
-// An activation costs the 256 tile, which has nothing to run beside it, 8 us more.
-double tile_us(bool bf16, int tile, double blocks, double slabs, bool act) {
-  const double full = bf16 ? (tile == 256 ? 1.4 : tile == 128 ? 1.0 : 0.42) : tile == 128 ? 3.6 : 0.9;
-  const double alone = bf16 ? (tile == 256 ? 1.15 : tile == 128 ? 0.53 : 0.29) : tile == 128 ? 1.8 : 0.45;
-  const double rest = (tile == 256 ? 6 : tile == 128 ? 4.5 : 3) + (act && tile == 256 ? 8 : 0);
-  const double slots = tile == 256 ? kCUs : 2 * kCUs;
-  if (blocks <= kCUs) return slabs * alone + rest;
-  if (tile == 256) {
-    const double rounds = std::floor(blocks / slots), left = blocks - rounds * slots;
-    return rounds * (slabs * full + rest) + (left > 0 ? slabs * alone + rest : 0);
+// The tile kernels, and the measured times their expected run time is made of:
+// us a slab (64 K in bf16, 32 in fp32) with the chip full and with one block on a
+// CU, us for everything else of a tile (its first loads and its epilogue; act:
+// more for an activation where nothing runs beside it), and blocks per CU.  Where
+// two blocks share a CU, `full` is for the two.  fp32's slab times are its MFMAs'.
+struct TileKind {
+  Choice::Kernel kernel;
+  int tm, tn;
+  double full, alone, rest, act;
+  int per_cu;
+};
+constexpr TileKind kBf16Tiles[] = {{Choice::TILE256, 256, 256, 1.55, 1.1, 7, 8, 1},
+                                   {Choice::TILE128X256, 128, 256, 0.9, 0.66, 5, 4, 1},
+                                   {Choice::TILE128, 128, 128, 0.95, 0.53, 5, 0, 2},
+                                   {Choice::TILE64, 64, 64, 0.4, 0.29, 3, 0, 2}};
+constexpr TileKind kF32Tiles[] = {{Choice::TILE128, 128, 128, 3.6, 1.8, 4.5, 0, 2},
+                                  {Choice::TILE64, 64, 64, 0.9, 0.45, 3, 0, 2}};
+
+double tile_us(const TileKind& k, double blocks, double slabs, bool act) {
+  const double rest = k.rest + (act ? k.act : 0), cus = kCUs;
+  if (k.per_cu == 1) {
+    const double rounds = std::floor(blocks / cus), left = blocks - rounds * cus;
+    return rounds * (slabs * k.full + rest) +
+           (left > 0 ? slabs * (k.alone + (k.full - k.alone) * left / cus) + rest : 0);
   }
-  if (blocks <= slots) return slabs * (alone + (full - alone) * (blocks / kCUs - 1)) + rest;
-  return blocks / slots * (slabs * full + rest);
+  if (blocks <= cus) return slabs * k.alone + rest;
+  return (blocks <= 2 * cus ? 1 : blocks / (2 * cus)) * (slabs * k.full + rest);
 }
 
 // Partial results are written and read once in fp32 (4 bytes a pass at about
@@ -183,21 +191,23 @@ Choice choose(bool bf16, int form, int group, int64_t M, int64_t N, int64_t K, i
   }
   const int64_t bk = bf16 ? 64 : 32;
   double best = 0;
-  for (int tile : {256, 128, 64}) {
-    if (tile == 256 && !bf16) continue;
-    const int64_t nt = ceil_div(N, tile);
-    double blocks = double(ceil_div(M, tile) * nt), slabs = double(ceil_div(K, bk));
-    if (group == GROUP_ROWS) blocks = (double(M) / tile + 0.5 * (experts < M ? experts : M)) * nt;
+  const TileKind* kinds = bf16 ? kBf16Tiles : kF32Tiles;
+  for (int i = 0; i < (bf16 ? 4 : 2); ++i) {
+    const TileKind& k = kinds[i];
+    const int64_t nt = ceil_div(N, k.tn);
+    double blocks = double(ceil_div(M, k.tm) * nt), slabs = double(ceil_div(K, bk));
+    // experts: half a tile of rows (half a slab) is lost on each
+    if (group == GROUP_ROWS) blocks = (double(M) / k.tm + 0.5 * (experts < M ? experts : M)) * nt;
     if (group == GROUP_SUM) {
       blocks *= experts;
       slabs = double(K) / experts / bk + 0.5;
     }
     for (int s = 1; s <= 16; ++s) {
       if (s > 1 && (group != GROUP_NONE || slabs < 4 * s)) break;
-      const double us = tile_us(bf16, tile, blocks * s, std::ceil(slabs / s), act) + reduce_us(M, N, s);
+      const double us = tile_us(k, blocks * s, std::ceil(slabs / s), act) + reduce_us(M, N, s);
       if (best == 0 || us < best) {
         best = us;
-        c.kernel = tile == 256 ? Choice::TILE256 : tile == 128 ? Choice::TILE128 : Choice::TILE64;
+        c.kernel = k.kernel;
         c.splits = s;
       }
     }
@@ -278,6 +288,7 @@ hipError_t product(bool bf16, int form, int group, Product p, const Table* t, Sc
     case Choice::TILE128:
       e = bf16 ? launch_tile128_bf16(form, group, p, t, st) : launch_tile128_f32(form, group, p, t, st);
       break;
+    case Choice::TILE128X256: e = launch_tile128x256_bf16(form, group, p, t, st); break;
     case Choice::TILE256: e = launch_tile256_bf16(form, group, p, t, st); break;
   }
   return e == hipSuccess && c.splits > 1 ? launch_reduce(bf16, p, st) : e;

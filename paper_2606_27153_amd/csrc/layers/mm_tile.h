@@ -1,15 +1,15 @@
-// Matrix products on the matrix cores, one block of four waves per T x T tile
-// of C.
+// Matrix products on the matrix cores, one block of four waves per TM x TN
+// tile of C.
 //
 // K advances in slabs of 128 bytes of a K-contiguous row (64 bf16, 32 fp32).  An
 // operand's slab is a unit of the LDS ring, filled straight from global memory
 // (16 bytes per lane and instruction).  A "row" operand's unit holds its rows,
-// 128 bytes each; a "tr" operand's holds BK rows of T elements as they lie in
-// memory, and the fragment reads transpose: ds_read_b64_tr_b16 for bf16, single
+// 128 bytes each; a "tr" operand's holds BK rows of TM (TN) elements as they
+// lie in memory, and the fragment reads transpose: ds_read_b64_tr_b16 for bf16, single
 // words for fp32.  16-byte chunks (32-byte segments) are XOR-swizzled with the
 // row so that the fragment reads are free of bank conflicts.
 //
-// Each wave owns a (T / 2) x (T / 2) piece of 32 x 32 MFMA blocks.  A slab is
+// Each wave owns a (TM / 2) x (TN / 2) piece of 32 x 32 MFMA blocks.  A slab is
 // four K steps; the fragments of the next step are read while the current
 // step's MFMAs run, one memory instruction per MFMA or so.  The ring has U
 // units, A's and B's slabs in turn; before the last step of a slab comes the
@@ -36,15 +36,19 @@ namespace muon {
 namespace layers {
 namespace {
 
-template <typename E, int T_, int U_>
+template <typename E, int TM_, int TN_, int U_>
 struct Tile {
-  static constexpr int T = T_;                      // C's tile is T x T
+  static constexpr int TM = TM_, TN = TN_;          // C's tile
   static constexpr int U = U_;                      // units of the LDS ring
   static constexpr int EPC = 16 / int(sizeof(E));   // elements of a 16-byte chunk
   static constexpr int BK = 8 * EPC;                // K elements of a slab
-  static constexpr int WT = T / 2;                  // wave piece: WT x WT
-  static constexpr int NB = WT / 32;
-  static constexpr int UNIT = T * 128;              // bytes of one operand's slab
+  static constexpr int WTM = TM / 2, WTN = TN / 2;  // wave piece
+  static constexpr int NBM = WTM / 32, NBN = WTN / 32;
+  static constexpr int UA = TM * 128, UB = TN * 128;  // bytes of an operand's slab
+  static_assert(TM == TN || U % 2 == 0, "a slot holds A's and B's slabs in turn where U is odd");
+  // unit u's place in the ring, and the ring's bytes
+  static constexpr int at(int u) { return u / 2 * (UA + UB) + (u & 1) * UA; }
+  static constexpr int RING = U % 2 ? U * UA : U / 2 * (UA + UB);
 };
 
 __device__ const float4 kZeros[4] = {};
@@ -200,10 +204,10 @@ __device__ __forceinline__ int xcd_runs(int pid, int run) {
   return (round * 8 + (r & 7)) * run + (r >> 3);
 }
 
-template <typename E, int T, int U, int FORM, int GROUP>
+template <typename E, int TM, int TN, int U, int FORM, int GROUP>
 __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<GROUP>::T& tab, int pid, int run, int lane,
                                        Work<E>& w) {
-  const int nt = (p.N + T - 1) / T, mt = (p.M + T - 1) / T;
+  const int nt = (p.N + TN - 1) / TN, mt = (p.M + TM - 1) / TM;
   const E* a = static_cast<const E*>(p.a);
   const E* b = static_cast<const E*>(p.b);
   w.c = static_cast<E*>(p.c);
@@ -212,7 +216,7 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
   if constexpr (GROUP == GROUP_ROWS) {
     const int id = xcd_runs(pid, run);
     RowTile t;
-    if (!find_row_tile<T>(p.offsets, p.experts, p.M, id / nt, lane, t)) return false;
+    if (!find_row_tile<TM>(p.offsets, p.experts, p.M, id / nt, lane, t)) return false;
     ni = id % nt;
     w.m0 = t.row0;
     w.rows = t.rows;
@@ -230,8 +234,8 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
       expert_range(p.offsets, e, p.K, lane, k0, k1);
     } else {
       id = xcd_order(pid, mt * nt);
-      const int slabs = (p.K + Tile<E, T, U>::BK - 1) / Tile<E, T, U>::BK;
-      const int per = (slabs + p.splits - 1) / p.splits * Tile<E, T, U>::BK;
+      const int slabs = (p.K + Tile<E, TM, TN, U>::BK - 1) / Tile<E, TM, TN, U>::BK;
+      const int per = (slabs + p.splits - 1) / p.splits * Tile<E, TM, TN, U>::BK;
       k0 = min(p.K, int(blockIdx.y) * per);
       k1 = min(p.K, k0 + per);
     }
@@ -239,11 +243,11 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
     const int band = id / (8 * nt), in = id - band * 8 * nt, h = min(8, mt - band * 8);
     ni = in / h;
     mi = band * 8 + in - ni * h;
-    w.m0 = int64_t(mi) * T;
-    w.rows = min(T, p.M - int(w.m0));
+    w.m0 = int64_t(mi) * TM;
+    w.rows = min(TM, p.M - int(w.m0));
   }
-  w.n0 = int64_t(ni) * T;
-  w.cols = min(T, p.N - int(w.n0));
+  w.n0 = int64_t(ni) * TN;
+  w.cols = min(TN, p.N - int(w.n0));
   w.K = k1 - k0;
   w.a = FORM == FORM_TT ? a + k0 * p.lda + w.m0 : a + w.m0 * p.lda + k0;
   w.b = FORM == FORM_RR ? b + w.n0 * p.ldb + k0 : b + k0 * p.ldb + w.n0;
@@ -261,13 +265,13 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
 // the type stored (E, or float for partial results, which get no epilogue).
 template <class C>
 struct Staging {
-  static constexpr int LD = C::WT + 4;                 // floats of a row: rows 4 banks apart
+  static constexpr int LD = C::WTN + 4;                // floats of a row: rows 4 banks apart
   static constexpr int BYTES = 32 * LD * 4;            // of a wave
-  static constexpr int LPR = C::WT / 8, RPI = 64 / LPR;  // lanes of a row, rows of a store instruction
+  static constexpr int LPR = C::WTN / 8, RPI = 64 / LPR;  // lanes of a row, rows of a store instruction
 };
 template <class C, typename E, typename OUT, int ACT, bool EPI>
 __device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ldc, const Work<E>& o,
-                                            const f32x16 (&acc)[C::NB][C::NB], float* region, int wm, int wn,
+                                            const f32x16 (&acc)[C::NBM][C::NBN], float* region, int wm, int wn,
                                             int lane) {
   using S = Staging<C>;
   const E* bias = EPI ? static_cast<const E*>(p.bias) : nullptr;
@@ -284,9 +288,9 @@ __device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ld
   const E* rp = res + m * p.ldr + n;
   E* zp = z + m * p.ldz + n;
   int left = in ? o.rows - wm - r0 : 0;                         // rows from this lane's on
-  static_for<C::NB>([&](auto it) {
+  static_for<C::NBM>([&](auto it) {
     constexpr int i = decltype(it)::value;
-    static_for<4 * C::NB>([&](auto jg) {
+    static_for<4 * C::NBN>([&](auto jg) {
       constexpr int j = decltype(jg)::value / 4, g = decltype(jg)::value % 4;
       *reinterpret_cast<f32x4*>(to + 32 * j + 8 * g) =
           f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
@@ -324,10 +328,10 @@ __device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ld
 
 // Any number of columns: element by element.
 template <class C, typename E, bool EPI>
-__device__ __forceinline__ void store_elements(const Product& p, const Work<E>& o, const f32x16 (&acc)[C::NB][C::NB],
+__device__ __forceinline__ void store_elements(const Product& p, const Work<E>& o, const f32x16 (&acc)[C::NBM][C::NBN],
                                                int wm, int wn, int lane) {
-  static_for<C::NB>([&](auto jt) {
-    static_for<C::NB>([&](auto it) {
+  static_for<C::NBN>([&](auto jt) {
+    static_for<C::NBM>([&](auto it) {
       constexpr int i = decltype(it)::value, j = decltype(jt)::value;
       const int row = wm + 32 * i + (lane & 31);
       // (a loop over a copy in registers of its own would be one over memory)
@@ -357,7 +361,7 @@ __device__ __forceinline__ void store_elements(const Product& p, const Work<E>& 
 }
 
 template <class C, typename E, bool EPI>
-__device__ __forceinline__ void store_tile(const Product& p, const Work<E>& o, const f32x16 (&acc)[C::NB][C::NB],
+__device__ __forceinline__ void store_tile(const Product& p, const Work<E>& o, const f32x16 (&acc)[C::NBM][C::NBN],
                                            float* region, int wm, int wn, int lane) {
   if (p.N % 8) {
     store_elements<C, E, EPI>(p, o, acc, wm, wn, lane);
@@ -371,28 +375,28 @@ __device__ __forceinline__ void store_tile(const Product& p, const Work<E>& o, c
   }
 }
 
-template <typename E, int T, int U, int FORM, int GROUP>
-__global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
+template <typename E, int TM, int TN, int U, int FORM, int GROUP>
+__global__ __launch_bounds__(256, (Tile<E, TM, TN, U>::RING > 80 * 1024 ? 1 : 2)) void mm_tile_kernel(
     Product p, typename TableOf<GROUP>::T tab, int run, int blocks) {
-  using C = Tile<E, T, U>;
+  using C = Tile<E, TM, TN, U>;
   constexpr bool ATR = FORM == FORM_TT, BTR = FORM != FORM_RR;
-  __shared__ __attribute__((aligned(1024))) char lds[U * C::UNIT];
+  __shared__ __attribute__((aligned(1024))) char lds[C::RING];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // The block's tiles: blockIdx.x and every gridDim.x-th after it that exists.
   auto find = [&](int& pid, Work<E>& at) {
     for (; pid < blocks; pid += gridDim.x)
-      if (locate<E, T, U, FORM, GROUP>(p, tab, pid, run, lane, at)) return true;
+      if (locate<E, TM, TN, U, FORM, GROUP>(p, tab, pid, run, lane, at)) return true;
     return false;
   };
   Work<E> w;
   int pid = blockIdx.x;
   if (!find(pid, w)) return;
-  const int wm = (wid >> 1) * C::WT, wn = (wid & 1) * C::WT;
+  const int wm = (wid >> 1) * C::WTM, wn = (wid & 1) * C::WTN;
 
-  using LA = Loader<E, T, ATR>;
-  using LB = Loader<E, T, BTR>;
-  using RA = Reader<E, T, C::NB, ATR>;
-  using RB = Reader<E, T, C::NB, BTR>;
+  using LA = Loader<E, TM, ATR>;
+  using LB = Loader<E, TN, BTR>;
+  using RA = Reader<E, TM, C::NBM, ATR>;
+  using RB = Reader<E, TN, C::NBN, BTR>;
   typedef typename Frag<E>::T F;
   LA la;
   LB lb;
@@ -400,7 +404,7 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
   RB rb;
   ra.init(wm, lane);
   rb.init(wn, lane);
-  rb.move(C::UNIT);
+  rb.move(C::UA);
   const uint32_t base = lds_addr(lds);
   // The first U units of a tile's slabs.
   auto fill = [&]() {
@@ -408,27 +412,25 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
     lb.init(w.b, p.ldb, w.cols, w.K, wid, lane);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+      if (u & 1) {
 #pragma unroll
-      for (int i = 0; i < LA::N; ++i) {
-        if (u & 1)
-          lb.load(i, base + u * C::UNIT, wid);
-        else
-          la.load(i, base + u * C::UNIT, wid);
-      }
-      if (u & 1)
+        for (int i = 0; i < LB::N; ++i) lb.load(i, base + C::at(u), wid);
         lb.next();
-      else
+      } else {
+#pragma unroll
+        for (int i = 0; i < LA::N; ++i) la.load(i, base + C::at(u), wid);
         la.next();
+      }
     }
   };
   fill();
 
   for (;;) {
-  f32x16 acc[C::NB][C::NB];
+  f32x16 acc[C::NBM][C::NBN];
 #pragma unroll
-  for (int i = 0; i < C::NB; ++i)
+  for (int i = 0; i < C::NBM; ++i)
 #pragma unroll
-    for (int j = 0; j < C::NB; ++j)
+    for (int j = 0; j < C::NBN; ++j)
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
   // the next tile is looked up while this one's first loads arrive
@@ -437,11 +439,16 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
   const bool more = find(pid, next);
 
   const int nk = (w.K + C::BK - 1) / C::BK;
-  constexpr int LOADS = LA::N;                            // of a unit
-  F fa[2][C::NB], fb[2][C::NB];
+  // loads of units u0 .. u1 - 1
+  auto loads = [](int u0, int u1) constexpr {
+    int n = 0;
+    for (int u = u0; u < u1; ++u) n += u & 1 ? LB::N : LA::N;
+    return n;
+  };
+  F fa[2][C::NBM], fb[2][C::NBN];
   constexpr int READS = RA::READS + RB::READS;
   constexpr int Q = sizeof(E) == 2 ? 1 : 4;               // MFMAs per block and K step
-  constexpr int MFMAS = C::NB * C::NB * Q;
+  constexpr int MFMAS = C::NBM * C::NBN * Q;
   auto read_one = [&](int s, int r, int buf) {
     if (r < RB::READS)
       rb.read(lds, s, r, fb[buf]);
@@ -462,7 +469,7 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
 #pragma unroll
       for (int i = l0; i < l1; ++i)
         if ((i - l0) * MFMAS / (l1 - l0) == t) L.load(i, to, wid);
-      const int q = t / (C::NB * C::NB), ij = t % (C::NB * C::NB), i = ij / C::NB, j = ij % C::NB;
+      const int q = t / (C::NBM * C::NBN), ij = t % (C::NBM * C::NBN), i = ij / C::NBN, j = ij % C::NBN;
       acc[i][j] = mfma<E>(fb[buf][j], fa[buf][i], acc[i][j], q);
       __builtin_amdgcn_sched_barrier(0);
       if (t + 1 == MID) mid();
@@ -470,9 +477,9 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
   };
   auto nothing = []() {};
 
-  int ua = 0, ub = C::UNIT;   // the current slab's units
+  int ua = 0, ub = C::UA;   // the current slab's units
   if (nk > 0) {
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"((U - 2) * LOADS) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"(loads(2, U)) : "memory");
     __builtin_amdgcn_sched_barrier(0);
     uint32_t free1 = 0;         // the unit whose loads go out in steps 0 and 1
 #pragma unroll
@@ -480,25 +487,26 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
     // The loads that step 3 starts go first, and are A's where U is even.
     auto& first = pick<(U & 1) == 0>(la, lb);
     auto& second = pick<(U & 1) != 0>(la, lb);
-    constexpr int L1 = LOADS / 2;
-    auto wrap = [](int v) { return v >= U * C::UNIT ? v - U * C::UNIT : v; };
+    constexpr int L = (U & 1) ? LA::N : LB::N, L1 = L / 2;   // second's loads
+    constexpr int L0 = (U & 1) ? LB::N : LA::N;               // first's
+    auto wrap = [](int v) { return v >= C::RING ? v - C::RING : v; };
     // Step 2 reads the slab's last fragments early and meets the other waves
     // before its own last MFMAs: this slab is read, the next one has landed;
     // U - 4 units may be in flight.
     constexpr int EARLY = MFMAS >= 4 ? MFMAS / 2 : MFMAS;
     auto publish = [&]() {
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"((U - 4) * LOADS) : "memory");
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(loads(4, U)) : "memory");
       __builtin_amdgcn_sched_barrier(0);
     };
     auto last_step = [&]() {
       const uint32_t free0 = base + ua;
       free1 = base + ub;
-      const int na = wrap(ua + 2 * C::UNIT), nb = wrap(ub + 2 * C::UNIT);
+      const int na = wrap(ua + C::UA + C::UB), nb = wrap(ub + C::UA + C::UB);
       ra.move(na - ua);
       rb.move(nb - ub);
       ua = na;
       ub = nb;
-      k_step(first, 0, LOADS, 0, 1, free0, SPAN, nothing);
+      k_step(first, 0, L0, 0, 1, free0, SPAN, nothing);
       first.next();
     };
     // The first slab's steps load nothing: every unit of the ring is taken.
@@ -508,17 +516,17 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
     last_step();
     for (int kt = 1; kt < nk; ++kt) {
       k_step(second, 0, L1, 1, 0, free1, SPAN, nothing);
-      k_step(second, L1, LOADS, 2, 1, free1, SPAN, nothing);
+      k_step(second, L1, L, 2, 1, free1, SPAN, nothing);
       second.next();
       k_step(second, 0, 0, 3, 0, 0, EARLY, publish);
       last_step();
     }
   }
   ra.move(-ua);
-  rb.move(C::UNIT - ub);
+  rb.move(C::UA - ub);
   // the last slabs' loads (past K) and every wave's reads end here
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  static_assert(4 * Staging<C>::BYTES <= U * C::UNIT, "the waves' parts of the ring");
+  static_assert(4 * Staging<C>::BYTES <= C::RING, "the waves' parts of the ring");
   store_tile<C, E, GROUP == GROUP_NONE && FORM != FORM_TT>(
       p, w, acc, reinterpret_cast<float*>(lds + wid * Staging<C>::BYTES), wm, wn, lane);
   if (!more) break;
@@ -529,50 +537,53 @@ __global__ __launch_bounds__(256, T* U > 640 ? 1 : 2) void mm_tile_kernel(
   }
 }
 
-// Tiles in a row that one XCD takes of a grouped product (xcd_runs).
+// Tiles in a row that one XCD takes of a grouped product (xcd_runs).  Rows by
+// expert: two rows of tiles, which share the expert's weight in the XCD's L2 (64
+// experts, 24576 x 2048 x 1408: 179 us, 195 in runs of half a row).  Sums by
+// expert: half a row of tiles; experts differ in size, and short runs spread the
+// large ones over the XCDs (1408 x 2048: 255 us, 278 in runs of a whole expert).
 template <int GROUP>
-int run_length(int64_t mt, int64_t nt) {
-  return int(GROUP == GROUP_ROWS ? 2 * nt : mt * nt);
+int64_t run_length(int64_t nt) {
+  return GROUP == GROUP_ROWS ? 2 * nt : (nt + 1) / 2;
 }
 
-template <typename E, int T, int U, int FORM, int GROUP>
+template <typename E, int TM, int TN, int U, int FORM, int GROUP>
 hipError_t launch_one(const Product& p, const Table* t, hipStream_t st) {
-  const int64_t nt = (int64_t(p.N) + T - 1) / T, mt = (int64_t(p.M) + T - 1) / T;
+  const int64_t nt = (int64_t(p.N) + TN - 1) / TN, mt = (int64_t(p.M) + TM - 1) / TM;
   int64_t blocks = nt * mt;
   int run = 1;
-  if constexpr (GROUP == GROUP_ROWS) blocks = nt * row_tiles_bound(p.M, p.experts, T);
+  if constexpr (GROUP == GROUP_ROWS) blocks = nt * row_tiles_bound(p.M, p.experts, TM);
   if constexpr (GROUP == GROUP_SUM) blocks *= p.experts;
   if constexpr (GROUP != GROUP_NONE) {
-    const int64_t want = run_length<GROUP>(mt, nt), most = (blocks + 7) / 8;
+    const int64_t want = run_length<GROUP>(nt), most = (blocks + 7) / 8;
     run = int(want < most ? want : most);
     if (run < 1) run = 1;
     blocks = (blocks + 8 * run - 1) / (8 * run) * (8 * run);
   }
   if (blocks >= (int64_t(1) << 24)) return hipErrorInvalidConfiguration;
   if (!blocks) return hipSuccess;
-  // A block of the 256 tile has its CU to itself: no more of them than CUs, each
-  // with several tiles, so that a tile's first loads hide behind the stores of
-  // the one before.  The smaller tiles' blocks share a CU and hide each other's.
+  // A block whose ring fills a CU's LDS has the CU to itself: no more of them than
+  // CUs, each with several tiles.  The smaller tiles' blocks share a CU.
   int64_t grid = blocks;
-  if (T == 256 && grid > kCUs / p.splits) grid = kCUs / p.splits;
+  if (Tile<E, TM, TN, U>::RING > 80 * 1024 && grid > kCUs / p.splits) grid = kCUs / p.splits;
   const dim3 g{unsigned(grid), unsigned(p.splits)}, b{256};
   if constexpr (GROUP == GROUP_NONE)
-    hipLaunchKernelGGL((mm_tile_kernel<E, T, U, FORM, GROUP>), g, b, 0, st, p, NoTable{}, run, int(blocks));
+    hipLaunchKernelGGL((mm_tile_kernel<E, TM, TN, U, FORM, GROUP>), g, b, 0, st, p, NoTable{}, run, int(blocks));
   else
-    hipLaunchKernelGGL((mm_tile_kernel<E, T, U, FORM, GROUP>), g, b, 0, st, p, *t, run, int(blocks));
+    hipLaunchKernelGGL((mm_tile_kernel<E, TM, TN, U, FORM, GROUP>), g, b, 0, st, p, *t, run, int(blocks));
   return hipGetLastError();
 }
 
 // The forms and groupings the layers use.
-template <typename E, int T, int U>
+template <typename E, int TM, int TN, int U>
 hipError_t launch_form(int form, int group, const Product& p, const Table* t, hipStream_t st) {
-  if (group == GROUP_SUM) return launch_one<E, T, U, FORM_TT, GROUP_SUM>(p, t, st);
+  if (group == GROUP_SUM) return launch_one<E, TM, TN, U, FORM_TT, GROUP_SUM>(p, t, st);
   if (group == GROUP_ROWS)
-    return form == FORM_RT ? launch_one<E, T, U, FORM_RT, GROUP_ROWS>(p, t, st)
-                           : launch_one<E, T, U, FORM_RR, GROUP_ROWS>(p, t, st);
-  if (form == FORM_RT) return launch_one<E, T, U, FORM_RT, GROUP_NONE>(p, t, st);
-  if (form == FORM_RR) return launch_one<E, T, U, FORM_RR, GROUP_NONE>(p, t, st);
-  return launch_one<E, T, U, FORM_TT, GROUP_NONE>(p, t, st);
+    return form == FORM_RT ? launch_one<E, TM, TN, U, FORM_RT, GROUP_ROWS>(p, t, st)
+                           : launch_one<E, TM, TN, U, FORM_RR, GROUP_ROWS>(p, t, st);
+  if (form == FORM_RT) return launch_one<E, TM, TN, U, FORM_RT, GROUP_NONE>(p, t, st);
+  if (form == FORM_RR) return launch_one<E, TM, TN, U, FORM_RR, GROUP_NONE>(p, t, st);
+  return launch_one<E, TM, TN, U, FORM_TT, GROUP_NONE>(p, t, st);
 }
 
 }  // namespace

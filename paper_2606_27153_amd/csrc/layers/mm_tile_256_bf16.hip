@@ -5,7 +5,7 @@ namespace muon {
 namespace layers {
 
 hipError_t launch_tile256_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st) {
-  return launch_form<__bf16, 256, 5>(form, group, p, t, st);
+  return launch_form<__bf16, 256, 256, 5>(form, group, p, t, st);
 }
 
 }  // namespace layers
