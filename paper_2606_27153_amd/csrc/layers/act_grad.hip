@@ -56,24 +56,24 @@ __global__ __launch_bounds__(256) void act_grad_kernel(ActGradArgs a, int chunk)
   }
 }
 
-// Adds `chunks` rows of fp32 partial sums: 64 columns per block, its 16 waves
-// every 16th row, then their sums in order.
+// Adds `chunks` rows of fp32 partial sums: 16 columns per block, a thread every
+// 64th row of one of them, then their sums in order.
 template <typename E>
 __global__ __launch_bounds__(1024) void column_sum_kernel(const float* part, int chunks, int N, E* out) {
-  __shared__ float red[16][64];
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  const int col = blockIdx.x * 64 + lane;
+  __shared__ float red[64][17];
+  const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
+  const int col = blockIdx.x * 16 + c;
   float s = 0.f;
   if (col < N) {
-#pragma unroll 8
-    for (int r = wid; r < chunks; r += 16) s += part[int64_t(r) * N + col];
+#pragma unroll 4
+    for (int r = g; r < chunks; r += 64) s += part[int64_t(r) * N + col];
   }
-  red[wid][lane] = s;
+  red[g][c] = s;
   __syncthreads();
-  if (wid || col >= N) return;
+  if (g || col >= N) return;
   s = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s += red[i][lane];
+  for (int i = 0; i < 64; ++i) s += red[i][c];
   out[col] = E(s);
 }
 
@@ -125,7 +125,7 @@ hipError_t launch(const ActGradArgs& a, hipStream_t st) {
     if (e != hipSuccess) return e;
   }
   if (a.dbias)
-    hipLaunchKernelGGL((column_sum_kernel<E>), dim3(unsigned((int64_t(a.N) + 63) / 64)), dim3(1024), 0, st, a.part,
+    hipLaunchKernelGGL((column_sum_kernel<E>), dim3(unsigned((int64_t(a.N) + 15) / 16)), dim3(1024), 0, st, a.part,
                        chunks, a.N, static_cast<E*>(a.dbias));
   return hipGetLastError();
 }

@@ -187,8 +187,9 @@ __global__ __launch_bounds__(Shape<T>::THREADS) void norm_forward_kernel(NormArg
 
 // The columns' sums over a block's rows stay in registers; at the end its rows'
 // threads add theirs in order through LDS, into the block's rows of part.  SUMS:
-// whether dw and db are wanted.  The weights are read again for each row (from
-// the caches): the registers they would take are worth another wave.
+// whether dw and db are wanted.  The weights lie in LDS in fp32: the registers
+// they would take are worth another wave, and read from the caches for each row
+// they would hold up both its passes.
 template <typename E, int NV, int T, bool SUMS>
 __global__ __launch_bounds__(Shape<T>::THREADS, T < 1024 && NV * 16 / sizeof(E) <= 16 ? 3 : 1) void
 norm_backward_kernel(NormArgs a) {
@@ -196,7 +197,28 @@ norm_backward_kernel(NormArgs a) {
   constexpr int V = 16 / int(sizeof(E));
   __shared__ float red[2][2 * S::THREADS / 64];
   __shared__ float sums[SUMS && S::ROWS > 1 ? S::ROWS : 1][SUMS && S::ROWS > 1 ? T * NV * V : 1];
+  // thread t's chunk j at (j T + t) V, as it holds it
+  __shared__ __attribute__((aligned(16))) float weights[T * NV * V];
   const int t = threadIdx.x % T, row = threadIdx.x / T;
+  if (row == 0) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      float v[V];
+      load_weights<E>(a.weight, a.wf32, place<V, T>(t, j, a.cols).col, 1.f, v);
+#pragma unroll
+      for (int e = 0; e < V; ++e) weights[(j * T + t) * V + e] = v[e];
+    }
+  }
+  __syncthreads();
+  auto weight = [&](int j, float (&v)[V]) {
+#pragma unroll
+    for (int q = 0; q < V; q += 4) {
+      typedef float f4 __attribute__((ext_vector_type(4)));
+      const f4 x = *reinterpret_cast<const f4*>(weights + (j * T + t) * V + q);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[q + e] = x[e];
+    }
+  };
   const int64_t step = int64_t(gridDim.x) * S::ROWS;
   float pw[NV][V], pb[NV][V];
 #pragma unroll
@@ -233,15 +255,14 @@ norm_backward_kernel(NormArgs a) {
       dr[j] = d[j];
     }
     if constexpr (AHEAD) load(r + step);
-    // (a pointer of this row's own, so that its loads are not kept in registers)
-    const void* weight = a.weight;
-    asm volatile("" : "+s"(weight));
+    // (read anew in each pass, not kept in registers)
+    asm volatile("" ::: "memory");
     float s[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       float w[V];
       const Place at = place<V, T>(t, j, a.cols);
-      load_weights<E>(weight, a.wf32, at.col, 1.f, w);
+      weight(j, w);
       const int from = r < a.rows ? at.dup : V;   // (nothing of rows past the last)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
@@ -257,7 +278,7 @@ norm_backward_kernel(NormArgs a) {
       }
     }
     row_sums<T>(s, red[turn]);
-    asm volatile("" : "+s"(weight));
+    asm volatile("" ::: "memory");
     const float s1 = s[0] / float(a.cols), s2 = s[1] / float(a.cols);
     if (a.dx && r < a.rows) {
       E* dx = static_cast<E*>(a.dx) + r * a.lddx;
@@ -265,7 +286,7 @@ norm_backward_kernel(NormArgs a) {
       for (int j = 0; j < NV; ++j) {
         float w[V];
         const Place at = place<V, T>(t, j, a.cols);
-        load_weights<E>(weight, a.wf32, at.col, 1.f, w);
+        weight(j, w);
         Chunk<E> o;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
@@ -371,26 +392,26 @@ __global__ __launch_bounds__(256) void norm_backward_loop_kernel(NormArgs a) {
   }
 }
 
-// Sums the blocks' partial rows in order: 64 columns per block, its 16 waves
-// every 16th partial.  blockIdx.y: 0 for dw, 1 for db.
+// Sums the blocks' partial rows: 16 columns per block, a thread every 64th
+// partial of one of them, then their sums in order.  blockIdx.y: 0 for dw, 1 for db.
 template <typename E>
 __global__ __launch_bounds__(1024) void norm_column_sum_kernel(NormArgs a, int blocks) {
-  __shared__ float red[16][64];
+  __shared__ float red[64][17];
   void* out = blockIdx.y ? a.dbias : a.dweight;
   if (!out) return;
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  const int col = blockIdx.x * 64 + lane;
+  const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
+  const int col = blockIdx.x * 16 + c;
   float s = 0.f;
   if (col < a.cols) {
-#pragma unroll 8
-    for (int b = wid; b < blocks; b += 16) s += a.part[(int64_t(b) * 2 + blockIdx.y) * a.cols + col];
+#pragma unroll 4
+    for (int b = g; b < blocks; b += 64) s += a.part[(int64_t(b) * 2 + blockIdx.y) * a.cols + col];
   }
-  red[wid][lane] = s;
+  red[g][c] = s;
   __syncthreads();
-  if (wid || col >= a.cols) return;
+  if (g || col >= a.cols) return;
   s = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s += red[i][lane];
+  for (int i = 0; i < 64; ++i) s += red[i][c];
   if (a.wf32)
     static_cast<float*>(out)[col] = s;
   else
@@ -465,7 +486,7 @@ hipError_t backward(const NormArgs& a, hipStream_t st) {
     if (e != hipSuccess) return e;
   }
   if (a.dweight || a.dbias)
-    hipLaunchKernelGGL((norm_column_sum_kernel<E>), dim3(unsigned((int64_t(a.cols) + 63) / 64), 2), dim3(1024), 0, st,
+    hipLaunchKernelGGL((norm_column_sum_kernel<E>), dim3(unsigned((int64_t(a.cols) + 15) / 16), 2), dim3(1024), 0, st,
                        a, blocks);
   return hipGetLastError();
 }
