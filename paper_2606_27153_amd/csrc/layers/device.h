@@ -143,6 +143,57 @@ __device__ __forceinline__ void expert_range(const int32_t* off, int e, int rows
   hi = max(lo, __builtin_amdgcn_readfirstlane(clamp_row(off[e + 1], rows)));
 }
 
+// The experts by size: the ranks (0: most rows; the lower index first among
+// equals) of experts lane, lane + 64, ... .  All 64 lanes take part.
+struct Ranks {
+  static constexpr int N = MUON_GROUPED_MAX_EXPERTS / 64;
+  int rank[N];
+};
+__device__ __forceinline__ void rank_experts(const int32_t* off, int experts, int rows, int lane, Ranks& r) {
+  int size[Ranks::N];
+  int top = clamp_row(off[0], rows);
+#pragma unroll
+  for (int q = 0; q < Ranks::N; ++q) {
+    const int e = q * 64 + lane;
+    size[q] = -1;
+    r.rank[q] = -1;
+    if (q * 64 >= experts) continue;
+    int hi = clamp_row(off[min(e, experts - 1) + 1], rows);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int v = __shfl_up(hi, d);
+      if (lane >= d) hi = max(hi, v);
+    }
+    hi = max(hi, top);
+    int lo = __shfl_up(hi, 1);
+    if (lane == 0) lo = top;
+    top = __builtin_amdgcn_readlane(hi, 63);
+    if (e < experts) {
+      size[q] = hi - lo;
+      r.rank[q] = 0;
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < Ranks::N; ++p) {
+    for (int j = p * 64; j < min(experts, p * 64 + 64); ++j) {
+      const int s = __builtin_amdgcn_readlane(size[p], j & 63);
+#pragma unroll
+      for (int q = 0; q < Ranks::N; ++q)
+        if (q * 64 < experts && size[q] >= 0) r.rank[q] += s > size[q] || (s == size[q] && j < q * 64 + lane);
+    }
+  }
+}
+// The expert of rank `want` (< experts).
+__device__ __forceinline__ int expert_of_rank(const Ranks& r, int want) {
+  int e = 0;
+#pragma unroll
+  for (int q = 0; q < Ranks::N; ++q) {
+    const unsigned long long at = __ballot(r.rank[q] == want);
+    if (at) e = q * 64 + __builtin_ctzll(at);
+  }
+  return e;
+}
+
 // Row tile `want` (of TM rows each) of a product grouped by rows: the experts'
 // tiles in order, then those of the rows nobody owns.  Group g is the rows
 // before the first offset (g = 0), expert g - 1, or the rows after the last

@@ -206,7 +206,7 @@ __device__ __forceinline__ int xcd_runs(int pid, int run) {
 
 template <typename E, int TM, int TN, int U, int FORM, int GROUP>
 __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<GROUP>::T& tab, int pid, int run, int lane,
-                                       Work<E>& w) {
+                                       const Ranks& ranks, Work<E>& w) {
   const int nt = (p.N + TN - 1) / TN, mt = (p.M + TM - 1) / TM;
   const E* a = static_cast<const E*>(p.a);
   const E* b = static_cast<const E*>(p.b);
@@ -226,9 +226,10 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
     int id, mi;
     if constexpr (GROUP == GROUP_SUM) {
       id = xcd_runs(pid, run);
-      const int e = id / (mt * nt);
-      if (e >= p.experts) return false;
-      id -= e * (mt * nt);
+      const int at = id / (mt * nt);
+      if (at >= p.experts) return false;
+      id -= at * (mt * nt);
+      const int e = expert_of_rank(ranks, at);
       w.c = const_cast<E*>(static_cast<const E*>(tab.p[e]));
       if (!w.c) return false;
       expert_range(p.offsets, e, p.K, lane, k0, k1);
@@ -382,15 +383,24 @@ __global__ __launch_bounds__(256, (Tile<E, TM, TN, U>::RING > 80 * 1024 ? 1 : 2)
   constexpr bool ATR = FORM == FORM_TT, BTR = FORM != FORM_RR;
   __shared__ __attribute__((aligned(1024))) char lds[C::RING];
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // The block's tiles: blockIdx.x and every gridDim.x-th after it that exists.
-  auto find = [&](int& pid, Work<E>& at) {
-    for (; pid < blocks; pid += gridDim.x)
-      if (locate<E, TM, TN, U, FORM, GROUP>(p, tab, pid, run, lane, at)) return true;
+  // The block's tiles: one of each round of gridDim.x.  Sums by expert take the
+  // experts by falling size, and every other round in reverse, so that the blocks'
+  // shares come out alike (64 experts of uneven sizes, weight gradients of 1408 x
+  // 2048: in order of the experts the largest share was half as large again as
+  // the mean).
+  Ranks ranks;
+  if constexpr (GROUP == GROUP_SUM) rank_experts(p.offsets, p.experts, p.K, lane, ranks);
+  auto find = [&](int& round, Work<E>& at) {
+    for (; round * int(gridDim.x) < blocks; ++round) {
+      const int i = GROUP == GROUP_SUM && (round & 1) ? int(gridDim.x) - 1 - int(blockIdx.x) : int(blockIdx.x);
+      const int pid = round * int(gridDim.x) + i;
+      if (pid < blocks && locate<E, TM, TN, U, FORM, GROUP>(p, tab, pid, run, lane, ranks, at)) return true;
+    }
     return false;
   };
   Work<E> w;
-  int pid = blockIdx.x;
-  if (!find(pid, w)) return;
+  int round = 0;
+  if (!find(round, w)) return;
   const int wm = (wid >> 1) * C::WTM, wn = (wid & 1) * C::WTN;
 
   using LA = Loader<E, TM, ATR>;
@@ -435,8 +445,8 @@ __global__ __launch_bounds__(256, (Tile<E, TM, TN, U>::RING > 80 * 1024 ? 1 : 2)
       for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
   // the next tile is looked up while this one's first loads arrive
   Work<E> next;
-  pid += gridDim.x;
-  const bool more = find(pid, next);
+  ++round;
+  const bool more = find(round, next);
 
   const int nk = (w.K + C::BK - 1) / C::BK;
   // loads of units u0 .. u1 - 1
@@ -537,14 +547,12 @@ __global__ __launch_bounds__(256, (Tile<E, TM, TN, U>::RING > 80 * 1024 ? 1 : 2)
   }
 }
 
-// Tiles in a row that one XCD takes of a grouped product (xcd_runs).  Rows by
-// expert: two rows of tiles, which share the expert's weight in the XCD's L2 (64
-// experts, 24576 x 2048 x 1408: 179 us, 195 in runs of half a row).  Sums by
-// expert: half a row of tiles; experts differ in size, and short runs spread the
-// large ones over the XCDs (1408 x 2048: 255 us, 278 in runs of a whole expert).
+// Tiles in a row that one XCD takes of a grouped product (xcd_runs), which share
+// operands in its L2.  Sums by expert: a whole expert.  Rows by expert: eight rows
+// of tiles, an expert or two.
 template <int GROUP>
-int64_t run_length(int64_t nt) {
-  return GROUP == GROUP_ROWS ? 2 * nt : (nt + 1) / 2;
+int64_t run_length(int64_t mt, int64_t nt) {
+  return GROUP == GROUP_ROWS ? 8 * nt : mt * nt;
 }
 
 template <typename E, int TM, int TN, int U, int FORM, int GROUP>
@@ -555,7 +563,7 @@ hipError_t launch_one(const Product& p, const Table* t, hipStream_t st) {
   if constexpr (GROUP == GROUP_ROWS) blocks = nt * row_tiles_bound(p.M, p.experts, TM);
   if constexpr (GROUP == GROUP_SUM) blocks *= p.experts;
   if constexpr (GROUP != GROUP_NONE) {
-    const int64_t want = run_length<GROUP>(nt), most = (blocks + 7) / 8;
+    const int64_t want = run_length<GROUP>(mt, nt), most = (blocks + 7) / 8;
     run = int(want < most ? want : most);
     if (run < 1) run = 1;
     blocks = (blocks + 8 * run - 1) / (8 * run) * (8 * run);

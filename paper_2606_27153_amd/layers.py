@@ -18,6 +18,7 @@ TypeError before anything is launched.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import Optional, Sequence, Union
 
 import torch
@@ -105,25 +106,21 @@ def _activation(name: str) -> int:
     return code
 
 
-class _On:
-    """Makes the tensors' device current for a call, if it is not already, and
-    names torch's current stream there."""
+def _on_device(fn):
+    """Runs fn with its first tensor's device current (which it nearly always is)."""
+    @functools.wraps(fn)
+    def run(*args, **kwargs):
+        index = (args[0] if args else next(iter(kwargs.values()))).device.index
+        if index is None or index == torch._C._cuda_getDevice():
+            return fn(*args, **kwargs)
+        with torch.cuda.device(index):
+            return fn(*args, **kwargs)
+    return run
 
-    def __init__(self, device):
-        self.index = device.index
-        self.before = None
 
-    def __enter__(self):
-        now = torch.cuda.current_device()
-        if now != self.index:
-            self.before = now
-            torch.cuda.set_device(self.index)
-        return torch._C._cuda_getCurrentRawStream(self.index)
-
-    def __exit__(self, *exc):
-        if self.before is not None:
-            torch.cuda.set_device(self.before)
-        return False
+def _stream(t: torch.Tensor) -> int:
+    """torch's current stream on the tensor's device."""
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
 
 
 def _flags(backward: int, x: torch.Tensor, outer: int, *addresses: int) -> int:
@@ -151,6 +148,7 @@ def _workspace(n: int, like: torch.Tensor):
 
 # ------------------------------------------------------------------- linear
 
+@_on_device
 def linear_forward(x: torch.Tensor, weight: torch.Tensor, *, bias: Optional[torch.Tensor] = None,
                    residual: Optional[torch.Tensor] = None, activation: str = "none",
                    keep_preactivation: bool = False):
@@ -169,16 +167,16 @@ def linear_forward(x: torch.Tensor, weight: torch.Tensor, *, bias: Optional[torc
         raise ValueError("weight has no output features")
     bp = _vector(bias, "bias", x, outer)
     rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", x, rows, outer)
-    with _On(x.device) as stream:
-        y = torch.empty(rows, outer, dtype=x.dtype, device=x.device)
-        z = torch.empty_like(y) if keep_preactivation and act else None
-        size = x.element_size()
-        need = _bytes(lib.muon_linear_workspace_bytes, rows, inner, outer, code, act,
-                      _flags(0, x, outer, xp, ldx * size, wp, ldw * size))
-        ws = _workspace(need, x)
-        LL.check(lib.muon_linear_forward(xp, ldx, wp, ldw, wt, bp, rp, ldr, y.data_ptr(), outer,
-                                         None if z is None else z.data_ptr(), outer, rows, inner, outer, code, act,
-                                         None if ws is None else ws.data_ptr(), need, stream))
+    stream = _stream(x)
+    y = torch.empty(rows, outer, dtype=x.dtype, device=x.device)
+    z = torch.empty_like(y) if keep_preactivation and act else None
+    size = x.element_size()
+    need = _bytes(lib.muon_linear_workspace_bytes, rows, inner, outer, code, act,
+                  _flags(0, x, outer, xp, ldx * size, wp, ldw * size))
+    ws = _workspace(need, x)
+    LL.check(lib.muon_linear_forward(xp, ldx, wp, ldw, wt, bp, rp, ldr, y.data_ptr(), outer,
+                                     None if z is None else z.data_ptr(), outer, rows, inner, outer, code, act,
+                                     None if ws is None else ws.data_ptr(), need, stream))
     return (y, z) if keep_preactivation else y
 
 
@@ -189,6 +187,7 @@ def _like_weight(weight: torch.Tensor, transposed: int) -> torch.Tensor:
     return torch.empty(weight.size(0), weight.size(1), dtype=weight.dtype, device=weight.device)
 
 
+@_on_device
 def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, *,
                     preactivation: Optional[torch.Tensor] = None, activation: str = "none", bias_grad: bool = False,
                     input_grad: bool = True, weight_grad: bool = True):
@@ -210,19 +209,19 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, *,
         if preactivation is None:
             raise ValueError(f"the backward pass of {activation!r} needs the forward pass's preactivation")
         zp, ldz = _rows(preactivation, "preactivation", x, rows, outer)
-    with _On(x.device) as stream:
-        dx = torch.empty(rows, inner, dtype=x.dtype, device=x.device) if input_grad else None
-        dw = _like_weight(weight, wt) if weight_grad else None
-        db = torch.empty(outer, dtype=x.dtype, device=x.device) if bias_grad else None
-        size = x.element_size()
-        need = _bytes(lib.muon_linear_workspace_bytes, rows, inner, outer, code, act,
-                      _flags(1, x, outer, xp, ldx * size, wp, ldw * size, gp, ldg * size))
-        ws = _workspace(need, x)
-        LL.check(lib.muon_linear_backward(gp, ldg, xp, ldx, wp, ldw, wt, zp, ldz,
-                                          None if dx is None else dx.data_ptr(), inner,
-                                          None if dw is None else dw.data_ptr(), inner if wt else outer,
-                                          None if db is None else db.data_ptr(), rows, inner, outer, code, act,
-                                          None if ws is None else ws.data_ptr(), need, stream))
+    stream = _stream(x)
+    dx = torch.empty(rows, inner, dtype=x.dtype, device=x.device) if input_grad else None
+    dw = _like_weight(weight, wt) if weight_grad else None
+    db = torch.empty(outer, dtype=x.dtype, device=x.device) if bias_grad else None
+    size = x.element_size()
+    need = _bytes(lib.muon_linear_workspace_bytes, rows, inner, outer, code, act,
+                  _flags(1, x, outer, xp, ldx * size, wp, ldw * size, gp, ldg * size))
+    ws = _workspace(need, x)
+    LL.check(lib.muon_linear_backward(gp, ldg, xp, ldx, wp, ldw, wt, zp, ldz,
+                                      None if dx is None else dx.data_ptr(), inner,
+                                      None if dw is None else dw.data_ptr(), inner if wt else outer,
+                                      None if db is None else db.data_ptr(), rows, inner, outer, code, act,
+                                      None if ws is None else ws.data_ptr(), need, stream))
     return dx, dw, db
 
 
@@ -311,6 +310,7 @@ def _offsets(offsets: torch.Tensor, n: int, like: torch.Tensor) -> int:
     return offsets.data_ptr()
 
 
+@_on_device
 def grouped_linear_forward(x: torch.Tensor, weights: Weights, offsets: torch.Tensor) -> torch.Tensor:
     """``y[t] = x[t] @ weights[e]`` for offsets[e] <= t < offsets[e + 1]: rows
     sorted by expert, int32 offsets on the GPU (the host never reads them).
@@ -324,18 +324,19 @@ def grouped_linear_forward(x: torch.Tensor, weights: Weights, offsets: torch.Ten
     if outer == 0:
         raise ValueError("the weights have no output features")
     op = _offsets(offsets, n, x)
-    with _On(x.device) as stream:
-        y = torch.empty(rows, outer, dtype=x.dtype, device=x.device)
-        size = x.element_size()
-        need = _bytes(lib.muon_grouped_linear_workspace_bytes, rows, inner, outer, n, code,
-                      _flags(0, x, outer, xp, ldx * size, ldw * size, *ptrs))
-        ws = _workspace(need, x)
-        LL.check(lib.muon_grouped_linear_forward(xp, ldx, (ctypes.c_void_p * n)(*ptrs), ldw, wt, op, n, y.data_ptr(),
-                                                 outer, rows, inner, outer, code,
-                                                 None if ws is None else ws.data_ptr(), need, stream))
+    stream = _stream(x)
+    y = torch.empty(rows, outer, dtype=x.dtype, device=x.device)
+    size = x.element_size()
+    need = _bytes(lib.muon_grouped_linear_workspace_bytes, rows, inner, outer, n, code,
+                  _flags(0, x, outer, xp, ldx * size, ldw * size, *ptrs))
+    ws = _workspace(need, x)
+    LL.check(lib.muon_grouped_linear_forward(xp, ldx, (ctypes.c_void_p * n)(*ptrs), ldw, wt, op, n, y.data_ptr(),
+                                             outer, rows, inner, outer, code,
+                                             None if ws is None else ws.data_ptr(), need, stream))
     return y
 
 
+@_on_device
 def grouped_linear_backward(dy: torch.Tensor, x: torch.Tensor, weights: Weights, offsets: torch.Tensor, *,
                             input_grad: bool = True, weight_grad: Union[bool, Sequence[bool]] = True):
     """Gradients ``(dx, dweights)`` of ``grouped_linear_forward``.  dweights is
@@ -358,25 +359,25 @@ def grouped_linear_backward(dy: torch.Tensor, x: torch.Tensor, weights: Weights,
         if len(want) != n:
             raise ValueError(f"weight_grad names {len(want)} experts, there are {n}")
         weight_grad = any(want)
-    with _On(x.device) as stream:
-        dx = torch.empty(rows, inner, dtype=x.dtype, device=x.device) if input_grad else None
-        dw = dptrs = None
-        if weight_grad:
-            a, b = (outer, inner) if wt else (inner, outer)
-            dw = torch.empty(n, a, b, dtype=x.dtype, device=x.device)
-            step = a * b * dw.element_size()
-            base = dw.data_ptr()
-            dptrs = (ctypes.c_void_p * n)(*[base + i * step if want is None or want[i] else None for i in range(n)])
-            if wt:
-                dw = dw.transpose(1, 2)
-        size = x.element_size()
-        need = _bytes(lib.muon_grouped_linear_workspace_bytes, rows, inner, outer, n, code,
-                      _flags(1, x, outer, xp, ldx * size, ldw * size, gp, ldg * size, *ptrs))
-        ws = _workspace(need, x)
-        LL.check(lib.muon_grouped_linear_backward(gp, ldg, xp, ldx, (ctypes.c_void_p * n)(*ptrs), ldw, wt, op, n,
-                                                  None if dx is None else dx.data_ptr(), inner, dptrs,
-                                                  inner if wt else outer, rows, inner, outer, code,
-                                                  None if ws is None else ws.data_ptr(), need, stream))
+    stream = _stream(x)
+    dx = torch.empty(rows, inner, dtype=x.dtype, device=x.device) if input_grad else None
+    dw = dptrs = None
+    if weight_grad:
+        a, b = (outer, inner) if wt else (inner, outer)
+        dw = torch.empty(n, a, b, dtype=x.dtype, device=x.device)
+        step = a * b * dw.element_size()
+        base = dw.data_ptr()
+        dptrs = (ctypes.c_void_p * n)(*[base + i * step if want is None or want[i] else None for i in range(n)])
+        if wt:
+            dw = dw.transpose(1, 2)
+    size = x.element_size()
+    need = _bytes(lib.muon_grouped_linear_workspace_bytes, rows, inner, outer, n, code,
+                  _flags(1, x, outer, xp, ldx * size, ldw * size, gp, ldg * size, *ptrs))
+    ws = _workspace(need, x)
+    LL.check(lib.muon_grouped_linear_backward(gp, ldg, xp, ldx, (ctypes.c_void_p * n)(*ptrs), ldw, wt, op, n,
+                                              None if dx is None else dx.data_ptr(), inner, dptrs,
+                                              inner if wt else outer, rows, inner, outer, code,
+                                              None if ws is None else ws.data_ptr(), need, stream))
     if dw is not None and (want is not None or not isinstance(weights, torch.Tensor)):
         dw = [dw[i] if want is None or want[i] else None for i in range(n)]
     return dx, dw
@@ -434,6 +435,7 @@ def _norm_vectors(x: torch.Tensor, vectors, cols: int):
     return (*ptrs, _DTYPES[x.dtype] if code is None else code)
 
 
+@_on_device
 def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
                        eps: float = 1e-5, keep_stats: bool = False):
     """Layer norm over the columns of x [rows, cols].  With ``keep_stats``
@@ -444,18 +446,19 @@ def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, b
     rows, cols = x.shape
     xp, ldx = _rows(x, "x", x, rows, cols)
     wp, bp, wcode = _norm_vectors(x, (("weight", weight), ("bias", bias)), cols)
-    with _On(x.device) as stream:
-        y = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
-        mean = rstd = None
-        if keep_stats:
-            mean, rstd = torch.empty(2, rows, dtype=torch.float32, device=x.device).unbind(0)
-        LL.check(lib.muon_layer_norm_forward(xp, ldx, wp, bp, y.data_ptr(), cols,
-                                             None if mean is None else mean.data_ptr(),
-                                             None if rstd is None else rstd.data_ptr(), rows, cols, eps, code, wcode,
-                                             stream))
+    stream = _stream(x)
+    y = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
+    mean = rstd = None
+    if keep_stats:
+        mean, rstd = torch.empty(2, rows, dtype=torch.float32, device=x.device).unbind(0)
+    LL.check(lib.muon_layer_norm_forward(xp, ldx, wp, bp, y.data_ptr(), cols,
+                                         None if mean is None else mean.data_ptr(),
+                                         None if rstd is None else rstd.data_ptr(), rows, cols, eps, code, wcode,
+                                         stream))
     return (y, mean, rstd) if keep_stats else y
 
 
+@_on_device
 def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor,
                         rstd: torch.Tensor, *, input_grad: bool = True, weight_grad: bool = True,
                         bias_grad: bool = True):
@@ -474,18 +477,18 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
             raise ValueError(f"{name} must be a contiguous float32 vector of {rows} elements")
         if t.device != x.device:
             raise ValueError(f"{name} is on {t.device}, expected {x.device}")
-    with _On(x.device) as stream:
-        dx = torch.empty(rows, cols, dtype=x.dtype, device=x.device) if input_grad else None
-        wdt = torch.float32 if wcode == MUON_F32 else x.dtype
-        dw = torch.empty(cols, dtype=wdt, device=x.device) if weight_grad else None
-        db = torch.empty(cols, dtype=wdt, device=x.device) if bias_grad else None
-        need = _bytes(lib.muon_layer_norm_workspace_bytes, rows, cols) if weight_grad or bias_grad else 0
-        ws = _workspace(need, x)
-        LL.check(lib.muon_layer_norm_backward(gp, ldg, xp, ldx, wp, mean.data_ptr(), rstd.data_ptr(),
-                                              None if dx is None else dx.data_ptr(), cols,
-                                              None if dw is None else dw.data_ptr(),
-                                              None if db is None else db.data_ptr(), rows, cols, code, wcode,
-                                              None if ws is None else ws.data_ptr(), need, stream))
+    stream = _stream(x)
+    dx = torch.empty(rows, cols, dtype=x.dtype, device=x.device) if input_grad else None
+    wdt = torch.float32 if wcode == MUON_F32 else x.dtype
+    dw = torch.empty(cols, dtype=wdt, device=x.device) if weight_grad else None
+    db = torch.empty(cols, dtype=wdt, device=x.device) if bias_grad else None
+    need = _bytes(lib.muon_layer_norm_workspace_bytes, rows, cols) if weight_grad or bias_grad else 0
+    ws = _workspace(need, x)
+    LL.check(lib.muon_layer_norm_backward(gp, ldg, xp, ldx, wp, mean.data_ptr(), rstd.data_ptr(),
+                                          None if dx is None else dx.data_ptr(), cols,
+                                          None if dw is None else dw.data_ptr(),
+                                          None if db is None else db.data_ptr(), rows, cols, code, wcode,
+                                          None if ws is None else ws.data_ptr(), need, stream))
     return dx, dw, db
 
 
