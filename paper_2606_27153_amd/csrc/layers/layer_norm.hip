@@ -37,8 +37,8 @@ __device__ __forceinline__ float weight_at(const void* w, int, int64_t i, const 
 }
 
 // Rows that fit the registers of T threads stay there: one read of x (and dy),
-// one write.  T is 64 -- a wave per row, no barrier -- for short rows, then 256
-// or 1024 threads.  A block holds a few rows at a time and takes every
+// one write.  T is 64 -- a wave per row, no barrier -- for short rows, then 256,
+// 512 or 1024 threads.  A block holds a few rows at a time and takes every
 // gridDim.x-th group of them; the next group's loads are issued before the
 // current one is reduced, so that the memory never waits for the reductions.
 // Loads and stores are 16 bytes at any alignment, and no load sits in a branch
@@ -225,8 +225,8 @@ norm_backward_kernel(NormArgs a) {
   for (int j = 0; j < NV; ++j)
 #pragma unroll
     for (int e = 0; e < V; ++e) pw[j][e] = pb[j][e] = 0.f;
-  // (with 1024 threads the registers hold one row only)
-  constexpr bool AHEAD = T < 1024;
+  // (with 512 threads the registers hold one row only)
+  constexpr bool AHEAD = T < 512;
   Chunk<E> x[NV], d[NV];
   float mean = 0.f, rstd = 0.f;
   auto load = [&](int64_t r) {
@@ -419,14 +419,16 @@ __global__ __launch_bounds__(1024) void norm_column_sum_kernel(NormArgs a, int b
 }
 
 // Threads per row, so that a thread holds at most 32 elements (16 with 1024
-// threads) forward, 24 (8) backward, where the sums take registers too.  0: the row
+// threads) forward, 24 (32 with 512 threads, which hold no second row) backward,
+// where the sums take registers too.  0: the row
 // does not fit, or is shorter than a chunk.
 int forward_threads(int64_t cols) { return cols < 8 ? 0 : cols <= 2048 ? 64 : cols <= 8192 ? 256 : cols <= 16384 ? 1024 : 0; }
-int backward_threads(int64_t cols) { return cols < 8 ? 0 : cols <= 1536 ? 64 : cols <= 6144 ? 256 : cols <= 8192 ? 1024 : 0; }
+int backward_threads(int64_t cols) { return cols < 8 ? 0 : cols <= 1536 ? 64 : cols <= 6144 ? 256 : cols <= 16384 ? 512 : 0; }
 
-// f(chunks per thread tag, threads tag) for rows of `cols` on t threads: the
+// f(chunks per thread tag, threads tag) for rows of `cols` on t threads (64, 256 or
+// MOST): the
 // smallest chunk count that covers them, in quarters of 32 elements.
-template <typename E, class F>
+template <typename E, int MOST, class F>
 void with_shape(int64_t cols, int t, F f) {
   constexpr int V = 16 / int(sizeof(E)), Q = 8 / V;
   const int64_t nv = (cols + int64_t(V) * t - 1) / (int64_t(V) * t);
@@ -438,7 +440,7 @@ void with_shape(int64_t cols, int t, F f) {
   };
   if (t == 64) at(IntTag<64>{});
   else if (t == 256) at(IntTag<256>{});
-  else at(IntTag<1024>{});
+  else at(IntTag<MOST>{});
 }
 
 template <typename E>
@@ -448,7 +450,7 @@ hipError_t forward(const NormArgs& a, hipStream_t st) {
   if (!t) {
     hipLaunchKernelGGL((norm_forward_loop_kernel<E>), dim3(unsigned(a.rows)), dim3(256), 0, st, a);
   } else {
-    with_shape<E>(a.cols, t, [&](auto nv, auto tt) {
+    with_shape<E, 1024>(a.cols, t, [&](auto nv, auto tt) {
       using S = Shape<decltype(tt)::value>;
       // as many blocks as the chip holds at once, 2048 threads per CU
       const int64_t groups = (int64_t(a.rows) + S::ROWS - 1) / S::ROWS, most = int64_t(kCUs) * 2048 / S::THREADS;
@@ -470,11 +472,11 @@ hipError_t backward(const NormArgs& a, hipStream_t st) {
     if (!t) {
       hipLaunchKernelGGL((norm_backward_loop_kernel<E>), dim3(unsigned(blocks)), dim3(256), 0, st, a);
     } else {
-      with_shape<E>(a.cols, t, [&](auto nv, auto tt) {
+      with_shape<E, 512>(a.cols, t, [&](auto nv, auto tt) {
         constexpr int NV = decltype(nv)::value, TT = decltype(tt)::value;
         const dim3 g{unsigned(blocks)}, b{Shape<TT>::THREADS};
         // (a thread holds no more: backward_threads)
-        if constexpr (NV * 16 / int(sizeof(E)) <= (TT == 1024 ? 8 : 24)) {
+        if constexpr (NV * 16 / int(sizeof(E)) <= (TT == 512 ? 32 : 24)) {
           if (a.dweight || a.dbias)
             hipLaunchKernelGGL((norm_backward_kernel<E, NV, TT, true>), g, b, 0, st, a);
           else
@@ -494,11 +496,11 @@ hipError_t backward(const NormArgs& a, hipStream_t st) {
 }  // namespace
 
 // Blocks of the backward pass: what the chip holds at once (3 of 256 threads, 1
-// of 1024 per CU), and at least two rows per thread group, so that their partial
+// of 512 per CU), and at least two rows per thread group, so that their partial
 // sums stay few.
 int norm_blocks(int64_t rows, int64_t cols) {
   const int t = backward_threads(cols);
-  const int64_t group = t == 64 ? 4 : 1, most = kCUs * (t == 1024 ? 1 : 3);
+  const int64_t group = t == 64 ? 4 : 1, most = kCUs * (t == 512 ? 1 : 3);
   const int64_t n = (rows + 2 * group - 1) / (2 * group);
   return int(n < 1 ? 1 : n < most ? n : most);
 }

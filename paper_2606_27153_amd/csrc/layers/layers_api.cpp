@@ -139,7 +139,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // us a slab (64 K in bf16, 32 in fp32) with the chip full and with one block on a
 // CU, us for everything else of a tile (its first loads and its epilogue; act:
 // more for an activation where nothing runs beside it), and blocks per CU.  Where
-// two blocks share a CU, `full` is for the two.  fp32's slab times are its MFMAs'.
+// two blocks share a CU, `full` is for the two.
 struct TileKind {
   Choice::Kernel kernel;
   int tm, tn;
@@ -150,8 +150,8 @@ constexpr TileKind kBf16Tiles[] = {{Choice::TILE256, 256, 256, 1.55, 1.1, 7, 8, 
                                    {Choice::TILE128X256, 128, 256, 0.9, 0.66, 5, 4, 1},
                                    {Choice::TILE128, 128, 128, 0.95, 0.53, 5, 0, 2},
                                    {Choice::TILE64, 64, 64, 0.4, 0.29, 3, 0, 2}};
-constexpr TileKind kF32Tiles[] = {{Choice::TILE128, 128, 128, 3.6, 1.8, 4.5, 0, 2},
-                                  {Choice::TILE64, 64, 64, 0.9, 0.45, 3, 0, 2}};
+constexpr TileKind kF32Tiles[] = {{Choice::TILE128, 128, 128, 4.0, 2.05, 4.5, 0, 2},
+                                  {Choice::TILE64, 64, 64, 1.08, 0.57, 3.5, 0, 2}};
 
 double tile_us(const TileKind& k, double blocks, double slabs, bool act) {
   const double rest = k.rest + (act ? k.act : 0), cus = kCUs;

@@ -549,7 +549,8 @@ __global__ __launch_bounds__(256, (Tile<E, TM, TN, U>::RING > 80 * 1024 ? 1 : 2)
 
 // Tiles in a row that one XCD takes of a grouped product (xcd_runs), which share
 // operands in its L2.  Sums by expert: a whole expert.  Rows by expert: eight rows
-// of tiles, an expert or two.
+// of tiles, an expert or two.  At least four runs per XCD (launch_one), so that
+// the XCDs' shares come out alike.
 template <int GROUP>
 int64_t run_length(int64_t mt, int64_t nt) {
   return GROUP == GROUP_ROWS ? 8 * nt : mt * nt;
@@ -563,7 +564,7 @@ hipError_t launch_one(const Product& p, const Table* t, hipStream_t st) {
   if constexpr (GROUP == GROUP_ROWS) blocks = nt * row_tiles_bound(p.M, p.experts, TM);
   if constexpr (GROUP == GROUP_SUM) blocks *= p.experts;
   if constexpr (GROUP != GROUP_NONE) {
-    const int64_t want = run_length<GROUP>(mt, nt), most = (blocks + 7) / 8;
+    const int64_t want = run_length<GROUP>(mt, nt), most = blocks / 32;
     run = int(want < most ? want : most);
     if (run < 1) run = 1;
     blocks = (blocks + 8 * run - 1) / (8 * run) * (8 * run);
