@@ -5,7 +5,11 @@
 // every fourth row of the chunk, a lane V consecutive columns (16 bytes where
 // the rows allow it).  The waves' column sums meet in LDS, the chunks' in a
 // second kernel that adds them in order, so the sum does not depend on timing.
-// The sums take dz before it is rounded.  Memory bound: reads dy and z, writes dz.
+// The sums take dz before it is rounded.  dz itself is rounded to the operands'
+// type, for the two products that read it to run on the matrix cores: in bf16
+// that is one more rounding of 2^-8 on each of a sum's terms, about as much as
+// the rounding of the sum.  Memory bound: reads dy and z, writes dz; 5832 x 4304 in
+// bf16 28 us (5.3 TB/s), the column sums 4.7.
 #include "device.h"
 
 namespace muon {

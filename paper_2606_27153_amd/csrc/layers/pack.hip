@@ -4,8 +4,8 @@
 //
 // One launch copies both operands of a product (and every expert's).  A thread
 // moves a chunk: 16 bytes from any alignment, or element by element at a row's
-// end.  Memory bound; next to a product of any size it is small: a 16384 x 4001
-// operand takes 60 us where the product runs for 400.
+// end.  Memory bound: 16384 x 4001 (the weight 4001 x 4096 lies on whole chunks)
+// 53 us, 5.0 TB/s, ahead of a product of 466 us.
 #include "device.h"
 
 namespace muon {
