@@ -31,8 +31,8 @@
  *  - NaN and infinities propagate within the rows and columns they belong to.
  *  - No output may overlap an input or another output, except that y may be
  *    the residual's own buffer (same ld).
- *  - Dimensions are at most 2^30; rows may be 0 (weight and bias gradients are
- *    then 0), inner, outer and cols may not.
+ *  - rows is at most 2^30 and may be 0 (weight and bias gradients are then 0);
+ *    inner, outer and cols are 1 to 2^24.
  *  - Workspaces are 256-byte aligned device memory of at least the bytes the
  *    workspace function names (which may be 0: NULL is then accepted), need
  *    no initialisation, and must not be shared by calls that may overlap.

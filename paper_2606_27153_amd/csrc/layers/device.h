@@ -14,6 +14,23 @@ namespace {
 // the instructions of a division.
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
 
+// The normal distribution function, from the rational approximation of erf by
+// Abramowitz and Stegun (7.1.26, off by 1.5e-7 at most, the size of fp32's own
+// rounding of 1 + erf), and e = exp(-z^2 / 2), which its density needs too.  A
+// seventh of the instructions of the library's erf, which took a third of the
+// time of a 512 x 256 x 1024 product in fp32.
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float a = fabsf(z) * 0.70710678118654752f;
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.f));
+  e = __expf(-a * a);
+  float p = fmaf(1.061405429f, t, -1.453152027f);
+  p = fmaf(p, t, 1.421413741f);
+  p = fmaf(p, t, -0.284496736f);
+  p = fmaf(p, t, 0.254829592f);
+  const float tail = 0.5f * p * t * e;   // of the side beyond |z|
+  return z < 0.f ? tail : 1.f - tail;
+}
+
 constexpr float kGeluC = 0.7978845608028654f;   // sqrt(2 / pi)
 constexpr float kGeluA = 0.044715f;
 
@@ -21,7 +38,10 @@ constexpr float kGeluA = 0.044715f;
 template <int ACT>
 __device__ __forceinline__ float act_one(float z) {
   if constexpr (ACT == MUON_ACT_RELU) return z < 0.f ? 0.f : z;   // (NaN stays)
-  if constexpr (ACT == MUON_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+  if constexpr (ACT == MUON_ACT_GELU) {
+    float e;
+    return z * normal_cdf(z, e);
+  }
   if constexpr (ACT == MUON_ACT_GELU_TANH) return z * sigmoid(2.f * kGeluC * z * fmaf(kGeluA * z, z, 1.f));
   if constexpr (ACT == MUON_ACT_SILU) return z * sigmoid(z);
   return z;
@@ -34,7 +54,9 @@ __device__ __forceinline__ float act_grad_one(float z) {
   if constexpr (ACT == MUON_ACT_RELU) return z > 0.f ? 1.f : z != z ? z : 0.f;
   if constexpr (ACT == MUON_ACT_GELU) {
     const float c = fminf(fmaxf(z, -30.f), 30.f);
-    return z != z ? z : 0.5f * (1.f + erff(c * 0.70710678118654752f)) + c * 0.3989422804014327f * __expf(-0.5f * c * c);
+    float e;
+    const float cdf = normal_cdf(c, e);
+    return z != z ? z : fmaf(c * 0.3989422804014327f, e, cdf);
   }
   if constexpr (ACT == MUON_ACT_GELU_TANH) {
     const float c = fminf(fmaxf(z, -30.f), 30.f);

@@ -334,27 +334,28 @@ norm_backward_kernel(NormArgs a) {
 template <typename E>
 __global__ __launch_bounds__(256) void norm_forward_loop_kernel(NormArgs a) {
   __shared__ float red[4];
-  const int64_t r = blockIdx.x;
-  const E* x = static_cast<const E*>(a.x) + r * a.ldx;
-  float s = 0.f;
-  for (int c = threadIdx.x; c < a.cols; c += 256) s += float(x[c]);
-  const float mean = block_sum<256>(s, red) / float(a.cols);
-  s = 0.f;
-  for (int c = threadIdx.x; c < a.cols; c += 256) {
-    const float d = float(x[c]) - mean;
-    s = fmaf(d, d, s);
-  }
-  const float rstd = 1.f / sqrtf(block_sum<256>(s, red) / float(a.cols) + a.eps);
-  if (threadIdx.x == 0) {
-    if (a.mean) a.mean[r] = mean;
-    if (a.rstd) a.rstd[r] = rstd;
-  }
-  E* y = static_cast<E*>(a.y) + r * a.ldy;
-  for (int c = threadIdx.x; c < a.cols; c += 256) {
-    float v = (float(x[c]) - mean) * rstd;
-    if (a.weight) v *= weight_at(a.weight, a.wf32, c, x);
-    if (a.bias) v += weight_at(a.bias, a.wf32, c, x);
-    y[c] = E(v);
+  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const E* x = static_cast<const E*>(a.x) + r * a.ldx;
+    float s = 0.f;
+    for (int c = threadIdx.x; c < a.cols; c += 256) s += float(x[c]);
+    const float mean = block_sum<256>(s, red) / float(a.cols);
+    s = 0.f;
+    for (int c = threadIdx.x; c < a.cols; c += 256) {
+      const float d = float(x[c]) - mean;
+      s = fmaf(d, d, s);
+    }
+    const float rstd = 1.f / sqrtf(block_sum<256>(s, red) / float(a.cols) + a.eps);
+    if (threadIdx.x == 0) {
+      if (a.mean) a.mean[r] = mean;
+      if (a.rstd) a.rstd[r] = rstd;
+    }
+    E* y = static_cast<E*>(a.y) + r * a.ldy;
+    for (int c = threadIdx.x; c < a.cols; c += 256) {
+      float v = (float(x[c]) - mean) * rstd;
+      if (a.weight) v *= weight_at(a.weight, a.wf32, c, x);
+      if (a.bias) v += weight_at(a.bias, a.wf32, c, x);
+      y[c] = E(v);
+    }
   }
 }
 
@@ -425,8 +426,12 @@ __global__ __launch_bounds__(1024) void norm_column_sum_kernel(NormArgs a, int b
 // threads) forward, 24 (32 with 512 threads, which hold no second row) backward,
 // where the sums take registers too.  0: the row
 // does not fit, or is shorter than a chunk.
-int forward_threads(int64_t cols) { return cols < 8 ? 0 : cols <= 2048 ? 64 : cols <= 8192 ? 256 : cols <= 16384 ? 1024 : 0; }
-int backward_threads(int64_t cols) { return cols < 8 ? 0 : cols <= 1536 ? 64 : cols <= 6144 ? 256 : cols <= 16384 ? 512 : 0; }
+int forward_threads(int64_t cols) {
+  return cols < 8 || cols > 16384 ? 0 : cols <= 2048 ? 64 : cols <= 8192 ? 256 : 1024;
+}
+int backward_threads(int64_t cols) {
+  return cols < 8 || cols > 16384 ? 0 : cols <= 1536 ? 64 : cols <= 6144 ? 256 : 512;
+}
 
 // f(chunks per thread tag, threads tag) for rows of `cols` on t threads (64, 256 or
 // MOST): the
@@ -451,7 +456,8 @@ hipError_t forward(const NormArgs& a, hipStream_t st) {
   if (!a.rows) return hipSuccess;
   const int t = forward_threads(a.cols);
   if (!t) {
-    hipLaunchKernelGGL((norm_forward_loop_kernel<E>), dim3(unsigned(a.rows)), dim3(256), 0, st, a);
+    const unsigned blocks = unsigned(a.rows < 65536 ? a.rows : 65536);
+    hipLaunchKernelGGL((norm_forward_loop_kernel<E>), dim3(blocks), dim3(256), 0, st, a);
   } else {
     with_shape<E, 1024>(a.cols, t, [&](auto nv, auto tt) {
       using S = Shape<decltype(tt)::value>;
@@ -499,12 +505,12 @@ hipError_t backward(const NormArgs& a, hipStream_t st) {
 }  // namespace
 
 // Blocks of the backward pass: what the chip holds at once (3 of 256 threads, 1
-// of 512 per CU), and at least two rows per thread group, so that their partial
+// of 512 per CU), and at least four rows per thread group, so that their partial
 // sums stay few.
 int norm_blocks(int64_t rows, int64_t cols) {
   const int t = backward_threads(cols);
   const int64_t group = t == 64 ? 4 : 1, most = kCUs * (t == 512 ? 1 : 3);
-  const int64_t n = (rows + 2 * group - 1) / (2 * group);
+  const int64_t n = (rows + 4 * group - 1) / (4 * group);
   return int(n < 1 ? 1 : n < most ? n : most);
 }
 

@@ -21,12 +21,13 @@ muon_status fail(muon_status s, const char* fmt, ...) {
 }
 
 muon_status done(hipError_t e, const char* what) {
+  if (e == hipErrorInvalidConfiguration) return fail(MUON_ERR_UNSUPPORTED, "%s: more tiles than one grid holds", what);
   if (e != hipSuccess) return fail(MUON_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
   g_error[0] = 0;
   return MUON_OK;
 }
 
-constexpr int64_t kMaxDim = int64_t(1) << 30;
+constexpr int64_t kMaxRows = int64_t(1) << 30, kMaxDim = int64_t(1) << 24;
 constexpr int64_t kMaxLd = int64_t(1) << 40;
 
 bool known_dtype(int32_t d) { return d == MUON_F32 || d == MUON_BF16; }
@@ -34,11 +35,11 @@ size_t size_of(int32_t dtype) { return dtype == MUON_BF16 ? 2 : 4; }
 size_t padded(size_t v) { return (v + 255) / 256 * 256; }
 
 muon_status check_sizes(int64_t rows, int64_t inner, int64_t outer, int32_t dtype) {
-  if (rows < 0 || rows > kMaxDim) return fail(MUON_ERR_INVALID_ARG, "rows %lld out of [0, 2^30]", (long long)rows);
+  if (rows < 0 || rows > kMaxRows) return fail(MUON_ERR_INVALID_ARG, "rows %lld out of [0, 2^30]", (long long)rows);
   if (inner < 1 || inner > kMaxDim)
-    return fail(MUON_ERR_INVALID_ARG, "inner %lld out of [1, 2^30]", (long long)inner);
+    return fail(MUON_ERR_INVALID_ARG, "inner %lld out of [1, 2^24]", (long long)inner);
   if (outer < 1 || outer > kMaxDim)
-    return fail(MUON_ERR_INVALID_ARG, "outer %lld out of [1, 2^30]", (long long)outer);
+    return fail(MUON_ERR_INVALID_ARG, "outer %lld out of [1, 2^24]", (long long)outer);
   if (!known_dtype(dtype)) return fail(MUON_ERR_UNSUPPORTED, "dtype %d: MUON_F32 or MUON_BF16", dtype);
   return MUON_OK;
 }
@@ -57,7 +58,8 @@ muon_status check_flags(int32_t f) {
 // at least its columns.
 muon_status check_matrix(const char* name, const void* p, int64_t ld, int64_t cols, size_t esize) {
   if (!p) return fail(MUON_ERR_INVALID_ARG, "%s is NULL", name);
-  if (reinterpret_cast<uintptr_t>(p) % esize) return fail(MUON_ERR_INVALID_ARG, "%s is not aligned to its element", name);
+  if (reinterpret_cast<uintptr_t>(p) % esize)
+    return fail(MUON_ERR_INVALID_ARG, "%s is not aligned to its element", name);
   if (ld < cols || ld > kMaxLd)
     return fail(MUON_ERR_INVALID_ARG, "%s has leading dimension %lld, needs at least %lld", name, (long long)ld,
                 (long long)cols);
@@ -65,11 +67,15 @@ muon_status check_matrix(const char* name, const void* p, int64_t ld, int64_t co
 }
 
 muon_status check_vector(const char* name, const void* p, size_t esize) {
-  if (reinterpret_cast<uintptr_t>(p) % esize) return fail(MUON_ERR_INVALID_ARG, "%s is not aligned to its element", name);
+  if (reinterpret_cast<uintptr_t>(p) % esize)
+    return fail(MUON_ERR_INVALID_ARG, "%s is not aligned to its element", name);
   return MUON_OK;
 }
 
 muon_status check_workspace(const void* ws, size_t have, size_t need) {
+  // (more than the need may be used: for copies)
+  if (have && reinterpret_cast<uintptr_t>(ws) % 256)
+    return fail(MUON_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
   if (!need) return MUON_OK;
   if (!ws) return fail(MUON_ERR_INVALID_ARG, "workspace is NULL, %zu bytes are needed", need);
   if (reinterpret_cast<uintptr_t>(ws) % 256) return fail(MUON_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
@@ -256,7 +262,8 @@ hipError_t product(bool bf16, int form, int group, Product p, const Table* t, Sc
         used += copy_bytes(k.b, epc, n);
       }
       // (the tile kernels' 32-bit offsets hold for the copies too)
-      const bool near = k.a.ld_dst * 16 / epc * 256 < (int64_t(1) << 31) && k.b.ld_dst * 16 / epc * 256 < (int64_t(1) << 31);
+      const int64_t longest = k.a.ld_dst > k.b.ld_dst ? k.a.ld_dst : k.b.ld_dst;
+      const bool near = longest * 16 / epc * 256 < (int64_t(1) << 31);
       if (ws.p && used <= ws.bytes && near && p.K > 0) {
         static const Table none{};
         e = launch_pack(bf16, k, group == GROUP_ROWS ? *t : none, st);
@@ -269,8 +276,8 @@ hipError_t product(bool bf16, int form, int group, Product p, const Table* t, Sc
           p.b = k.b.dst;
           p.ldb = k.b.ld_dst;
           if (group == GROUP_ROWS) {
-            for (int32_t i = 0; i < p.experts; ++i)
-              copies.p[i] = static_cast<char*>(k.b.dst) + size_t(i) * size_t(k.b.rows) * size_t(k.b.ld_dst) * size_t(16 / epc);
+            const size_t step = size_t(k.b.rows) * size_t(k.b.ld_dst) * size_t(16 / epc);
+            for (int32_t i = 0; i < p.experts; ++i) copies.p[i] = static_cast<char*>(k.b.dst) + i * step;
             t = &copies;
           }
         }
@@ -284,7 +291,9 @@ hipError_t product(bool bf16, int form, int group, Product p, const Table* t, Sc
   switch (c.kernel) {
     case Choice::SIMPLE: e = launch_simple(bf16, form, group, p, t, st); break;
     case Choice::SKINNY: e = launch_skinny(bf16, form, group, c.mt, p, t, st); break;
-    case Choice::TILE64: e = bf16 ? launch_tile64_bf16(form, group, p, t, st) : launch_tile64_f32(form, group, p, t, st); break;
+    case Choice::TILE64:
+      e = bf16 ? launch_tile64_bf16(form, group, p, t, st) : launch_tile64_f32(form, group, p, t, st);
+      break;
     case Choice::TILE128:
       e = bf16 ? launch_tile128_bf16(form, group, p, t, st) : launch_tile128_f32(form, group, p, t, st);
       break;
@@ -369,9 +378,9 @@ MUON_API muon_status muon_linear_workspace_bytes(int64_t rows, int64_t inner, in
   TRY(check_sizes(rows, inner, outer, dtype));
   TRY(check_activation(activation));
   TRY(check_flags(flags));
-  const bool copies = flags & MUON_LAYERS_UNALIGNED;
+  const bool copies = flags & MUON_LAYERS_UNALIGNED, act = activation != MUON_ACT_NONE;
   *bytes = flags & MUON_LAYERS_BACKWARD ? backward_layout(rows, inner, outer, dtype, activation, copies).total
-                                        : forward_bytes(GROUP_NONE, rows, inner, outer, 0, dtype, activation != MUON_ACT_NONE, copies);
+                                        : forward_bytes(GROUP_NONE, rows, inner, outer, 0, dtype, act, copies);
   return done(hipSuccess, "");
 }
 
@@ -390,7 +399,8 @@ MUON_API muon_status muon_linear_forward(const void* x, int64_t ldx, const void*
   if (residual) TRY(check_matrix("residual", residual, ldr, outer, es));
   if (preact) TRY(check_matrix("preact", preact, ldz, outer, es));
   TRY(check_vector("bias", bias, es));
-  TRY(check_workspace(workspace, workspace_bytes, forward_bytes(GROUP_NONE, rows, inner, outer, 0, dtype, activation != MUON_ACT_NONE, false)));
+  const bool act = activation != MUON_ACT_NONE;
+  TRY(check_workspace(workspace, workspace_bytes, forward_bytes(GROUP_NONE, rows, inner, outer, 0, dtype, act, false)));
   Product p{};
   p.a = x; p.lda = ldx;
   p.b = w; p.ldb = ldw;
@@ -450,7 +460,8 @@ MUON_API muon_status muon_linear_backward(const void* dy, int64_t lddy, const vo
     p.b = w; p.ldb = ldw;
     p.c = dx; p.ldc = lddx;
     p.M = int32_t(rows); p.N = int32_t(inner); p.K = int32_t(outer);
-    TRY(done(product(bf16, w_transposed ? FORM_RT : FORM_RR, GROUP_NONE, p, nullptr, scratch, st), "linear input gradient"));
+    TRY(done(product(bf16, w_transposed ? FORM_RT : FORM_RR, GROUP_NONE, p, nullptr, scratch, st),
+             "linear input gradient"));
   }
   if (dw) {
     Product p{};
@@ -543,7 +554,8 @@ MUON_API muon_status muon_grouped_linear_backward(const void* dy, int64_t lddy, 
     p.ldb = ldw;
     p.c = dx; p.ldc = lddx;
     p.M = int32_t(rows); p.N = int32_t(inner); p.K = int32_t(outer);
-    TRY(done(product(bf16, w_transposed ? FORM_RT : FORM_RR, GROUP_ROWS, p, &tw, scratch, st), "grouped input gradient"));
+    TRY(done(product(bf16, w_transposed ? FORM_RT : FORM_RR, GROUP_ROWS, p, &tw, scratch, st),
+             "grouped input gradient"));
   }
   if (dw) {
     p.c = nullptr; p.ldc = lddw;

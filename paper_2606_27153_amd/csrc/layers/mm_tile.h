@@ -98,7 +98,7 @@ struct Loader {
       const int row = wid * RPC + lane / LPR, slot = lane % LPR;
       int chunk = slot;
       if constexpr (sizeof(E) == 2) chunk = (((slot >> 1) ^ seg_swz<ROWB>(row)) << 1) | (slot & 1);
-      const int col = min(chunk * EPC, (valid + EPC - 1) / EPC * EPC - EPC);   // (rows are whole chunks)
+      const int col = min(chunk * EPC, (valid + EPC - 1) / EPC * EPC - EPC);  // (rows are whole chunks)
       step = BK * ld * int64_t(sizeof(E));
       off[0] = uint32_t(row * ld * int64_t(sizeof(E)) + col * int64_t(sizeof(E)));
       stride = uint32_t(4 * RPC * ld * int64_t(sizeof(E)));
@@ -216,8 +216,8 @@ __device__ __forceinline__ int xcd_runs(int pid, int run) {
 }
 
 template <typename E, int TM, int TN, int U, int FORM, int GROUP>
-__device__ __forceinline__ bool locate(const Product& p, const typename TableOf<GROUP>::T& tab, int pid, int run, int lane,
-                                       const Ranks& ranks, Work<E>& w) {
+__device__ __forceinline__ bool locate(const Product& p, const typename TableOf<GROUP>::T& tab, int pid, int run,
+                                       int lane, const Ranks& ranks, Work<E>& w) {
   const int nt = (p.N + TN - 1) / TN, mt = (p.M + TM - 1) / TM;
   const E* a = static_cast<const E*>(p.a);
   const E* b = static_cast<const E*>(p.b);
@@ -447,114 +447,114 @@ __global__ __launch_bounds__(256, (Tile<E, TM, TN, U>::RING > 80 * 1024 ? 1 : 2)
   fill();
 
   for (;;) {
-  f32x16 acc[C::NBM][C::NBN];
+    f32x16 acc[C::NBM][C::NBN];
 #pragma unroll
-  for (int i = 0; i < C::NBM; ++i)
+    for (int i = 0; i < C::NBM; ++i)
 #pragma unroll
-    for (int j = 0; j < C::NBN; ++j)
+      for (int j = 0; j < C::NBN; ++j)
 #pragma unroll
-      for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
-  // the next tile is looked up while this one's first loads arrive
-  Work<E> next;
-  ++round;
-  const bool more = find(round, next);
+        for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.f;
+    // the next tile is looked up while this one's first loads arrive
+    Work<E> next;
+    ++round;
+    const bool more = find(round, next);
 
-  const int nk = (w.K + C::BK - 1) / C::BK;
-  // loads of units u0 .. u1 - 1
-  auto loads = [](int u0, int u1) constexpr {
-    int n = 0;
-    for (int u = u0; u < u1; ++u) n += u & 1 ? LB::N : LA::N;
-    return n;
-  };
-  F fa[2][C::NBM], fb[2][C::NBN];
-  constexpr int READS = RA::READS + RB::READS;
-  constexpr int Q = sizeof(E) == 2 ? 1 : 4;               // MFMAs per block and K step
-  constexpr int MFMAS = C::NBM * C::NBN * Q;
-  auto read_one = [&](int s, int r, int buf) {
-    if (r < RB::READS)
-      rb.read(lds, s, r, fb[buf]);
-    else
-      ra.read(lds, s, r - RB::READS, fa[buf]);
-  };
-  // MFMAs of a K step (fragments buf) with the reads of step rs spread over the
-  // first SPAN of them and the loads l0 .. l1 - 1 of a unit of operand L over
-  // all; `mid` runs after MID of them.  No branch surrounds an MFMA: the
-  // accumulators would be copied where the paths meet.
-  constexpr int SPAN = MFMAS >= 4 ? MFMAS * 3 / 4 : MFMAS, MID = SPAN;
-  auto k_step = [&](const auto& L, int l0, int l1, int rs, int buf, uint32_t to, int span, auto mid) {
+    const int nk = (w.K + C::BK - 1) / C::BK;
+    // loads of units u0 .. u1 - 1
+    auto loads = [](int u0, int u1) constexpr {
+      int n = 0;
+      for (int u = u0; u < u1; ++u) n += u & 1 ? LB::N : LA::N;
+      return n;
+    };
+    F fa[2][C::NBM], fb[2][C::NBN];
+    constexpr int READS = RA::READS + RB::READS;
+    constexpr int Q = sizeof(E) == 2 ? 1 : 4;               // MFMAs per block and K step
+    constexpr int MFMAS = C::NBM * C::NBN * Q;
+    auto read_one = [&](int s, int r, int buf) {
+      if (r < RB::READS)
+        rb.read(lds, s, r, fb[buf]);
+      else
+        ra.read(lds, s, r - RB::READS, fa[buf]);
+    };
+    // MFMAs of a K step (fragments buf) with the reads of step rs spread over the
+    // first SPAN of them and the loads l0 .. l1 - 1 of a unit of operand L over
+    // all; `mid` runs after MID of them.  No branch surrounds an MFMA: the
+    // accumulators would be copied where the paths meet.
+    constexpr int SPAN = MFMAS >= 4 ? MFMAS * 3 / 4 : MFMAS, MID = SPAN;
+    auto k_step = [&](const auto& L, int l0, int l1, int rs, int buf, uint32_t to, int span, auto mid) {
 #pragma unroll
-    for (int t = 0; t < MFMAS; ++t) {
+      for (int t = 0; t < MFMAS; ++t) {
 #pragma unroll
-      for (int r = 0; r < READS; ++r)
-        if (r * span / READS == t) read_one(rs, r, buf ^ 1);
+        for (int r = 0; r < READS; ++r)
+          if (r * span / READS == t) read_one(rs, r, buf ^ 1);
 #pragma unroll
-      for (int i = l0; i < l1; ++i)
-        if ((i - l0) * MFMAS / (l1 - l0) == t) L.load(i, to, wid);
-      const int q = t / (C::NBM * C::NBN), ij = t % (C::NBM * C::NBN), i = ij / C::NBN, j = ij % C::NBN;
-      acc[i][j] = mfma<E>(fb[buf][j], fa[buf][i], acc[i][j], q);
-      __builtin_amdgcn_sched_barrier(0);
-      if (t + 1 == MID) mid();
-    }
-  };
-  auto nothing = []() {};
+        for (int i = l0; i < l1; ++i)
+          if ((i - l0) * MFMAS / (l1 - l0) == t) L.load(i, to, wid);
+        const int q = t / (C::NBM * C::NBN), ij = t % (C::NBM * C::NBN), i = ij / C::NBN, j = ij % C::NBN;
+        acc[i][j] = mfma<E>(fb[buf][j], fa[buf][i], acc[i][j], q);
+        __builtin_amdgcn_sched_barrier(0);
+        if (t + 1 == MID) mid();
+      }
+    };
+    auto nothing = []() {};
 
-  int ua = 0, ub = C::UA;   // the current slab's units
-  if (nk > 0) {
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"(loads(2, U)) : "memory");
-    __builtin_amdgcn_sched_barrier(0);
-    uint32_t free1 = 0;         // the unit whose loads go out in steps 0 and 1
-#pragma unroll
-    for (int r = 0; r < READS; ++r) read_one(0, r, 0);
-    // The loads that step 3 starts go first, and are A's where U is even.
-    auto& first = pick<(U & 1) == 0>(la, lb);
-    auto& second = pick<(U & 1) != 0>(la, lb);
-    constexpr int L = (U & 1) ? LA::N : LB::N, L1 = L / 2;   // second's loads
-    constexpr int L0 = (U & 1) ? LB::N : LA::N;               // first's
-    auto wrap = [](int v) { return v >= C::RING ? v - C::RING : v; };
-    // Step 2 reads the slab's last fragments early and meets the other waves
-    // before its own last MFMAs: this slab is read, the next one has landed;
-    // U - 4 units may be in flight.
-    constexpr int EARLY = MFMAS >= 4 ? MFMAS / 2 : MFMAS;
-    auto publish = [&]() {
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(loads(4, U)) : "memory");
+    int ua = 0, ub = C::UA;   // the current slab's units
+    if (nk > 0) {
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"(loads(2, U)) : "memory");
       __builtin_amdgcn_sched_barrier(0);
-    };
-    auto last_step = [&]() {
-      const uint32_t free0 = base + ua;
-      free1 = base + ub;
-      const int na = wrap(ua + C::UA + C::UB), nb = wrap(ub + C::UA + C::UB);
-      ra.move(na - ua);
-      rb.move(nb - ub);
-      ua = na;
-      ub = nb;
-      k_step(first, 0, L0, 0, 1, free0, SPAN, nothing);
-      first.next();
-    };
-    // The first slab's steps load nothing: every unit of the ring is taken.
-    k_step(la, 0, 0, 1, 0, 0, SPAN, nothing);
-    k_step(la, 0, 0, 2, 1, 0, SPAN, nothing);
-    k_step(la, 0, 0, 3, 0, 0, EARLY, publish);
-    last_step();
-    for (int kt = 1; kt < nk; ++kt) {
-      k_step(second, 0, L1, 1, 0, free1, SPAN, nothing);
-      k_step(second, L1, L, 2, 1, free1, SPAN, nothing);
-      second.next();
-      k_step(second, 0, 0, 3, 0, 0, EARLY, publish);
+      uint32_t free1 = 0;         // the unit whose loads go out in steps 0 and 1
+#pragma unroll
+      for (int r = 0; r < READS; ++r) read_one(0, r, 0);
+      // The loads that step 3 starts go first, and are A's where U is even.
+      auto& first = pick<(U & 1) == 0>(la, lb);
+      auto& second = pick<(U & 1) != 0>(la, lb);
+      constexpr int L = (U & 1) ? LA::N : LB::N, L1 = L / 2;   // second's loads
+      constexpr int L0 = (U & 1) ? LB::N : LA::N;               // first's
+      auto wrap = [](int v) { return v >= C::RING ? v - C::RING : v; };
+      // Step 2 reads the slab's last fragments early and meets the other waves
+      // before its own last MFMAs: this slab is read, the next one has landed;
+      // U - 4 units may be in flight.
+      constexpr int EARLY = MFMAS >= 4 ? MFMAS / 2 : MFMAS;
+      auto publish = [&]() {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(loads(4, U)) : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      auto last_step = [&]() {
+        const uint32_t free0 = base + ua;
+        free1 = base + ub;
+        const int na = wrap(ua + C::UA + C::UB), nb = wrap(ub + C::UA + C::UB);
+        ra.move(na - ua);
+        rb.move(nb - ub);
+        ua = na;
+        ub = nb;
+        k_step(first, 0, L0, 0, 1, free0, SPAN, nothing);
+        first.next();
+      };
+      // The first slab's steps load nothing: every unit of the ring is taken.
+      k_step(la, 0, 0, 1, 0, 0, SPAN, nothing);
+      k_step(la, 0, 0, 2, 1, 0, SPAN, nothing);
+      k_step(la, 0, 0, 3, 0, 0, EARLY, publish);
       last_step();
+      for (int kt = 1; kt < nk; ++kt) {
+        k_step(second, 0, L1, 1, 0, free1, SPAN, nothing);
+        k_step(second, L1, L, 2, 1, free1, SPAN, nothing);
+        second.next();
+        k_step(second, 0, 0, 3, 0, 0, EARLY, publish);
+        last_step();
+      }
     }
-  }
-  ra.move(-ua);
-  rb.move(C::UA - ub);
-  // the last slabs' loads (past K) and every wave's reads end here
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  static_assert(4 * Staging<C>::BYTES <= C::RING, "the waves' parts of the ring");
-  store_tile<C, E, GROUP == GROUP_NONE && FORM != FORM_TT>(
-      p, w, acc, reinterpret_cast<float*>(lds + wid * Staging<C>::BYTES), wm, wn, lane);
-  if (!more) break;
-  // every wave's part is free again for the next tile's first slabs
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  w = next;
-  fill();
+    ra.move(-ua);
+    rb.move(C::UA - ub);
+    // the last slabs' loads (past K) and every wave's reads end here
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    static_assert(4 * Staging<C>::BYTES <= C::RING, "the waves' parts of the ring");
+    store_tile<C, E, GROUP == GROUP_NONE && FORM != FORM_TT>(
+        p, w, acc, reinterpret_cast<float*>(lds + wid * Staging<C>::BYTES), wm, wn, lane);
+    if (!more) break;
+    // every wave's part is free again for the next tile's first slabs
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    w = next;
+    fill();
   }
 }
 

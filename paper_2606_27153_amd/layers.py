@@ -5,8 +5,8 @@ with a fused epilogue (``linear``), the same grouped by expert
 Each operator comes as a function torch's autograd sees (``linear``,
 ``grouped_linear``, ``layer_norm``) and as its two passes (``*_forward``,
 ``*_backward``), which only enqueue HIP kernels on torch's current stream of the
-tensors' device: no host synchronisation, no copies, nothing cached between
-calls.  Weights are [in, out] like the optimizer's workloads; the transposed
+tensors' device: no host synchronisation, no copies, nothing of the data kept
+between calls.  Weights are [in, out] like the optimizer's workloads; the transposed
 view of an [out, in] weight is taken as it lies.  Weight gradients come in the
 weight's own memory layout, so that ``Muon`` steps them without a copy.
 
@@ -134,16 +134,18 @@ def _flags(backward: int, x: torch.Tensor, outer: int, *addresses: int) -> int:
     return backward | (2 if bits & 15 else 0)
 
 
-def _bytes(fn, *args) -> int:
+@functools.lru_cache(maxsize=4096)
+def _bytes(name: str, *args) -> int:
+    """What the library's workspace function says of these sizes."""
     n = ctypes.c_size_t()
-    LL.check(fn(*args, ctypes.byref(n)))
+    LL.check(getattr(_load(), name)(*args, ctypes.byref(n)))
     return n.value
 
 
 def _workspace(n: int, like: torch.Tensor):
     """A workspace from torch's allocator: it belongs to the current stream, and
     goes back to it when the call that enqueued its use returns."""
-    return torch.empty(n, dtype=torch.uint8, device=like.device) if n else None
+    return like.new_empty((n,), dtype=torch.uint8) if n else None
 
 
 # ------------------------------------------------------------------- linear
@@ -168,10 +170,10 @@ def linear_forward(x: torch.Tensor, weight: torch.Tensor, *, bias: Optional[torc
     bp = _vector(bias, "bias", x, outer)
     rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", x, rows, outer)
     stream = _stream(x)
-    y = torch.empty(rows, outer, dtype=x.dtype, device=x.device)
-    z = torch.empty_like(y) if keep_preactivation and act else None
+    y = x.new_empty((rows, outer))
+    z = x.new_empty((rows, outer)) if keep_preactivation and act else None
     size = x.element_size()
-    need = _bytes(lib.muon_linear_workspace_bytes, rows, inner, outer, code, act,
+    need = _bytes("muon_linear_workspace_bytes", rows, inner, outer, code, act,
                   _flags(0, x, outer, xp, ldx * size, wp, ldw * size))
     ws = _workspace(need, x)
     LL.check(lib.muon_linear_forward(xp, ldx, wp, ldw, wt, bp, rp, ldr, y.data_ptr(), outer,
@@ -183,8 +185,8 @@ def linear_forward(x: torch.Tensor, weight: torch.Tensor, *, bias: Optional[torc
 def _like_weight(weight: torch.Tensor, transposed: int) -> torch.Tensor:
     """An uninitialised gradient in the weight's own layout, dense."""
     if transposed:
-        return torch.empty(weight.size(1), weight.size(0), dtype=weight.dtype, device=weight.device).t()
-    return torch.empty(weight.size(0), weight.size(1), dtype=weight.dtype, device=weight.device)
+        return weight.new_empty((weight.size(1), weight.size(0))).t()
+    return weight.new_empty(tuple(weight.shape))
 
 
 @_on_device
@@ -210,11 +212,11 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, *,
             raise ValueError(f"the backward pass of {activation!r} needs the forward pass's preactivation")
         zp, ldz = _rows(preactivation, "preactivation", x, rows, outer)
     stream = _stream(x)
-    dx = torch.empty(rows, inner, dtype=x.dtype, device=x.device) if input_grad else None
+    dx = x.new_empty((rows, inner)) if input_grad else None
     dw = _like_weight(weight, wt) if weight_grad else None
-    db = torch.empty(outer, dtype=x.dtype, device=x.device) if bias_grad else None
+    db = x.new_empty((outer,)) if bias_grad else None
     size = x.element_size()
-    need = _bytes(lib.muon_linear_workspace_bytes, rows, inner, outer, code, act,
+    need = _bytes("muon_linear_workspace_bytes", rows, inner, outer, code, act,
                   _flags(1, x, outer, xp, ldx * size, wp, ldw * size, gp, ldg * size))
     ws = _workspace(need, x)
     LL.check(lib.muon_linear_backward(gp, ldg, xp, ldx, wp, ldw, wt, zp, ldz,
@@ -325,9 +327,9 @@ def grouped_linear_forward(x: torch.Tensor, weights: Weights, offsets: torch.Ten
         raise ValueError("the weights have no output features")
     op = _offsets(offsets, n, x)
     stream = _stream(x)
-    y = torch.empty(rows, outer, dtype=x.dtype, device=x.device)
+    y = x.new_empty((rows, outer))
     size = x.element_size()
-    need = _bytes(lib.muon_grouped_linear_workspace_bytes, rows, inner, outer, n, code,
+    need = _bytes("muon_grouped_linear_workspace_bytes", rows, inner, outer, n, code,
                   _flags(0, x, outer, xp, ldx * size, ldw * size, *ptrs))
     ws = _workspace(need, x)
     LL.check(lib.muon_grouped_linear_forward(xp, ldx, (ctypes.c_void_p * n)(*ptrs), ldw, wt, op, n, y.data_ptr(),
@@ -360,18 +362,18 @@ def grouped_linear_backward(dy: torch.Tensor, x: torch.Tensor, weights: Weights,
             raise ValueError(f"weight_grad names {len(want)} experts, there are {n}")
         weight_grad = any(want)
     stream = _stream(x)
-    dx = torch.empty(rows, inner, dtype=x.dtype, device=x.device) if input_grad else None
+    dx = x.new_empty((rows, inner)) if input_grad else None
     dw = dptrs = None
     if weight_grad:
         a, b = (outer, inner) if wt else (inner, outer)
-        dw = torch.empty(n, a, b, dtype=x.dtype, device=x.device)
+        dw = x.new_empty((n, a, b))
         step = a * b * dw.element_size()
         base = dw.data_ptr()
         dptrs = (ctypes.c_void_p * n)(*[base + i * step if want is None or want[i] else None for i in range(n)])
         if wt:
             dw = dw.transpose(1, 2)
     size = x.element_size()
-    need = _bytes(lib.muon_grouped_linear_workspace_bytes, rows, inner, outer, n, code,
+    need = _bytes("muon_grouped_linear_workspace_bytes", rows, inner, outer, n, code,
                   _flags(1, x, outer, xp, ldx * size, ldw * size, gp, ldg * size, *ptrs))
     ws = _workspace(need, x)
     LL.check(lib.muon_grouped_linear_backward(gp, ldg, xp, ldx, (ctypes.c_void_p * n)(*ptrs), ldw, wt, op, n,
@@ -447,10 +449,10 @@ def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, b
     xp, ldx = _rows(x, "x", x, rows, cols)
     wp, bp, wcode = _norm_vectors(x, (("weight", weight), ("bias", bias)), cols)
     stream = _stream(x)
-    y = torch.empty(rows, cols, dtype=x.dtype, device=x.device)
+    y = x.new_empty((rows, cols))
     mean = rstd = None
     if keep_stats:
-        mean, rstd = torch.empty(2, rows, dtype=torch.float32, device=x.device).unbind(0)
+        mean, rstd = x.new_empty((rows,), dtype=torch.float32), x.new_empty((rows,), dtype=torch.float32)
     LL.check(lib.muon_layer_norm_forward(xp, ldx, wp, bp, y.data_ptr(), cols,
                                          None if mean is None else mean.data_ptr(),
                                          None if rstd is None else rstd.data_ptr(), rows, cols, eps, code, wcode,
@@ -478,11 +480,11 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
         if t.device != x.device:
             raise ValueError(f"{name} is on {t.device}, expected {x.device}")
     stream = _stream(x)
-    dx = torch.empty(rows, cols, dtype=x.dtype, device=x.device) if input_grad else None
+    dx = x.new_empty((rows, cols)) if input_grad else None
     wdt = torch.float32 if wcode == MUON_F32 else x.dtype
-    dw = torch.empty(cols, dtype=wdt, device=x.device) if weight_grad else None
-    db = torch.empty(cols, dtype=wdt, device=x.device) if bias_grad else None
-    need = _bytes(lib.muon_layer_norm_workspace_bytes, rows, cols) if weight_grad or bias_grad else 0
+    dw = x.new_empty((cols,), dtype=wdt) if weight_grad else None
+    db = x.new_empty((cols,), dtype=wdt) if bias_grad else None
+    need = _bytes("muon_layer_norm_workspace_bytes", rows, cols) if weight_grad or bias_grad else 0
     ws = _workspace(need, x)
     LL.check(lib.muon_layer_norm_backward(gp, ldg, xp, ldx, wp, mean.data_ptr(), rstd.data_ptr(),
                                           None if dx is None else dx.data_ptr(), cols,

@@ -82,6 +82,18 @@ def test_dtypes_and_small_workspaces_are_refused(lay):
                                         None) == L.MUON_ERR_WORKSPACE_TOO_SMALL
 
 
+def test_workspace_beyond_the_need_must_be_aligned_too(lay):
+    """A forward pass that needs no workspace may still use one, for copies of unaligned operands."""
+    n = ctypes.c_size_t()
+    for flags, some in ((0, False), (2, True)):
+        assert lay.muon_linear_workspace_bytes(100, 63, 65, L.MUON_BF16, 0, flags, ctypes.byref(n)) == L.MUON_OK
+        assert (n.value > 100 * 63 * 2) == some
+    a = [X, 63, X, 65, 0, None, None, 0, Y, 65, None, 0, 100, 63, 65, L.MUON_BF16, 0]
+    assert lay.muon_linear_forward(*a, 0x1010, n.value, None) == L.MUON_ERR_INVALID_ARG
+    assert "aligned" in lay.muon_layers_last_error().decode()
+    assert lay.muon_linear_workspace_bytes(100, 63, 65, L.MUON_BF16, 0, 4, ctypes.byref(n)) == L.MUON_ERR_INVALID_ARG
+
+
 def test_grouped_refusals(lay):
     ptrs = (ctypes.c_void_p * 3)(X, X, X)
     hole = (ctypes.c_void_p * 3)(X, None, X)
