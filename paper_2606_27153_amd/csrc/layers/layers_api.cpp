@@ -132,7 +132,8 @@ size_t copy_bytes(const PackOne& o, int64_t epc, int64_t copies) {
 }
 
 // Which kernel runs a product, and into how many ranges it cuts the summed
-// dimension (plain products only: each range leaves an fp32 partial result).
+// dimension (each range leaves an fp32 partial result; not where experts own
+// ranges of it).
 struct Choice {
   enum Kernel { SIMPLE, SKINNY, TILE64, TILE128, TILE128X256, TILE256 } kernel = SIMPLE;
   int mt = 0;       // SKINNY: 16-row tiles per block
@@ -186,13 +187,13 @@ Choice choose(bool bf16, int form, int group, int64_t M, int64_t N, int64_t K, i
   if (form != FORM_TT && N >= epc && per_expert <= (group == GROUP_ROWS ? 16 : 64)) {
     c.kernel = Choice::SKINNY;
     c.mt = group == GROUP_ROWS || M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    if (group == GROUP_NONE) {
-      // 512 blocks (two per CU) keep enough loads in flight; at least 4 K steps per wave
-      const int64_t blocks = ceil_div(N, 16 * epc), steps = ceil_div(K, 4 * epc);
-      int64_t s = 512 / blocks;
-      s = s < steps / 16 ? s : steps / 16;
-      c.splits = int(s < 1 ? 1 : s);
-    }
+    // 512 blocks (two per CU) keep enough loads in flight; at least 4 K steps per
+    // wave.  Of experts, as many as rows or half of them are taken to be met.
+    const int64_t met = group == GROUP_NONE ? 1 : M < (experts + 1) / 2 ? M : (experts + 1) / 2;
+    const int64_t blocks = ceil_div(N, 16 * epc) * met, steps = ceil_div(K, 4 * epc);
+    int64_t s = 512 / blocks;
+    s = s < steps / 16 ? s : steps / 16;
+    c.splits = int(s < 1 ? 1 : s);
     return c;
   }
   const int64_t bk = bf16 ? 64 : 32;
@@ -209,7 +210,7 @@ Choice choose(bool bf16, int form, int group, int64_t M, int64_t N, int64_t K, i
       slabs = double(K) / experts / bk + 0.5;
     }
     for (int s = 1; s <= 16; ++s) {
-      if (s > 1 && (group != GROUP_NONE || slabs < 4 * s)) break;
+      if (s > 1 && (group == GROUP_SUM || slabs < 4 * s)) break;
       const double us = tile_us(k, blocks * s, std::ceil(slabs / s), act) + reduce_us(M, N, s);
       if (best == 0 || us < best) {
         best = us;

@@ -224,6 +224,12 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
   w.c = static_cast<E*>(p.c);
   int k0 = 0, k1 = p.K;
   int ni;
+  if constexpr (GROUP != GROUP_SUM) {   // this block's range of K: whole slabs
+    constexpr int BK = Tile<E, TM, TN, U>::BK;
+    const int slabs = (p.K + BK - 1) / BK, per = (slabs + p.splits - 1) / p.splits * BK;
+    k0 = min(p.K, int(blockIdx.y) * per);
+    k1 = min(p.K, k0 + per);
+  }
   if constexpr (GROUP == GROUP_ROWS) {
     const int id = xcd_runs(pid, run);
     RowTile t;
@@ -231,7 +237,7 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
     ni = id % nt;
     w.m0 = t.row0;
     w.rows = t.rows;
-    if (t.expert < 0) k1 = 0;
+    if (t.expert < 0) k1 = k0;
     b = static_cast<const E*>(tab.p[max(t.expert, 0)]);
   } else {
     int id, mi;
@@ -246,10 +252,6 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
       expert_range(p.offsets, e, p.K, lane, k0, k1);
     } else {
       id = xcd_order(pid, mt * nt);
-      const int slabs = (p.K + Tile<E, TM, TN, U>::BK - 1) / Tile<E, TM, TN, U>::BK;
-      const int per = (slabs + p.splits - 1) / p.splits * Tile<E, TM, TN, U>::BK;
-      k0 = min(p.K, int(blockIdx.y) * per);
-      k1 = min(p.K, k0 + per);
     }
     // bands of 8 tile rows, column by column
     const int band = id / (8 * nt), in = id - band * 8 * nt, h = min(8, mt - band * 8);

@@ -128,3 +128,11 @@ def test_layer_norm_large(rows, cols, dtype):
     for got, terms in ((dw, dy.double() * h), (db, dy.double())):
         want, e = terms.sum(0), (rows + 16) * R.U * terms.abs().sum(0)
         R.check(got, want, e + q * (want.abs() + e), "column sums")
+
+
+@pytest.mark.parametrize("experts,rows,inner,outer,dtype,transposed", [
+    (4, 3, 5632, 4096, F32, False), (8, 345, 14336, 264, BF, False), (8, 345, 4096, 264, F32, True),
+    (16, 2, 2257, 727, BF, False), (64, 48, 2048, 1408, BF, True), (2, 30, 8192, 72, BF, False)])
+def test_grouped_few_rows_long_sums(experts, rows, inner, outer, dtype, transposed):
+    """Sums cut into ranges, whose partial results of all experts' rows are added in one go."""
+    test_grouped_large(experts, rows, inner, outer, dtype, transposed)
