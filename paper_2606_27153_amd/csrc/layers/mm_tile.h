@@ -277,13 +277,14 @@ __device__ __forceinline__ bool locate(const Product& p, const typename TableOf<
 // 1408 x 2048 took 224 us, 75 of them for the stores.)  A lane's vector
 // instructions count: with one wave per SIMD nothing else runs meanwhile.  OUT:
 // the type stored (E, or float for partial results, which get no epilogue).
+// RAGGED: C's columns end inside a group of 8.
 template <class C>
 struct Staging {
   static constexpr int LD = C::WTN + 4;                // floats of a row: rows 4 banks apart
   static constexpr int BYTES = 32 * LD * 4;            // of a wave
   static constexpr int LPR = C::WTN / 8, RPI = 64 / LPR;  // lanes of a row, rows of a store instruction
 };
-template <class C, typename E, typename OUT, int ACT, bool EPI>
+template <class C, typename E, typename OUT, int ACT, bool EPI, bool RAGGED>
 __device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ldc, const Work<E>& o,
                                             const f32x16 (&acc)[C::NBM][C::NBN], float* region, int wm, int wn,
                                             int lane) {
@@ -292,9 +293,10 @@ __device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ld
   const E* res = EPI ? static_cast<const E*>(p.res) : nullptr;
   E* z = EPI ? static_cast<E*>(p.z) : nullptr;
   const int r0 = lane / S::LPR, col = wn + lane % S::LPR * 8;   // this lane's first row of a pass, its columns
-  const bool in = col < o.cols;                                 // (whole groups of 8: N is a multiple)
+  const bool in = col < o.cols;
+  const int count = RAGGED ? o.cols - col : 8;                  // columns of the lane's 8 that exist
   float bv[8] = {};
-  if (bias && in) load8(bias + o.n0 + col, 8, bv);
+  if (bias && in) load8(bias + o.n0 + col, count, bv);
   const float* from = region + r0 * S::LD + lane % S::LPR * 8;
   float* to = region + (lane & 31) * S::LD + 4 * (lane >> 5);
   const int64_t m = o.m0 + wm + r0, n = o.n0 + col;
@@ -318,17 +320,17 @@ __device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ld
         if constexpr (EPI) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] += bv[e];
-          if (z) store8(zp, 8, v);
+          if (z) store8(zp, count, v);
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = act_one<ACT>(v[e]);
           if (res) {
             float rv[8];
-            load8(rp, 8, rv);
+            load8(rp, count, rv);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += rv[e];
           }
         }
-        store8(cp, 8, v);
+        store8(cp, count, v);
       }
       left -= S::RPI;
       cp += S::RPI * ldc;
@@ -340,53 +342,26 @@ __device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ld
   });
 }
 
-// Any number of columns: element by element.
-template <class C, typename E, bool EPI>
-__device__ __forceinline__ void store_elements(const Product& p, const Work<E>& o, const f32x16 (&acc)[C::NBM][C::NBN],
-                                               int wm, int wn, int lane) {
-  static_for<C::NBN>([&](auto jt) {
-    static_for<C::NBM>([&](auto it) {
-      constexpr int i = decltype(it)::value, j = decltype(jt)::value;
-      const int row = wm + 32 * i + (lane & 31);
-      // (a loop over a copy in registers of its own would be one over memory)
-      static_for<16>([&](auto qt) {
-        constexpr int q = decltype(qt)::value;
-        const int col = wn + 32 * j + 8 * (q / 4) + 4 * (lane >> 5) + q % 4;
-        float v = acc[i][j][q];
-        asm volatile("" : "+v"(v));
-        if (row < o.rows && col < o.cols) {
-          const int64_t m = o.m0 + row, n = o.n0 + col;
-          if (p.splits > 1) {
-            p.part[(int64_t(blockIdx.y) * p.M + m) * p.N + n] = v;
-          } else {
-            if constexpr (EPI) {
-              if (p.bias) v += float(static_cast<const E*>(p.bias)[n]);
-              if (p.z) static_cast<E*>(p.z)[m * p.ldz + n] = E(v);
-              v = act_of(p.act, v);
-              if (p.res) v += float(static_cast<const E*>(p.res)[m * p.ldr + n]);
-            }
-            o.c[m * p.ldc + n] = E(v);
-          }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      });
+template <class C, typename E, bool EPI, bool RAGGED>
+__device__ __forceinline__ void store_columns(const Product& p, const Work<E>& o,
+                                              const f32x16 (&acc)[C::NBM][C::NBN], float* region, int wm, int wn,
+                                              int lane) {
+  if (p.splits > 1) {
+    store_piece<C, E, float, MUON_ACT_NONE, false, RAGGED>(p, p.part + int64_t(blockIdx.y) * p.M * p.N, p.N, o, acc,
+                                                           region, wm, wn, lane);
+  } else {
+    with_act<EPI>(p.act, [&](auto act) {
+      store_piece<C, E, E, decltype(act)::value, EPI, RAGGED>(p, o.c, p.ldc, o, acc, region, wm, wn, lane);
     });
-  });
+  }
 }
-
 template <class C, typename E, bool EPI>
 __device__ __forceinline__ void store_tile(const Product& p, const Work<E>& o, const f32x16 (&acc)[C::NBM][C::NBN],
                                            float* region, int wm, int wn, int lane) {
-  if (p.N % 8) {
-    store_elements<C, E, EPI>(p, o, acc, wm, wn, lane);
-  } else if (p.splits > 1) {
-    store_piece<C, E, float, MUON_ACT_NONE, false>(p, p.part + int64_t(blockIdx.y) * p.M * p.N, p.N, o, acc, region,
-                                                   wm, wn, lane);
-  } else {
-    with_act<EPI>(p.act, [&](auto act) {
-      store_piece<C, E, E, decltype(act)::value, EPI>(p, o.c, p.ldc, o, acc, region, wm, wn, lane);
-    });
-  }
+  if (o.cols % 8)
+    store_columns<C, E, EPI, true>(p, o, acc, region, wm, wn, lane);
+  else
+    store_columns<C, E, EPI, false>(p, o, acc, region, wm, wn, lane);
 }
 
 template <typename E, int TM, int TN, int U, int FORM, int GROUP>
