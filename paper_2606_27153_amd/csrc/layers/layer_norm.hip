@@ -199,7 +199,7 @@ norm_backward_kernel(NormArgs a) {
   using S = Shape<T>;
   constexpr int V = 16 / int(sizeof(E));
   __shared__ float red[2][2 * S::THREADS / 64];
-  __shared__ float sums[SUMS && S::ROWS > 1 ? S::ROWS : 1][SUMS && S::ROWS > 1 ? T * NV * V : 1];
+  __shared__ __attribute__((aligned(16))) float sums[SUMS && S::ROWS > 1 ? S::ROWS : 1][SUMS && S::ROWS > 1 ? T * NV * V : 1];
   // thread t's chunk j at (j T + t) V, as it holds it
   __shared__ __attribute__((aligned(16))) float weights[T * NV * V];
   const int t = threadIdx.x % T, row = threadIdx.x / T;
@@ -301,27 +301,43 @@ norm_backward_kernel(NormArgs a) {
     }
   }
   if constexpr (SUMS) {
+    typedef float f4 __attribute__((ext_vector_type(4)));
+    struct __attribute__((packed, aligned(4))) P4 {
+      f4 v;
+    };
     for (int k = 0; k < 2; ++k) {
       float* part = a.part + (int64_t(blockIdx.x) * 2 + k) * a.cols;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const Place at = place<V, T>(t, j, a.cols);
+        float v[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float v = k ? pb[j][e] : pw[j][e];
-          if (e < at.dup) continue;
-          if constexpr (S::ROWS > 1)
-            sums[row][at.col + e] = v;
-          else
-            part[at.col + e] = v;
+        for (int e = 0; e < V; ++e) v[e] = k ? pb[j][e] : pw[j][e];
+        if constexpr (S::ROWS > 1) {
+          // (as the threads hold them)
+#pragma unroll
+          for (int q = 0; q < V; q += 4)
+            *reinterpret_cast<f4*>(&sums[row][(j * T + t) * V + q]) = f4{v[q], v[q + 1], v[q + 2], v[q + 3]};
+        } else {
+          const Place at = place<V, T>(t, j, a.cols);
+          if (at.dup == 0) {
+#pragma unroll
+            for (int q = 0; q < V; q += 4)
+              *reinterpret_cast<P4*>(part + at.col + q) = P4{f4{v[q], v[q + 1], v[q + 2], v[q + 3]}};
+          } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+              if (e >= at.dup) part[at.col + e] = v[e];
+          }
         }
       }
       if constexpr (S::ROWS > 1) {
         __syncthreads();
+        const int whole = a.cols / V * V;   // the columns from here on lie in a chunk that was moved back
         for (int c = threadIdx.x; c < a.cols; c += S::THREADS) {
+          const int at = c < whole ? c : whole + c - (a.cols - V);
           float v = 0.f;
 #pragma unroll
-          for (int q = 0; q < S::ROWS; ++q) v += sums[q][c];
+          for (int q = 0; q < S::ROWS; ++q) v += sums[q][at];
           part[c] = v;
         }
         __syncthreads();
