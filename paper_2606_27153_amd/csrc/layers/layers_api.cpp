@@ -145,7 +145,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // The tile kernels, and the measured times their expected run time is made of:
 // us a slab (64 K in bf16, 32 in fp32) with the chip full and with one block on a
 // CU, us for everything else of a tile (its first loads and its epilogue; act:
-// more for an activation where nothing runs beside it), and blocks per CU.  Where
+// more for an activation), and blocks per CU.  Where
 // two blocks share a CU, `full` is for the two.
 struct TileKind {
   Choice::Kernel kernel;
@@ -153,10 +153,10 @@ struct TileKind {
   double full, alone, rest, act;
   int per_cu;
 };
-constexpr TileKind kBf16Tiles[] = {{Choice::TILE256, 256, 256, 1.55, 1.1, 7, 8, 1},
-                                   {Choice::TILE128X256, 128, 256, 0.9, 0.66, 5, 4, 1},
-                                   {Choice::TILE128, 128, 128, 0.95, 0.53, 5, 0, 2},
-                                   {Choice::TILE64, 64, 64, 0.4, 0.29, 3, 0, 2}};
+constexpr TileKind kBf16Tiles[] = {{Choice::TILE256, 256, 256, 1.55, 1.1, 7, 5, 1},
+                                   {Choice::TILE128X256, 128, 256, 0.9, 0.66, 5, 3, 1},
+                                   {Choice::TILE128, 128, 128, 0.95, 0.53, 5, 3.5, 2},
+                                   {Choice::TILE64, 64, 64, 0.4, 0.29, 3, 1, 2}};
 constexpr TileKind kF32Tiles[] = {{Choice::TILE128, 128, 128, 4.0, 2.05, 4.5, 0, 2},
                                   {Choice::TILE64, 64, 64, 1.08, 0.57, 3.5, 0, 2}};
 
