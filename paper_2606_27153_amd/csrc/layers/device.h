@@ -16,9 +16,9 @@ __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf
 
 // The normal distribution function, from the rational approximation of erf by
 // Abramowitz and Stegun (7.1.26, off by 1.5e-7 at most, the size of fp32's own
-// rounding of 1 + erf), and e = exp(-z^2 / 2), which its density needs too.  A
-// seventh of the instructions of the library's erf, which took a third of the
-// time of a 512 x 256 x 1024 product in fp32.
+// rounding of 1 + erf), and e = exp(-z^2 / 2), which its density needs too.  With
+// the library's erf, whose branches a wave takes both, a 512 x 256 x 1024 product
+// in fp32 took 12.3 us instead of 11.1, its activation gradient 7.5 instead of 5.8.
 __device__ __forceinline__ float normal_cdf(float z, float& e) {
   const float a = fabsf(z) * 0.70710678118654752f;
   const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, a, 1.f));

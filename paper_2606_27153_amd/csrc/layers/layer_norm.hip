@@ -8,9 +8,9 @@
 //
 // All sums are fp32.  The variance is summed around the mean (a second pass),
 // not as E[x^2] - mean^2, which cancels for rows far from 0.  Memory bound:
-// 16384 x 4096 in bf16 50 us forward (5.4 TB/s) and 93 us backward (4.3 TB/s of x,
-// dy and dx; its partial sums are another 25 MB), 5832 x 1152 18 us backward, where
-// a wave has two rows and the chain of its loads and sums shows.
+// 16384 x 4096 in bf16 50 us forward (5.4 TB/s) and 86 us backward (4.7 TB/s of x,
+// dy and dx; its partial sums are another 25 MB), 5832 x 1152 17 us backward, where
+// a wave has four rows and the chain of its loads and sums shows.
 #include "device.h"
 
 namespace muon {

@@ -145,8 +145,8 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // The tile kernels, and the measured times their expected run time is made of:
 // us a slab (64 K in bf16, 32 in fp32) with the chip full and with one block on a
 // CU, us for everything else of a tile (its first loads and its epilogue; act:
-// more for an activation), and blocks per CU.  Where
-// two blocks share a CU, `full` is for the two.
+// more for an activation), and blocks per CU.  Where two blocks share a CU, `full`
+// is for the two.
 struct TileKind {
   Choice::Kernel kernel;
   int tm, tn;
