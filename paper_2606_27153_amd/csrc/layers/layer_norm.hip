@@ -46,7 +46,6 @@ __device__ __forceinline__ float weight_at(const void* w, int, int64_t i, const 
 // current one is reduced, so that the memory never waits for the reductions.
 // Loads and stores are 16 bytes at any alignment, and no load sits in a branch
 // (which would end in a wait for it).
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <typename E>
 struct __attribute__((packed, aligned(sizeof(E)))) Chunk {
   E v[16 / sizeof(E)];

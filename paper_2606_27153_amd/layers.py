@@ -110,7 +110,8 @@ def _on_device(fn):
     """Runs fn with its first tensor's device current (which it nearly always is)."""
     @functools.wraps(fn)
     def run(*args, **kwargs):
-        index = (args[0] if args else next(iter(kwargs.values()))).device.index
+        t = args[0] if args else kwargs.get("dy", kwargs.get("x"))
+        index = None if t is None else t.device.index
         if index is None or index == torch._C._cuda_getDevice():
             return fn(*args, **kwargs)
         with torch.cuda.device(index):
@@ -463,10 +464,10 @@ def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, b
 @_on_device
 def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor,
                         rstd: torch.Tensor, *, input_grad: bool = True, weight_grad: bool = True,
-                        bias_grad: bool = True):
+                        bias_grad: bool = True, bias_dtype: Optional[torch.dtype] = None):
     """Gradients ``(dx, dweight, dbias)`` of ``layer_norm_forward``; those not
-    asked for are None.  dweight and dbias have the weight's dtype (x's without
-    a weight)."""
+    asked for are None.  dweight and dbias have the weight's dtype; without a
+    weight, ``bias_dtype`` (float32 or x's, which is the default)."""
     lib = _load()
     _input(x)
     code = _dtype_code(x)
@@ -474,6 +475,10 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
     xp, ldx = _rows(x, "x", x, rows, cols)
     gp, ldg = _rows(dy, "dy", x, rows, cols)
     wp, _, wcode = _norm_vectors(x, (("weight", weight), ("bias", None)), cols)
+    if weight is None and bias_dtype is not None:
+        if bias_dtype not in (torch.float32, x.dtype):
+            raise ValueError(f"bias_dtype {bias_dtype}, expected float32 or {x.dtype}")
+        wcode = _DTYPES[bias_dtype]
     for name, t in (("mean", mean), ("rstd", rstd)):
         if t.dtype != torch.float32 or t.dim() != 1 or t.size(0) != rows or (rows > 1 and t.stride(0) != 1):
             raise ValueError(f"{name} must be a contiguous float32 vector of {rows} elements")
@@ -508,8 +513,8 @@ class _LayerNorm(torch.autograd.Function):
         x, weight, mean, rstd = ctx.saved_tensors
         nx, nw, nb = ctx.needs_input_grad[:3]
         dx, dw, db = layer_norm_backward(_dense(dy), x, weight, mean, rstd, input_grad=nx, weight_grad=nw,
-                                         bias_grad=nb)
-        return dx, dw, db if db is None else db.to(ctx.bias_dtype), None
+                                         bias_grad=nb, bias_dtype=ctx.bias_dtype)
+        return dx, dw, db, None
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,

@@ -652,3 +652,23 @@ def test_bad_arguments_are_refused():
         layers.layer_norm_forward(x, eps=-1.0)
     with pytest.raises(MuonError, match="eps"):
         layers.layer_norm_forward(x, eps=float("nan"))
+
+
+def test_layer_norm_bias_of_another_dtype_without_a_weight():
+    g = gen(71)
+    x, b = rand(g, 40, 96, dtype=torch.bfloat16).requires_grad_(), rand(g, 96).requires_grad_()
+    c = rand(g, 40, 96, dtype=torch.bfloat16)
+    (layers.layer_norm(x, None, b) * c).sum().backward()
+    assert b.grad.dtype == torch.float32
+    want = R.f64(c).sum(0)
+    assert ((R.f64(b.grad) - want).abs() <= 48 * R.U * R.f64(c).abs().sum(0)).all()
+
+
+def test_operators_take_keywords():
+    g = gen(72)
+    x, w = rand(g, 3, 16), rand(g, 16, 8)
+    y = layers.linear_forward(x=x, weight=w)
+    assert torch.equal(y, layers.linear_forward(x, w))
+    dx, dw, _ = layers.linear_backward(x=x, dy=y, weight=w)
+    assert all(torch.equal(a, b) for a, b in zip((dx, dw), layers.linear_backward(y, x, w)[:2]))
+    assert torch.equal(layers.layer_norm_forward(weight=None, x=x), layers.layer_norm_forward(x))
