@@ -259,8 +259,11 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     lead = x.shape[:-1]
     x2 = x.reshape(-1, x.shape[-1]) if x.dim() != 2 else x
     r2 = residual
-    if residual is not None and residual.dim() != 2:
-        r2 = residual.reshape(-1, residual.shape[-1])
+    if residual is not None:
+        if residual.shape[:-1] != lead:   # (as many rows in another order are other rows)
+            raise ValueError(f"residual has shape {tuple(residual.shape)}, expected {(*lead, weight.shape[-1])}")
+        if residual.dim() != 2:
+            r2 = residual.reshape(-1, residual.shape[-1])
     y = _Linear.apply(_dense(x2), weight, bias, None if r2 is None else _dense(r2), activation)
     return y if x.dim() == 2 else y.view(*lead, y.shape[-1])
 

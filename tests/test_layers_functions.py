@@ -1,0 +1,51 @@
+"""The differentiable layer functions without a GPU: what they check themselves
+and what they ask of the passes, which are replaced by plain torch ones."""
+import pytest
+import torch
+
+from paper_2606_27153_amd import layers
+
+
+@pytest.fixture
+def passes(monkeypatch):
+    """Plain passes that note how they were called."""
+    seen = []
+
+    def linear_forward(x, weight, *, bias=None, residual=None, activation="none", keep_preactivation=False):
+        seen.append(("linear_forward", keep_preactivation))
+        z = x @ weight if bias is None else x @ weight + bias
+        y = torch.relu(z) if activation == "relu" else z
+        y = y if residual is None else y + residual
+        return (y, z) if keep_preactivation else y
+
+    def linear_backward(dy, x, weight, *, preactivation=None, activation="none", bias_grad=False, input_grad=True,
+                        weight_grad=True):
+        seen.append(("linear_backward", dy.stride(), dy.data_ptr()))
+        dz = dy * (preactivation > 0) if activation == "relu" else dy
+        return (dz @ weight.t() if input_grad else None, x.t() @ dz if weight_grad else None,
+                dz.sum(0) if bias_grad else None)
+
+    def layer_norm_forward(x, weight=None, bias=None, *, eps=1e-5, keep_stats=False):
+        seen.append(("layer_norm_forward", keep_stats))
+        mean = x.mean(1)
+        rstd = torch.rsqrt(x.var(1, unbiased=False) + eps)
+        y = (x - mean[:, None]) * rstd[:, None]
+        return (y, mean, rstd) if keep_stats else y
+
+    for f in (linear_forward, linear_backward, layer_norm_forward):
+        monkeypatch.setattr(layers, f.__name__, f)
+    return seen
+
+
+def test_linear_refuses_a_residual_of_other_leading_dimensions(passes):
+    """As many rows are not enough: with its dimensions swapped, the residual's rows are others."""
+    x, w = torch.randn(2, 9, 20), torch.randn(20, 12)
+    for shape in ((9, 2, 12), (18, 12), (1, 2, 9, 12), (3, 6, 12), (12,)):
+        with pytest.raises(ValueError, match="residual"):
+            layers.linear(x, w, residual=torch.randn(shape))
+    with pytest.raises(ValueError, match="residual"):
+        layers.linear(x.view(18, 20), w, residual=torch.randn(2, 9, 12))
+    r = torch.randn(2, 9, 12)
+    assert torch.allclose(layers.linear(x, w, residual=r), x @ w + r, atol=1e-5)
+    assert layers.linear(x[0, 0], w, residual=r[0, 0]).shape == (12,)
+    assert layers.linear(x[:0], w, residual=r[:0]).shape == (0, 9, 12)
