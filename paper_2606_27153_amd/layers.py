@@ -230,8 +230,9 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, *,
 
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, residual, activation):
-        need = any(ctx.needs_input_grad[:3])
+    def forward(ctx, x, weight, bias, residual, activation, grad_mode):
+        # needs_input_grad says what requires a gradient, also where none is taken
+        need = grad_mode and any(ctx.needs_input_grad[:3])
         y, z = linear_forward(x, weight, bias=bias, residual=residual, activation=activation,
                               keep_preactivation=True) if need else \
             (linear_forward(x, weight, bias=bias, residual=residual, activation=activation), None)
@@ -248,7 +249,7 @@ class _Linear(torch.autograd.Function):
         if nx or nw or nb:
             dx, dw, db = linear_backward(dy.contiguous(), x, weight, preactivation=z, activation=ctx.activation,
                                          bias_grad=nb, input_grad=nx, weight_grad=nw)
-        return dx, dw, db, dy if nr else None, None
+        return dx, dw, db, dy if nr else None, None, None
 
 
 def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, *,
@@ -264,7 +265,8 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
             raise ValueError(f"residual has shape {tuple(residual.shape)}, expected {(*lead, weight.shape[-1])}")
         if residual.dim() != 2:
             r2 = residual.reshape(-1, residual.shape[-1])
-    y = _Linear.apply(_dense(x2), weight, bias, None if r2 is None else _dense(r2), activation)
+    y = _Linear.apply(_dense(x2), weight, bias, None if r2 is None else _dense(r2), activation,
+                      torch.is_grad_enabled())
     return y if x.dim() == 2 else y.view(*lead, y.shape[-1])
 
 
@@ -504,7 +506,9 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
 
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, eps):
+    def forward(ctx, x, weight, bias, eps, grad_mode):
+        if not (grad_mode and any(ctx.needs_input_grad[:3])):
+            return layer_norm_forward(x, weight, bias, eps=eps)
         y, mean, rstd = layer_norm_forward(x, weight, bias, eps=eps, keep_stats=True)
         ctx.bias_dtype = None if bias is None else bias.dtype
         ctx.save_for_backward(x, weight, mean, rstd)
@@ -517,12 +521,12 @@ class _LayerNorm(torch.autograd.Function):
         nx, nw, nb = ctx.needs_input_grad[:3]
         dx, dw, db = layer_norm_backward(_dense(dy), x, weight, mean, rstd, input_grad=nx, weight_grad=nw,
                                          bias_grad=nb, bias_dtype=ctx.bias_dtype)
-        return dx, dw, db, None
+        return dx, dw, db, None, None
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
                eps: float = 1e-5) -> torch.Tensor:
     """Layer norm over the last dimension of x, differentiable once."""
     x2 = x.reshape(-1, x.shape[-1]) if x.dim() != 2 else x
-    y = _LayerNorm.apply(_dense(x2), weight, bias, float(eps))
+    y = _LayerNorm.apply(_dense(x2), weight, bias, float(eps), torch.is_grad_enabled())
     return y if x.dim() == 2 else y.view(x.shape)

@@ -49,3 +49,22 @@ def test_linear_refuses_a_residual_of_other_leading_dimensions(passes):
     assert torch.allclose(layers.linear(x, w, residual=r), x @ w + r, atol=1e-5)
     assert layers.linear(x[0, 0], w, residual=r[0, 0]).shape == (12,)
     assert layers.linear(x[:0], w, residual=r[:0]).shape == (0, 9, 12)
+
+
+@pytest.mark.parametrize("mode", [torch.no_grad, torch.inference_mode])
+def test_nothing_is_kept_where_nothing_will_be_differentiated(passes, mode):
+    x, w, b = torch.randn(5, 8), torch.nn.Parameter(torch.randn(8, 6)), torch.nn.Parameter(torch.zeros(6))
+    n = torch.nn.Parameter(torch.ones(8))
+    with mode():
+        layers.linear(x, w, b, activation="relu")
+        layers.layer_norm(x, n)
+    assert passes == [("linear_forward", False), ("layer_norm_forward", False)]
+    passes.clear()
+    layers.linear(x, w.detach(), residual=torch.zeros(5, 6, requires_grad=True), activation="relu")
+    layers.layer_norm(x, n.detach())
+    assert passes == [("linear_forward", False), ("layer_norm_forward", False)]
+    passes.clear()
+    layers.linear(x, w.detach(), b, activation="relu").sum().backward()
+    layers.layer_norm(x, n)
+    assert [p[:2] for p in passes if "forward" in p[0]] == [("linear_forward", True), ("layer_norm_forward", True)]
+    assert b.grad is not None
