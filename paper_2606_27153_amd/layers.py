@@ -247,7 +247,7 @@ class _Linear(torch.autograd.Function):
         nx, nw, nb, nr = ctx.needs_input_grad[:4]
         dx = dw = db = None
         if nx or nw or nb:
-            dx, dw, db = linear_backward(dy.contiguous(), x, weight, preactivation=z, activation=ctx.activation,
+            dx, dw, db = linear_backward(_once(dy), x, weight, preactivation=z, activation=ctx.activation,
                                          bias_grad=nb, input_grad=nx, weight_grad=nw)
         return dx, dw, db, dy if nr else None, None, None
 
@@ -275,6 +275,15 @@ def _dense(t: torch.Tensor) -> torch.Tensor:
     if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.size(1):
         return t
     return t.contiguous()
+
+
+def _once(dy: torch.Tensor) -> torch.Tensor:
+    """A gradient for both products that read it: as it lies, or copied here where
+    each of them would have to (rows off 16-byte chunks)."""
+    dy = _dense(dy)
+    if (dy.stride(0) * dy.element_size() | dy.data_ptr()) & 15:
+        return dy.contiguous()
+    return dy
 
 
 # ----------------------------------------------------------- grouped linear

@@ -22,3 +22,22 @@ def test_no_preactivation_is_written_where_no_gradient_will_be_taken(mode):
         got = layers.linear(x, w, activation="silu")
         assert torch.cuda.max_memory_allocated() - before < 1.5 * size
     assert not got.requires_grad and torch.equal(got, y)
+
+
+def test_strided_output_gradients_give_the_same_gradients():
+    """Halves of a concatenation's gradient, at aligned and unaligned rows, against contiguous ones."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    for dtype in (torch.float32, torch.bfloat16):
+        for rows, inner, outer, wide, act in ((300, 128, 64, 192, "none"), (300, 128, 64, 192, "gelu"),
+                                              (70, 65, 33, 40, "none"), (5, 40, 24, 27, "silu")):
+            x = torch.randn(rows, inner, generator=g, device=DEV).to(dtype)
+            w = torch.randn(inner, outer, generator=g, device=DEV).to(dtype)
+            dy = torch.randn(rows, wide, generator=g, device=DEV).to(dtype)
+            grads = []
+            for d in (dy[:, :outer], dy[:, :outer].clone()):
+                xx, ww = x.clone().requires_grad_(), w.clone().requires_grad_()
+                layers.linear(xx, ww, activation=act).backward(d)
+                grads.append((xx.grad, ww.grad))
+            for a, b in zip(*grads):
+                assert torch.equal(a, b)

@@ -68,3 +68,22 @@ def test_nothing_is_kept_where_nothing_will_be_differentiated(passes, mode):
     layers.layer_norm(x, n)
     assert [p[:2] for p in passes if "forward" in p[0]] == [("linear_forward", True), ("layer_norm_forward", True)]
     assert b.grad is not None
+
+
+def test_a_strided_output_gradient_is_taken_as_it_lies(passes):
+    """Half of a concatenation's gradient: rows of 6 in rows of 16."""
+    x, w = torch.randn(5, 8), torch.randn(8, 6, requires_grad=True)
+    other = torch.randn(5, 10)
+    g = torch.randn(5, 16)
+    torch.cat([layers.linear(x, w), other], dim=1).backward(g)
+    assert passes[-1][0] == "linear_backward" and passes[-1][1] == (16, 1)
+    assert torch.allclose(w.grad, x.t() @ g[:, :6], atol=1e-5)
+    w.grad = None
+    layers.linear(x, w).backward(torch.randn(6, 5).t())      # rows that are not contiguous are copied
+    assert passes[-1][1] == (6, 1)
+    w.grad = None
+    layers.linear(x, w).sum().backward()                      # so is an expanded one
+    assert passes[-1][1] == (6, 1)
+    w.grad = None
+    torch.cat([layers.linear(x, w), other[:, :9]], dim=1).backward(torch.randn(5, 15))
+    assert passes[-1][1] == (6, 1)                            # and one off 16-byte rows: once, for both products
