@@ -13,7 +13,8 @@ weight's own memory layout, so that ``Muon`` steps them without a copy.
 Tensors are fp32 or bf16 (one dtype per call; layer norm's weight and bias may be
 fp32 next to bf16 activations), sums are fp32.  Rows may be strided (a slice of
 wider rows), their elements may not.  A bad argument raises ValueError or
-TypeError before anything is launched.
+TypeError before anything is launched; a number that the library refuses (eps, sizes
+out of its range) MuonError.
 """
 from __future__ import annotations
 
@@ -37,6 +38,11 @@ def _load():
     return _lib
 
 
+def _tensor(t, name: str) -> None:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor, not {type(t).__name__}")
+
+
 def _dtype_code(t: torch.Tensor) -> int:
     code = _DTYPES.get(t.dtype)
     if code is None:
@@ -46,6 +52,7 @@ def _dtype_code(t: torch.Tensor) -> int:
 
 def _rows(t: torch.Tensor, name: str, like: torch.Tensor, rows: Optional[int], cols: int):
     """(pointer, leading dimension) of a 2-D tensor whose rows are contiguous."""
+    _tensor(t, name)
     if t.dim() != 2 or t.size(1) != cols or (rows is not None and t.size(0) != rows):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({'rows' if rows is None else rows}, {cols})")
     _same(t, name, like)
@@ -69,6 +76,7 @@ def _same(t: torch.Tensor, name: str, like: torch.Tensor) -> None:
 def _vector(t: Optional[torch.Tensor], name: str, like: torch.Tensor, n: int):
     if t is None:
         return None
+    _tensor(t, name)
     if t.dim() != 1 or t.size(0) != n or (n > 1 and t.stride(0) != 1):
         raise ValueError(f"{name} must be a contiguous vector of {n} elements")
     _same(t, name, like)
@@ -78,6 +86,7 @@ def _vector(t: Optional[torch.Tensor], name: str, like: torch.Tensor, n: int):
 def _weight(w: torch.Tensor, like: torch.Tensor, inner: int):
     """(pointer, leading dimension, transposed, outer) of a weight [inner, outer]
     kept by rows, or by columns (the transposed view of an [outer, inner] one)."""
+    _tensor(w, "weight")
     if w.dim() != 2 or w.size(0) != inner:
         raise ValueError(f"weight has shape {tuple(w.shape)}, expected ({inner}, out)")
     _same(w, "weight", like)
@@ -91,6 +100,7 @@ def _weight(w: torch.Tensor, like: torch.Tensor, inner: int):
 
 
 def _input(x: torch.Tensor, name: str = "x") -> None:
+    _tensor(x, name)
     if x.dim() != 2:
         raise ValueError(f"{name} must be 2-D [rows, features], got shape {tuple(x.shape)}")
     if not x.is_cuda:
@@ -111,7 +121,7 @@ def _on_device(fn):
     @functools.wraps(fn)
     def run(*args, **kwargs):
         t = args[0] if args else kwargs.get("dy", kwargs.get("x"))
-        index = None if t is None else t.device.index
+        index = t.device.index if isinstance(t, torch.Tensor) else None
         if index is None or index == torch._C._cuda_getDevice():
             return fn(*args, **kwargs)
         with torch.cuda.device(index):
@@ -257,10 +267,13 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     """``act(x @ weight + bias) + residual`` over the last dimension of x,
     differentiable once.  weight is [in, out] (or the transposed view of an
     [out, in] one); activation is "none", "relu", "gelu", "gelu_tanh" or "silu"."""
+    _tensor(x, "x")
+    _tensor(weight, "weight")
     lead = x.shape[:-1]
     x2 = x.reshape(-1, x.shape[-1]) if x.dim() != 2 else x
     r2 = residual
     if residual is not None:
+        _tensor(residual, "residual")
         if residual.shape[:-1] != lead:   # (as many rows in another order are other rows)
             raise ValueError(f"residual has shape {tuple(residual.shape)}, expected {(*lead, weight.shape[-1])}")
         if residual.dim() != 2:
@@ -311,6 +324,7 @@ def _experts(weights: Weights, like: torch.Tensor, inner: int):
     ptrs = [p]
     for i in range(1, n):
         w = weights[i]
+        _tensor(w, f"weight {i}")
         if w.shape != first.shape or w.stride() != first.stride():
             raise ValueError(f"weight {i} has shape {tuple(w.shape)} and stride {w.stride()}, the first one "
                              f"{tuple(first.shape)} and {first.stride()}")
@@ -320,6 +334,7 @@ def _experts(weights: Weights, like: torch.Tensor, inner: int):
 
 
 def _offsets(offsets: torch.Tensor, n: int, like: torch.Tensor) -> int:
+    _tensor(offsets, "offsets")
     if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.size(0) != n + 1 or offsets.stride(0) != 1:
         raise ValueError(f"offsets must be a contiguous int32 vector of {n + 1} elements")
     if offsets.device != like.device:
@@ -403,7 +418,7 @@ def grouped_linear_backward(dy: torch.Tensor, x: torch.Tensor, weights: Weights,
 class _GroupedLinear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, offsets, *weights):
-        ctx.stacked = len(weights) == 1 and weights[0].dim() == 3
+        ctx.stacked = len(weights) == 1 and isinstance(weights[0], torch.Tensor) and weights[0].dim() == 3
         ctx.save_for_backward(x, offsets, *weights)
         return grouped_linear_forward(x, weights[0] if ctx.stacked else weights, offsets)
 
@@ -425,6 +440,7 @@ def grouped_linear(x: torch.Tensor, weights: Weights, offsets: torch.Tensor) -> 
     """``y[t] = x[t] @ weights[e]`` for the rows offsets[e] <= t < offsets[e + 1]
     of x [rows, in], differentiable once.  weights: one [experts, in, out]
     tensor, or the experts' own [in, out] parameters (which ``Muon`` steps)."""
+    _tensor(x, "x")
     ws = (weights,) if isinstance(weights, torch.Tensor) else tuple(weights)
     return _GroupedLinear.apply(_dense(x), offsets, *ws)
 
@@ -438,6 +454,7 @@ def _norm_vectors(x: torch.Tensor, vectors, cols: int):
         if t is None:
             ptrs.append(None)
             continue
+        _tensor(t, name)
         if t.dim() != 1 or t.size(0) != cols or (cols > 1 and t.stride(0) != 1):
             raise ValueError(f"{name} must be a contiguous vector of {cols} elements")
         if t.device != x.device:
@@ -463,6 +480,7 @@ def layer_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, b
     rows, cols = x.shape
     xp, ldx = _rows(x, "x", x, rows, cols)
     wp, bp, wcode = _norm_vectors(x, (("weight", weight), ("bias", bias)), cols)
+    eps = float(eps)
     stream = _stream(x)
     y = x.new_empty((rows, cols))
     mean = rstd = None
@@ -494,6 +512,7 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
             raise ValueError(f"bias_dtype {bias_dtype}, expected float32 or {x.dtype}")
         wcode = _DTYPES[bias_dtype]
     for name, t in (("mean", mean), ("rstd", rstd)):
+        _tensor(t, name)
         if t.dtype != torch.float32 or t.dim() != 1 or t.size(0) != rows or (rows > 1 and t.stride(0) != 1):
             raise ValueError(f"{name} must be a contiguous float32 vector of {rows} elements")
         if t.device != x.device:
@@ -536,6 +555,7 @@ class _LayerNorm(torch.autograd.Function):
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
                eps: float = 1e-5) -> torch.Tensor:
     """Layer norm over the last dimension of x, differentiable once."""
+    _tensor(x, "x")
     x2 = x.reshape(-1, x.shape[-1]) if x.dim() != 2 else x
     y = _LayerNorm.apply(_dense(x2), weight, bias, float(eps), torch.is_grad_enabled())
     return y if x.dim() == 2 else y.view(x.shape)

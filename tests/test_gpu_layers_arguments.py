@@ -41,3 +41,31 @@ def test_strided_output_gradients_give_the_same_gradients():
                 grads.append((xx.grad, ww.grad))
             for a, b in zip(*grads):
                 assert torch.equal(a, b)
+
+
+def test_arguments_that_are_no_tensors_are_type_errors():
+    x, w, r = torch.randn(4, 8, device=DEV), torch.randn(8, 6, device=DEV), torch.randn(4, device=DEV)
+    dy = torch.randn(4, 6, device=DEV)
+    off = torch.tensor([0, 2, 4], dtype=torch.int32, device=DEV)
+    for bad in (3, [1.0], "w"):
+        for f in (lambda: layers.linear(x, bad), lambda: layers.linear(x, w, bad),
+                  lambda: layers.linear(x, w, residual=bad), lambda: layers.linear_forward(x, bad),
+                  lambda: layers.linear_forward(x, w, bias=bad), lambda: layers.linear_forward(x, w, residual=bad),
+                  lambda: layers.linear_backward(bad, x, w),
+                  lambda: layers.linear_backward(dy, x, w, preactivation=bad, activation="silu"),
+                  lambda: layers.grouped_linear_forward(x, [w, bad], off),
+                  lambda: layers.grouped_linear_forward(x, [bad, w], off),
+                  lambda: layers.grouped_linear_forward(x, [w, w], bad),
+                  lambda: layers.grouped_linear(x, [bad], off), lambda: layers.grouped_linear(x, bad, off),
+                  lambda: layers.grouped_linear(x, [w, w], bad), lambda: layers.layer_norm(x, bad),
+                  lambda: layers.grouped_linear_backward(bad, x, [w, w], off),
+                  lambda: layers.layer_norm_forward(x, bad), lambda: layers.layer_norm_forward(x, None, bad),
+                  lambda: layers.layer_norm_backward(bad, x, None, r, r),
+                  lambda: layers.layer_norm_backward(x, x, None, bad, r),
+                  lambda: layers.layer_norm_backward(x, x, None, r, bad)):
+            with pytest.raises(TypeError):
+                f()
+    with pytest.raises(TypeError):
+        layers.layer_norm_backward(x, x, None, None, r)
+    with pytest.raises(TypeError):
+        layers.layer_norm_forward(x, eps=None)

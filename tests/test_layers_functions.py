@@ -87,3 +87,18 @@ def test_a_strided_output_gradient_is_taken_as_it_lies(passes):
     w.grad = None
     torch.cat([layers.linear(x, w), other[:, :9]], dim=1).backward(torch.randn(5, 15))
     assert passes[-1][1] == (6, 1)                            # and one off 16-byte rows: once, for both products
+
+
+def test_arguments_that_are_no_tensors_are_type_errors():
+    x, w = torch.randn(4, 8), torch.randn(8, 6)
+    off = torch.zeros(2, dtype=torch.int32)
+    for bad in (None, 3, [[1.0] * 8] * 4, "x"):
+        for f in (lambda: layers.linear(bad, w), lambda: layers.layer_norm(bad), lambda: layers.grouped_linear(bad, [w], off),
+                  lambda: layers.linear_forward(bad, w), lambda: layers.linear_backward(x, bad, w),
+                  lambda: layers.layer_norm_forward(bad), lambda: layers.grouped_linear_forward(bad, [w], off),
+                  lambda: layers.linear_forward(x=bad, weight=w),
+                  lambda: layers.layer_norm_backward(x, bad, None, x, x)):
+            with pytest.raises(TypeError):
+                f()
+    with pytest.raises(TypeError):
+        layers.linear(x, w, residual=[1.0])
