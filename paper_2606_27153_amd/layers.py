@@ -267,19 +267,16 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     """``act(x @ weight + bias) + residual`` over the last dimension of x,
     differentiable once.  weight is [in, out] (or the transposed view of an
     [out, in] one); activation is "none", "relu", "gelu", "gelu_tanh" or "silu"."""
-    _tensor(x, "x")
     _tensor(weight, "weight")
+    x2 = _flat(x, "x")
     lead = x.shape[:-1]
-    x2 = x.reshape(-1, x.shape[-1]) if x.dim() != 2 else x
     r2 = residual
     if residual is not None:
         _tensor(residual, "residual")
         if residual.shape[:-1] != lead:   # (as many rows in another order are other rows)
-            raise ValueError(f"residual has shape {tuple(residual.shape)}, expected {(*lead, weight.shape[-1])}")
-        if residual.dim() != 2:
-            r2 = residual.reshape(-1, residual.shape[-1])
-    y = _Linear.apply(_dense(x2), weight, bias, None if r2 is None else _dense(r2), activation,
-                      torch.is_grad_enabled())
+            raise ValueError(f"residual has leading dimensions {tuple(residual.shape[:-1])}, x has {tuple(lead)}")
+        r2 = _flat(residual, "residual")
+    y = _Linear.apply(x2, weight, bias, r2, activation, torch.is_grad_enabled())
     return y if x.dim() == 2 else y.view(*lead, y.shape[-1])
 
 
@@ -288,6 +285,16 @@ def _dense(t: torch.Tensor) -> torch.Tensor:
     if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.size(1):
         return t
     return t.contiguous()
+
+
+def _flat(t: torch.Tensor, name: str) -> torch.Tensor:
+    """t as dense rows of its last dimension."""
+    _tensor(t, name)
+    if t.dim() != 2:
+        if t.dim() == 0 or t.size(-1) == 0:
+            raise ValueError(f"{name} has no features, its shape is {tuple(t.shape)}")
+        t = t.reshape(-1, t.size(-1))
+    return _dense(t)
 
 
 def _once(dy: torch.Tensor) -> torch.Tensor:
@@ -555,7 +562,5 @@ class _LayerNorm(torch.autograd.Function):
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, *,
                eps: float = 1e-5) -> torch.Tensor:
     """Layer norm over the last dimension of x, differentiable once."""
-    _tensor(x, "x")
-    x2 = x.reshape(-1, x.shape[-1]) if x.dim() != 2 else x
-    y = _LayerNorm.apply(_dense(x2), weight, bias, float(eps), torch.is_grad_enabled())
+    y = _LayerNorm.apply(_flat(x, "x"), weight, bias, float(eps), torch.is_grad_enabled())
     return y if x.dim() == 2 else y.view(x.shape)

@@ -102,3 +102,14 @@ def test_arguments_that_are_no_tensors_are_type_errors():
                 f()
     with pytest.raises(TypeError):
         layers.linear(x, w, residual=[1.0])
+
+
+def test_inputs_without_features_are_value_errors():
+    w = torch.randn(8, 6)
+    for bad in (torch.tensor(1.0), torch.zeros(2, 3, 0), torch.zeros(0)):
+        with pytest.raises(ValueError):
+            layers.linear(bad, w)
+        with pytest.raises(ValueError):
+            layers.layer_norm(bad)
+    with pytest.raises(ValueError):
+        layers.linear(torch.zeros(2, 8), torch.tensor(1.0), residual=torch.zeros(2, 1, 6))
