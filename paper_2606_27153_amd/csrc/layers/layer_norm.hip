@@ -8,9 +8,10 @@
 //
 // All sums are fp32.  The variance is summed around the mean (a second pass),
 // not as E[x^2] - mean^2, which cancels for rows far from 0.  Memory bound:
-// 16384 x 4096 in bf16 50 us forward (5.4 TB/s) and 86 us backward (4.7 TB/s of x,
-// dy and dx; its partial sums are another 25 MB), 5832 x 1152 17 us backward, where
-// a wave has four rows and the chain of its loads and sums shows.
+// 16384 x 4096 in bf16 49 us forward (5.4 TB/s) and 85 us backward (4.7 TB/s of x,
+// dy and dx; its partial sums are another 25 MB), in fp32 94 and 158; 5832 x 1152
+// 17 to 18 us backward (fp32: 19), where a wave has four rows and the chain of its loads
+// and sums shows.
 #include "device.h"
 
 namespace muon {
@@ -476,7 +477,9 @@ hipError_t forward(const NormArgs& a, hipStream_t st) {
   } else {
     with_shape<E, 1024>(a.cols, t, [&](auto nv, auto tt) {
       using S = Shape<decltype(tt)::value>;
-      // as many blocks as the chip holds at once, 2048 threads per CU
+      // 2048 threads per CU: what the chip holds of rows of one chunk per thread (54 to
+      // 62 registers); of two to four bf16 chunks a thread has 84 to 164, and 3 to 5
+      // blocks of 256 run at a time (fp32: 62 to 184, 2 to 8)
       const int64_t groups = (int64_t(a.rows) + S::ROWS - 1) / S::ROWS, most = int64_t(kCUs) * 2048 / S::THREADS;
       const dim3 g{unsigned(groups < most ? groups : most)}, b{S::THREADS};
       // (1024 threads hold 16 elements each: forward_threads)
@@ -519,9 +522,10 @@ hipError_t backward(const NormArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Blocks of the backward pass: what the chip holds at once (3 of 256 threads, 1
-// of 512 per CU), and at least four rows per thread group, so that their partial
-// sums stay few.
+// Blocks of the backward pass: 3 of 256 threads, 1 of 512 per CU, and at least four
+// rows per thread group, so that their partial sums stay few.  The chip holds them all
+// at once but for fp32 rows of 1025 to 1536 and of 4097 to 6144 columns, whose threads
+// take 190 and 206 registers: two of their blocks fit on a CU, the others follow.
 int norm_blocks(int64_t rows, int64_t cols) {
   const int t = backward_threads(cols);
   const int64_t group = t == 64 ? 4 : 1, most = kCUs * (t == 512 ? 1 : 3);

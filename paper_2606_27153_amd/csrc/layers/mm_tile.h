@@ -27,16 +27,18 @@
 // sums are never stored.  Where K ends inside a slab, the chunks past it come
 // from a block of zeros.
 //
-// Bound by the matrix cores and the chip's power: 256 x 256 tiles reach 1425
-// TFLOP/s on 8192^3 with K-contiguous operands (772 us; 916 with a tr B, 816 with
-// both tr), 1340 on 16384 x 14336 x 4096.  Four waves of 128 x 128 read half the LDS
-// bytes per MFMA of eight of 128 x 64; with one wave per SIMD nothing hides a
-// wave's own waits, which is what the ring and the spread loads are for (two
-// whole-slab stages, loaded in one burst: 8192^3 870 us).  128 x 128 tiles with two
-// blocks per CU reach 1150, and fill the chip from a quarter of the size on;
-// 128 x 256 lies between; 64 x 64 serves products of a few hundred rows (1024 x
-// 2048 x 2048 17 us).  fp32 runs at 135 TFLOP/s on 128 x 128 tiles (4096^3), 154 being
-// what the matrix cores sustain.
+// Bound by the matrix cores and the chip's power (71% of the cycles are MFMA's at
+// 1.4 GHz on 16384 x 14336 x 4096): launched back to back, 256 x 256 tiles take 794 to
+// 805 us on 8192^3 with K-contiguous operands (1365 to 1385 TFLOP/s), 822 to 825 with a
+// tr B, 825 to 833 with both tr, and reach 1295 TFLOP/s on 16384 x 14336 x 4096.  Four
+// waves of 128 x 128 read half the LDS bytes per MFMA of eight of 128 x 64; with one
+// wave per SIMD nothing hides a wave's own waits, which is what the ring and the spread
+// loads are for (two whole-slab stages, loaded in one burst, took 13% longer on
+// 8192^3).  128 x 256 tiles reach 1130 to 1215 TFLOP/s there, 128 x 128 with two
+// blocks per CU 1060 to 1105, and fill the chip from a quarter of the size on; 64 x 64
+// (560 to 670) serves products of a few hundred rows (1024 x 2048 x 2048 17 us).  fp32
+// runs at 137 to 139 TFLOP/s on 128 x 128 tiles (4096^3, every form; 123 to 127 on
+// 64 x 64), 154 being what the matrix cores sustain.
 #ifndef MUON_LAYERS_MM_TILE_H
 #define MUON_LAYERS_MM_TILE_H
 
