@@ -52,10 +52,12 @@ def _dtype_code(t: torch.Tensor) -> int:
 
 def _rows(t: torch.Tensor, name: str, like: torch.Tensor, rows: Optional[int], cols: int):
     """(pointer, leading dimension) of a 2-D tensor whose rows are contiguous."""
-    _tensor(t, name)
+    if t is not like:
+        _tensor(t, name)
     if t.dim() != 2 or t.size(1) != cols or (rows is not None and t.size(0) != rows):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({'rows' if rows is None else rows}, {cols})")
-    _same(t, name, like)
+    if t is not like:
+        _same(t, name, like)
     ld, step = t.stride()
     if step != 1 and cols != 1:
         raise ValueError(f"{name}'s rows are not contiguous (stride {t.stride()})")
@@ -267,15 +269,13 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     """``act(x @ weight + bias) + residual`` over the last dimension of x,
     differentiable once.  weight is [in, out] (or the transposed view of an
     [out, in] one); activation is "none", "relu", "gelu", "gelu_tanh" or "silu"."""
-    _tensor(weight, "weight")
     x2 = _flat(x, "x")
     lead = x.shape[:-1]
-    r2 = residual
+    r2 = None
     if residual is not None:
-        _tensor(residual, "residual")
+        r2 = _flat(residual, "residual")
         if residual.shape[:-1] != lead:   # (as many rows in another order are other rows)
             raise ValueError(f"residual has leading dimensions {tuple(residual.shape[:-1])}, x has {tuple(lead)}")
-        r2 = _flat(residual, "residual")
     y = _Linear.apply(x2, weight, bias, r2, activation, torch.is_grad_enabled())
     return y if x.dim() == 2 else y.view(*lead, y.shape[-1])
 
@@ -289,7 +289,8 @@ def _dense(t: torch.Tensor) -> torch.Tensor:
 
 def _flat(t: torch.Tensor, name: str) -> torch.Tensor:
     """t as dense rows of its last dimension."""
-    _tensor(t, name)
+    if not isinstance(t, torch.Tensor):
+        _tensor(t, name)
     if t.dim() != 2:
         if t.dim() == 0 or t.size(-1) == 0:
             raise ValueError(f"{name} has no features, its shape is {tuple(t.shape)}")
@@ -328,14 +329,17 @@ def _experts(weights: Weights, like: torch.Tensor, inner: int):
         raise ValueError(f"{n} experts; 1 to {LL.MUON_GROUPED_MAX_EXPERTS} are supported")
     p, ld, t, outer = _weight(weights[0], like, inner)
     first = weights[0]
+    shape, stride, dtype, device = first.shape, first.stride(), like.dtype, like.device
     ptrs = [p]
-    for i in range(1, n):
+    for i in range(1, n):   # (on every call: kept to what it takes)
         w = weights[i]
-        _tensor(w, f"weight {i}")
-        if w.shape != first.shape or w.stride() != first.stride():
+        if not isinstance(w, torch.Tensor):
+            _tensor(w, f"weight {i}")
+        if w.shape != shape or w.stride() != stride:
             raise ValueError(f"weight {i} has shape {tuple(w.shape)} and stride {w.stride()}, the first one "
-                             f"{tuple(first.shape)} and {first.stride()}")
-        _same(w, f"weight {i}", like)
+                             f"{tuple(shape)} and {stride}")
+        if w.dtype != dtype or w.device != device:
+            _same(w, f"weight {i}", like)
         ptrs.append(w.data_ptr())
     return ptrs, ld, t, outer, n
 
