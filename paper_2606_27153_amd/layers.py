@@ -312,6 +312,11 @@ def _once(dy: torch.Tensor) -> torch.Tensor:
 Weights = Union[torch.Tensor, Sequence[torch.Tensor]]
 
 
+def _steps(t: torch.Tensor):
+    """The strides that say where elements lie: those of more than one."""
+    return [s for s, n in zip(t.stride(), t.shape) if n > 1]
+
+
 def _experts(weights: Weights, like: torch.Tensor, inner: int):
     """(pointers, leading dimension, transposed, outer, count) of the experts'
     weights: one [experts, in, out] tensor or a sequence of [in, out] ones."""
@@ -335,7 +340,7 @@ def _experts(weights: Weights, like: torch.Tensor, inner: int):
         w = weights[i]
         if not isinstance(w, torch.Tensor):
             _tensor(w, f"weight {i}")
-        if w.shape != shape or w.stride() != stride:
+        if w.shape != shape or (w.stride() != stride and _steps(w) != _steps(first)):
             raise ValueError(f"weight {i} has shape {tuple(w.shape)} and stride {w.stride()}, the first one "
                              f"{tuple(shape)} and {stride}")
         if w.dtype != dtype or w.device != device:

@@ -113,3 +113,20 @@ def test_inputs_without_features_are_value_errors():
             layers.layer_norm(bad)
     with pytest.raises(ValueError):
         layers.linear(torch.zeros(2, 8), torch.tensor(1.0), residual=torch.zeros(2, 1, 6))
+
+
+def test_strides_of_single_rows_and_columns_do_not_tell_experts_apart():
+    x = torch.randn(3, 1)
+    ws = [torch.randn(1, 8), torch.randn(1, 16)[:, :8], torch.randn(4, 8)[::4]]
+    assert len({w.stride() for w in ws}) > 1
+    ptrs, _, transposed, outer, n = layers._experts(ws, x, 1)
+    assert ptrs == [w.data_ptr() for w in ws] and (transposed, outer, n) == (0, 8, 3)
+    x = torch.randn(3, 8)
+    ws = [torch.randn(8, 1), torch.randn(1, 8).t(), torch.randn(1, 16)[:, :8].t()]
+    assert len({w.stride() for w in ws}) > 1
+    ptrs, ld, transposed, outer, n = layers._experts(ws, x, 8)
+    assert ptrs == [w.data_ptr() for w in ws] and (ld, transposed, outer, n) == (1, 0, 1, 3)
+    with pytest.raises(ValueError):
+        layers._experts([torch.randn(8, 1), torch.randn(8, 2)[:, :1]], x, 8)    # columns of other strides
+    with pytest.raises(ValueError):
+        layers._experts([torch.randn(8, 6), torch.randn(6, 8).t()], x, 8)
