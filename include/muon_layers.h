@@ -11,6 +11,13 @@
  *   norm     mean, rstd = 1 / sqrt(var + eps) per row,
  *            y = (x - mean) rstd w + b;  dx, dw, db
  *
+ * and those at a model's ends and on the way to its experts:
+ *
+ *   embedding              rows of a table by token, and the table's gradient
+ *   sort_by_expert, dispatch, combine
+ *                          a router's choices sorted, tokens to their experts and back
+ *   linear_cross_entropy   softmax cross entropy of x W over a vocabulary
+ *
  * Conventions of muon.h hold: every function returns a muon_status and
  * nothing aborts or throws; muon_layers_last_error() has the message of the
  * last failure on this thread; device buffers and the stream are the
@@ -135,6 +142,105 @@ MUON_API muon_status muon_layer_norm_backward(const void* dy, int64_t lddy, cons
 
 /* Workspace bytes of muon_layer_norm_backward. */
 MUON_API muon_status muon_layer_norm_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes);
+
+/* ------------------------------------------------- tokens and experts by number
+ *
+ * Numbers (tokens, targets, experts' indexes) are int32 or int64 (id_bytes 4 or
+ * 8) on the GPU; the host never reads them.  One outside its range stands for
+ * nobody: no table row, no target, no expert. */
+
+/* y[i] = scale W[ids[i]] for a table W of vocab x cols; 0 for a number outside
+ * [0, vocab). */
+MUON_API muon_status muon_embedding_forward(const void* ids, int32_t id_bytes, const void* w, int64_t ldw, void* y,
+                                            int64_t ldy, int64_t rows, int64_t vocab, int64_t cols, float scale,
+                                            int32_t dtype, void* hip_stream);
+
+/* dW[v] = scale times the sum of dy[i] over the i with ids[i] = v, all vocab rows
+ * of it (0 where there is none).  The sums are taken in the order of i. */
+MUON_API muon_status muon_embedding_backward(const void* dy, int64_t lddy, const void* ids, int32_t id_bytes, void* dw,
+                                             int64_t lddw, int64_t rows, int64_t vocab, int64_t cols, float scale,
+                                             int32_t dtype, void* workspace, size_t workspace_bytes,
+                                             void* hip_stream);
+
+/* Workspace bytes of muon_embedding_backward. */
+MUON_API muon_status muon_embedding_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes);
+
+/* A router's choices ids[tokens][top] sorted by expert, in their own order within
+ * each: offsets (experts + 1) as muon_grouped_linear_* take them; position
+ * (tokens x top), each choice's row among the sorted, -1 if it names no expert;
+ * source (tokens * top), each row's choice t * top + j, -1 behind the last.
+ * tokens * top is at most 2^30, top and experts at most MUON_GROUPED_MAX_EXPERTS. */
+MUON_API muon_status muon_sort_by_expert(const void* ids, int32_t id_bytes, int64_t tokens, int32_t top,
+                                         int32_t experts, int32_t* offsets, int32_t* position, int32_t* source,
+                                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Workspace bytes of muon_sort_by_expert. */
+MUON_API muon_status muon_sort_by_expert_workspace_bytes(int64_t tokens, int32_t top, size_t* bytes);
+
+/* rows[position[t][j]] = x[t]; rows from offsets[experts] on get 0.  position and
+ * offsets are those of muon_sort_by_expert; a position outside [0, tokens * top) is
+ * taken as -1. */
+MUON_API muon_status muon_dispatch_forward(const void* x, int64_t ldx, const int32_t* position, const int32_t* offsets,
+                                           int32_t experts, void* rows, int64_t ldr, int64_t tokens, int32_t top,
+                                           int64_t cols, int32_t dtype, void* hip_stream);
+
+/* dx[t] = the sum of drows[position[t][j]] over j. */
+MUON_API muon_status muon_dispatch_backward(const void* drows, int64_t ldr, const int32_t* position, void* dx,
+                                            int64_t ldx, int64_t tokens, int32_t top, int64_t cols, int32_t dtype,
+                                            void* hip_stream);
+
+/* y[t] = residual[t] + the sum of weights[t][j] rows[position[t][j]] over j.
+ * weights: tokens x top of weight_dtype (MUON_F32 or dtype).  residual may be
+ * NULL; y may be its buffer (same ld). */
+MUON_API muon_status muon_combine_forward(const void* rows, int64_t ldr, const void* weights, int32_t weight_dtype,
+                                          const int32_t* position, const void* residual, int64_t ldres, void* y,
+                                          int64_t ldy, int64_t tokens, int32_t top, int64_t cols, int32_t dtype,
+                                          void* hip_stream);
+
+/* drows[position[t][j]] = weights[t][j] dy[t] (0 from offsets[experts] on);
+ * dweights[t][j] = <dy[t], rows[position[t][j]]> (0 for a choice of no expert).
+ * drows and dweights may be NULL; rows is read only for dweights.  The residual's
+ * gradient is dy itself. */
+MUON_API muon_status muon_combine_backward(const void* dy, int64_t lddy, const void* rows, int64_t ldr,
+                                           const void* weights, int32_t weight_dtype, const int32_t* position,
+                                           const int32_t* offsets, int32_t experts, void* drows, int64_t lddr,
+                                           void* dweights, int64_t tokens, int32_t top, int64_t cols, int32_t dtype,
+                                           void* hip_stream);
+
+typedef enum muon_loss_reduction {
+  MUON_LOSS_ROWS = 0,  /* a loss for every row */
+  MUON_LOSS_SUM = 1,
+  MUON_LOSS_MEAN = 2   /* over the rows with a target; 0 if there are none */
+} muon_loss_reduction;
+
+/* Softmax cross entropy of z = x W: lse[i] = log of the sum of exp(z[i][v]) over
+ * v, loss[i] = lse[i] - z[i][targets[i]].  z exists a piece at a time, in the
+ * workspace or not at all.  A row whose target is `ignore` or outside [0, outer)
+ * has loss 0.  loss: rows fp32, or one (SUM, MEAN); lse: rows fp32, which the
+ * backward pass reads.  inner is at most 2^21. */
+MUON_API muon_status muon_linear_cross_entropy_forward(const void* x, int64_t ldx, const void* w, int64_t ldw,
+                                                       int32_t w_transposed, const void* targets,
+                                                       int32_t target_bytes, int64_t ignore, int32_t reduction,
+                                                       float* loss, float* lse, int64_t rows, int64_t inner,
+                                                       int64_t outer, int32_t dtype, void* workspace,
+                                                       size_t workspace_bytes, void* hip_stream);
+
+/* Its gradients for dloss (rows fp32, or one): z is computed again piece by piece.
+ * dz is rounded to dtype before the products that read it.  dx and dw may be NULL;
+ * dw is kept like w.  Rows without a target have dx = 0 and add nothing to dw. */
+MUON_API muon_status muon_linear_cross_entropy_backward(const float* dloss, const void* x, int64_t ldx, const void* w,
+                                                        int64_t ldw, int32_t w_transposed, const void* targets,
+                                                        int32_t target_bytes, int64_t ignore, int32_t reduction,
+                                                        const float* lse, void* dx, int64_t lddx, void* dw,
+                                                        int64_t lddw, int64_t rows, int64_t inner, int64_t outer,
+                                                        int32_t dtype, void* workspace, size_t workspace_bytes,
+                                                        void* hip_stream);
+
+/* Workspace bytes of either pass (flags: MUON_LAYERS_BACKWARD,
+ * MUON_LAYERS_UNALIGNED -- which these passes need where x or w are off 16-byte
+ * chunks). */
+MUON_API muon_status muon_linear_cross_entropy_workspace_bytes(int64_t rows, int64_t inner, int64_t outer,
+                                                               int32_t dtype, int32_t flags, size_t* bytes);
 
 /* Thread-local description of the last failure of a function of this header
  * on this thread ("" if none). */

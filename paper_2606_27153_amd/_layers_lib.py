@@ -15,6 +15,8 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), LIB_NAME)
 # muon_activation
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 MUON_GROUPED_MAX_EXPERTS = 256
+# muon_loss_reduction
+REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
 
 _P, _I32, _I64, _SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 _PP = ctypes.POINTER(ctypes.c_void_p)
@@ -38,6 +40,22 @@ SIGNATURES = {
     "muon_layer_norm_backward": (_ST, [_P, _I64, _P, _I64, _P, _P, _P, _P, _I64, _P, _P, _I64, _I64, _I32, _I32, _P,
                                        _SZ, _P]),
     "muon_layer_norm_workspace_bytes": (_ST, [_I64, _I64, _PSZ]),
+    "muon_embedding_forward": (_ST, [_P, _I32, _P, _I64, _P, _I64, _I64, _I64, _I64, ctypes.c_float, _I32, _P]),
+    "muon_embedding_backward": (_ST, [_P, _I64, _P, _I32, _P, _I64, _I64, _I64, _I64, ctypes.c_float, _I32, _P, _SZ,
+                                      _P]),
+    "muon_embedding_workspace_bytes": (_ST, [_I64, _I64, _PSZ]),
+    "muon_sort_by_expert": (_ST, [_P, _I32, _I64, _I32, _I32, _P, _P, _P, _P, _SZ, _P]),
+    "muon_sort_by_expert_workspace_bytes": (_ST, [_I64, _I32, _PSZ]),
+    "muon_dispatch_forward": (_ST, [_P, _I64, _P, _P, _I32, _P, _I64, _I64, _I32, _I64, _I32, _P]),
+    "muon_dispatch_backward": (_ST, [_P, _I64, _P, _P, _I64, _I64, _I32, _I64, _I32, _P]),
+    "muon_combine_forward": (_ST, [_P, _I64, _P, _I32, _P, _P, _I64, _P, _I64, _I64, _I32, _I64, _I32, _P]),
+    "muon_combine_backward": (_ST, [_P, _I64, _P, _I64, _P, _I32, _P, _P, _I32, _P, _I64, _P, _I64, _I32, _I64, _I32,
+                                    _P]),
+    "muon_linear_cross_entropy_forward": (_ST, [_P, _I64, _P, _I64, _I32, _P, _I32, _I64, _I32, _P, _P, _I64, _I64,
+                                                _I64, _I32, _P, _SZ, _P]),
+    "muon_linear_cross_entropy_backward": (_ST, [_P, _P, _I64, _P, _I64, _I32, _P, _I32, _I64, _I32, _P, _P, _I64, _P,
+                                                 _I64, _I64, _I64, _I64, _I32, _P, _SZ, _P]),
+    "muon_linear_cross_entropy_workspace_bytes": (_ST, [_I64, _I64, _I64, _I32, _I32, _PSZ]),
     "muon_layers_last_error": (ctypes.c_char_p, []),
 }
 

@@ -1,0 +1,197 @@
+// Rows of a table by token, scaled, and the table's gradient.
+//
+//   y[i] = s W[id[i]],   dW[v] = s sum of dy[i] over the i with id[i] = v
+//
+// Forward: a copy of rows, a thread per 8 columns.
+//
+// Backward: the tokens are sorted (sort.h), so that a table row's gradient is a sum
+// over a run of the sorted list, in the list's order: no atomics, the result does
+// not depend on timing.  Every row of dW is written once, by the block that has
+// it: the sum of its run, or zeros (most of a large table).  A frequent token's run
+// can be a good part of the list: groups of 64 places that lie inside one run are
+// summed first, by blocks of their own, and the row adds up the groups.
+// Bound by memory: dy read once, dW written once.
+#include "sort.h"
+
+namespace muon {
+namespace layers {
+namespace {
+
+// One digit of the tokens' numbers.  Those outside the table count as `vocab`, the
+// largest, and come last.
+struct TokenJob {
+  const void* ids;         // first digit: the tokens themselves
+  const int32_t* keys;     // later ones: as the digit before left them
+  const int32_t* index;
+  int32_t* keys_out;
+  int32_t* index_out;
+  int32_t id_bytes, vocab, shift, bins, bits;
+  __device__ __forceinline__ int digit(int i, int& key) const {
+    if (ids) {
+      const int64_t v = id_at(ids, id_bytes, i);
+      key = v >= 0 && v < vocab ? int(v) : vocab;
+    } else {
+      key = keys[i];
+    }
+    return (key >> shift) & (kSortBins - 1);
+  }
+  __device__ __forceinline__ void start(int, int) const {}
+  __device__ __forceinline__ void put(int i, int key, int, int place) const {
+    keys_out[place] = key;
+    index_out[place] = ids ? i : index[i];
+  }
+};
+
+template <typename E>
+__global__ __launch_bounds__(256) void lookup_kernel(EmbeddingArgs a) {
+  const int chunks = (a.cols + 7) / 8;
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, r = i / chunks;
+  if (r >= a.rows) return;
+  const int c = int(i - r * chunks) * 8, n = min(8, a.cols - c);
+  const int64_t id = id_at(a.ids, a.id_bytes, r);
+  float v[8] = {};
+  if (id >= 0 && id < a.vocab) {
+    load8(static_cast<const E*>(a.w) + id * a.ldw + c, n, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= a.scale;
+  }
+  store8(static_cast<E*>(a.y) + r * a.ldy + c, n, v);
+}
+
+constexpr int kRun = 64;    // places of a group
+constexpr int kRows = 16;   // table rows of a block
+
+// v[0..7] += the gradients of places lo .. hi - 1, in order, 4 in flight.
+template <typename E>
+__device__ __forceinline__ void add_run(const EmbeddingArgs& a, int lo, int hi, int c, int n, float (&v)[8]) {
+  const E* dy = static_cast<const E*>(a.dy) + c;
+  for (int p = lo; p < hi; p += 4) {
+    int64_t row[4];
+    float x[4][8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) row[k] = a.index[min(p + k, hi - 1)];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) load8(dy + row[k] * a.lddy, n, x[k]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += p + k < hi ? x[k][e] : 0.f;
+  }
+}
+
+// The sums of the groups inside one run; the others' places in `part` stay as they are.
+template <typename E>
+__global__ __launch_bounds__(256) void group_kernel(EmbeddingArgs a) {
+  const int first = blockIdx.x * kRun;
+  const int key = a.keys[first];
+  if (key >= a.vocab || a.keys[first + kRun - 1] != key) return;
+  const int c = (blockIdx.y * 256 + threadIdx.x) * 8, n = min(8, a.cols - c);
+  if (n <= 0) return;
+  float v[8] = {};
+  add_run<E>(a, first, first + kRun, c, n, v);
+  store8(a.part + int64_t(blockIdx.x) * a.cols + c, n, v);
+}
+
+template <typename E>
+__global__ __launch_bounds__(256) void table_grad_kernel(EmbeddingArgs a) {
+  __shared__ int32_t starts[kRows + 1];
+  const int64_t v0 = int64_t(blockIdx.x) * kRows;
+  if (threadIdx.x <= kRows) {   // where the runs begin: the first place of at least this token
+    const int64_t want = v0 + threadIdx.x;
+    int lo = 0, hi = a.rows;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (a.keys[mid] < want)
+        lo = mid + 1;
+      else
+        hi = mid;
+    }
+    starts[threadIdx.x] = lo;
+  }
+  __syncthreads();
+  const int chunks = (a.cols + 7) / 8;
+  const int rows = int(min(int64_t(kRows), a.vocab - v0));
+  for (int i = threadIdx.x; i < rows * chunks; i += 256) {
+    const int r = i / chunks, c = (i - r * chunks) * 8, n = min(8, a.cols - c);
+    const int lo = starts[r], hi = starts[r + 1];
+    float v[8] = {};
+    const int g0 = (lo + kRun - 1) / kRun, g1 = hi / kRun;
+    if (g0 < g1) {
+      add_run<E>(a, lo, g0 * kRun, c, n, v);
+      for (int g = g0; g < g1; ++g) {
+        float x[8];
+        load8(a.part + int64_t(g) * a.cols + c, n, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += x[e];
+      }
+      add_run<E>(a, g1 * kRun, hi, c, n, v);
+    } else if (lo < hi) {
+      add_run<E>(a, lo, hi, c, n, v);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= a.scale;
+    store8(static_cast<E*>(a.dw) + (v0 + r) * a.lddw + c, n, v);
+  }
+}
+
+template <typename E>
+hipError_t forward(const EmbeddingArgs& a, hipStream_t st) {
+  const int64_t blocks = (int64_t(a.rows) * ((a.cols + 7) / 8) + 255) / 256;
+  if (blocks >= (int64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  if (blocks) hipLaunchKernelGGL((lookup_kernel<E>), dim3{unsigned(blocks)}, dim3{256}, 0, st, a);
+  return hipGetLastError();
+}
+
+template <typename E>
+hipError_t backward(EmbeddingArgs a, int32_t* const (&keys)[2], int32_t* const (&index)[2], int32_t* counts,
+                    hipStream_t st) {
+  int at = 0;
+  for (int shift = 0; a.rows && (shift == 0 || (a.vocab >> shift)); shift += kSortBits, at ^= 1) {
+    TokenJob job{};
+    if (shift == 0) job.ids = a.ids;
+    job.keys = keys[at ^ 1];
+    job.index = index[at ^ 1];
+    job.keys_out = keys[at];
+    job.index_out = index[at];
+    job.id_bytes = a.id_bytes;
+    job.vocab = a.vocab;
+    job.shift = shift;
+    for (job.bits = 1; job.bits < kSortBits && (a.vocab >> shift >> job.bits); ++job.bits) {
+    }
+    job.bins = 1 << job.bits;
+    const hipError_t e = launch_sort(job, a.rows, counts, st);
+    if (e != hipSuccess) return e;
+  }
+  a.keys = keys[at ^ 1];
+  a.index = index[at ^ 1];
+  const int columns = (a.cols + 2047) / 2048;
+  if (a.rows >= kRun)
+    hipLaunchKernelGGL((group_kernel<E>), (dim3{unsigned(a.rows / kRun), unsigned(columns)}), dim3{256}, 0, st, a);
+  hipLaunchKernelGGL((table_grad_kernel<E>), dim3{unsigned((a.vocab + kRows - 1) / kRows)}, dim3{256}, 0, st, a);
+  return hipGetLastError();
+}
+
+size_t whole(size_t v) { return (v + 255) / 256 * 256; }
+
+}  // namespace
+
+size_t embedding_bytes(int64_t rows, int64_t cols) {
+  return 4 * whole(size_t(rows) * 4) + whole(sort_bytes(rows)) + whole(size_t(rows / kRun) * size_t(cols) * 4);
+}
+
+hipError_t launch_embedding_forward(bool bf16, const EmbeddingArgs& a, hipStream_t st) {
+  return bf16 ? forward<__bf16>(a, st) : forward<float>(a, st);
+}
+
+hipError_t launch_embedding_backward(bool bf16, EmbeddingArgs a, void* workspace, hipStream_t st) {
+  char* p = static_cast<char*>(workspace);
+  const size_t step = whole(size_t(a.rows) * 4);
+  int32_t* const keys[2] = {reinterpret_cast<int32_t*>(p), reinterpret_cast<int32_t*>(p + step)};
+  int32_t* const index[2] = {reinterpret_cast<int32_t*>(p + 2 * step), reinterpret_cast<int32_t*>(p + 3 * step)};
+  int32_t* counts = reinterpret_cast<int32_t*>(p + 4 * step);
+  a.part = reinterpret_cast<float*>(p + 4 * step + whole(sort_bytes(a.rows)));
+  return bf16 ? backward<__bf16>(a, keys, index, counts, st) : backward<float>(a, keys, index, counts, st);
+}
+
+}  // namespace layers
+}  // namespace muon

@@ -46,6 +46,11 @@ struct Product {
   int32_t experts;
   int32_t act;
   int32_t splits;         // ranges the summed dimension is cut into (1: none)
+  int32_t raw;            // != 0: C is left in `part` as it is summed, also where splits is 1
+                          // (not by the simple kernel)
+  int32_t add;            // raw: added to what `part` holds
+  int32_t pad_a, pad_b;   // elements that exist of each row of A and B as they lie, zeros beyond
+                          // the matrix (0: none beyond)
 };
 
 // Pointers of the experts' matrices (grouped products), passed by value.
@@ -93,7 +98,82 @@ struct ActGradArgs {
   int32_t rows, N, act;
 };
 
+// Tokens to their experts and back (routing.hip).
+struct RouteArgs {
+  const void* x;          // dispatch: tokens x cols
+  void* rows;             // tokens * top x cols: dispatch writes them, the others read them
+  const void* weights;    // tokens x top, or NULL (1)
+  const void* res;        // tokens x cols or NULL
+  void* y;                // tokens x cols
+  const void* dy;
+  void* drows;            // or NULL
+  void* dweights;         // or NULL
+  const int32_t* position;
+  const int32_t* offsets;
+  int64_t ldx, ldr, ldres, ldy, lddy, lddr;
+  int32_t tokens, top, experts, cols;
+  int32_t wf32;           // weights and their gradients are fp32
+};
+enum RoutePass { ROUTE_DISPATCH, ROUTE_GATHER, ROUTE_COMBINE_GRAD };
+
+struct EmbeddingArgs {
+  const void* ids;
+  const void* w;
+  void* y;
+  const void* dy;
+  void* dw;
+  const int32_t* keys;    // backward: the tokens sorted, and where each was
+  const int32_t* index;
+  float* part;            // sums of groups of places inside one token's run
+  int64_t ldw, ldy, lddy, lddw;
+  int32_t rows, cols, vocab, id_bytes;
+  float scale;
+};
+
+// Softmax cross entropy over the columns of z = x W, of which a piece at a time
+// exists (loss.hip).
+struct LossArgs {
+  const void* targets;
+  const float* dloss;     // a number for every row (each), or one
+  int32_t* label;         // the target's column, -1: none
+  float* grad;            // factor of the row's gradient
+  float* alpha;           // factor of all gradients
+  float2* part;           // strips x rows: the largest logit and the sum of the others relative to it
+  float* logit;           // the target's
+  float* loss;            // of every row
+  float* lse;
+  float* total;           // of all rows, or NULL
+  const float* raw;       // splits x rows x cols: a piece of z, to be added up
+  void* dz;               // rows x lddz: the gradient of a piece of z
+  int64_t ignore, lddz;
+  int32_t rows, vocab, target_bytes, each, mean;
+  int32_t first, cols;    // the piece
+  int32_t splits, strip, strips;
+};
+constexpr int kRawStrip = 2048;   // columns of a strip of `raw`
+// What the tile kernels make of the loss's products: part and logit, or dz, of a
+// piece of z; x^T dz times alpha.
+enum LossStep { LOSS_STRIPS, LOSS_GRAD, LOSS_WEIGHT };
+
 // Launchers: enqueue and return hipGetLastError's answer.
+size_t expert_sort_bytes(int64_t n);
+hipError_t launch_expert_sort(const void* ids, int id_bytes, int64_t n, int experts, int32_t* offsets,
+                              int32_t* position, int32_t* source, int32_t* counts, hipStream_t st);
+hipError_t launch_route(bool bf16, int pass, const RouteArgs& a, hipStream_t st);
+
+size_t embedding_bytes(int64_t rows, int64_t cols);
+hipError_t launch_embedding_forward(bool bf16, const EmbeddingArgs& a, hipStream_t st);
+hipError_t launch_embedding_backward(bool bf16, EmbeddingArgs a, void* workspace, hipStream_t st);
+
+hipError_t launch_loss_labels(const LossArgs& a, hipStream_t st);   // label; with dloss grad and alpha
+hipError_t launch_loss_strips(const LossArgs& a, hipStream_t st);   // raw -> part and logit
+hipError_t launch_loss_finish(const LossArgs& a, hipStream_t st);   // part -> lse and loss
+hipError_t launch_loss_total(const LossArgs& a, hipStream_t st);    // loss -> total
+hipError_t launch_loss_grad(bool bf16, const LossArgs& a, hipStream_t st);   // raw -> dz
+// y = *alpha times the sum of `splits` partial results of rows x cols
+hipError_t launch_loss_sum(bool bf16, const float* part, int splits, const float* alpha, void* y, int64_t ldy,
+                           int64_t rows, int64_t cols, hipStream_t st);
+
 hipError_t launch_simple(bool bf16, int form, int group, const Product& p, const Table* t, hipStream_t st);
 
 // Matrix-core kernels on tiles of 256 x 256 and 128 x 256 (bf16 only), 128 x 128
@@ -105,6 +185,13 @@ hipError_t launch_tile128_bf16(int form, int group, const Product& p, const Tabl
 hipError_t launch_tile128_f32(int form, int group, const Product& p, const Table* t, hipStream_t st);
 hipError_t launch_tile64_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st);
 hipError_t launch_tile64_f32(int form, int group, const Product& p, const Table* t, hipStream_t st);
+
+hipError_t launch_loss256_bf16(int step, int form, const Product& p, const LossArgs& a, hipStream_t st);
+hipError_t launch_loss128x256_bf16(int step, int form, const Product& p, const LossArgs& a, hipStream_t st);
+hipError_t launch_loss128_bf16(int step, int form, const Product& p, const LossArgs& a, hipStream_t st);
+hipError_t launch_loss64_bf16(int step, int form, const Product& p, const LossArgs& a, hipStream_t st);
+hipError_t launch_loss128_f32(int step, int form, const Product& p, const LossArgs& a, hipStream_t st);
+hipError_t launch_loss64_f32(int step, int form, const Product& p, const LossArgs& a, hipStream_t st);
 
 // Few rows: tiles of 16 mt rows (mt 1, 2 or 4), forms RT and RR, any alignment,
 // at least 16 bytes of columns.

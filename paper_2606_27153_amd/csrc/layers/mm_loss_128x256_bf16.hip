@@ -1,0 +1,12 @@
+// The loss's products on 128 x 256 tiles of bf16 operands.
+#include "mm_tile.h"
+
+namespace muon {
+namespace layers {
+
+hipError_t launch_loss128x256_bf16(int step, int form, const Product& p, const LossArgs& a, hipStream_t st) {
+  return launch_loss_step<__bf16, 128, 256, 6>(step, form, p, a, st);
+}
+
+}  // namespace layers
+}  // namespace muon

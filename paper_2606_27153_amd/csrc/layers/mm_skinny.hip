@@ -232,10 +232,18 @@ __global__ __launch_bounds__(256, MT == 4 ? 1 : 2) void mm_skinny_kernel(Product
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = red[0][row * LD + c + e] + red[1][row * LD + c + e];
-    if (p.splits > 1)
-      store8(p.part + (int64_t(blockIdx.y) * p.M + m0 + row) * p.N + n0 + c, n, v);
-    else
+    if (p.splits > 1 || p.raw) {
+      float* to = p.part + (int64_t(blockIdx.y) * p.M + m0 + row) * p.N + n0 + c;
+      if (p.add) {
+        float x[8];
+        load8(to, n, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += x[e];
+      }
+      store8(to, n, v);
+    } else {
       finish8<E>(p, m0 + row, n0 + c, n, v);
+    }
   }
 }
 

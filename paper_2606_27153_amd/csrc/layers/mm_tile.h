@@ -286,7 +286,7 @@ struct Staging {
   static constexpr int BYTES = 32 * LD * 4;            // of a wave
   static constexpr int LPR = C::WTN / 8, RPI = 64 / LPR;  // lanes of a row, rows of a store instruction
 };
-template <class C, typename E, typename OUT, int ACT, bool EPI, bool RAGGED>
+template <class C, typename E, typename OUT, int ACT, bool EPI, bool RAGGED, bool ADD = false>
 __device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ldc, const Work<E>& o,
                                             const f32x16 (&acc)[C::NBM][C::NBN], float* region, int wm, int wn,
                                             int lane) {
@@ -332,6 +332,12 @@ __device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ld
             for (int e = 0; e < 8; ++e) v[e] += rv[e];
           }
         }
+        if (ADD) {
+          float old[8];
+          load8(cp, count, old);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] += old[e];
+        }
         store8(cp, count, v);
       }
       left -= S::RPI;
@@ -348,9 +354,12 @@ template <class C, typename E, bool EPI, bool RAGGED>
 __device__ __forceinline__ void store_columns(const Product& p, const Work<E>& o,
                                               const f32x16 (&acc)[C::NBM][C::NBN], float* region, int wm, int wn,
                                               int lane) {
-  if (p.splits > 1) {
-    store_piece<C, E, float, MUON_ACT_NONE, false, RAGGED>(p, p.part + int64_t(blockIdx.y) * p.M * p.N, p.N, o, acc,
-                                                           region, wm, wn, lane);
+  if (p.splits > 1 || p.raw) {
+    float* part = p.part + int64_t(blockIdx.y) * p.M * p.N;
+    if (p.add)
+      store_piece<C, E, float, MUON_ACT_NONE, false, RAGGED, true>(p, part, p.N, o, acc, region, wm, wn, lane);
+    else
+      store_piece<C, E, float, MUON_ACT_NONE, false, RAGGED>(p, part, p.N, o, acc, region, wm, wn, lane);
   } else {
     with_act<EPI>(p.act, [&](auto act) {
       store_piece<C, E, E, decltype(act)::value, EPI, RAGGED>(p, o.c, p.ldc, o, acc, region, wm, wn, lane);
@@ -366,9 +375,125 @@ __device__ __forceinline__ void store_tile(const Product& p, const Work<E>& o, c
     store_columns<C, E, EPI, false>(p, o, acc, region, wm, wn, lane);
 }
 
-template <typename E, int TM, int TN, int U, int FORM, int GROUP>
+// A wave's piece of logits, whose columns are a strip: per row the largest and the
+// sum of exp(z - largest), both within the lanes that hold the row (l and l + 32), and the
+// target's logit where the strip has it.  exp(z - m) = 2^(z log2(e) - m log2(e)), one
+// fused multiply-add before the instruction; columns past the last count as -inf.
+template <class C, typename E>
+__device__ __forceinline__ void strip_piece(const LossArgs& a, const Work<E>& o, const f32x16 (&acc)[C::NBM][C::NBN],
+                                            int wm, int wn, int lane) {
+  constexpr float kLog2e = 1.4426950408889634f;
+  const int left = o.cols - wn - 4 * (lane >> 5);   // columns from the lane's first on
+  if (o.cols <= wn) return;
+  auto piece = [&](auto ragged) {
+    static_for<C::NBM>([&](auto it) {
+      constexpr int i = decltype(it)::value;
+      auto value = [&](int j, int q) {
+        const float v = acc[i][j][q];
+        return decltype(ragged)::value && 32 * j + 8 * (q / 4) + q % 4 >= left ? -INFINITY : v;
+      };
+      float m = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < C::NBN; ++j)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) m = fmaxf(m, value(j, q));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      m = m == -INFINITY ? 0.f : m;
+      const float shift = -m * kLog2e;
+      float s[4] = {};
+#pragma unroll
+      for (int j = 0; j < C::NBN; ++j)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) s[q % 4] += __builtin_amdgcn_exp2f(fmaf(value(j, q), kLog2e, shift));
+      float sum = (s[0] + s[1]) + (s[2] + s[3]);
+      sum += __shfl_xor(sum, 32);
+      const int r = wm + 32 * i + (lane & 31);
+      const int64_t row = o.m0 + r;
+      if (r < o.rows) {
+        if (lane < 32) a.part[int64_t(a.strip + (o.n0 + wn) / C::WTN) * a.rows + row] = make_float2(m, sum);
+        const int label = a.label[row], t = label - a.first - int(o.n0) - wn;
+        if (label >= 0 && t >= 0 && t < min(C::WTN, o.cols - wn) && ((t >> 2) & 1) == lane >> 5) {
+          float z = 0.f;
+#pragma unroll
+          for (int j = 0; j < C::NBN; ++j)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) z = t - 4 * (lane >> 5) == 32 * j + 8 * (q / 4) + q % 4 ? acc[i][j][q] : z;
+          a.logit[row] = z;
+        }
+      }
+    });
+  };
+  if (wn + C::WTN > o.cols)
+    piece(IntTag<1>{});
+  else
+    piece(IntTag<0>{});
+}
+
+// The gradient of a wave's piece of logits in its place: (exp(z - lse) - [target]) g,
+// 0 in rows without a target and past the last column.
+template <class C, typename E>
+__device__ __forceinline__ void grad_piece(const LossArgs& a, const Work<E>& o, f32x16 (&acc)[C::NBM][C::NBN], int wm,
+                                           int wn, int lane) {
+  const int left = o.cols - wn - 4 * (lane >> 5);
+  static_for<C::NBM>([&](auto it) {
+    constexpr int i = decltype(it)::value;
+    const int64_t row = o.m0 + min(wm + 32 * i + (lane & 31), o.rows - 1);
+    const int label = a.label[row], t = label - a.first - int(o.n0) - wn - 4 * (lane >> 5);
+    const float lse = a.lse[row], g = a.grad[row];
+#pragma unroll
+    for (int j = 0; j < C::NBN; ++j)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[i][j][q] = __expf(acc[i][j][q] - lse);
+    if (__any(label >= 0 && t >= 0 && t < C::WTN)) {
+      const int at = label >= 0 ? t : -1;
+#pragma unroll
+      for (int j = 0; j < C::NBN; ++j)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[i][j][q] -= at == 32 * j + 8 * (q / 4) + q % 4 ? 1.f : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < C::NBN; ++j)
+#pragma unroll
+      for (int q = 0; q < 16; ++q) acc[i][j][q] *= g;
+    if (__any(label < 0)) {
+#pragma unroll
+      for (int j = 0; j < C::NBN; ++j)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[i][j][q] = label < 0 ? 0.f : acc[i][j][q];
+    }
+    if (wn + C::WTN > o.cols) {
+#pragma unroll
+      for (int j = 0; j < C::NBN; ++j)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) acc[i][j][q] = 32 * j + 8 * (q / 4) + q % 4 >= left ? 0.f : acc[i][j][q];
+    }
+  });
+}
+
+// What becomes of a tile: C with bias, activation and residual; C as it is; and, of
+// a product that is a piece of logits, the strips' sums, their gradient; C times a
+// number that is on the GPU.
+enum Epilogue { EP_LINEAR, EP_PLAIN, EP_STRIP, EP_GRAD, EP_SCALE };
+template <int EP>
+struct ExtraOf {
+  typedef NoTable T;
+};
+template <>
+struct ExtraOf<EP_STRIP> {
+  typedef LossArgs T;
+};
+template <>
+struct ExtraOf<EP_GRAD> {
+  typedef LossArgs T;
+};
+template <>
+struct ExtraOf<EP_SCALE> {
+  typedef const float* T;
+};
+
+template <typename E, int TM, int TN, int U, int FORM, int GROUP, int EP>
 __global__ __launch_bounds__(256, (Tile<E, TM, TN, U>::RING > 80 * 1024 ? 1 : 2)) void mm_tile_kernel(
-    Product p, typename TableOf<GROUP>::T tab, int run, int blocks) {
+    Product p, typename TableOf<GROUP>::T tab, int run, int blocks, typename ExtraOf<EP>::T extra) {
   using C = Tile<E, TM, TN, U>;
   constexpr bool ATR = FORM == FORM_TT, BTR = FORM != FORM_RR;
   __shared__ __attribute__((aligned(1024))) char lds[C::RING];
@@ -527,8 +652,24 @@ __global__ __launch_bounds__(256, (Tile<E, TM, TN, U>::RING > 80 * 1024 ? 1 : 2)
     // the last slabs' loads (past K) and every wave's reads end here
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     static_assert(4 * Staging<C>::BYTES <= C::RING, "the waves' parts of the ring");
-    store_tile<C, E, GROUP == GROUP_NONE && FORM != FORM_TT>(
-        p, w, acc, reinterpret_cast<float*>(lds + wid * Staging<C>::BYTES), wm, wn, lane);
+    float* const region = reinterpret_cast<float*>(lds + wid * Staging<C>::BYTES);
+    if constexpr (EP == EP_STRIP) {
+      strip_piece<C>(extra, w, acc, wm, wn, lane);
+    } else if constexpr (EP == EP_GRAD) {
+      grad_piece<C>(extra, w, acc, wm, wn, lane);
+      w.cols = (w.cols + 7) & ~7;   // (dz has room for whole groups of 8)
+      store_piece<C, E, E, MUON_ACT_NONE, false, false>(p, w.c, p.ldc, w, acc, region, wm, wn, lane);
+    } else {
+      if constexpr (EP == EP_SCALE) {
+        const float f = *extra;
+        static_for<C::NBM * C::NBN>([&](auto ij) {
+          constexpr int i = decltype(ij)::value / C::NBN, j = decltype(ij)::value % C::NBN;
+#pragma unroll
+          for (int q = 0; q < 16; ++q) acc[i][j][q] *= f;
+        });
+      }
+      store_tile<C, E, EP == EP_LINEAR>(p, w, acc, region, wm, wn, lane);
+    }
     if (!more) break;
     // every wave's part is free again for the next tile's first slabs
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -546,8 +687,9 @@ int64_t run_length(int64_t mt, int64_t nt) {
   return GROUP == GROUP_ROWS ? 8 * nt : mt * nt;
 }
 
-template <typename E, int TM, int TN, int U, int FORM, int GROUP>
-hipError_t launch_one(const Product& p, const Table* t, hipStream_t st) {
+template <typename E, int TM, int TN, int U, int FORM, int GROUP,
+          int EP = GROUP == GROUP_NONE && FORM != FORM_TT ? EP_LINEAR : EP_PLAIN>
+hipError_t launch_one(const Product& p, const Table* t, hipStream_t st, typename ExtraOf<EP>::T extra = {}) {
   const int64_t nt = (int64_t(p.N) + TN - 1) / TN, mt = (int64_t(p.M) + TM - 1) / TM;
   int64_t blocks = nt * mt;
   int run = 1;
@@ -567,9 +709,10 @@ hipError_t launch_one(const Product& p, const Table* t, hipStream_t st) {
   if (Tile<E, TM, TN, U>::RING > 80 * 1024 && grid > kCUs / p.splits) grid = kCUs / p.splits;
   const dim3 g{unsigned(grid), unsigned(p.splits)}, b{256};
   if constexpr (GROUP == GROUP_NONE)
-    hipLaunchKernelGGL((mm_tile_kernel<E, TM, TN, U, FORM, GROUP>), g, b, 0, st, p, NoTable{}, run, int(blocks));
+    hipLaunchKernelGGL((mm_tile_kernel<E, TM, TN, U, FORM, GROUP, EP>), g, b, 0, st, p, NoTable{}, run, int(blocks),
+                       extra);
   else
-    hipLaunchKernelGGL((mm_tile_kernel<E, TM, TN, U, FORM, GROUP>), g, b, 0, st, p, *t, run, int(blocks));
+    hipLaunchKernelGGL((mm_tile_kernel<E, TM, TN, U, FORM, GROUP, EP>), g, b, 0, st, p, *t, run, int(blocks), extra);
   return hipGetLastError();
 }
 
@@ -583,6 +726,19 @@ hipError_t launch_form(int form, int group, const Product& p, const Table* t, hi
   if (form == FORM_RT) return launch_one<E, TM, TN, U, FORM_RT, GROUP_NONE>(p, t, st);
   if (form == FORM_RR) return launch_one<E, TM, TN, U, FORM_RR, GROUP_NONE>(p, t, st);
   return launch_one<E, TM, TN, U, FORM_TT, GROUP_NONE>(p, t, st);
+}
+
+// The products of the loss.
+template <typename E, int TM, int TN, int U>
+hipError_t launch_loss_step(int step, int form, const Product& p, const LossArgs& a, hipStream_t st) {
+  constexpr int G = GROUP_NONE;
+  if (step == LOSS_STRIPS)
+    return form == FORM_RT ? launch_one<E, TM, TN, U, FORM_RT, G, EP_STRIP>(p, nullptr, st, a)
+                           : launch_one<E, TM, TN, U, FORM_RR, G, EP_STRIP>(p, nullptr, st, a);
+  if (step == LOSS_GRAD)
+    return form == FORM_RT ? launch_one<E, TM, TN, U, FORM_RT, G, EP_GRAD>(p, nullptr, st, a)
+                           : launch_one<E, TM, TN, U, FORM_RR, G, EP_GRAD>(p, nullptr, st, a);
+  return launch_one<E, TM, TN, U, FORM_TT, G, EP_SCALE>(p, nullptr, st, a.alpha);
 }
 
 }  // namespace

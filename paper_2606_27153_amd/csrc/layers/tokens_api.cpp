@@ -1,0 +1,565 @@
+// C ABI of the operators that take token or expert numbers: lookup in a table and
+// its gradient, the way to the experts and back, and the loss over a vocabulary.
+// Argument checks, workspace layouts and launch order.
+#include "host.h"
+
+namespace {
+
+using namespace muon::layers;
+
+constexpr int64_t kMaxInner = int64_t(1) << 21;   // of the loss: 256 rows of it within 32-bit offsets
+
+muon_status check_count(const char* name, int64_t v, int64_t lo, int64_t hi) {
+  if (v < lo || v > hi)
+    return fail(MUON_ERR_INVALID_ARG, "%s %lld out of [%lld, %lld]", name, (long long)v, (long long)lo, (long long)hi);
+  return MUON_OK;
+}
+
+muon_status check_ids(const char* name, const void* ids, int32_t bytes, int64_t n) {
+  if (bytes != 4 && bytes != 8) return fail(MUON_ERR_UNSUPPORTED, "%s of %d bytes: 4 or 8", name, bytes);
+  if (n && !ids) return fail(MUON_ERR_INVALID_ARG, "%s is NULL", name);
+  if (reinterpret_cast<uintptr_t>(ids) % size_t(bytes))
+    return fail(MUON_ERR_INVALID_ARG, "%s is not aligned to its element", name);
+  return MUON_OK;
+}
+
+muon_status check_dtype(int32_t dtype) {
+  return known_dtype(dtype) ? MUON_OK : fail(MUON_ERR_UNSUPPORTED, "dtype %d: MUON_F32 or MUON_BF16", dtype);
+}
+
+muon_status check_needed(const char* name, const void* p, size_t esize) {
+  if (!p) return fail(MUON_ERR_INVALID_ARG, "%s is NULL", name);
+  return check_vector(name, p, esize);
+}
+
+// ----------------------------------------------------------------- routing
+
+muon_status check_choices(int64_t tokens, int64_t top) {
+  TRY(check_count("tokens", tokens, 0, kMaxRows));
+  TRY(check_count("top", top, 1, MUON_GROUPED_MAX_EXPERTS));
+  if (tokens * top > kMaxRows) return fail(MUON_ERR_INVALID_ARG, "tokens * top is over 2^30");
+  return MUON_OK;
+}
+
+muon_status check_route(int64_t tokens, int64_t top, int64_t cols, int32_t dtype) {
+  TRY(check_choices(tokens, top));
+  TRY(check_count("cols", cols, 1, kMaxDim));
+  return check_dtype(dtype);
+}
+
+muon_status check_weights(const void* w, int32_t weight_dtype, int32_t dtype) {
+  if (weight_dtype != MUON_F32 && weight_dtype != dtype)
+    return fail(MUON_ERR_UNSUPPORTED, "weight_dtype %d: MUON_F32 or the dtype of the rows", weight_dtype);
+  return check_needed("weights", w, size_of(weight_dtype));
+}
+
+RouteArgs route_args(int64_t tokens, int64_t top, int64_t cols, const int32_t* position) {
+  RouteArgs a{};
+  a.tokens = int32_t(tokens);
+  a.top = int32_t(top);
+  a.cols = int32_t(cols);
+  a.position = position;
+  return a;
+}
+
+// -------------------------------------------------------------------- loss
+
+// Rows of a forward pass at a time: its strips' sums take 8 bytes a row and 128
+// columns or so.
+constexpr int64_t kLossRows = 32768;
+// Columns of a piece: as many as one grid has tiles for; where the weight has to
+// be copied, fewer, so that the copy stays small; of a gradient piece, 2^29 elements at most
+// (and 2048 columns at least).
+constexpr int64_t kPiece = int64_t(1) << 18, kCopyPiece = int64_t(1) << 15;
+constexpr int64_t kGradPiece = int64_t(1) << 29;
+
+int64_t even_piece(int64_t outer, int64_t most) {
+  const int64_t pieces = ceil_div(outer, most);
+  const int64_t p = ceil_div(ceil_div(outer, pieces), 256) * 256;
+  return p < outer ? p : outer;
+}
+size_t larger(size_t a, size_t b) { return a > b ? a : b; }
+
+struct LossLayout {
+  int64_t rows = 0;    // at a time
+  int64_t piece = 0;   // columns at a time
+  Choice z, x, w;      // the kernels of x W, dz W^T and x^T dz (a last piece has fewer columns, and the same ones)
+  size_t label = 0, logit = 0, loss = 0, grad = 0, alpha = 0, part = 0, raw = 0, dz = 0, dx = 0, scratch = 0, total = 0;
+  void take(size_t& p, size_t bytes) {
+    p = total;
+    total += padded(bytes);
+  }
+};
+
+// What the copies for a piece of x W take.
+size_t logit_copies(const LossLayout& l, bool bf16, int64_t inner, bool w_transposed) {
+  if (l.z.kernel == Choice::SKINNY) return 0;
+  const int64_t epc = bf16 ? 8 : 4;
+  const int form = w_transposed ? FORM_RR : FORM_RT;
+  return copy_bytes(copy_of_a(form, l.rows, inner, epc), epc, 1) +
+         copy_bytes(copy_of_b(form, l.piece, inner, epc), epc, 1);
+}
+
+// The kernel of a piece of x W: few rows leave it in memory (`raw`), tiles do not.
+Choice choose_logits(bool bf16, int64_t rows, int64_t piece, int64_t inner) {
+  const Choice c = choose(bf16, FORM_RT, GROUP_NONE, rows, piece, inner, 0, false);
+  return c.kernel == Choice::SKINNY ? c : choose_tile(bf16, GROUP_NONE, rows, piece, inner, 0, true, 1);
+}
+// Columns of its strips: a wave has half of a tile's.
+int64_t strip_columns(const Choice& c) {
+  switch (c.kernel) {
+    case Choice::TILE256:
+    case Choice::TILE128X256: return 128;
+    case Choice::TILE128: return 64;
+    case Choice::TILE64: return 32;
+    default: return kRawStrip;
+  }
+}
+size_t raw_bytes(const LossLayout& l) {
+  return l.z.kernel == Choice::SKINNY ? size_t(l.z.splits) * size_t(l.rows) * size_t(l.piece) * 4 : 0;
+}
+
+hipError_t launch_loss_tile(const Choice& c, int step, bool bf16, int form, const Product& p, const LossArgs& a,
+                            hipStream_t st) {
+  switch (c.kernel) {
+    case Choice::TILE64:
+      return bf16 ? launch_loss64_bf16(step, form, p, a, st) : launch_loss64_f32(step, form, p, a, st);
+    case Choice::TILE128:
+      return bf16 ? launch_loss128_bf16(step, form, p, a, st) : launch_loss128_f32(step, form, p, a, st);
+    case Choice::TILE128X256: return launch_loss128x256_bf16(step, form, p, a, st);
+    case Choice::TILE256: return launch_loss256_bf16(step, form, p, a, st);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+// A product of the loss by the kernel chosen for it; the operands' copies have room
+// in ws (a partial result's comes first).
+hipError_t loss_product(const Choice& c, int step, bool bf16, int form, Product p, const LossArgs& a, Scratch ws,
+                        hipStream_t st) {
+  Choice k = c;
+  const Table* none = nullptr;
+  Table copies;
+  hipError_t e = fit_operands(bf16, form, GROUP_NONE, p, none, copies, k, ws, st);
+  if (e != hipSuccess) return e;
+  p.splits = c.splits;
+  p.part = reinterpret_cast<float*>(ws.p);
+  e = launch_loss_tile(k, step, bf16, form, p, a, st);
+  return e == hipSuccess && c.splits > 1 ? launch_reduce(bf16, p, st) : e;
+}
+
+LossLayout forward_layout(int64_t rows, int64_t inner, int64_t outer, bool w_transposed, bool bf16, bool unaligned) {
+  LossLayout l;
+  l.rows = rows < kLossRows ? rows : kLossRows;
+  l.piece = even_piece(outer, unaligned ? kCopyPiece : kPiece);
+  l.z = choose_logits(bf16, l.rows, l.piece, inner);
+  l.take(l.label, size_t(rows) * 4);
+  l.take(l.logit, size_t(rows) * 4);
+  l.take(l.loss, size_t(rows) * 4);
+  l.take(l.part, size_t(ceil_div(outer, l.piece)) * size_t(ceil_div(l.piece, strip_columns(l.z))) * size_t(l.rows) * 8);
+  l.take(l.raw, raw_bytes(l));
+  l.take(l.scratch, unaligned ? logit_copies(l, bf16, inner, w_transposed) : 0);
+  return l;
+}
+
+LossLayout backward_layout(int64_t rows, int64_t inner, int64_t outer, bool w_transposed, bool bf16, bool unaligned) {
+  LossLayout l;
+  const int64_t epc = bf16 ? 8 : 4, cap = unaligned ? kCopyPiece : kPiece;
+  int64_t most = kGradPiece / (rows > 0 ? rows : 1) / 256 * 256;
+  most = most < 2048 ? 2048 : most > cap ? cap : most;
+  l.rows = rows < kLossRows ? rows : kLossRows;
+  l.piece = even_piece(outer, most);
+  l.z = choose_logits(bf16, l.rows, l.piece, inner);
+  l.x = choose(bf16, FORM_RT, GROUP_NONE, rows, inner, l.piece, 0, false);
+  const int64_t wm = w_transposed ? l.piece : inner, wn = w_transposed ? inner : l.piece;
+  l.w = choose(bf16, FORM_TT, GROUP_NONE, wm, wn, rows, 0, false);
+  l.take(l.label, size_t(rows) * 4);
+  l.take(l.grad, size_t(rows) * 4);
+  l.take(l.alpha, 4);
+  l.take(l.dz, size_t(rows) * size_t(ceil_div(l.piece, 8) * 8) * (bf16 ? 2 : 4));
+  l.take(l.raw, raw_bytes(l));
+  l.take(l.dx, size_t(l.x.splits) * size_t(rows) * size_t(inner) * 4);
+  size_t scratch = part_bytes(l.w, wm, wn);
+  if (unaligned) {
+    scratch += copy_bytes(copy_of_a(FORM_TT, inner, rows, epc), epc, 1);   // x, as either operand
+    scratch = larger(scratch, logit_copies(l, bf16, inner, w_transposed));
+    const int form = w_transposed ? FORM_RT : FORM_RR;
+    scratch = larger(scratch, copy_bytes(copy_of_b(form, inner, l.piece, epc), epc, 1));
+  }
+  l.take(l.scratch, scratch);
+  return l;
+}
+
+muon_status check_loss(int64_t rows, int64_t inner, int64_t outer, int32_t dtype, int32_t reduction) {
+  TRY(check_sizes(rows, inner, outer, dtype));
+  if (inner > kMaxInner) return fail(MUON_ERR_UNSUPPORTED, "inner %lld: at most 2^21", (long long)inner);
+  if (reduction < MUON_LOSS_ROWS || reduction > MUON_LOSS_MEAN)
+    return fail(MUON_ERR_INVALID_ARG, "unknown reduction %d", reduction);
+  return MUON_OK;
+}
+
+// Whether the tile kernels can fetch x and w where they lie.
+bool operands_fit(const void* x, int64_t ldx, const void* w, int64_t ldw, int32_t w_transposed, int64_t inner,
+                  int64_t outer, bool bf16) {
+  const int64_t epc = bf16 ? 8 : 4;
+  return rows_fit(x, ldx, inner, epc) && rows_fit(w, ldw, w_transposed ? inner : outer, epc);
+}
+
+// Columns first .. of a weight.
+const void* columns(const void* w, int64_t ldw, int32_t w_transposed, int64_t first, size_t es) {
+  return static_cast<const char*>(w) + size_t(w_transposed ? first * ldw : first) * es;
+}
+
+}  // namespace
+
+extern "C" {
+
+MUON_API muon_status muon_sort_by_expert_workspace_bytes(int64_t tokens, int32_t top, size_t* bytes) {
+  if (!bytes) return fail(MUON_ERR_INVALID_ARG, "bytes is NULL");
+  TRY(check_choices(tokens, top));
+  *bytes = padded(expert_sort_bytes(tokens * top));
+  return done(hipSuccess, "");
+}
+
+MUON_API muon_status muon_sort_by_expert(const void* ids, int32_t id_bytes, int64_t tokens, int32_t top,
+                                         int32_t experts, int32_t* offsets, int32_t* position, int32_t* source,
+                                         void* workspace, size_t workspace_bytes, void* hip_stream) {
+  TRY(check_choices(tokens, top));
+  TRY(check_count("experts", experts, 1, MUON_GROUPED_MAX_EXPERTS));
+  const int64_t n = tokens * top;
+  TRY(check_ids("ids", ids, id_bytes, n));
+  TRY(check_needed("offsets", offsets, 4));
+  if (n) {
+    TRY(check_needed("position", position, 4));
+    TRY(check_needed("source", source, 4));
+  }
+  size_t need = 0;
+  TRY(muon_sort_by_expert_workspace_bytes(tokens, top, &need));
+  TRY(check_workspace(workspace, workspace_bytes, need));
+  return done(launch_expert_sort(ids, id_bytes, n, experts, offsets, position, source,
+                                 static_cast<int32_t*>(workspace), hipStream_t(hip_stream)),
+              "sort by expert");
+}
+
+MUON_API muon_status muon_dispatch_forward(const void* x, int64_t ldx, const int32_t* position, const int32_t* offsets,
+                                           int32_t experts, void* rows, int64_t ldr, int64_t tokens, int32_t top,
+                                           int64_t cols, int32_t dtype, void* hip_stream) {
+  TRY(check_route(tokens, top, cols, dtype));
+  TRY(check_experts(experts, offsets));
+  if (!tokens) return done(hipSuccess, "");
+  const size_t es = size_of(dtype);
+  TRY(check_matrix("x", x, ldx, cols, es));
+  TRY(check_matrix("rows", rows, ldr, cols, es));
+  TRY(check_needed("position", position, 4));
+  RouteArgs a = route_args(tokens, top, cols, position);
+  a.x = x; a.ldx = ldx;
+  a.rows = rows; a.ldr = ldr;
+  a.offsets = offsets; a.experts = experts;
+  return done(launch_route(dtype == MUON_BF16, ROUTE_DISPATCH, a, hipStream_t(hip_stream)), "dispatch");
+}
+
+MUON_API muon_status muon_dispatch_backward(const void* drows, int64_t ldr, const int32_t* position, void* dx,
+                                            int64_t ldx, int64_t tokens, int32_t top, int64_t cols, int32_t dtype,
+                                            void* hip_stream) {
+  TRY(check_route(tokens, top, cols, dtype));
+  if (!tokens) return done(hipSuccess, "");
+  const size_t es = size_of(dtype);
+  TRY(check_matrix("drows", drows, ldr, cols, es));
+  TRY(check_matrix("dx", dx, ldx, cols, es));
+  TRY(check_needed("position", position, 4));
+  RouteArgs a = route_args(tokens, top, cols, position);
+  a.rows = const_cast<void*>(drows); a.ldr = ldr;
+  a.y = dx; a.ldy = ldx;
+  return done(launch_route(dtype == MUON_BF16, ROUTE_GATHER, a, hipStream_t(hip_stream)), "dispatch backward");
+}
+
+MUON_API muon_status muon_combine_forward(const void* rows, int64_t ldr, const void* weights, int32_t weight_dtype,
+                                          const int32_t* position, const void* residual, int64_t ldres, void* y,
+                                          int64_t ldy, int64_t tokens, int32_t top, int64_t cols, int32_t dtype,
+                                          void* hip_stream) {
+  TRY(check_route(tokens, top, cols, dtype));
+  if (!tokens) return done(hipSuccess, "");
+  const size_t es = size_of(dtype);
+  TRY(check_matrix("rows", rows, ldr, cols, es));
+  TRY(check_weights(weights, weight_dtype, dtype));
+  TRY(check_needed("position", position, 4));
+  if (residual) TRY(check_matrix("residual", residual, ldres, cols, es));
+  TRY(check_matrix("y", y, ldy, cols, es));
+  RouteArgs a = route_args(tokens, top, cols, position);
+  a.rows = const_cast<void*>(rows); a.ldr = ldr;
+  a.weights = weights; a.wf32 = weight_dtype == MUON_F32;
+  a.res = residual; a.ldres = ldres;
+  a.y = y; a.ldy = ldy;
+  return done(launch_route(dtype == MUON_BF16, ROUTE_GATHER, a, hipStream_t(hip_stream)), "combine");
+}
+
+MUON_API muon_status muon_combine_backward(const void* dy, int64_t lddy, const void* rows, int64_t ldr,
+                                           const void* weights, int32_t weight_dtype, const int32_t* position,
+                                           const int32_t* offsets, int32_t experts, void* drows, int64_t lddr,
+                                           void* dweights, int64_t tokens, int32_t top, int64_t cols, int32_t dtype,
+                                           void* hip_stream) {
+  TRY(check_route(tokens, top, cols, dtype));
+  TRY(check_experts(experts, offsets));
+  if (!tokens) return done(hipSuccess, "");
+  const size_t es = size_of(dtype);
+  TRY(check_matrix("dy", dy, lddy, cols, es));
+  if (dweights) TRY(check_matrix("rows", rows, ldr, cols, es));
+  TRY(check_weights(weights, weight_dtype, dtype));
+  TRY(check_needed("position", position, 4));
+  if (drows) TRY(check_matrix("drows", drows, lddr, cols, es));
+  TRY(check_vector("dweights", dweights, size_of(weight_dtype)));
+  RouteArgs a = route_args(tokens, top, cols, position);
+  a.dy = dy; a.lddy = lddy;
+  a.rows = const_cast<void*>(rows); a.ldr = ldr;
+  a.weights = weights; a.wf32 = weight_dtype == MUON_F32;
+  a.offsets = offsets; a.experts = experts;
+  a.drows = drows; a.lddr = lddr;
+  a.dweights = dweights;
+  return done(launch_route(dtype == MUON_BF16, ROUTE_COMBINE_GRAD, a, hipStream_t(hip_stream)), "combine backward");
+}
+
+MUON_API muon_status muon_embedding_forward(const void* ids, int32_t id_bytes, const void* w, int64_t ldw, void* y,
+                                            int64_t ldy, int64_t rows, int64_t vocab, int64_t cols, float scale,
+                                            int32_t dtype, void* hip_stream) {
+  TRY(check_count("rows", rows, 0, kMaxRows));
+  TRY(check_count("vocab", vocab, 1, kMaxDim));
+  TRY(check_count("cols", cols, 1, kMaxDim));
+  TRY(check_dtype(dtype));
+  if (!std::isfinite(scale)) return fail(MUON_ERR_INVALID_ARG, "scale must be finite");
+  TRY(check_ids("ids", ids, id_bytes, rows));
+  if (!rows) return done(hipSuccess, "");
+  const size_t es = size_of(dtype);
+  TRY(check_matrix("w", w, ldw, cols, es));
+  TRY(check_matrix("y", y, ldy, cols, es));
+  EmbeddingArgs a{};
+  a.ids = ids; a.id_bytes = id_bytes;
+  a.w = w; a.ldw = ldw;
+  a.y = y; a.ldy = ldy;
+  a.rows = int32_t(rows); a.cols = int32_t(cols); a.vocab = int32_t(vocab);
+  a.scale = scale;
+  return done(launch_embedding_forward(dtype == MUON_BF16, a, hipStream_t(hip_stream)), "embedding");
+}
+
+MUON_API muon_status muon_embedding_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes) {
+  if (!bytes) return fail(MUON_ERR_INVALID_ARG, "bytes is NULL");
+  TRY(check_count("rows", rows, 0, kMaxRows));
+  TRY(check_count("cols", cols, 1, kMaxDim));
+  *bytes = embedding_bytes(rows, cols);
+  return done(hipSuccess, "");
+}
+
+MUON_API muon_status muon_embedding_backward(const void* dy, int64_t lddy, const void* ids, int32_t id_bytes, void* dw,
+                                             int64_t lddw, int64_t rows, int64_t vocab, int64_t cols, float scale,
+                                             int32_t dtype, void* workspace, size_t workspace_bytes,
+                                             void* hip_stream) {
+  TRY(check_count("rows", rows, 0, kMaxRows));
+  TRY(check_count("vocab", vocab, 1, kMaxDim));
+  TRY(check_count("cols", cols, 1, kMaxDim));
+  TRY(check_dtype(dtype));
+  if (!std::isfinite(scale)) return fail(MUON_ERR_INVALID_ARG, "scale must be finite");
+  TRY(check_ids("ids", ids, id_bytes, rows));
+  const size_t es = size_of(dtype);
+  if (rows) TRY(check_matrix("dy", dy, lddy, cols, es));
+  TRY(check_matrix("dw", dw, lddw, cols, es));
+  TRY(check_workspace(workspace, workspace_bytes, embedding_bytes(rows, cols)));
+  EmbeddingArgs a{};
+  a.ids = ids; a.id_bytes = id_bytes;
+  a.dy = dy; a.lddy = lddy;
+  a.dw = dw; a.lddw = lddw;
+  a.rows = int32_t(rows); a.cols = int32_t(cols); a.vocab = int32_t(vocab);
+  a.scale = scale;
+  return done(launch_embedding_backward(dtype == MUON_BF16, a, workspace, hipStream_t(hip_stream)),
+              "embedding backward");
+}
+
+MUON_API muon_status muon_linear_cross_entropy_workspace_bytes(int64_t rows, int64_t inner, int64_t outer,
+                                                               int32_t dtype, int32_t flags, size_t* bytes) {
+  if (!bytes) return fail(MUON_ERR_INVALID_ARG, "bytes is NULL");
+  TRY(check_loss(rows, inner, outer, dtype, MUON_LOSS_ROWS));
+  TRY(check_flags(flags));
+  size_t most = 0;
+  for (bool transposed : {false, true})
+    for (bool unaligned : {false, true}) {
+      if (unaligned && !(flags & MUON_LAYERS_UNALIGNED)) continue;
+      const auto layout = flags & MUON_LAYERS_BACKWARD ? backward_layout : forward_layout;
+      most = larger(most, layout(rows, inner, outer, transposed, dtype == MUON_BF16, unaligned).total);
+    }
+  *bytes = most;
+  return done(hipSuccess, "");
+}
+
+MUON_API muon_status muon_linear_cross_entropy_forward(const void* x, int64_t ldx, const void* w, int64_t ldw,
+                                                       int32_t w_transposed, const void* targets,
+                                                       int32_t target_bytes, int64_t ignore, int32_t reduction,
+                                                       float* loss, float* lse, int64_t rows, int64_t inner,
+                                                       int64_t outer, int32_t dtype, void* workspace,
+                                                       size_t workspace_bytes, void* hip_stream) {
+  TRY(check_loss(rows, inner, outer, dtype, reduction));
+  TRY(check_ids("targets", targets, target_bytes, rows));
+  const size_t es = size_of(dtype);
+  const bool bf16 = dtype == MUON_BF16, each = reduction == MUON_LOSS_ROWS;
+  if (rows || !each) TRY(check_needed("loss", loss, 4));
+  bool unaligned = false;
+  if (rows) {
+    TRY(check_needed("lse", lse, 4));
+    TRY(check_matrix("x", x, ldx, inner, es));
+    TRY(check_matrix("w", w, ldw, w_transposed ? inner : outer, es));
+    unaligned = !operands_fit(x, ldx, w, ldw, w_transposed, inner, outer, bf16);
+  }
+  const LossLayout l = forward_layout(rows, inner, outer, w_transposed, bf16, unaligned);
+  TRY(check_workspace(workspace, workspace_bytes, l.total));
+  const hipStream_t st = hipStream_t(hip_stream);
+  char* ws = static_cast<char*>(workspace);
+  const Scratch scratch{ws + l.scratch, l.total - l.scratch};
+  LossArgs a{};
+  a.targets = targets; a.target_bytes = target_bytes; a.ignore = ignore;
+  a.rows = int32_t(rows); a.vocab = int32_t(outer);
+  a.label = reinterpret_cast<int32_t*>(ws + l.label);
+  a.logit = reinterpret_cast<float*>(ws + l.logit);
+  a.loss = each ? loss : reinterpret_cast<float*>(ws + l.loss);
+  a.lse = lse;
+  if (rows) TRY(done(launch_loss_labels(a, st), "loss labels"));
+  LossArgs b = a;
+  const int form = w_transposed ? FORM_RR : FORM_RT;
+  for (int64_t r = 0; r < rows; r += l.rows) {
+    const int64_t n = rows - r < l.rows ? rows - r : l.rows;
+    b.label = a.label + r;
+    b.logit = a.logit + r;
+    b.loss = a.loss + r;
+    b.lse = a.lse + r;
+    b.rows = int32_t(n);
+    b.part = reinterpret_cast<float2*>(ws + l.part);
+    b.raw = reinterpret_cast<float*>(ws + l.raw);
+    b.strip = 0;
+    for (int64_t c = 0; c < outer; c += l.piece) {
+      Product p{};
+      p.M = b.rows;
+      p.N = int32_t(outer - c < l.piece ? outer - c : l.piece);
+      p.K = int32_t(inner);
+      p.a = static_cast<const char*>(x) + size_t(r * ldx) * es; p.lda = ldx;
+      p.b = columns(w, ldw, w_transposed, c, es); p.ldb = ldw;
+      b.first = int32_t(c);
+      b.cols = p.N;
+      if (l.z.kernel == Choice::SKINNY) {
+        TRY(done(product_sums(l.z, bf16, form, p, reinterpret_cast<float*>(ws + l.raw), scratch, st), "logits"));
+        b.splits = l.z.splits;
+        TRY(done(launch_loss_strips(b, st), "loss strips"));
+      } else {
+        TRY(done(loss_product(l.z, LOSS_STRIPS, bf16, form, p, b, scratch, st), "loss strips"));
+      }
+      b.strip += int32_t(ceil_div(p.N, strip_columns(l.z)));
+    }
+    b.strips = b.strip;
+    TRY(done(launch_loss_finish(b, st), "loss"));
+  }
+  if (!each) {
+    a.total = loss;
+    a.mean = reduction == MUON_LOSS_MEAN;
+    TRY(done(launch_loss_total(a, st), "loss"));
+  }
+  return done(hipSuccess, "");
+}
+
+MUON_API muon_status muon_linear_cross_entropy_backward(const float* dloss, const void* x, int64_t ldx, const void* w,
+                                                        int64_t ldw, int32_t w_transposed, const void* targets,
+                                                        int32_t target_bytes, int64_t ignore, int32_t reduction,
+                                                        const float* lse, void* dx, int64_t lddx, void* dw,
+                                                        int64_t lddw, int64_t rows, int64_t inner, int64_t outer,
+                                                        int32_t dtype, void* workspace, size_t workspace_bytes,
+                                                        void* hip_stream) {
+  TRY(check_loss(rows, inner, outer, dtype, reduction));
+  TRY(check_ids("targets", targets, target_bytes, rows));
+  const size_t es = size_of(dtype);
+  const bool bf16 = dtype == MUON_BF16;
+  bool unaligned = false;
+  if (rows) {
+    TRY(check_needed("dloss", dloss, 4));
+    TRY(check_needed("lse", lse, 4));
+    TRY(check_matrix("x", x, ldx, inner, es));
+    TRY(check_matrix("w", w, ldw, w_transposed ? inner : outer, es));
+    if (dx) TRY(check_matrix("dx", dx, lddx, inner, es));
+    unaligned = !operands_fit(x, ldx, w, ldw, w_transposed, inner, outer, bf16);
+  }
+  if (dw) TRY(check_matrix("dw", dw, lddw, w_transposed ? inner : outer, es));
+  const LossLayout l = backward_layout(rows, inner, outer, w_transposed, bf16, unaligned);
+  TRY(check_workspace(workspace, workspace_bytes, l.total));
+  const hipStream_t st = hipStream_t(hip_stream);
+  char* ws = static_cast<char*>(workspace);
+  const Scratch scratch{ws + l.scratch, l.total - l.scratch};
+  LossArgs a{};
+  a.targets = targets; a.target_bytes = target_bytes; a.ignore = ignore;
+  a.rows = int32_t(rows); a.vocab = int32_t(outer);
+  a.label = reinterpret_cast<int32_t*>(ws + l.label);
+  a.grad = reinterpret_cast<float*>(ws + l.grad);
+  a.alpha = reinterpret_cast<float*>(ws + l.alpha);
+  a.dloss = dloss;
+  a.each = reduction == MUON_LOSS_ROWS;
+  a.mean = reduction == MUON_LOSS_MEAN;
+  a.lse = const_cast<float*>(lse);
+  if (!rows && !dw) return done(hipSuccess, "");
+  if (rows) TRY(done(launch_loss_labels(a, st), "loss labels"));
+  const int64_t lddz = ceil_div(l.piece, 8) * 8;
+  float* raw = reinterpret_cast<float*>(ws + l.raw);
+  float* sums = reinterpret_cast<float*>(ws + l.dx);
+  for (int64_t c = 0; c < outer; c += l.piece) {
+    const int64_t cols = outer - c < l.piece ? outer - c : l.piece;
+    const void* wc = columns(w, ldw, w_transposed, c, es);
+    for (int64_t r = 0; r < rows; r += l.rows) {
+      LossArgs b = a;
+      b.rows = int32_t(rows - r < l.rows ? rows - r : l.rows);
+      b.label = a.label + r;
+      b.grad = a.grad + r;
+      b.lse = a.lse + r;
+      b.raw = raw;
+      b.splits = l.z.splits;
+      b.dz = ws + l.dz + size_t(r * lddz) * es;
+      b.lddz = lddz;
+      b.first = int32_t(c);
+      b.cols = int32_t(cols);
+      Product p{};
+      p.M = b.rows; p.N = b.cols; p.K = int32_t(inner);
+      p.a = static_cast<const char*>(x) + size_t(r * ldx) * es; p.lda = ldx;
+      p.b = wc; p.ldb = ldw;
+      p.c = b.dz; p.ldc = lddz;
+      const int form = w_transposed ? FORM_RR : FORM_RT;
+      if (l.z.kernel == Choice::SKINNY) {
+        TRY(done(product_sums(l.z, bf16, form, p, raw, scratch, st), "logits"));
+        TRY(done(launch_loss_grad(bf16, b, st), "loss gradient"));
+      } else {
+        TRY(done(loss_product(l.z, LOSS_GRAD, bf16, form, p, b, scratch, st), "loss gradient"));
+      }
+    }
+    const int32_t pad = int32_t(ceil_div(cols, 8) * 8);
+    if (dx && rows) {
+      Product p{};
+      p.M = int32_t(rows); p.N = int32_t(inner); p.K = int32_t(cols);
+      p.a = ws + l.dz; p.lda = lddz; p.pad_a = pad;
+      p.b = wc; p.ldb = ldw;
+      p.add = c > 0;
+      TRY(done(product_sums(l.x, bf16, w_transposed ? FORM_RT : FORM_RR, p, sums, scratch, st),
+               "loss input gradient"));
+    }
+    if (dw) {
+      Product p{};
+      p.K = int32_t(rows);
+      p.c = const_cast<void*>(columns(dw, lddw, w_transposed, c, es)); p.ldc = lddw;
+      if (w_transposed) {
+        p.a = ws + l.dz; p.lda = lddz; p.pad_a = pad;
+        p.b = x; p.ldb = ldx;
+        p.M = int32_t(cols); p.N = int32_t(inner);
+      } else {
+        p.a = x; p.lda = ldx;
+        p.b = ws + l.dz; p.ldb = lddz; p.pad_b = pad;
+        p.M = int32_t(inner); p.N = int32_t(cols);
+      }
+      // (without rows there is no alpha, and dw is 0)
+      TRY(done(rows ? loss_product(l.w, LOSS_WEIGHT, bf16, FORM_TT, p, a, scratch, st)
+                    : product_by(l.w, bf16, FORM_TT, GROUP_NONE, p, nullptr, scratch, st),
+               "loss weight gradient"));
+    }
+  }
+  if (dx && rows)
+    TRY(done(launch_loss_sum(bf16, sums, l.x.splits, a.alpha, dx, lddx, rows, inner, st), "loss input gradient"));
+  return done(hipSuccess, "");
+}
+
+}  // extern "C"

@@ -1,9 +1,12 @@
 """Layer operators around the matrices the Muon step updates: a matrix product
 with a fused epilogue (``linear``), the same grouped by expert
-(``grouped_linear``) and ``layer_norm``, each with its backward pass.
+(``grouped_linear``) and ``layer_norm``, each with its backward pass; and those
+at a model's ends and on the way to its experts: ``embedding``,
+``linear_cross_entropy``, and ``sort_by_expert`` with ``dispatch`` and ``combine``.
 
 Each operator comes as a function torch's autograd sees (``linear``,
-``grouped_linear``, ``layer_norm``) and as its two passes (``*_forward``,
+``grouped_linear``, ``layer_norm``, ``embedding``, ``linear_cross_entropy``,
+``dispatch``, ``combine``) and as its two passes (``*_forward``,
 ``*_backward``), which only enqueue HIP kernels on torch's current stream of the
 tensors' device: no host synchronisation, no copies, nothing of the data kept
 between calls.  Weights are [in, out] like the optimizer's workloads; the transposed
@@ -12,7 +15,9 @@ weight's own memory layout, so that ``Muon`` steps them without a copy.
 
 Tensors are fp32 or bf16 (one dtype per call; layer norm's weight and bias may be
 fp32 next to bf16 activations), sums are fp32.  Rows may be strided (a slice of
-wider rows), their elements may not.  A bad argument raises ValueError or
+wider rows), their elements may not.  Tokens, targets and experts come as int32 or
+int64 numbers on the GPU, which the host never reads: one outside its range
+stands for nobody (no table row, no target, no expert).  A bad argument raises ValueError or
 TypeError before anything is launched; a number that the library refuses (eps, sizes
 out of its range) MuonError.
 """
@@ -20,7 +25,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
-from typing import Optional, Sequence, Union
+from typing import NamedTuple, Optional, Sequence, Union
 
 import torch
 
@@ -122,7 +127,7 @@ def _on_device(fn):
     """Runs fn with its first tensor's device current (which it nearly always is)."""
     @functools.wraps(fn)
     def run(*args, **kwargs):
-        t = args[0] if args else kwargs.get("dy", kwargs.get("x"))
+        t = args[0] if args else next((v for v in kwargs.values() if isinstance(v, torch.Tensor)), None)
         index = t.device.index if isinstance(t, torch.Tensor) else None
         if index is None or index == torch._C._cuda_getDevice():
             return fn(*args, **kwargs)
@@ -573,3 +578,399 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
     """Layer norm over the last dimension of x, differentiable once."""
     y = _LayerNorm.apply(_flat(x, "x"), weight, bias, float(eps), torch.is_grad_enabled())
     return y if x.dim() == 2 else y.view(x.shape)
+
+
+# ------------------------------------------------- tokens, targets, experts
+
+_NUMBERS = {torch.int32: 4, torch.int64: 8}
+
+
+def _numbers(t: torch.Tensor, name: str, shape=None, like: Optional[torch.Tensor] = None):
+    """(pointer, bytes of an element) of a contiguous tensor of numbers."""
+    _tensor(t, name)
+    size = _NUMBERS.get(t.dtype)
+    if size is None:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected int32 or int64")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous (stride {t.stride()})")
+    if not t.is_cuda:
+        raise ValueError(f"{name} is not on a GPU")
+    if like is not None and t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+    return t.data_ptr(), size
+
+
+# ---------------------------------------------------------------- embedding
+
+@_on_device
+def embedding_forward(ids: torch.Tensor, weight: torch.Tensor, *, scale: float = 1.0) -> torch.Tensor:
+    """``scale * weight[ids]`` for ids of any shape and a table [vocab, cols]; a
+    number outside [0, vocab) gets a row of 0."""
+    lib = _load()
+    ip, size = _numbers(ids, "ids")
+    _input(weight, "weight")
+    code = _dtype_code(weight)
+    vocab, cols = weight.shape
+    if vocab == 0:
+        raise ValueError("weight has no rows")
+    _numbers(ids, "ids", None, weight)
+    wp, ldw = _rows(weight, "weight", weight, vocab, cols)
+    scale = float(scale)
+    stream = _stream(weight)
+    y = weight.new_empty((*ids.shape, cols))
+    LL.check(lib.muon_embedding_forward(ip, size, wp, ldw, y.data_ptr(), cols, ids.numel(), vocab, cols, scale, code,
+                                        stream))
+    return y
+
+
+@_on_device
+def embedding_backward(dy: torch.Tensor, ids: torch.Tensor, vocab: int, *, scale: float = 1.0) -> torch.Tensor:
+    """The table's gradient [vocab, cols] for the output gradient dy [*ids.shape,
+    cols]: ``scale`` times the sum of each token's rows, taken in their order."""
+    lib = _load()
+    _tensor(dy, "dy")
+    ip, size = _numbers(ids, "ids")
+    if dy.dim() != ids.dim() + 1 or dy.shape[:-1] != ids.shape:
+        raise ValueError(f"dy has shape {tuple(dy.shape)}, expected {(*ids.shape, 'cols')}")
+    dy = _flat(dy, "dy")
+    _input(dy, "dy")
+    code = _dtype_code(dy)
+    rows, cols = dy.shape
+    _numbers(ids, "ids", None, dy)
+    gp, ldg = _rows(dy, "dy", dy, rows, cols)
+    vocab, scale = int(vocab), float(scale)
+    if vocab < 1:
+        raise ValueError(f"vocab {vocab}: a table has at least one row")
+    stream = _stream(dy)
+    dw = dy.new_empty((vocab, cols))
+    need = _bytes("muon_embedding_workspace_bytes", rows, cols)
+    ws = _workspace(need, dy)
+    LL.check(lib.muon_embedding_backward(gp, ldg, ip, size, dw.data_ptr(), cols, rows, vocab, cols, scale, code,
+                                         None if ws is None else ws.data_ptr(), need, stream))
+    return dw
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, ids, weight, scale):
+        ctx.vocab, ctx.scale = weight.size(0), scale
+        ctx.save_for_backward(ids)
+        return embedding_forward(ids, weight, scale=scale)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        if not ctx.needs_input_grad[1]:
+            return None, None, None
+        return None, embedding_backward(dy, ctx.saved_tensors[0], ctx.vocab, scale=ctx.scale), None
+
+
+def embedding(ids: torch.Tensor, weight: torch.Tensor, *, scale: float = 1.0) -> torch.Tensor:
+    """``scale * weight[ids]``, differentiable once in the table [vocab, cols].  The
+    table can be the transposed weight of ``linear_cross_entropy`` too."""
+    _tensor(ids, "ids")
+    _tensor(weight, "weight")
+    return _Embedding.apply(ids.contiguous(), _dense(weight), float(scale))
+
+
+# ----------------------------------------- tokens to their experts and back
+
+class Routing(NamedTuple):
+    """A router's choices sorted by expert (``sort_by_expert``)."""
+    offsets: torch.Tensor    # int32 [experts + 1]: each expert's rows, as grouped_linear takes them
+    position: torch.Tensor   # int32 [tokens, top]: each choice's row, -1 for one of no expert
+    source: torch.Tensor     # int32 [tokens * top]: each row's choice t * top + j, -1 behind the last
+
+
+@_on_device
+def sort_by_expert(experts: torch.Tensor, count: int) -> Routing:
+    """The choices experts [tokens, top] of ``count`` experts sorted by expert, in
+    their own order within each.  One outside [0, count) goes to no expert."""
+    lib = _load()
+    ip, size = _numbers(experts, "experts")
+    if experts.dim() != 2:
+        raise ValueError(f"experts must be [tokens, top], got shape {tuple(experts.shape)}")
+    tokens, top = experts.shape
+    count = int(count)
+    for name, n in (("top", top), ("count", count)):
+        if n < 1 or n > LL.MUON_GROUPED_MAX_EXPERTS:
+            raise ValueError(f"{name} {n}; 1 to {LL.MUON_GROUPED_MAX_EXPERTS} are supported")
+    stream = _stream(experts)
+    n = tokens * top
+    new = lambda *s: torch.empty(s, dtype=torch.int32, device=experts.device)
+    routing = Routing(new(count + 1), new(tokens, top), new(n))
+    need = _bytes("muon_sort_by_expert_workspace_bytes", tokens, top)
+    ws = _workspace(need, experts)
+    LL.check(lib.muon_sort_by_expert(ip, size, tokens, top, count, routing.offsets.data_ptr(),
+                                     routing.position.data_ptr(), routing.source.data_ptr(),
+                                     None if ws is None else ws.data_ptr(), need, stream))
+    return routing
+
+
+def _routing(routing, like: torch.Tensor):
+    """(pointer of position, of offsets, experts, tokens, top)."""
+    if not isinstance(routing, tuple) or len(routing) != 3:
+        raise TypeError(f"routing must come from sort_by_expert, got {type(routing).__name__}")
+    offsets, position, _ = routing
+    for t, name, dim in ((position, "position", 2), (offsets, "offsets", 1)):
+        _tensor(t, name)
+        if t.dtype != torch.int32 or t.dim() != dim or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 tensor of {dim} dimensions")
+        if t.device != like.device:
+            raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+    return (position.data_ptr(), offsets.data_ptr(), offsets.size(0) - 1, *position.shape)
+
+
+def _router_weights(weights: torch.Tensor, x: torch.Tensor, tokens: int, top: int):
+    _tensor(weights, "weights")
+    if weights.shape != (tokens, top) or not weights.is_contiguous():
+        raise ValueError(f"weights must be contiguous and [{tokens}, {top}], got shape {tuple(weights.shape)} and "
+                         f"stride {weights.stride()}")
+    if weights.device != x.device:
+        raise ValueError(f"weights is on {weights.device}, expected {x.device}")
+    if weights.dtype not in (torch.float32, x.dtype):
+        raise ValueError(f"weights has dtype {weights.dtype}, expected float32 or {x.dtype}")
+    return weights.data_ptr(), _DTYPES[weights.dtype]
+
+
+@_on_device
+def dispatch_forward(x: torch.Tensor, routing: Routing) -> torch.Tensor:
+    """Every token's row x[t] at its choices' rows [tokens * top, cols], sorted by
+    expert; rows behind the last expert's get 0."""
+    lib = _load()
+    _input(x)
+    code = _dtype_code(x)
+    pp, op, experts, tokens, top = _routing(routing, x)
+    cols = x.size(1)
+    xp, ldx = _rows(x, "x", x, tokens, cols)
+    stream = _stream(x)
+    rows = x.new_empty((tokens * top, cols))
+    LL.check(lib.muon_dispatch_forward(xp, ldx, pp, op, experts, rows.data_ptr(), cols, tokens, top, cols, code,
+                                       stream))
+    return rows
+
+
+@_on_device
+def dispatch_backward(drows: torch.Tensor, routing: Routing) -> torch.Tensor:
+    """dx [tokens, cols]: the sum of each token's choices' rows."""
+    lib = _load()
+    _input(drows, "drows")
+    code = _dtype_code(drows)
+    pp, _, _, tokens, top = _routing(routing, drows)
+    cols = drows.size(1)
+    rp, ldr = _rows(drows, "drows", drows, tokens * top, cols)
+    stream = _stream(drows)
+    dx = drows.new_empty((tokens, cols))
+    LL.check(lib.muon_dispatch_backward(rp, ldr, pp, dx.data_ptr(), cols, tokens, top, cols, code, stream))
+    return dx
+
+
+@_on_device
+def combine_forward(rows: torch.Tensor, weights: torch.Tensor, routing: Routing, *,
+                    residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``y[t] = residual[t] + sum of weights[t, j] * rows[position[t, j]]`` over the
+    token's choices; weights [tokens, top] are fp32 or of the rows' dtype."""
+    lib = _load()
+    _input(rows, "rows")
+    code = _dtype_code(rows)
+    pp, _, _, tokens, top = _routing(routing, rows)
+    cols = rows.size(1)
+    rp, ldr = _rows(rows, "rows", rows, tokens * top, cols)
+    wp, wcode = _router_weights(weights, rows, tokens, top)
+    sp, lds = (None, 0) if residual is None else _rows(residual, "residual", rows, tokens, cols)
+    stream = _stream(rows)
+    y = rows.new_empty((tokens, cols))
+    LL.check(lib.muon_combine_forward(rp, ldr, wp, wcode, pp, sp, lds, y.data_ptr(), cols, tokens, top, cols, code,
+                                      stream))
+    return y
+
+
+@_on_device
+def combine_backward(dy: torch.Tensor, rows: torch.Tensor, weights: torch.Tensor, routing: Routing, *,
+                     rows_grad: bool = True, weights_grad: bool = True):
+    """Gradients ``(drows, dweights)`` of ``combine_forward`` (the residual's is dy);
+    those not asked for are None.  Rows behind the last expert's get 0."""
+    lib = _load()
+    _input(dy, "dy")
+    code = _dtype_code(dy)
+    pp, op, experts, tokens, top = _routing(routing, dy)
+    cols = dy.size(1)
+    gp, ldg = _rows(dy, "dy", dy, tokens, cols)
+    rp, ldr = _rows(rows, "rows", dy, tokens * top, cols)
+    wp, wcode = _router_weights(weights, dy, tokens, top)
+    stream = _stream(dy)
+    drows = dy.new_empty((tokens * top, cols)) if rows_grad else None
+    dweights = torch.empty_like(weights) if weights_grad else None
+    LL.check(lib.muon_combine_backward(gp, ldg, rp, ldr, wp, wcode, pp, op, experts,
+                                       None if drows is None else drows.data_ptr(), cols,
+                                       None if dweights is None else dweights.data_ptr(), tokens, top, cols, code,
+                                       stream))
+    return drows, dweights
+
+
+class _Dispatch(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, *routing):
+        ctx.save_for_backward(*routing)
+        return dispatch_forward(x, Routing(*routing))
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, drows):
+        dx = dispatch_backward(_dense(drows), Routing(*ctx.saved_tensors)) if ctx.needs_input_grad[0] else None
+        return dx, None, None, None
+
+
+class _Combine(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, rows, weights, residual, *routing):
+        ctx.save_for_backward(rows, weights, *routing)
+        return combine_forward(rows, weights, Routing(*routing), residual=residual)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        rows, weights, *routing = ctx.saved_tensors
+        nr, nw, ns = ctx.needs_input_grad[:3]
+        drows = dweights = None
+        if nr or nw:
+            drows, dweights = combine_backward(_dense(dy), rows, weights, Routing(*routing), rows_grad=nr,
+                                               weights_grad=nw)
+        return drows, dweights, dy if ns else None, None, None, None
+
+
+def dispatch(x: torch.Tensor, routing: Routing) -> torch.Tensor:
+    """The rows [tokens * top, cols] that ``grouped_linear`` takes with
+    ``routing.offsets``, differentiable once in x [tokens, cols]."""
+    _tensor(x, "x")
+    return _Dispatch.apply(_dense(x), *routing)
+
+
+def combine(rows: torch.Tensor, weights: torch.Tensor, routing: Routing, *,
+            residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The experts' outputs back at their tokens, weighted and added up (to the
+    residual), differentiable once in rows, weights and residual."""
+    _tensor(rows, "rows")
+    _tensor(weights, "weights")
+    if residual is not None:
+        _tensor(residual, "residual")
+        residual = _dense(residual)
+    return _Combine.apply(_dense(rows), weights.contiguous(), residual, *routing)
+
+
+# ------------------------------------------------------ linear cross entropy
+
+def _reduction(name: str) -> int:
+    code = LL.REDUCTIONS.get(name)
+    if code is None:
+        raise ValueError(f"unknown reduction {name!r}; choose from {tuple(LL.REDUCTIONS)}")
+    return code
+
+
+@_on_device
+def linear_cross_entropy_forward(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, *,
+                                 reduction: str = "mean", ignore_index: int = -100):
+    """``(loss, lse)``: softmax cross entropy of the logits x @ weight for x [rows,
+    in], weight [in, vocab], targets [rows], and the rows' log of the sum of
+    exponentials, which the backward pass reads.  The logits are never kept: the
+    vocabulary is gone through in pieces.  A row whose target is ignore_index or
+    outside [0, vocab) has loss 0 and does not count in the mean.  Both are fp32;
+    loss is one number unless the reduction is "none"."""
+    lib = _load()
+    _input(x)
+    red = _reduction(reduction)
+    code = _dtype_code(x)
+    rows, inner = x.shape
+    xp, ldx = _rows(x, "x", x, rows, inner)
+    wp, ldw, wt, outer = _weight(weight, x, inner)
+    if outer == 0:
+        raise ValueError("weight has no output features")
+    tp, tsize = _numbers(targets, "targets", (rows,), x)
+    ignore = int(ignore_index)
+    stream = _stream(x)
+    lse = x.new_empty((rows,), dtype=torch.float32)
+    loss = x.new_empty((rows,) if red == 0 else (), dtype=torch.float32)
+    size = x.element_size()
+    need = _bytes("muon_linear_cross_entropy_workspace_bytes", rows, inner, outer, code,
+                  _flags(0, x, outer, xp, ldx * size, wp, ldw * size))
+    ws = _workspace(need, x)
+    LL.check(lib.muon_linear_cross_entropy_forward(xp, ldx, wp, ldw, wt, tp, tsize, ignore, red, loss.data_ptr(),
+                                                   lse.data_ptr(), rows, inner, outer, code,
+                                                   None if ws is None else ws.data_ptr(), need, stream))
+    return loss, lse
+
+
+@_on_device
+def linear_cross_entropy_backward(dloss: torch.Tensor, x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor,
+                                  lse: torch.Tensor, *, reduction: str = "mean", ignore_index: int = -100,
+                                  input_grad: bool = True, weight_grad: bool = True):
+    """Gradients ``(dx, dweight)`` of ``linear_cross_entropy_forward`` for the
+    loss's fp32 gradient (of its shape); those not asked for are None.  The logits
+    are computed again, piece by piece.  dweight is kept like the weight."""
+    lib = _load()
+    _input(x)
+    red = _reduction(reduction)
+    code = _dtype_code(x)
+    rows, inner = x.shape
+    xp, ldx = _rows(x, "x", x, rows, inner)
+    wp, ldw, wt, outer = _weight(weight, x, inner)
+    if outer == 0:
+        raise ValueError("weight has no output features")
+    tp, tsize = _numbers(targets, "targets", (rows,), x)
+    for name, t, shape in (("dloss", dloss, (rows,) if red == 0 else ()), ("lse", lse, (rows,))):
+        _tensor(t, name)
+        if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous float32 tensor of shape {shape}")
+        if t.device != x.device:
+            raise ValueError(f"{name} is on {t.device}, expected {x.device}")
+    ignore = int(ignore_index)
+    stream = _stream(x)
+    dx = x.new_empty((rows, inner)) if input_grad else None
+    dw = _like_weight(weight, wt) if weight_grad else None
+    size = x.element_size()
+    need = _bytes("muon_linear_cross_entropy_workspace_bytes", rows, inner, outer, code,
+                  _flags(1, x, outer, xp, ldx * size, wp, ldw * size))
+    ws = _workspace(need, x)
+    LL.check(lib.muon_linear_cross_entropy_backward(dloss.data_ptr(), xp, ldx, wp, ldw, wt, tp, tsize, ignore, red,
+                                                    lse.data_ptr(), None if dx is None else dx.data_ptr(), inner,
+                                                    None if dw is None else dw.data_ptr(), inner if wt else outer,
+                                                    rows, inner, outer, code,
+                                                    None if ws is None else ws.data_ptr(), need, stream))
+    return dx, dw
+
+
+class _LinearCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, targets, reduction, ignore_index, grad_mode):
+        loss, lse = linear_cross_entropy_forward(x, weight, targets, reduction=reduction, ignore_index=ignore_index)
+        if grad_mode and any(ctx.needs_input_grad[:2]):
+            ctx.how = dict(reduction=reduction, ignore_index=ignore_index)
+            ctx.save_for_backward(x, weight, targets, lse)
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        x, weight, targets, lse = ctx.saved_tensors
+        nx, nw = ctx.needs_input_grad[:2]
+        dx, dw = linear_cross_entropy_backward(dloss.contiguous(), x, weight, targets, lse, input_grad=nx,
+                                               weight_grad=nw, **ctx.how)
+        return dx, dw, None, None, None, None
+
+
+def linear_cross_entropy(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, *, reduction: str = "mean",
+                         ignore_index: int = -100) -> torch.Tensor:
+    """Softmax cross entropy of the logits x @ weight over the last dimension of x,
+    without the logits, differentiable once in x and weight.  targets has x's
+    leading dimensions; weight is [in, vocab], or the transposed view of an embedding
+    table [vocab, in].  reduction is "mean" (over the rows with a target; 0 if there are
+    none), "sum" or "none"."""
+    x2 = _flat(x, "x")
+    _tensor(targets, "targets")
+    if targets.shape != x.shape[:-1]:
+        raise ValueError(f"targets has shape {tuple(targets.shape)}, x has leading dimensions {tuple(x.shape[:-1])}")
+    loss = _LinearCrossEntropy.apply(x2, weight, targets.reshape(-1).contiguous(), reduction, int(ignore_index),
+                                     torch.is_grad_enabled())
+    return loss.view(targets.shape) if reduction == "none" else loss
