@@ -286,10 +286,38 @@ struct Staging {
   static constexpr int BYTES = 32 * LD * 4;            // of a wave
   static constexpr int LPR = C::WTN / 8, RPI = 64 / LPR;  // lanes of a row, rows of a store instruction
 };
-template <class C, typename E, typename OUT, int ACT, bool EPI, bool RAGGED, bool ADD = false>
+// Rows 32 I .. 32 I + 31 of a wave's piece to the staging (`to`: the lane's place).
+template <class C, int I>
+__device__ __forceinline__ void stage_rows(const f32x16 (&acc)[C::NBM][C::NBN], float* to) {
+  static_for<4 * C::NBN>([&](auto jg) {
+    constexpr int j = decltype(jg)::value / 4, g = decltype(jg)::value % 4;
+    *reinterpret_cast<f32x4*>(to + 32 * j + 8 * g) =
+        f32x4{acc[I][j][4 * g], acc[I][j][4 * g + 1], acc[I][j][4 * g + 2], acc[I][j][4 * g + 3]};
+  });
+}
+
+// What a product's epilogue knows of its rows and does to 8 columns of one: rows()
+// puts what it needs of row `lane` of 32 into the 4 floats that follow it in the staging,
+// columns() gets them with the values.
+struct AsSummed {
+  template <class C>
+  __device__ __forceinline__ void rows(int, float*, int) const {}
+  template <class C>
+  __device__ __forceinline__ void columns(float (&)[8], const float*, int) const {}
+};
+struct Scaled : AsSummed {
+  float f;
+  __device__ __forceinline__ explicit Scaled(float v) : f(v) {}
+  template <class C>
+  __device__ __forceinline__ void columns(float (&v)[8], const float*, int) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= f;
+  }
+};
+template <class C, typename E, typename OUT, int ACT, bool EPI, bool RAGGED, bool ADD = false, class OP = AsSummed>
 __device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ldc, const Work<E>& o,
                                             const f32x16 (&acc)[C::NBM][C::NBN], float* region, int wm, int wn,
-                                            int lane) {
+                                            int lane, const OP& op = OP()) {
   using S = Staging<C>;
   const E* bias = EPI ? static_cast<const E*>(p.bias) : nullptr;
   const E* res = EPI ? static_cast<const E*>(p.res) : nullptr;
@@ -308,17 +336,15 @@ __device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ld
   int left = in ? o.rows - wm - r0 : 0;                         // rows from this lane's on
   static_for<C::NBM>([&](auto it) {
     constexpr int i = decltype(it)::value;
-    static_for<4 * C::NBN>([&](auto jg) {
-      constexpr int j = decltype(jg)::value / 4, g = decltype(jg)::value % 4;
-      *reinterpret_cast<f32x4*>(to + 32 * j + 8 * g) =
-          f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-    });
+    stage_rows<C, i>(acc, to);
+    op.template rows<C>(i, region, lane);
 #pragma unroll 2
     for (int k = 0; k < 32 / S::RPI; ++k) {
       const f32x4 lo = *reinterpret_cast<const f32x4*>(from + k * S::RPI * S::LD);
       const f32x4 hi = *reinterpret_cast<const f32x4*>(from + k * S::RPI * S::LD + 4);
       float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
       if (left > 0) {
+        op.template columns<C>(v, region + (r0 + k * S::RPI) * S::LD + C::WTN, lane % S::LPR * 8);
         if constexpr (EPI) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] += bv[e];
@@ -350,125 +376,122 @@ __device__ __forceinline__ void store_piece(const Product& p, OUT* c, int64_t ld
   });
 }
 
-template <class C, typename E, bool EPI, bool RAGGED>
+template <class C, typename E, bool EPI, bool RAGGED, class OP>
 __device__ __forceinline__ void store_columns(const Product& p, const Work<E>& o,
                                               const f32x16 (&acc)[C::NBM][C::NBN], float* region, int wm, int wn,
-                                              int lane) {
+                                              int lane, const OP& op) {
   if (p.splits > 1 || p.raw) {
     float* part = p.part + int64_t(blockIdx.y) * p.M * p.N;
     if (p.add)
-      store_piece<C, E, float, MUON_ACT_NONE, false, RAGGED, true>(p, part, p.N, o, acc, region, wm, wn, lane);
+      store_piece<C, E, float, MUON_ACT_NONE, false, RAGGED, true>(p, part, p.N, o, acc, region, wm, wn, lane, op);
     else
-      store_piece<C, E, float, MUON_ACT_NONE, false, RAGGED>(p, part, p.N, o, acc, region, wm, wn, lane);
+      store_piece<C, E, float, MUON_ACT_NONE, false, RAGGED, false>(p, part, p.N, o, acc, region, wm, wn, lane, op);
   } else {
     with_act<EPI>(p.act, [&](auto act) {
-      store_piece<C, E, E, decltype(act)::value, EPI, RAGGED>(p, o.c, p.ldc, o, acc, region, wm, wn, lane);
+      store_piece<C, E, E, decltype(act)::value, EPI, RAGGED, false>(p, o.c, p.ldc, o, acc, region, wm, wn, lane, op);
     });
   }
 }
-template <class C, typename E, bool EPI>
+template <class C, typename E, bool EPI, class OP = AsSummed>
 __device__ __forceinline__ void store_tile(const Product& p, const Work<E>& o, const f32x16 (&acc)[C::NBM][C::NBN],
-                                           float* region, int wm, int wn, int lane) {
+                                           float* region, int wm, int wn, int lane, const OP& op = OP()) {
   if (o.cols % 8)
-    store_columns<C, E, EPI, true>(p, o, acc, region, wm, wn, lane);
+    store_columns<C, E, EPI, true>(p, o, acc, region, wm, wn, lane, op);
   else
-    store_columns<C, E, EPI, false>(p, o, acc, region, wm, wn, lane);
+    store_columns<C, E, EPI, false>(p, o, acc, region, wm, wn, lane, op);
+}
+
+// The sum or the largest over the LPR lanes that share a row, in all of them.
+template <int LPR, class F>
+__device__ __forceinline__ float over_row(float v, F f) {
+  auto with = [&](auto ctrl) {
+    const int o = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, false);
+    v = f(v, __builtin_bit_cast(float, o));
+  };
+  with(IntTag<0xB1>{});                            // quad_perm: lane ^ 1
+  with(IntTag<0x4E>{});                            // quad_perm: lane ^ 2
+  if constexpr (LPR >= 8) with(IntTag<0x141>{});   // row_half_mirror: the other quad of 8
+  if constexpr (LPR >= 16) with(IntTag<0x140>{});  // row_mirror: the other 8 of 16
+  return v;
 }
 
 // A wave's piece of logits, whose columns are a strip: per row the largest and the
-// sum of exp(z - largest), both within the lanes that hold the row (l and l + 32), and the
-// target's logit where the strip has it.  exp(z - m) = 2^(z log2(e) - m log2(e)), one
-// fused multiply-add before the instruction; columns past the last count as -inf.
+// sum of exp(z - largest), and the target's logit where the strip has it.
+// exp(z - m) = 2^(z log2(e) - m log2(e)), one fused multiply-add before the
+// instruction; columns past the last count as -inf.
 template <class C, typename E>
 __device__ __forceinline__ void strip_piece(const LossArgs& a, const Work<E>& o, const f32x16 (&acc)[C::NBM][C::NBN],
-                                            int wm, int wn, int lane) {
+                                            float* region, int wm, int wn, int lane) {
+  using S = Staging<C>;
   constexpr float kLog2e = 1.4426950408889634f;
-  const int left = o.cols - wn - 4 * (lane >> 5);   // columns from the lane's first on
   if (o.cols <= wn) return;
-  auto piece = [&](auto ragged) {
-    static_for<C::NBM>([&](auto it) {
-      constexpr int i = decltype(it)::value;
-      auto value = [&](int j, int q) {
-        const float v = acc[i][j][q];
-        return decltype(ragged)::value && 32 * j + 8 * (q / 4) + q % 4 >= left ? -INFINITY : v;
-      };
-      float m = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < C::NBN; ++j)
-#pragma unroll
-        for (int q = 0; q < 16; ++q) m = fmaxf(m, value(j, q));
-      m = fmaxf(m, __shfl_xor(m, 32));
-      m = m == -INFINITY ? 0.f : m;
-      const float shift = -m * kLog2e;
-      float s[4] = {};
-#pragma unroll
-      for (int j = 0; j < C::NBN; ++j)
-#pragma unroll
-        for (int q = 0; q < 16; ++q) s[q % 4] += __builtin_amdgcn_exp2f(fmaf(value(j, q), kLog2e, shift));
-      float sum = (s[0] + s[1]) + (s[2] + s[3]);
-      sum += __shfl_xor(sum, 32);
-      const int r = wm + 32 * i + (lane & 31);
-      const int64_t row = o.m0 + r;
-      if (r < o.rows) {
-        if (lane < 32) a.part[int64_t(a.strip + (o.n0 + wn) / C::WTN) * a.rows + row] = make_float2(m, sum);
-        const int label = a.label[row], t = label - a.first - int(o.n0) - wn;
-        if (label >= 0 && t >= 0 && t < min(C::WTN, o.cols - wn) && ((t >> 2) & 1) == lane >> 5) {
-          float z = 0.f;
-#pragma unroll
-          for (int j = 0; j < C::NBN; ++j)
-#pragma unroll
-            for (int q = 0; q < 16; ++q) z = t - 4 * (lane >> 5) == 32 * j + 8 * (q / 4) + q % 4 ? acc[i][j][q] : z;
-          a.logit[row] = z;
-        }
-      }
-    });
-  };
-  if (wn + C::WTN > o.cols)
-    piece(IntTag<1>{});
-  else
-    piece(IntTag<0>{});
-}
-
-// The gradient of a wave's piece of logits in its place: (exp(z - lse) - [target]) g,
-// 0 in rows without a target and past the last column.
-template <class C, typename E>
-__device__ __forceinline__ void grad_piece(const LossArgs& a, const Work<E>& o, f32x16 (&acc)[C::NBM][C::NBN], int wm,
-                                           int wn, int lane) {
-  const int left = o.cols - wn - 4 * (lane >> 5);
+  const int r0 = lane / S::LPR, c0 = lane % S::LPR * 8, count = o.cols - wn - c0;
+  const float* from = region + r0 * S::LD + c0;
+  float* to = region + (lane & 31) * S::LD + 4 * (lane >> 5);
+  const bool ragged = wn + C::WTN > o.cols;
+  float2* part = a.part + int64_t(a.strip + (o.n0 + wn) / C::WTN) * a.rows + o.m0;
   static_for<C::NBM>([&](auto it) {
     constexpr int i = decltype(it)::value;
-    const int64_t row = o.m0 + min(wm + 32 * i + (lane & 31), o.rows - 1);
-    const int label = a.label[row], t = label - a.first - int(o.n0) - wn - 4 * (lane >> 5);
-    const float lse = a.lse[row], g = a.grad[row];
+    // the targets' places in the strip, of row `lane` of the 32
+    const int row = wm + 32 * i + (lane & 31);
+    const int label = row < o.rows ? a.label[o.m0 + row] : -1;
+    const int place = label >= 0 ? label - a.first - int(o.n0) - wn : -1;
+    stage_rows<C, i>(acc, to);
+    if (lane < 32 && place >= 0 && place < min(C::WTN, o.cols - wn))
+      a.logit[o.m0 + row] = region[lane * S::LD + place];
+#pragma unroll 2
+    for (int k = 0; k < 32 / S::RPI; ++k) {
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(from + k * S::RPI * S::LD);
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(from + k * S::RPI * S::LD + 4);
+      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      if (ragged) {
 #pragma unroll
-    for (int j = 0; j < C::NBN; ++j)
+        for (int e = 0; e < 8; ++e) v[e] = e < count ? v[e] : -INFINITY;
+      }
+      const auto larger = [](float x, float y) { return fmaxf(x, y); };
+      float m = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+      m = over_row<S::LPR>(m, larger);
+      m = m == -INFINITY ? 0.f : m;
+      const float shift = -m * kLog2e;
+      float e[8];
 #pragma unroll
-      for (int q = 0; q < 16; ++q) acc[i][j][q] = __expf(acc[i][j][q] - lse);
-    if (__any(label >= 0 && t >= 0 && t < C::WTN)) {
-      const int at = label >= 0 ? t : -1;
-#pragma unroll
-      for (int j = 0; j < C::NBN; ++j)
-#pragma unroll
-        for (int q = 0; q < 16; ++q) acc[i][j][q] -= at == 32 * j + 8 * (q / 4) + q % 4 ? 1.f : 0.f;
-    }
-#pragma unroll
-    for (int j = 0; j < C::NBN; ++j)
-#pragma unroll
-      for (int q = 0; q < 16; ++q) acc[i][j][q] *= g;
-    if (__any(label < 0)) {
-#pragma unroll
-      for (int j = 0; j < C::NBN; ++j)
-#pragma unroll
-        for (int q = 0; q < 16; ++q) acc[i][j][q] = label < 0 ? 0.f : acc[i][j][q];
-    }
-    if (wn + C::WTN > o.cols) {
-#pragma unroll
-      for (int j = 0; j < C::NBN; ++j)
-#pragma unroll
-        for (int q = 0; q < 16; ++q) acc[i][j][q] = 32 * j + 8 * (q / 4) + q % 4 >= left ? 0.f : acc[i][j][q];
+      for (int q = 0; q < 8; ++q) e[q] = __builtin_amdgcn_exp2f(fmaf(v[q], kLog2e, shift));
+      float sum = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+      sum = over_row<S::LPR>(sum, [](float x, float y) { return x + y; });
+      const int r = wm + 32 * i + r0 + k * S::RPI;
+      if (c0 == 0 && r < o.rows) part[r] = make_float2(m, sum);
     }
   });
 }
+
+// The gradient of a piece of logits: (exp(z - lse) - [target]) g, 0 in rows without
+// a target and past the last column.
+template <typename E>
+struct GradOf {
+  const LossArgs& a;
+  const Work<E>& o;
+  int cols, wm, wn;   // cols: o's, before they are rounded up
+  template <class C>
+  __device__ __forceinline__ void rows(int i, float* region, int lane) const {
+    if (lane >= 32) return;
+    const int64_t row = o.m0 + min(wm + 32 * i + lane, o.rows - 1);
+    const int label = a.label[row];
+    const int place = label >= 0 ? label - a.first - int(o.n0) - wn : -1;
+    *reinterpret_cast<f32x4*>(region + lane * Staging<C>::LD + C::WTN) =
+        f32x4{a.lse[row], a.grad[row], __builtin_bit_cast(float, place), label >= 0 ? 1.f : 0.f};
+  }
+  template <class C>
+  __device__ __forceinline__ void columns(float (&v)[8], const float* row, int c) const {
+    const f32x4 r = *reinterpret_cast<const f32x4*>(row);
+    const int at = __builtin_bit_cast(int, float(r[2])) - c, count = cols - wn - c;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float p = __expf(v[e] - r[0]);
+      v[e] = (at == e ? p - 1.f : p) * r[1];
+      v[e] = r[3] != 0.f && e < count ? v[e] : 0.f;
+    }
+  }
+};
 
 // What becomes of a tile: C with bias, activation and residual; C as it is; and, of
 // a product that is a piece of logits, the strips' sums, their gradient; C times a
@@ -654,20 +677,14 @@ __global__ __launch_bounds__(256, (Tile<E, TM, TN, U>::RING > 80 * 1024 ? 1 : 2)
     static_assert(4 * Staging<C>::BYTES <= C::RING, "the waves' parts of the ring");
     float* const region = reinterpret_cast<float*>(lds + wid * Staging<C>::BYTES);
     if constexpr (EP == EP_STRIP) {
-      strip_piece<C>(extra, w, acc, wm, wn, lane);
+      strip_piece<C>(extra, w, acc, region, wm, wn, lane);
     } else if constexpr (EP == EP_GRAD) {
-      grad_piece<C>(extra, w, acc, wm, wn, lane);
+      const GradOf<E> op{extra, w, w.cols, wm, wn};
       w.cols = (w.cols + 7) & ~7;   // (dz has room for whole groups of 8)
-      store_piece<C, E, E, MUON_ACT_NONE, false, false>(p, w.c, p.ldc, w, acc, region, wm, wn, lane);
+      store_piece<C, E, E, MUON_ACT_NONE, false, false, false>(p, w.c, p.ldc, w, acc, region, wm, wn, lane, op);
+    } else if constexpr (EP == EP_SCALE) {
+      store_tile<C, E, false>(p, w, acc, region, wm, wn, lane, Scaled(*extra));
     } else {
-      if constexpr (EP == EP_SCALE) {
-        const float f = *extra;
-        static_for<C::NBM * C::NBN>([&](auto ij) {
-          constexpr int i = decltype(ij)::value / C::NBN, j = decltype(ij)::value % C::NBN;
-#pragma unroll
-          for (int q = 0; q < 16; ++q) acc[i][j][q] *= f;
-        });
-      }
       store_tile<C, E, EP == EP_LINEAR>(p, w, acc, region, wm, wn, lane);
     }
     if (!more) break;
