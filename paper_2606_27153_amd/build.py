@@ -1,6 +1,7 @@
 """Builds libmuon_mi355x.so (the optimizer), libmuon_layers.so (the layer
-operators) and libmuon_diag.so (a matrix-core ceiling probe the bench reports as
-context) for gfx950 with hipcc, in-tree, no JIT cache.
+operators), libmuon_adamw.so (the AdamW step) and libmuon_diag.so (a matrix-core
+ceiling probe the bench reports as context) for gfx950 with hipcc, in-tree, no JIT
+cache.
 
 Usage: python -m paper_2606_27153_amd.build [-v]
 """
@@ -32,6 +33,8 @@ LAYER_SOURCES = ["layers/layers_api.cpp", "layers/mm_simple.hip", "layers/mm_til
                  "layers/tokens_api.cpp", "layers/routing.hip", "layers/embedding.hip", "layers/loss.hip",
                  "layers/mm_loss_256_bf16.hip", "layers/mm_loss_128x256_bf16.hip", "layers/mm_loss_128_bf16.hip",
                  "layers/mm_loss_64_bf16.hip", "layers/mm_loss_128_f32.hip", "layers/mm_loss_64_f32.hip"]
+ADAMW_SOURCES = ["adamw/adamw_api.cpp", "adamw/adamw.hip"]
+ADAMW_LIB_PATH = os.path.join(PKG, "libmuon_adamw.so")
 LAYER_LIB_PATH = os.path.join(PKG, "libmuon_layers.so")
 DIAG_SOURCES = ["diag/mfma_ceiling.hip"]
 DIAG_LIB_PATH = os.path.join(PKG, "libmuon_diag.so")
@@ -78,7 +81,8 @@ def _link(objs, path: str, verbose: bool) -> None:
 
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
-    parts = ((SOURCES, LIB_PATH), (LAYER_SOURCES, LAYER_LIB_PATH), (DIAG_SOURCES, DIAG_LIB_PATH))
+    parts = ((SOURCES, LIB_PATH), (LAYER_SOURCES, LAYER_LIB_PATH), (ADAMW_SOURCES, ADAMW_LIB_PATH),
+             (DIAG_SOURCES, DIAG_LIB_PATH))
     srcs = [s for sources, _ in parts for s in sources]
     with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 4)) as ex:
         objs = dict(zip(srcs, ex.map(lambda s: _compile(s, verbose), srcs)))
