@@ -163,12 +163,13 @@ MUON_API muon_status muon_embedding_backward(const void* dy, int64_t lddy, const
                                              void* hip_stream);
 
 /* Workspace bytes of muon_embedding_backward. */
-MUON_API muon_status muon_embedding_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes);
+MUON_API muon_status muon_embedding_workspace_bytes(int64_t rows, int64_t vocab, int64_t cols, size_t* bytes);
 
 /* A router's choices ids[tokens][top] sorted by expert, in their own order within
  * each: offsets (experts + 1) as muon_grouped_linear_* take them; position
  * (tokens x top), each choice's row among the sorted, -1 if it names no expert;
- * source (tokens * top), each row's choice t * top + j, -1 behind the last.
+ * source (tokens * top), each row's choice t * top + j; behind the last, ~ (t * top
+ * + j) of the choices of no expert.
  * tokens * top is at most 2^30, top and experts at most MUON_GROUPED_MAX_EXPERTS. */
 MUON_API muon_status muon_sort_by_expert(const void* ids, int32_t id_bytes, int64_t tokens, int32_t top,
                                          int32_t experts, int32_t* offsets, int32_t* position, int32_t* source,
@@ -177,12 +178,12 @@ MUON_API muon_status muon_sort_by_expert(const void* ids, int32_t id_bytes, int6
 /* Workspace bytes of muon_sort_by_expert. */
 MUON_API muon_status muon_sort_by_expert_workspace_bytes(int64_t tokens, int32_t top, size_t* bytes);
 
-/* rows[position[t][j]] = x[t]; rows from offsets[experts] on get 0.  position and
- * offsets are those of muon_sort_by_expert; a position outside [0, tokens * top) is
- * taken as -1. */
-MUON_API muon_status muon_dispatch_forward(const void* x, int64_t ldx, const int32_t* position, const int32_t* offsets,
-                                           int32_t experts, void* rows, int64_t ldr, int64_t tokens, int32_t top,
-                                           int64_t cols, int32_t dtype, void* hip_stream);
+/* rows[r] = x[source[r] / top], 0 where source[r] is negative.  position and source
+ * are those of muon_sort_by_expert, here and below; a value that it would not give
+ * stands for no row and no choice. */
+MUON_API muon_status muon_dispatch_forward(const void* x, int64_t ldx, const int32_t* source, void* rows, int64_t ldr,
+                                           int64_t tokens, int32_t top, int64_t cols, int32_t dtype,
+                                           void* hip_stream);
 
 /* dx[t] = the sum of drows[position[t][j]] over j. */
 MUON_API muon_status muon_dispatch_backward(const void* drows, int64_t ldr, const int32_t* position, void* dx,
@@ -197,15 +198,14 @@ MUON_API muon_status muon_combine_forward(const void* rows, int64_t ldr, const v
                                           int64_t ldy, int64_t tokens, int32_t top, int64_t cols, int32_t dtype,
                                           void* hip_stream);
 
-/* drows[position[t][j]] = weights[t][j] dy[t] (0 from offsets[experts] on);
- * dweights[t][j] = <dy[t], rows[position[t][j]]> (0 for a choice of no expert).
- * drows and dweights may be NULL; rows is read only for dweights.  The residual's
- * gradient is dy itself. */
+/* drows[r] = weights[s] dy[s / top] for s = source[r], 0 where it is negative;
+ * dweights[s] = <dy[s / top], rows[r]>, 0 for a choice of no expert.  drows and
+ * dweights may be NULL; rows is read only for dweights.  The residual's gradient is dy
+ * itself. */
 MUON_API muon_status muon_combine_backward(const void* dy, int64_t lddy, const void* rows, int64_t ldr,
-                                           const void* weights, int32_t weight_dtype, const int32_t* position,
-                                           const int32_t* offsets, int32_t experts, void* drows, int64_t lddr,
-                                           void* dweights, int64_t tokens, int32_t top, int64_t cols, int32_t dtype,
-                                           void* hip_stream);
+                                           const void* weights, int32_t weight_dtype, const int32_t* source,
+                                           void* drows, int64_t lddr, void* dweights, int64_t tokens, int32_t top,
+                                           int64_t cols, int32_t dtype, void* hip_stream);
 
 typedef enum muon_loss_reduction {
   MUON_LOSS_ROWS = 0,  /* a loss for every row */

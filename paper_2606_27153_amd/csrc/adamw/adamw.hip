@@ -1,8 +1,7 @@
 // The AdamW step over many tensors: one launch for up to 56 of them.
 //
-// A workgroup has 4096 elements of one tensor, which it finds by its number; a
-// lane has 8 neighbours at a time, so that every access is 8 to 32 bytes.  Each byte is
-// moved once: 22 an element with bf16 parameters and gradients and fp32 states, 10
+// A workgroup has 4096 elements of one tensor, which it finds by its number.  Each
+// byte is moved once: 22 an element with bf16 parameters and gradients and fp32 states, 10
 // with states in 8 bits.
 //
 // States in 8 bits: 32 lanes have a block of 256 elements.  What is rounded is the
@@ -14,59 +13,60 @@ namespace muon {
 namespace adamw {
 namespace {
 
-template <typename E>
-struct __attribute__((packed, aligned(sizeof(E)))) Packed8 {
-  E v[8];
+// N neighbours at any alignment, of which the first n exist; WHOLE: all of them, which
+// leaves no branch around a load (it would end in a wait for it).
+template <typename E, int N>
+struct __attribute__((packed, aligned(sizeof(E)))) Packed {
+  E v[N];
 };
-template <typename E>
-__device__ __forceinline__ void load8(const E* p, int64_t n, float (&v)[8]) {
-  if (n >= 8) {
-    const Packed8<E> x = *reinterpret_cast<const Packed8<E>*>(p);
+template <bool WHOLE, typename E, int N>
+__device__ __forceinline__ void load(const E* p, int64_t n, float (&v)[N]) {
+  if (WHOLE || n >= N) {
+    const Packed<E, N> x = *reinterpret_cast<const Packed<E, N>*>(p);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = float(x.v[e]);
+    for (int e = 0; e < N; ++e) v[e] = float(x.v[e]);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n ? float(p[e]) : 0.f;
+    for (int e = 0; e < N; ++e) v[e] = e < n ? float(p[e]) : 0.f;
   }
 }
-template <typename E>
-__device__ __forceinline__ void store8(E* p, int64_t n, const float (&v)[8]) {
-  if (n >= 8) {
-    Packed8<E> x;
+template <bool WHOLE, typename E, int N>
+__device__ __forceinline__ void store(E* p, int64_t n, const float (&v)[N]) {
+  if (WHOLE || n >= N) {
+    Packed<E, N> x;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x.v[e] = E(v[e]);
-    *reinterpret_cast<Packed8<E>*>(p) = x;
+    for (int e = 0; e < N; ++e) x.v[e] = E(v[e]);
+    *reinterpret_cast<Packed<E, N>*>(p) = x;
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < N; ++e)
       if (e < n) p[e] = E(v[e]);
   }
 }
+// 8 codes, element e's in bits 8 (e % 4) of word e / 4.
 struct Codes {
-  uint8_t c[8];
+  uint32_t w[2];
+  __device__ __forceinline__ uint32_t operator[](int e) const { return w[e / 4] >> (8 * (e % 4)) & 255; }
 };
+struct __attribute__((packed, aligned(1))) PackedCodes {
+  Codes c;
+};
+template <bool WHOLE>
 __device__ __forceinline__ Codes load_codes(const uint8_t* p, int64_t n) {
-  Codes x;
-  if (n >= 8) {
-    const Packed8<uint8_t> y = *reinterpret_cast<const Packed8<uint8_t>*>(p);
+  if (WHOLE || n >= 8) return reinterpret_cast<const PackedCodes*>(p)->c;
+  Codes x{};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x.c[e] = y.v[e];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x.c[e] = e < n ? p[e] : 0;
-  }
+  for (int e = 0; e < 8; ++e) x.w[e / 4] |= (e < n ? uint32_t(p[e]) : 0) << (8 * (e % 4));
   return x;
 }
+template <bool WHOLE>
 __device__ __forceinline__ void store_codes(uint8_t* p, int64_t n, const Codes& x) {
-  if (n >= 8) {
-    Packed8<uint8_t> y;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y.v[e] = x.c[e];
-    *reinterpret_cast<Packed8<uint8_t>*>(p) = y;
+  if (WHOLE || n >= 8) {
+    reinterpret_cast<PackedCodes*>(p)->c = x;
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (e < n) p[e] = x.c[e];
+      if (e < n) p[e] = uint8_t(x[e]);
   }
 }
 
@@ -89,12 +89,12 @@ __device__ __forceinline__ int base_of(uint32_t largest) {
   return min(max(int(largest >> 20) + 1 - TOP, 0), 2047 - TOP);
 }
 template <bool SIGNED>
-__device__ __forceinline__ uint8_t encode(float v, int base, uint32_t add) {
+__device__ __forceinline__ uint32_t encode(float v, int base, uint32_t add) {
   constexpr int TOP = SIGNED ? 127 : 255;
   const uint32_t all = __builtin_bit_cast(uint32_t, v), bits = all & 0x7fffffffu;
   const int low = SIGNED ? 0 : int(bits != 0);
   const int size = max(min(int((bits + add) >> 20) - base, TOP), low);
-  return uint8_t(SIGNED && size ? size | (all >> 31 << 7) : size);
+  return SIGNED && size ? size | (all >> 31 << 7) : size;
 }
 
 // Products and sums that stay apart.
@@ -117,101 +117,149 @@ __device__ __forceinline__ int find_tensor(const Args& a, int block) {
   return lo;
 }
 
-template <typename P, typename G, int BITS>
-__global__ __launch_bounds__(256) void step_kernel(Args a) {
+// An element's averages and parameter.
+__device__ __forceinline__ void update(const Args& a, const Tensor& t, float g, float& w, float& m, float& v) {
+  m = average(m, a.b1, a.c1, g);
+  v = average(v, a.b2, a.c2, g * g);
+  w = fmaf(-t.step, m / fmaf(sqrtf(v), t.scale, a.eps), w * a.keep);
+}
+
+// fp32 states: a lane has 4 neighbours, 16 bytes of each average.
+template <bool WHOLE, typename P, typename G>
+__device__ __forceinline__ void step32(const Args& a, const Tensor& t, int64_t start) {
+  constexpr int N = 4, U = 2;
+  for (int c = 0; c < kChunk; c += 256 * N * U) {
+    float w[U][N], d[U][N], m[U][N], v[U][N];
+    const int64_t i = start + c + threadIdx.x * N;
+    if (!WHOLE && i >= t.n) return;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t k = i + u * 256 * N, n = t.n - k;
+      load<WHOLE>(static_cast<const P*>(t.p) + k, n, w[u]);
+      load<WHOLE>(static_cast<const G*>(t.g) + k, n, d[u]);
+      load<WHOLE>(static_cast<const float*>(t.m) + k, n, m[u]);
+      load<WHOLE>(static_cast<const float*>(t.v) + k, n, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t k = i + u * 256 * N, n = t.n - k;
+#pragma unroll
+      for (int e = 0; e < N; ++e) update(a, t, d[u][e], w[u][e], m[u][e], v[u][e]);
+      store<WHOLE>(static_cast<P*>(t.p) + k, n, w[u]);
+      store<WHOLE>(static_cast<float*>(t.m) + k, n, m[u]);
+      store<WHOLE>(static_cast<float*>(t.v) + k, n, v[u]);
+    }
+  }
+}
+
+template <typename P, typename G>
+__global__ __launch_bounds__(256) void step32_kernel(Args a) {
   const Tensor& t = a.t[find_tensor(a, blockIdx.x)];
   const int64_t start = int64_t(int(blockIdx.x) - t.first) * kChunk;
-  P* p = static_cast<P*>(t.p);
-  const G* g = static_cast<const G*>(t.g);
+  if (start + kChunk <= t.n)
+    step32<true, P, G>(a, t, start);
+  else
+    step32<false, P, G>(a, t, start);
+}
+
+// States in 8 bits: 32 lanes have a block of 256 elements; all of them stay for its
+// maximum, those past the end with zeros.
+template <bool WHOLE, typename P, typename G>
+__device__ __forceinline__ void step8(const Args& a, const Tensor& t, int64_t start) {
   uint32_t key = t.key;
   if (start >> 32) key = mix(key + uint32_t(start >> 32));   // (a chunk does not cross a multiple of 2^32)
 #pragma unroll
   for (int u = 0; u < kChunk / 2048; ++u) {
-    const int64_t i = start + u * 2048 + threadIdx.x * 8, left = t.n - i;
-    // (all lanes of a block stay for its maximum; those past the end have zeros)
-    if (BITS == 32 && left <= 0) return;
-    const int64_t n = left < 0 ? 0 : left;
+    const int64_t i = start + u * 2048 + threadIdx.x * 8, n = max(t.n - i, int64_t(0));
     float w[8], d[8], m[8], v[8];
-    load8(p + i, n, w);
-    load8(g + i, n, d);
+    load<WHOLE>(static_cast<const P*>(t.p) + i, n, w);
+    load<WHOLE>(static_cast<const G*>(t.g) + i, n, d);
+    const Codes om = load_codes<WHOLE>(static_cast<const uint8_t*>(t.m) + i, n);
+    const Codes ov = load_codes<WHOLE>(static_cast<const uint8_t*>(t.v) + i, n);
     int16_t* base = t.bases + i / kBlock * 2;
-    if constexpr (BITS == 32) {
-      load8(static_cast<const float*>(t.m) + i, n, m);
-      load8(static_cast<const float*>(t.v) + i, n, v);
-    } else {
-      const Codes cm = load_codes(static_cast<const uint8_t*>(t.m) + i, n);
-      const Codes cv = load_codes(static_cast<const uint8_t*>(t.v) + i, n);
-      const int bm = n ? base[0] : 0, bv = n ? base[1] : 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        m[e] = decode<true>(cm.c[e], bm);
-        v[e] = decode<false>(cv.c[e], bv);
-      }
-    }
+    const int obm = WHOLE || n ? base[0] : 0, obv = WHOLE || n ? base[1] : 0;
+    uint32_t top_m = 0, top_v = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      m[e] = average(m[e], a.b1, a.c1, d[e]);
-      v[e] = average(v[e], a.b2, a.c2, d[e] * d[e]);
-      const float q = m[e] / fmaf(sqrtf(v[e]), t.scale, a.eps);
-      w[e] = fmaf(-t.step, q, w[e] * a.keep);
+      m[e] = decode<true>(om[e], obm);
+      v[e] = decode<false>(ov[e], obv);
+      update(a, t, d[e], w[e], m[e], v[e]);
+      top_m = max(top_m, __builtin_bit_cast(uint32_t, m[e]) & 0x7fffffffu);
+      top_v = max(top_v, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
     }
-    store8(p + i, n, w);
-    if constexpr (BITS == 32) {
-      store8(static_cast<float*>(t.m) + i, n, m);
-      store8(static_cast<float*>(t.v) + i, n, v);
-    } else {
-      uint32_t top_m = 0, top_v = 0;
+    store<WHOLE>(static_cast<P*>(t.p) + i, n, w);
+    const int bm = base_of<true>(block_max(top_m)), bv = base_of<false>(block_max(top_v));
+    Codes cm{}, cv{};
+    uint32_t at = uint32_t(i) * 0x9E3779B1u;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        top_m = max(top_m, __builtin_bit_cast(uint32_t, m[e]) & 0x7fffffffu);
-        top_v = max(top_v, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
-      }
-      const int bm = base_of<true>(block_max(top_m)), bv = base_of<false>(block_max(top_v));
-      Codes cm, cv;
-      uint32_t at = uint32_t(i) * 0x9E3779B1u;
-#pragma unroll
-      for (int e = 0; e < 8; ++e, at += 0x9E3779B1u) {
-        const uint32_t h = mix(at ^ key);
-        cm.c[e] = encode<true>(m[e], bm, (h & 0xffff) << 4);
-        cv.c[e] = encode<false>(v[e], bv, h >> 16 << 4);
-      }
-      store_codes(static_cast<uint8_t*>(t.m) + i, n, cm);
-      store_codes(static_cast<uint8_t*>(t.v) + i, n, cv);
-      if ((threadIdx.x & 31) == 0 && n) {
-        base[0] = int16_t(bm);
-        base[1] = int16_t(bv);
-      }
+    for (int e = 0; e < 8; ++e, at += 0x9E3779B1u) {
+      const uint32_t h = mix(at ^ key);
+      cm.w[e / 4] |= encode<true>(m[e], bm, (h & 0xffff) << 4) << (8 * (e % 4));
+      cv.w[e / 4] |= encode<false>(v[e], bv, h >> 16 << 4) << (8 * (e % 4));
     }
+    store_codes<WHOLE>(static_cast<uint8_t*>(t.m) + i, n, cm);
+    store_codes<WHOLE>(static_cast<uint8_t*>(t.v) + i, n, cv);
+    if ((threadIdx.x & 31) == 0 && n) {
+      base[0] = int16_t(bm);
+      base[1] = int16_t(bv);
+    }
+  }
+}
+
+template <typename P, typename G>
+__global__ __launch_bounds__(256) void step8_kernel(Args a) {
+  const Tensor& t = a.t[find_tensor(a, blockIdx.x)];
+  const int64_t start = int64_t(int(blockIdx.x) - t.first) * kChunk;
+  if (start + kChunk <= t.n)
+    step8<true, P, G>(a, t, start);
+  else
+    step8<false, P, G>(a, t, start);
+}
+
+template <bool WHOLE>
+__device__ __forceinline__ void values(const uint8_t* m, const uint8_t* v, const int16_t* bases, int64_t start,
+                                       int64_t count, __bf16* mo, __bf16* vo) {
+  constexpr int U = kChunk / 2048;
+  Codes cm[U]{}, cv[U]{};
+  int bm[U], bv[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = start + u * 2048 + threadIdx.x * 8, n = max(count - i, int64_t(0));
+    const int16_t* base = bases + (WHOLE || n ? i : 0) / kBlock * 2;
+    bm[u] = base[0];
+    bv[u] = base[1];
+    if (mo) cm[u] = load_codes<WHOLE>(m + i, n);
+    if (vo) cv[u] = load_codes<WHOLE>(v + i, n);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = start + u * 2048 + threadIdx.x * 8, n = max(count - i, int64_t(0));
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = decode<true>(cm[u][e], bm[u]);
+    if (mo) store<WHOLE>(mo + i, n, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = decode<false>(cv[u][e], bv[u]);
+    if (vo) store<WHOLE>(vo + i, n, x);
   }
 }
 
 __global__ __launch_bounds__(256) void values_kernel(const uint8_t* m, const uint8_t* v, const int16_t* bases,
                                                      int64_t count, __bf16* mo, __bf16* vo) {
-  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 8, n = count - i;
-  if (n <= 0) return;
-  const int16_t* base = bases + i / kBlock * 2;
-  float x[8];
-  if (mo) {
-    const Codes c = load_codes(m + i, n);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = decode<true>(c.c[e], base[0]);
-    store8(mo + i, n, x);
-  }
-  if (vo) {
-    const Codes c = load_codes(v + i, n);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = decode<false>(c.c[e], base[1]);
-    store8(vo + i, n, x);
-  }
+  const int64_t start = int64_t(blockIdx.x) * kChunk;
+  if (start + kChunk <= count)
+    values<true>(m, v, bases, start, count, mo, vo);
+  else
+    values<false>(m, v, bases, start, count, mo, vo);
 }
 
 template <typename P, typename G>
 hipError_t launch(int bits, const Args& a, int64_t blocks, hipStream_t st) {
   const dim3 g{unsigned(blocks)}, b{256};
   if (bits == 32)
-    hipLaunchKernelGGL((step_kernel<P, G, 32>), g, b, 0, st, a);
+    hipLaunchKernelGGL((step32_kernel<P, G>), g, b, 0, st, a);
   else
-    hipLaunchKernelGGL((step_kernel<P, G, 8>), g, b, 0, st, a);
+    hipLaunchKernelGGL((step8_kernel<P, G>), g, b, 0, st, a);
   return hipGetLastError();
 }
 
@@ -225,7 +273,7 @@ hipError_t launch_step(bool param_bf16, bool grad_bf16, int bits, const Args& a,
 
 hipError_t launch_values(const uint8_t* m, const uint8_t* v, const int16_t* bases, int64_t n, void* mo, void* vo,
                          hipStream_t st) {
-  const int64_t blocks = (n + 2047) / 2048;
+  const int64_t blocks = (n + kChunk - 1) / kChunk;
   hipLaunchKernelGGL(values_kernel, dim3{unsigned(blocks)}, dim3{256}, 0, st, m, v, bases, n, static_cast<__bf16*>(mo),
                      static_cast<__bf16*>(vo));
   return hipGetLastError();

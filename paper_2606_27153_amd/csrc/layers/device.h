@@ -144,6 +144,17 @@ __device__ __forceinline__ void store8(E* p, int n, const float (&v)[8]) {
   }
 }
 
+// The same where all 8 exist (WHOLE): no branch around a load, which would end in a
+// wait for it.
+template <bool WHOLE, typename E>
+__device__ __forceinline__ void load_8(const E* p, int n, float (&v)[8]) {
+  load8(p, WHOLE ? 8 : n, v);
+}
+template <bool WHOLE, typename E>
+__device__ __forceinline__ void store_8(E* p, int n, const float (&v)[8]) {
+  store8(p, WHOLE ? 8 : n, v);
+}
+
 // A plain product takes no table.
 struct NoTable {};
 template <int GROUP>

@@ -8,7 +8,7 @@
 // over a run of the sorted list, in the list's order: no atomics, the result does
 // not depend on timing.  Every row of dW is written once, by the block that has
 // it: the sum of its run, or zeros (most of a large table).  A frequent token's run
-// can be a good part of the list: groups of 64 places that lie inside one run are
+// can be a good part of the list: groups of 16 places that lie inside one run are
 // summed first, by blocks of their own, and the row adds up the groups.
 // Bound by memory: dy read once, dW written once.
 #include "sort.h"
@@ -42,27 +42,26 @@ struct TokenJob {
   }
 };
 
-template <typename E>
+template <typename E, bool WHOLE>
 __global__ __launch_bounds__(256) void lookup_kernel(EmbeddingArgs a) {
   const int chunks = (a.cols + 7) / 8;
   const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, r = i / chunks;
   if (r >= a.rows) return;
   const int c = int(i - r * chunks) * 8, n = min(8, a.cols - c);
   const int64_t id = id_at(a.ids, a.id_bytes, r);
-  float v[8] = {};
-  if (id >= 0 && id < a.vocab) {
-    load8(static_cast<const E*>(a.w) + id * a.ldw + c, n, v);
+  const bool live = id >= 0 && id < a.vocab;
+  float v[8];
+  load_8<WHOLE>(static_cast<const E*>(a.w) + (live ? id : 0) * a.ldw + c, n, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= a.scale;
-  }
-  store8(static_cast<E*>(a.y) + r * a.ldy + c, n, v);
+  for (int e = 0; e < 8; ++e) v[e] = live ? v[e] * a.scale : 0.f;
+  store_8<WHOLE>(static_cast<E*>(a.y) + r * a.ldy + c, n, v);
 }
 
-constexpr int kRun = 64;    // places of a group
+constexpr int kRun = 16;    // places of a group
 constexpr int kRows = 16;   // table rows of a block
 
 // v[0..7] += the gradients of places lo .. hi - 1, in order, 4 in flight.
-template <typename E>
+template <typename E, bool WHOLE>
 __device__ __forceinline__ void add_run(const EmbeddingArgs& a, int lo, int hi, int c, int n, float (&v)[8]) {
   const E* dy = static_cast<const E*>(a.dy) + c;
   for (int p = lo; p < hi; p += 4) {
@@ -71,33 +70,35 @@ __device__ __forceinline__ void add_run(const EmbeddingArgs& a, int lo, int hi, 
 #pragma unroll
     for (int k = 0; k < 4; ++k) row[k] = a.index[min(p + k, hi - 1)];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) load8(dy + row[k] * a.lddy, n, x[k]);
+    for (int k = 0; k < 4; ++k) load_8<WHOLE>(dy + row[k] * a.lddy, n, x[k]);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += p + k < hi ? x[k][e] : 0.f;
   }
 }
-
-// The sums of the groups inside one run; the others' places in `part` stay as they are.
-template <typename E>
-__global__ __launch_bounds__(256) void group_kernel(EmbeddingArgs a) {
-  const int first = blockIdx.x * kRun;
-  const int key = a.keys[first];
-  if (key >= a.vocab || a.keys[first + kRun - 1] != key) return;
-  const int c = (blockIdx.y * 256 + threadIdx.x) * 8, n = min(8, a.cols - c);
-  if (n <= 0) return;
-  float v[8] = {};
-  add_run<E>(a, first, first + kRun, c, n, v);
-  store8(a.part + int64_t(blockIdx.x) * a.cols + c, n, v);
+// v[0..7] += the sums of groups g0 .. g1 - 1, 8 in flight.
+template <bool WHOLE>
+__device__ __forceinline__ void add_groups(const EmbeddingArgs& a, int g0, int g1, int c, int n, float (&v)[8]) {
+  for (int g = g0; g < g1; g += 8) {
+    float x[8][8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) load_8<WHOLE>(a.part + int64_t(min(g + k, g1 - 1)) * a.cols + c, n, x[k]);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += g + k < g1 ? x[k][e] : 0.f;
+  }
 }
 
-template <typename E>
-__global__ __launch_bounds__(256) void table_grad_kernel(EmbeddingArgs a) {
-  __shared__ int32_t starts[kRows + 1];
-  const int64_t v0 = int64_t(blockIdx.x) * kRows;
-  if (threadIdx.x <= kRows) {   // where the runs begin: the first place of at least this token
-    const int64_t want = v0 + threadIdx.x;
+// Blocks y > 0: the sums of the groups of places inside one run (the others' places
+// in `part` stay as they are).  Blocks y = 0: where the tokens' runs begin, the first place
+// of at least that token.
+template <typename E, bool WHOLE>
+__global__ __launch_bounds__(256) void group_kernel(EmbeddingArgs a, int groups) {
+  if (blockIdx.y == 0) {
+    const int64_t want = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (want > a.vocab) return;
     int lo = 0, hi = a.rows;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
@@ -106,43 +107,69 @@ __global__ __launch_bounds__(256) void table_grad_kernel(EmbeddingArgs a) {
       else
         hi = mid;
     }
-    starts[threadIdx.x] = lo;
+    a.starts[want] = lo;
+    return;
   }
-  __syncthreads();
+  if (int(blockIdx.x) >= groups) return;
+  const int first = blockIdx.x * kRun;
+  const int key = a.keys[first];
+  if (key >= a.vocab || a.keys[first + kRun - 1] != key) return;
+  const int c = ((blockIdx.y - 1) * 256 + threadIdx.x) * 8, n = min(8, a.cols - c);
+  if (n <= 0) return;
+  float v[8] = {};
+  add_run<E, WHOLE>(a, first, first + kRun, c, n, v);
+  store_8<WHOLE>(a.part + int64_t(blockIdx.x) * a.cols + c, n, v);
+}
+
+// A thread has 8 columns of 16 table rows: those of no token first, which wait for
+// nothing but where the runs begin, then the others' sums.
+template <typename E, bool WHOLE>
+__global__ __launch_bounds__(256) void table_grad_kernel(EmbeddingArgs a) {
   const int chunks = (a.cols + 7) / 8;
-  const int rows = int(min(int64_t(kRows), a.vocab - v0));
-  for (int i = threadIdx.x; i < rows * chunks; i += 256) {
-    const int r = i / chunks, c = (i - r * chunks) * 8, n = min(8, a.cols - c);
-    const int lo = starts[r], hi = starts[r + 1];
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, v0 = i / chunks * kRows;
+  if (v0 >= a.vocab) return;
+  const int c = int(i % chunks) * 8, n = min(8, a.cols - c);
+  E* to = static_cast<E*>(a.dw) + v0 * a.lddw + c;
+  int start[kRows + 1];
+#pragma unroll
+  for (int r = 0; r <= kRows; ++r) start[r] = a.rows ? a.starts[min(v0 + r, int64_t(a.vocab))] : 0;
+  const float zero[8] = {};
+  uint32_t met = 0;
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    if (start[r] < start[r + 1])
+      met |= 1u << r;
+    else if (v0 + r < a.vocab)
+      store_8<WHOLE>(to + r * a.lddw, n, zero);
+  }
+  while (met) {
+    const int r = __builtin_ctz(met);
+    met &= met - 1;
+    const int lo = a.starts[v0 + r], hi = a.starts[v0 + r + 1];
     float v[8] = {};
     const int g0 = (lo + kRun - 1) / kRun, g1 = hi / kRun;
     if (g0 < g1) {
-      add_run<E>(a, lo, g0 * kRun, c, n, v);
-      for (int g = g0; g < g1; ++g) {
-        float x[8];
-        load8(a.part + int64_t(g) * a.cols + c, n, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += x[e];
-      }
-      add_run<E>(a, g1 * kRun, hi, c, n, v);
-    } else if (lo < hi) {
-      add_run<E>(a, lo, hi, c, n, v);
+      add_run<E, WHOLE>(a, lo, g0 * kRun, c, n, v);
+      add_groups<WHOLE>(a, g0, g1, c, n, v);
+      add_run<E, WHOLE>(a, g1 * kRun, hi, c, n, v);
+    } else {
+      add_run<E, WHOLE>(a, lo, hi, c, n, v);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= a.scale;
-    store8(static_cast<E*>(a.dw) + (v0 + r) * a.lddw + c, n, v);
+    store_8<WHOLE>(to + r * a.lddw, n, v);
   }
 }
 
-template <typename E>
+template <typename E, bool WHOLE>
 hipError_t forward(const EmbeddingArgs& a, hipStream_t st) {
   const int64_t blocks = (int64_t(a.rows) * ((a.cols + 7) / 8) + 255) / 256;
   if (blocks >= (int64_t(1) << 31)) return hipErrorInvalidConfiguration;
-  if (blocks) hipLaunchKernelGGL((lookup_kernel<E>), dim3{unsigned(blocks)}, dim3{256}, 0, st, a);
+  if (blocks) hipLaunchKernelGGL((lookup_kernel<E, WHOLE>), dim3{unsigned(blocks)}, dim3{256}, 0, st, a);
   return hipGetLastError();
 }
 
-template <typename E>
+template <typename E, bool WHOLE>
 hipError_t backward(EmbeddingArgs a, int32_t* const (&keys)[2], int32_t* const (&index)[2], int32_t* counts,
                     hipStream_t st) {
   int at = 0;
@@ -164,10 +191,14 @@ hipError_t backward(EmbeddingArgs a, int32_t* const (&keys)[2], int32_t* const (
   }
   a.keys = keys[at ^ 1];
   a.index = index[at ^ 1];
-  const int columns = (a.cols + 2047) / 2048;
-  if (a.rows >= kRun)
-    hipLaunchKernelGGL((group_kernel<E>), (dim3{unsigned(a.rows / kRun), unsigned(columns)}), dim3{256}, 0, st, a);
-  hipLaunchKernelGGL((table_grad_kernel<E>), dim3{unsigned((a.vocab + kRows - 1) / kRows)}, dim3{256}, 0, st, a);
+  if (a.rows) {
+    const int64_t groups = a.rows / kRun, starts = (int64_t(a.vocab) + 256) / 256;
+    const dim3 g{unsigned(groups > starts ? groups : starts), unsigned((a.cols + 2047) / 2048 + 1)};
+    hipLaunchKernelGGL((group_kernel<E, WHOLE>), g, dim3{256}, 0, st, a, int(groups));
+  }
+  const int64_t blocks = ((int64_t(a.vocab) + kRows - 1) / kRows * ((a.cols + 7) / 8) + 255) / 256;
+  if (blocks >= (int64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((table_grad_kernel<E, WHOLE>), dim3{unsigned(blocks)}, dim3{256}, 0, st, a);
   return hipGetLastError();
 }
 
@@ -175,12 +206,14 @@ size_t whole(size_t v) { return (v + 255) / 256 * 256; }
 
 }  // namespace
 
-size_t embedding_bytes(int64_t rows, int64_t cols) {
-  return 4 * whole(size_t(rows) * 4) + whole(sort_bytes(rows)) + whole(size_t(rows / kRun) * size_t(cols) * 4);
+size_t embedding_bytes(int64_t rows, int64_t vocab, int64_t cols) {
+  return 4 * whole(size_t(rows) * 4) + whole(sort_bytes(rows)) + whole((size_t(vocab) + 1) * 4) +
+         whole(size_t(rows / kRun) * size_t(cols) * 4);
 }
 
 hipError_t launch_embedding_forward(bool bf16, const EmbeddingArgs& a, hipStream_t st) {
-  return bf16 ? forward<__bf16>(a, st) : forward<float>(a, st);
+  if (a.cols % 8) return bf16 ? forward<__bf16, false>(a, st) : forward<float, false>(a, st);
+  return bf16 ? forward<__bf16, true>(a, st) : forward<float, true>(a, st);
 }
 
 hipError_t launch_embedding_backward(bool bf16, EmbeddingArgs a, void* workspace, hipStream_t st) {
@@ -189,8 +222,13 @@ hipError_t launch_embedding_backward(bool bf16, EmbeddingArgs a, void* workspace
   int32_t* const keys[2] = {reinterpret_cast<int32_t*>(p), reinterpret_cast<int32_t*>(p + step)};
   int32_t* const index[2] = {reinterpret_cast<int32_t*>(p + 2 * step), reinterpret_cast<int32_t*>(p + 3 * step)};
   int32_t* counts = reinterpret_cast<int32_t*>(p + 4 * step);
-  a.part = reinterpret_cast<float*>(p + 4 * step + whole(sort_bytes(a.rows)));
-  return bf16 ? backward<__bf16>(a, keys, index, counts, st) : backward<float>(a, keys, index, counts, st);
+  p += 4 * step + whole(sort_bytes(a.rows));
+  a.starts = reinterpret_cast<int32_t*>(p);
+  a.part = reinterpret_cast<float*>(p + whole((size_t(a.vocab) + 1) * 4));
+  if (a.cols % 8)
+    return bf16 ? backward<__bf16, false>(a, keys, index, counts, st)
+                : backward<float, false>(a, keys, index, counts, st);
+  return bf16 ? backward<__bf16, true>(a, keys, index, counts, st) : backward<float, true>(a, keys, index, counts, st);
 }
 
 }  // namespace layers

@@ -109,9 +109,9 @@ struct RouteArgs {
   void* drows;            // or NULL
   void* dweights;         // or NULL
   const int32_t* position;
-  const int32_t* offsets;
+  const int32_t* source;
   int64_t ldx, ldr, ldres, ldy, lddy, lddr;
-  int32_t tokens, top, experts, cols;
+  int32_t tokens, top, cols;
   int32_t wf32;           // weights and their gradients are fp32
 };
 enum RoutePass { ROUTE_DISPATCH, ROUTE_GATHER, ROUTE_COMBINE_GRAD };
@@ -124,6 +124,7 @@ struct EmbeddingArgs {
   void* dw;
   const int32_t* keys;    // backward: the tokens sorted, and where each was
   const int32_t* index;
+  int32_t* starts;        // vocab + 1: where each token's places begin
   float* part;            // sums of groups of places inside one token's run
   int64_t ldw, ldy, lddy, lddw;
   int32_t rows, cols, vocab, id_bytes;
@@ -161,7 +162,7 @@ hipError_t launch_expert_sort(const void* ids, int id_bytes, int64_t n, int expe
                               int32_t* position, int32_t* source, int32_t* counts, hipStream_t st);
 hipError_t launch_route(bool bf16, int pass, const RouteArgs& a, hipStream_t st);
 
-size_t embedding_bytes(int64_t rows, int64_t cols);
+size_t embedding_bytes(int64_t rows, int64_t vocab, int64_t cols);
 hipError_t launch_embedding_forward(bool bf16, const EmbeddingArgs& a, hipStream_t st);
 hipError_t launch_embedding_backward(bool bf16, EmbeddingArgs a, void* workspace, hipStream_t st);
 

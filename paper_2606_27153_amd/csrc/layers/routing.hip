@@ -7,9 +7,8 @@
 //   y[t] = r[t] + sum_j w[t, j] rows[position[t, j]]
 //   drows[position[t, j]] = w[t, j] dy[t],  dw[t, j] = <dy[t], rows[position[t, j]]>
 //
-// Every pass goes by token: what a token has is read once, what its choices have is
-// read or written in whole rows wherever they lie, so that each byte moves once.
-// A thread has 8 columns (16 bytes of bf16) of a token and goes over its choices.
+// What is a sum over a token's choices goes by token and gathers their rows; what
+// is made for each choice goes by row.  A thread has 8 columns (16 bytes of bf16) at a time.
 #include "sort.h"
 
 namespace muon {
@@ -20,7 +19,7 @@ struct ExpertJob {
   const void* ids;
   int32_t* offsets;    // experts + 1
   int32_t* position;   // n
-  int32_t* source;     // n: the choice of each row, -1 behind the last
+  int32_t* source;     // n: the choice of each row; behind the last, ~ those of no expert
   int32_t id_bytes, experts, bins, bits;
   __device__ __forceinline__ int digit(int i, int& key) const {
     const int64_t e = id_at(ids, id_bytes, i);
@@ -30,11 +29,9 @@ struct ExpertJob {
   __device__ __forceinline__ void put(int i, int, int d, int place) const {
     const bool live = d < experts;
     position[i] = live ? place : -1;
-    source[place] = live ? i : -1;
+    source[place] = live ? i : ~i;
   }
 };
-
-constexpr int kGroup = 4;   // choices whose loads are in flight together
 
 // A choice's row, -1 where it has none (or names one that does not exist).
 __device__ __forceinline__ int row_of(const int32_t* position, int64_t slot, int64_t rows) {
@@ -47,105 +44,109 @@ __device__ __forceinline__ float weight_of(const RouteArgs& a, int64_t slot) {
   return a.wf32 ? static_cast<const float*>(a.weights)[slot] : float(static_cast<const E*>(a.weights)[slot]);
 }
 
-// The thread's token and first column; false past the last.
-__device__ __forceinline__ bool token_chunk(const RouteArgs& a, int64_t& t, int& c, int& n) {
+// The thread's row (of `rows`) and first column; false past the last.
+__device__ __forceinline__ bool row_chunk(const RouteArgs& a, int64_t rows, int64_t& r, int& c, int& n) {
   const int chunks = (a.cols + 7) / 8;
   const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  t = i / chunks;
-  c = int(i - t * chunks) * 8;
+  r = i / chunks;
+  c = int(i - r * chunks) * 8;
   n = min(8, a.cols - c);
-  return t < a.tokens;
+  return r < rows;
 }
 
-template <typename E>
+// By row: the rows are written as they lie, the tokens' are read once for each of
+// their choices, mostly from the 256 MB cache.  (By token, each read once and stored to
+// its choices' rows, 16384 x 2048 tokens of 6 choices took 125 us.)
+template <typename E, bool WHOLE>
 __global__ __launch_bounds__(256) void dispatch_kernel(RouteArgs a) {
-  int64_t t;
+  int64_t r;
   int c, n;
-  if (!token_chunk(a, t, c, n)) return;
   const int64_t all = int64_t(a.tokens) * a.top;
-  const int live = min(max(a.offsets[a.experts], 0), int(all));
+  if (!row_chunk(a, all, r, c, n)) return;
+  const int slot = a.source[r];
   float v[8];
-  load8(static_cast<const E*>(a.x) + t * a.ldx + c, n, v);
-  const float zero[8] = {};
-  E* rows = static_cast<E*>(a.rows) + c;
-  for (int j = 0; j < a.top; ++j) {
-    const int64_t slot = t * a.top + j;
-    const int p = row_of(a.position, slot, all);
-    if (p >= 0) store8(rows + p * a.ldr, n, v);
-    if (slot >= live) store8(rows + slot * a.ldr, n, zero);   // rows behind the last expert's
-  }
+  const bool live = slot >= 0 && slot < all;
+  load_8<WHOLE>(static_cast<const E*>(a.x) + (live ? slot / a.top : 0) * a.ldx + c, n, v);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = live ? v[e] : 0.f;
+  store_8<WHOLE>(static_cast<E*>(a.rows) + r * a.ldr + c, n, v);
 }
 
 // y[t] = r[t] + sum_j w[t, j] rows[position[t, j]]; without weights, the gradient of
-// dispatch.
-template <typename E>
+// dispatch.  K choices' loads are in flight together.
+template <typename E, int K, bool WHOLE>
 __global__ __launch_bounds__(256) void gather_kernel(RouteArgs a) {
   int64_t t;
   int c, n;
-  if (!token_chunk(a, t, c, n)) return;
+  if (!row_chunk(a, a.tokens, t, c, n)) return;
   const int64_t all = int64_t(a.tokens) * a.top;
   const E* rows = static_cast<const E*>(a.rows) + c;
   float v[8] = {};
-  if (a.res) load8(static_cast<const E*>(a.res) + t * a.ldres + c, n, v);
-  for (int j = 0; j < a.top; j += kGroup) {
-    float x[kGroup][8], w[kGroup];
-    int p[kGroup];
+  if (a.res) load_8<WHOLE>(static_cast<const E*>(a.res) + t * a.ldres + c, n, v);
+  for (int j = 0; j < a.top; j += K) {
+    float x[K][8], w[K];
+    int p[K];
 #pragma unroll
-    for (int k = 0; k < kGroup; ++k) {
+    for (int k = 0; k < K; ++k) {
       const int64_t slot = t * a.top + min(j + k, a.top - 1);
       p[k] = row_of(a.position, slot, all);
       if (j + k >= a.top) p[k] = -1;
       w[k] = weight_of<E>(a, slot);
     }
 #pragma unroll
-    for (int k = 0; k < kGroup; ++k) load8(rows + max(p[k], 0) * a.ldr, n, x[k]);
+    for (int k = 0; k < K; ++k) load_8<WHOLE>(rows + max(p[k], 0) * a.ldr, n, x[k]);
 #pragma unroll
-    for (int k = 0; k < kGroup; ++k)
+    for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = p[k] >= 0 ? fmaf(w[k], x[k][e], v[e]) : v[e];
   }
-  store8(static_cast<E*>(a.y) + t * a.ldy + c, n, v);
+  store_8<WHOLE>(static_cast<E*>(a.y) + t * a.ldy + c, n, v);
 }
 
-// A wave per choice: its row's gradient, and the product of both rows for the
-// weight's.
-template <typename E>
+// A wave per row: its gradient, and the product of both rows for the weight's.  A row
+// behind the last expert's stands for a choice of no expert: both are 0.  Two chunks of
+// 512 columns are in flight.
+template <typename E, bool WHOLE>
 __global__ __launch_bounds__(256) void combine_grad_kernel(RouteArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t slot = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6), all = int64_t(a.tokens) * a.top;
-  if (slot >= all) return;
-  const int64_t t = slot / a.top;
-  const int p = row_of(a.position, slot, all);
-  const int live = min(max(a.offsets[a.experts], 0), int(all));
-  const float w = weight_of<E>(a, slot);
-  const E* dy = static_cast<const E*>(a.dy) + t * a.lddy;
-  const E* h = static_cast<const E*>(a.rows) + max(p, 0) * a.ldr;
-  E* dh = static_cast<E*>(a.drows);
+  const int64_t r = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6), all = int64_t(a.tokens) * a.top;
+  if (r >= all) return;
+  const int from = __builtin_amdgcn_readfirstlane(a.source[r]);
+  const int slot = from < 0 ? ~from : from;
+  const bool named = slot < all, live = from >= 0 && named;
+  const float w = live ? weight_of<E>(a, slot) : 0.f;
+  const E* dy = static_cast<const E*>(a.dy) + (live ? slot / a.top : 0) * a.lddy;
+  const E* h = a.dweights ? static_cast<const E*>(a.rows) + r * a.ldr : dy;
+  E* dh = a.drows ? static_cast<E*>(a.drows) + r * a.lddr : nullptr;
   float dot = 0.f;
-  for (int c = lane * 8; c < a.cols; c += 512) {
-    const int n = min(8, a.cols - c);
-    if (p >= 0) {
-      float g[8], x[8];
-      load8(dy + c, n, g);
-      if (a.dweights) {
-        load8(h + c, n, x);
+  for (int c = lane * 8; c < a.cols; c += 1024) {
+    const int n = min(8, a.cols - c), n2 = min(8, a.cols - c - 512);
+    const bool two = n2 > 0;
+    float g[2][8], x[2][8];
+    const int c2 = two ? c + 512 : c;
+    load_8<WHOLE>(dy + c, n, g[0]);
+    load_8<WHOLE>(h + c, n, x[0]);
+    load_8<WHOLE>(dy + c2, two ? n2 : n, g[1]);
+    load_8<WHOLE>(h + c2, two ? n2 : n, x[1]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) dot = fmaf(g[e], x[e], dot);
-      }
-      if (dh) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] *= w;
-        store8(dh + p * a.lddr + c, n, g);
-      }
+    for (int e = 0; e < 8; ++e) {
+      dot = fmaf(g[0][e], x[0][e], dot);
+      g[0][e] = live ? g[0][e] * w : 0.f;
     }
-    if (dh && slot >= live) {
-      const float zero[8] = {};
-      store8(dh + slot * a.lddr + c, n, zero);
+    if (dh) store_8<WHOLE>(dh + c, n, g[0]);
+    if (two) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        dot = fmaf(g[1][e], x[1][e], dot);
+        g[1][e] = live ? g[1][e] * w : 0.f;
+      }
+      if (dh) store_8<WHOLE>(dh + c2, n2, g[1]);
     }
   }
-  if (!a.dweights) return;
+  if (!a.dweights || !named) return;
 #pragma unroll
   for (int d = 32; d; d >>= 1) dot += __shfl_xor(dot, d);
+  if (!live) dot = 0.f;
   if (lane == 0) {
     if (a.wf32)
       static_cast<float*>(a.dweights)[slot] = dot;
@@ -159,17 +160,26 @@ bool grid_of(int64_t blocks, dim3& g) {
   return blocks < (int64_t(1) << 31);
 }
 
-template <typename E>
+template <typename E, bool WHOLE>
 hipError_t launch(int pass, const RouteArgs& a, hipStream_t st) {
-  const int64_t chunks = (int64_t(a.cols) + 7) / 8;
-  const int64_t blocks = pass == ROUTE_COMBINE_GRAD ? (int64_t(a.tokens) * a.top + 3) / 4
-                                                    : (a.tokens * chunks + 255) / 256;
-  dim3 g;
+  const int64_t chunks = (int64_t(a.cols) + 7) / 8, rows = int64_t(a.tokens) * a.top;
+  const int64_t blocks = pass == ROUTE_COMBINE_GRAD ? (rows + 3) / 4
+                                                    : ((pass == ROUTE_DISPATCH ? rows : a.tokens) * chunks + 255) / 256;
+  dim3 g, b{256};
   if (!grid_of(blocks, g)) return hipErrorInvalidConfiguration;
   if (!blocks) return hipSuccess;
-  if (pass == ROUTE_DISPATCH) hipLaunchKernelGGL((dispatch_kernel<E>), g, dim3{256}, 0, st, a);
-  if (pass == ROUTE_GATHER) hipLaunchKernelGGL((gather_kernel<E>), g, dim3{256}, 0, st, a);
-  if (pass == ROUTE_COMBINE_GRAD) hipLaunchKernelGGL((combine_grad_kernel<E>), g, dim3{256}, 0, st, a);
+  if (pass == ROUTE_DISPATCH) hipLaunchKernelGGL((dispatch_kernel<E, WHOLE>), g, b, 0, st, a);
+  if (pass == ROUTE_COMBINE_GRAD) hipLaunchKernelGGL((combine_grad_kernel<E, WHOLE>), g, b, 0, st, a);
+  if (pass == ROUTE_GATHER) {
+    if (a.top <= 2)
+      hipLaunchKernelGGL((gather_kernel<E, 2, WHOLE>), g, b, 0, st, a);
+    else if (a.top <= 4)
+      hipLaunchKernelGGL((gather_kernel<E, 4, WHOLE>), g, b, 0, st, a);
+    else if (a.top <= 6)
+      hipLaunchKernelGGL((gather_kernel<E, 6, WHOLE>), g, b, 0, st, a);
+    else
+      hipLaunchKernelGGL((gather_kernel<E, 8, WHOLE>), g, b, 0, st, a);
+  }
   return hipGetLastError();
 }
 
@@ -185,7 +195,9 @@ hipError_t launch_expert_sort(const void* ids, int id_bytes, int64_t n, int expe
 }
 
 hipError_t launch_route(bool bf16, int pass, const RouteArgs& a, hipStream_t st) {
-  return bf16 ? launch<__bf16>(pass, a, st) : launch<float>(pass, a, st);
+  if (a.cols % 8)
+    return bf16 ? launch<__bf16, false>(pass, a, st) : launch<float, false>(pass, a, st);
+  return bf16 ? launch<__bf16, true>(pass, a, st) : launch<float, true>(pass, a, st);
 }
 
 }  // namespace layers

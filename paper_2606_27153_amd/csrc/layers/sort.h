@@ -126,10 +126,16 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(Job job, int n, con
       total = counts[int64_t(blocks) * kSortBins + tid];
     } else if (blocks > 1) {
       total = 0;
-      for (int b = 0; b < blocks; ++b) {
-        const int v = counts[int64_t(b) * kSortBins + tid];
-        mine += b < int(blockIdx.x) ? v : 0;
-        total += v;
+      for (int b = 0; b < blocks; b += 8) {
+        int v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = counts[int64_t(min(b + k, blocks - 1)) * kSortBins + tid];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (b + k >= blocks) v[k] = 0;
+          mine += b + k < int(blockIdx.x) ? v[k] : 0;
+          total += v[k];
+        }
       }
     }
   }

@@ -53,7 +53,7 @@ muon_status check_weights(const void* w, int32_t weight_dtype, int32_t dtype) {
   return check_needed("weights", w, size_of(weight_dtype));
 }
 
-RouteArgs route_args(int64_t tokens, int64_t top, int64_t cols, const int32_t* position) {
+RouteArgs route_args(int64_t tokens, int64_t top, int64_t cols, const int32_t* position = nullptr) {
   RouteArgs a{};
   a.tokens = int32_t(tokens);
   a.top = int32_t(top);
@@ -240,20 +240,19 @@ MUON_API muon_status muon_sort_by_expert(const void* ids, int32_t id_bytes, int6
               "sort by expert");
 }
 
-MUON_API muon_status muon_dispatch_forward(const void* x, int64_t ldx, const int32_t* position, const int32_t* offsets,
-                                           int32_t experts, void* rows, int64_t ldr, int64_t tokens, int32_t top,
-                                           int64_t cols, int32_t dtype, void* hip_stream) {
+MUON_API muon_status muon_dispatch_forward(const void* x, int64_t ldx, const int32_t* source, void* rows, int64_t ldr,
+                                           int64_t tokens, int32_t top, int64_t cols, int32_t dtype,
+                                           void* hip_stream) {
   TRY(check_route(tokens, top, cols, dtype));
-  TRY(check_experts(experts, offsets));
   if (!tokens) return done(hipSuccess, "");
   const size_t es = size_of(dtype);
   TRY(check_matrix("x", x, ldx, cols, es));
   TRY(check_matrix("rows", rows, ldr, cols, es));
-  TRY(check_needed("position", position, 4));
-  RouteArgs a = route_args(tokens, top, cols, position);
+  TRY(check_needed("source", source, 4));
+  RouteArgs a = route_args(tokens, top, cols);
+  a.source = source;
   a.x = x; a.ldx = ldx;
   a.rows = rows; a.ldr = ldr;
-  a.offsets = offsets; a.experts = experts;
   return done(launch_route(dtype == MUON_BF16, ROUTE_DISPATCH, a, hipStream_t(hip_stream)), "dispatch");
 }
 
@@ -293,25 +292,23 @@ MUON_API muon_status muon_combine_forward(const void* rows, int64_t ldr, const v
 }
 
 MUON_API muon_status muon_combine_backward(const void* dy, int64_t lddy, const void* rows, int64_t ldr,
-                                           const void* weights, int32_t weight_dtype, const int32_t* position,
-                                           const int32_t* offsets, int32_t experts, void* drows, int64_t lddr,
-                                           void* dweights, int64_t tokens, int32_t top, int64_t cols, int32_t dtype,
-                                           void* hip_stream) {
+                                           const void* weights, int32_t weight_dtype, const int32_t* source,
+                                           void* drows, int64_t lddr, void* dweights, int64_t tokens, int32_t top,
+                                           int64_t cols, int32_t dtype, void* hip_stream) {
   TRY(check_route(tokens, top, cols, dtype));
-  TRY(check_experts(experts, offsets));
   if (!tokens) return done(hipSuccess, "");
   const size_t es = size_of(dtype);
   TRY(check_matrix("dy", dy, lddy, cols, es));
   if (dweights) TRY(check_matrix("rows", rows, ldr, cols, es));
   TRY(check_weights(weights, weight_dtype, dtype));
-  TRY(check_needed("position", position, 4));
+  TRY(check_needed("source", source, 4));
   if (drows) TRY(check_matrix("drows", drows, lddr, cols, es));
   TRY(check_vector("dweights", dweights, size_of(weight_dtype)));
-  RouteArgs a = route_args(tokens, top, cols, position);
+  RouteArgs a = route_args(tokens, top, cols);
+  a.source = source;
   a.dy = dy; a.lddy = lddy;
   a.rows = const_cast<void*>(rows); a.ldr = ldr;
   a.weights = weights; a.wf32 = weight_dtype == MUON_F32;
-  a.offsets = offsets; a.experts = experts;
   a.drows = drows; a.lddr = lddr;
   a.dweights = dweights;
   return done(launch_route(dtype == MUON_BF16, ROUTE_COMBINE_GRAD, a, hipStream_t(hip_stream)), "combine backward");
@@ -339,11 +336,13 @@ MUON_API muon_status muon_embedding_forward(const void* ids, int32_t id_bytes, c
   return done(launch_embedding_forward(dtype == MUON_BF16, a, hipStream_t(hip_stream)), "embedding");
 }
 
-MUON_API muon_status muon_embedding_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes) {
+MUON_API muon_status muon_embedding_workspace_bytes(int64_t rows, int64_t vocab, int64_t cols,
+                                                    size_t* bytes) {
   if (!bytes) return fail(MUON_ERR_INVALID_ARG, "bytes is NULL");
   TRY(check_count("rows", rows, 0, kMaxRows));
+  TRY(check_count("vocab", vocab, 1, kMaxDim));
   TRY(check_count("cols", cols, 1, kMaxDim));
-  *bytes = embedding_bytes(rows, cols);
+  *bytes = embedding_bytes(rows, vocab, cols);
   return done(hipSuccess, "");
 }
 
@@ -360,7 +359,7 @@ MUON_API muon_status muon_embedding_backward(const void* dy, int64_t lddy, const
   const size_t es = size_of(dtype);
   if (rows) TRY(check_matrix("dy", dy, lddy, cols, es));
   TRY(check_matrix("dw", dw, lddw, cols, es));
-  TRY(check_workspace(workspace, workspace_bytes, embedding_bytes(rows, cols)));
+  TRY(check_workspace(workspace, workspace_bytes, embedding_bytes(rows, vocab, cols)));
   EmbeddingArgs a{};
   a.ids = ids; a.id_bytes = id_bytes;
   a.dy = dy; a.lddy = lddy;

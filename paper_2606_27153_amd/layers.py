@@ -645,7 +645,7 @@ def embedding_backward(dy: torch.Tensor, ids: torch.Tensor, vocab: int, *, scale
         raise ValueError(f"vocab {vocab}: a table has at least one row")
     stream = _stream(dy)
     dw = dy.new_empty((vocab, cols))
-    need = _bytes("muon_embedding_workspace_bytes", rows, cols)
+    need = _bytes("muon_embedding_workspace_bytes", rows, vocab, cols)
     ws = _workspace(need, dy)
     LL.check(lib.muon_embedding_backward(gp, ldg, ip, size, dw.data_ptr(), cols, rows, vocab, cols, scale, code,
                                          None if ws is None else ws.data_ptr(), need, stream))
@@ -681,7 +681,7 @@ class Routing(NamedTuple):
     """A router's choices sorted by expert (``sort_by_expert``)."""
     offsets: torch.Tensor    # int32 [experts + 1]: each expert's rows, as grouped_linear takes them
     position: torch.Tensor   # int32 [tokens, top]: each choice's row, -1 for one of no expert
-    source: torch.Tensor     # int32 [tokens * top]: each row's choice t * top + j, -1 behind the last
+    source: torch.Tensor     # int32 [tokens * top]: each row's choice t * top + j; behind the last, ~ those of no expert
 
 
 @_on_device
@@ -710,17 +710,21 @@ def sort_by_expert(experts: torch.Tensor, count: int) -> Routing:
 
 
 def _routing(routing, like: torch.Tensor):
-    """(pointer of position, of offsets, experts, tokens, top)."""
+    """(pointer of position, of source, tokens, top)."""
     if not isinstance(routing, tuple) or len(routing) != 3:
         raise TypeError(f"routing must come from sort_by_expert, got {type(routing).__name__}")
-    offsets, position, _ = routing
-    for t, name, dim in ((position, "position", 2), (offsets, "offsets", 1)):
-        _tensor(t, name)
+    _, position, source = routing
+    for t, name, dim in ((position, "position", 2), (source, "source", 1)):
+        if not isinstance(t, torch.Tensor):
+            _tensor(t, name)
         if t.dtype != torch.int32 or t.dim() != dim or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous int32 tensor of {dim} dimensions")
         if t.device != like.device:
             raise ValueError(f"{name} is on {t.device}, expected {like.device}")
-    return (position.data_ptr(), offsets.data_ptr(), offsets.size(0) - 1, *position.shape)
+    tokens, top = position.shape
+    if source.size(0) != tokens * top:
+        raise ValueError(f"source has {source.size(0)} rows, position {tokens} x {top} choices")
+    return position.data_ptr(), source.data_ptr(), tokens, top
 
 
 def _router_weights(weights: torch.Tensor, x: torch.Tensor, tokens: int, top: int):
@@ -742,13 +746,12 @@ def dispatch_forward(x: torch.Tensor, routing: Routing) -> torch.Tensor:
     lib = _load()
     _input(x)
     code = _dtype_code(x)
-    pp, op, experts, tokens, top = _routing(routing, x)
+    _, sp, tokens, top = _routing(routing, x)
     cols = x.size(1)
     xp, ldx = _rows(x, "x", x, tokens, cols)
     stream = _stream(x)
     rows = x.new_empty((tokens * top, cols))
-    LL.check(lib.muon_dispatch_forward(xp, ldx, pp, op, experts, rows.data_ptr(), cols, tokens, top, cols, code,
-                                       stream))
+    LL.check(lib.muon_dispatch_forward(xp, ldx, sp, rows.data_ptr(), cols, tokens, top, cols, code, stream))
     return rows
 
 
@@ -758,7 +761,7 @@ def dispatch_backward(drows: torch.Tensor, routing: Routing) -> torch.Tensor:
     lib = _load()
     _input(drows, "drows")
     code = _dtype_code(drows)
-    pp, _, _, tokens, top = _routing(routing, drows)
+    pp, _, tokens, top = _routing(routing, drows)
     cols = drows.size(1)
     rp, ldr = _rows(drows, "drows", drows, tokens * top, cols)
     stream = _stream(drows)
@@ -775,7 +778,7 @@ def combine_forward(rows: torch.Tensor, weights: torch.Tensor, routing: Routing,
     lib = _load()
     _input(rows, "rows")
     code = _dtype_code(rows)
-    pp, _, _, tokens, top = _routing(routing, rows)
+    pp, _, tokens, top = _routing(routing, rows)
     cols = rows.size(1)
     rp, ldr = _rows(rows, "rows", rows, tokens * top, cols)
     wp, wcode = _router_weights(weights, rows, tokens, top)
@@ -795,7 +798,7 @@ def combine_backward(dy: torch.Tensor, rows: torch.Tensor, weights: torch.Tensor
     lib = _load()
     _input(dy, "dy")
     code = _dtype_code(dy)
-    pp, op, experts, tokens, top = _routing(routing, dy)
+    _, sp, tokens, top = _routing(routing, dy)
     cols = dy.size(1)
     gp, ldg = _rows(dy, "dy", dy, tokens, cols)
     rp, ldr = _rows(rows, "rows", dy, tokens * top, cols)
@@ -803,10 +806,9 @@ def combine_backward(dy: torch.Tensor, rows: torch.Tensor, weights: torch.Tensor
     stream = _stream(dy)
     drows = dy.new_empty((tokens * top, cols)) if rows_grad else None
     dweights = torch.empty_like(weights) if weights_grad else None
-    LL.check(lib.muon_combine_backward(gp, ldg, rp, ldr, wp, wcode, pp, op, experts,
-                                       None if drows is None else drows.data_ptr(), cols,
-                                       None if dweights is None else dweights.data_ptr(), tokens, top, cols, code,
-                                       stream))
+    LL.check(lib.muon_combine_backward(gp, ldg, rp, ldr, wp, wcode, sp, None if drows is None else drows.data_ptr(),
+                                       cols, None if dweights is None else dweights.data_ptr(), tokens, top, cols,
+                                       code, stream))
     return drows, dweights
 
 

@@ -139,10 +139,14 @@ def test_routing_ignores_what_lies_in_rows_of_nobody(dtype):
     dy[2] = float("nan")
     drows, dw = layers.combine_backward(dy, h, w, routing)
     assert torch.isfinite(drows).all() and (drows[4:] == 0).all() and (dw[chosen < 0] == 0).all()
-    # positions that sort_by_expert would not give are nobody's either
-    wild = routing._replace(position=torch.tensor([[99, -7], [1 << 30, 0], [8, 7], [-1, 3]], dtype=torch.int32, device=DEV))
-    assert layers.dispatch_forward(rand(g, 4, 24, dtype=dtype), wild).shape == (8, 24)
-    layers.combine_backward(dy, h, w, wild)
+    # rows and choices that sort_by_expert would not give are nobody's either
+    wild = routing._replace(position=torch.tensor([[99, -7], [1 << 30, 0], [8, 7], [-1, 3]], dtype=torch.int32, device=DEV),
+                            source=torch.tensor([99, -99, 1 << 30, 3, 8, -1, 0, -(1 << 31)], dtype=torch.int32, device=DEV))
+    x = rand(g, 4, 24, dtype=dtype)
+    rows = layers.dispatch_forward(x, wild)
+    assert torch.equal(rows[3], x[1]) and torch.equal(rows[6], x[0]) and (rows[[0, 1, 2, 4, 5, 7]] == 0).all()
+    drows, _ = layers.combine_backward(dy, h, w, wild)
+    assert (drows[[0, 1, 2, 4, 5, 7]] == 0).all() and torch.equal(drows[3], dy[1])
     assert torch.equal(layers.dispatch_backward(h, wild)[0], torch.zeros_like(h[0]))
 
 

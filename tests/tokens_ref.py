@@ -51,8 +51,9 @@ def route(experts, count):
     position = [-1] * len(e)
     for r, i in enumerate(order):
         position[i] = r
+    nobody = [~i for i, v in enumerate(e) if not 0 <= v < count]
     as_int = lambda v: torch.tensor(v, dtype=torch.int32)
-    return as_int(offsets), as_int(position).view(experts.shape), as_int(order + [-1] * (len(e) - len(order)))
+    return as_int(offsets), as_int(position).view(experts.shape), as_int(order + nobody)
 
 
 def dispatch(x, position):
