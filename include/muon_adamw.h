@@ -6,8 +6,8 @@
  *   m = beta1 m + (1 - beta1) g          v = beta2 v + (1 - beta2) g^2
  *   w = w (1 - lr decay) - lr / (1 - beta1^k) m / (sqrt(v / (1 - beta2^k)) + eps)
  *
- * k is the tensor's step, counted from 1; everything is computed in fp32, the
- * parameter rounded once (to nearest).
+ * k is the tensor's step, counted from 1; everything is computed in fp32 (under
+ * the root, v counts as 2^-126 at least), the parameter rounded once (to nearest).
  *
  * States in 8 bits.  A code of 8 bits stands for the upper 12 bits of an fp32
  * number (sign, exponent, 3 bits of fraction) relative to a base that 256

@@ -178,12 +178,13 @@ MUON_API muon_status muon_sort_by_expert(const void* ids, int32_t id_bytes, int6
 /* Workspace bytes of muon_sort_by_expert. */
 MUON_API muon_status muon_sort_by_expert_workspace_bytes(int64_t tokens, int32_t top, size_t* bytes);
 
-/* rows[r] = x[source[r] / top], 0 where source[r] is negative.  position and source
- * are those of muon_sort_by_expert, here and below; a value that it would not give
- * stands for no row and no choice. */
-MUON_API muon_status muon_dispatch_forward(const void* x, int64_t ldx, const int32_t* source, void* rows, int64_t ldr,
-                                           int64_t tokens, int32_t top, int64_t cols, int32_t dtype,
-                                           void* hip_stream);
+/* rows[position[t][j]] = x[t], and 0 in the rows r where source[r] is negative.
+ * position and source are those of muon_sort_by_expert, here and below; a value
+ * that it would not give stands for no row and no choice (a row that nothing names
+ * is left as it is). */
+MUON_API muon_status muon_dispatch_forward(const void* x, int64_t ldx, const int32_t* position, const int32_t* source,
+                                           void* rows, int64_t ldr, int64_t tokens, int32_t top, int64_t cols,
+                                           int32_t dtype, void* hip_stream);
 
 /* dx[t] = the sum of drows[position[t][j]] over j. */
 MUON_API muon_status muon_dispatch_backward(const void* drows, int64_t ldr, const int32_t* position, void* dx,

@@ -46,7 +46,7 @@ SIGNATURES = {
     "muon_embedding_workspace_bytes": (_ST, [_I64, _I64, _I64, _PSZ]),
     "muon_sort_by_expert": (_ST, [_P, _I32, _I64, _I32, _I32, _P, _P, _P, _P, _SZ, _P]),
     "muon_sort_by_expert_workspace_bytes": (_ST, [_I64, _I32, _PSZ]),
-    "muon_dispatch_forward": (_ST, [_P, _I64, _P, _P, _I64, _I64, _I32, _I64, _I32, _P]),
+    "muon_dispatch_forward": (_ST, [_P, _I64, _P, _P, _P, _I64, _I64, _I32, _I64, _I32, _P]),
     "muon_dispatch_backward": (_ST, [_P, _I64, _P, _P, _I64, _I64, _I32, _I64, _I32, _P]),
     "muon_combine_forward": (_ST, [_P, _I64, _P, _I32, _P, _P, _I64, _P, _I64, _I64, _I32, _I64, _I32, _P]),
     "muon_combine_backward": (_ST, [_P, _I64, _P, _I64, _P, _I32, _P, _P, _I64, _P, _I64, _I32, _I64, _I32, _P]),

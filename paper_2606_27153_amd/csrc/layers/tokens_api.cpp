@@ -240,16 +240,17 @@ MUON_API muon_status muon_sort_by_expert(const void* ids, int32_t id_bytes, int6
               "sort by expert");
 }
 
-MUON_API muon_status muon_dispatch_forward(const void* x, int64_t ldx, const int32_t* source, void* rows, int64_t ldr,
-                                           int64_t tokens, int32_t top, int64_t cols, int32_t dtype,
-                                           void* hip_stream) {
+MUON_API muon_status muon_dispatch_forward(const void* x, int64_t ldx, const int32_t* position, const int32_t* source,
+                                           void* rows, int64_t ldr, int64_t tokens, int32_t top, int64_t cols,
+                                           int32_t dtype, void* hip_stream) {
   TRY(check_route(tokens, top, cols, dtype));
   if (!tokens) return done(hipSuccess, "");
   const size_t es = size_of(dtype);
   TRY(check_matrix("x", x, ldx, cols, es));
   TRY(check_matrix("rows", rows, ldr, cols, es));
+  TRY(check_needed("position", position, 4));
   TRY(check_needed("source", source, 4));
-  RouteArgs a = route_args(tokens, top, cols);
+  RouteArgs a = route_args(tokens, top, cols, position);
   a.source = source;
   a.x = x; a.ldx = ldx;
   a.rows = rows; a.ldr = ldr;

@@ -746,12 +746,12 @@ def dispatch_forward(x: torch.Tensor, routing: Routing) -> torch.Tensor:
     lib = _load()
     _input(x)
     code = _dtype_code(x)
-    _, sp, tokens, top = _routing(routing, x)
+    pp, sp, tokens, top = _routing(routing, x)
     cols = x.size(1)
     xp, ldx = _rows(x, "x", x, tokens, cols)
     stream = _stream(x)
     rows = x.new_empty((tokens * top, cols))
-    LL.check(lib.muon_dispatch_forward(xp, ldx, sp, rows.data_ptr(), cols, tokens, top, cols, code, stream))
+    LL.check(lib.muon_dispatch_forward(xp, ldx, pp, sp, rows.data_ptr(), cols, tokens, top, cols, code, stream))
     return rows
 
 
