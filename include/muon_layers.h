@@ -218,7 +218,7 @@ typedef enum muon_loss_reduction {
  * v, loss[i] = lse[i] - z[i][targets[i]].  z exists a piece at a time, in the
  * workspace or not at all.  A row whose target is `ignore` or outside [0, outer)
  * has loss 0.  loss: rows fp32, or one (SUM, MEAN); lse: rows fp32, which the
- * backward pass reads.  inner is at most 2^21. */
+ * backward pass reads.  inner is at most 2^20. */
 MUON_API muon_status muon_linear_cross_entropy_forward(const void* x, int64_t ldx, const void* w, int64_t ldw,
                                                        int32_t w_transposed, const void* targets,
                                                        int32_t target_bytes, int64_t ignore, int32_t reduction,

@@ -155,6 +155,16 @@ __device__ __forceinline__ void store_8(E* p, int n, const float (&v)[8]) {
   store8(p, WHOLE ? 8 : n, v);
 }
 
+// Number i of a list of int64 or int32.
+__device__ __forceinline__ int64_t id_at(const void* ids, int bytes, int64_t i) {
+  return bytes == 8 ? static_cast<const int64_t*>(ids)[i] : int64_t(static_cast<const int32_t*>(ids)[i]);
+}
+// The column of a row's target, -1 if it has none.
+__device__ __forceinline__ int label_of(const LossArgs& a, int64_t row) {
+  const int64_t t = id_at(a.targets, a.target_bytes, row);
+  return t >= 0 && t < a.vocab && t != a.ignore ? int(t) : -1;
+}
+
 // A plain product takes no table.
 struct NoTable {};
 template <int GROUP>

@@ -113,10 +113,8 @@ struct Fits {
 inline Fits tile_fits(bool bf16, int form, int group, const Product& p, const Table* t) {
   const int64_t epc = bf16 ? 8 : 4;
   Fits f;
-  const int64_t ca = form == FORM_TT ? p.M : p.K;
-  f.a = rows_fit(p.a, p.lda, ca > p.pad_a ? ca : p.pad_a, epc);
-  int64_t cols = form == FORM_RR ? p.K : p.N;
-  if (cols < p.pad_b) cols = p.pad_b;
+  f.a = rows_fit(p.a, p.lda, form == FORM_TT ? p.M : p.K, epc);
+  const int64_t cols = form == FORM_RR ? p.K : p.N;
   f.b = group != GROUP_ROWS && rows_fit(p.b, p.ldb, cols, epc);
   if (group == GROUP_ROWS) {
     f.b = true;
@@ -325,9 +323,9 @@ inline hipError_t launch_choice(bool bf16, int form, int group, const Choice& c,
   return hipErrorInvalidValue;
 }
 
-// One matrix product by the kernel chosen for it.
-inline hipError_t product_by(Choice c, bool bf16, int form, int group, Product p, const Table* t, Scratch ws,
-                             hipStream_t st) {
+// One matrix product: the kernel that suits it.
+inline hipError_t product(bool bf16, int form, int group, Product p, const Table* t, Scratch ws, hipStream_t st) {
+  Choice c = choose(bf16, form, group, p.M, p.N, p.K, p.experts, p.act != MUON_ACT_NONE);
   Table copies;
   hipError_t e = fit_operands(bf16, form, group, p, t, copies, c, ws, st);
   if (e != hipSuccess) return e;
@@ -335,28 +333,6 @@ inline hipError_t product_by(Choice c, bool bf16, int form, int group, Product p
   p.part = reinterpret_cast<float*>(ws.p);
   e = launch_choice(bf16, form, group, c, p, t, st);
   return e == hipSuccess && c.splits > 1 ? launch_reduce(bf16, p, st) : e;
-}
-inline hipError_t product(bool bf16, int form, int group, const Product& p, const Table* t, Scratch ws,
-                          hipStream_t st) {
-  const Choice c = choose(bf16, form, group, p.M, p.N, p.K, p.experts, p.act != MUON_ACT_NONE);
-  return product_by(c, bf16, form, group, p, t, ws, st);
-}
-
-// The same left in fp32 at `sums`, as p.splits partial results, or added to what is there.
-// The operands' copies need room in ws.
-inline hipError_t product_sums(const Choice& c, bool bf16, int form, Product p, float* sums, Scratch ws,
-                               hipStream_t st) {
-  Choice k = c;
-  k.splits = 1;   // (no partial results in ws)
-  const Table* none = nullptr;
-  Table copies;
-  const hipError_t e = fit_operands(bf16, form, GROUP_NONE, p, none, copies, k, ws, st);
-  if (e != hipSuccess) return e;
-  if (k.kernel != c.kernel) return hipErrorInvalidValue;
-  p.splits = c.splits;
-  p.raw = 1;
-  p.part = sums;
-  return launch_choice(bf16, form, GROUP_NONE, c, p, nullptr, st);
 }
 
 }  // namespace layers

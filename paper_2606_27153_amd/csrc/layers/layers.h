@@ -49,8 +49,6 @@ struct Product {
   int32_t raw;            // != 0: C is left in `part` as it is summed, also where splits is 1
                           // (not by the simple kernel)
   int32_t add;            // raw: added to what `part` holds
-  int32_t pad_a, pad_b;   // elements that exist of each row of A and B as they lie, zeros beyond
-                          // the matrix (0: none beyond)
 };
 
 // Pointers of the experts' matrices (grouped products), passed by value.
@@ -136,14 +134,12 @@ struct EmbeddingArgs {
 struct LossArgs {
   const void* targets;
   const float* dloss;     // a number for every row (each), or one
-  int32_t* label;         // the target's column, -1: none
-  float* grad;            // factor of the row's gradient
-  float* alpha;           // factor of all gradients
+  const float* alpha;     // factor of all gradients, or NULL (1)
   float2* part;           // strips x rows: the largest logit and the sum of the others relative to it
   float* logit;           // the target's
   float* loss;            // of every row
   float* lse;
-  float* total;           // of all rows, or NULL
+  float* total;           // of all rows
   const float* raw;       // splits x rows x cols: a piece of z, to be added up
   void* dz;               // rows x lddz: the gradient of a piece of z
   int64_t ignore, lddz;
@@ -166,7 +162,7 @@ size_t embedding_bytes(int64_t rows, int64_t vocab, int64_t cols);
 hipError_t launch_embedding_forward(bool bf16, const EmbeddingArgs& a, hipStream_t st);
 hipError_t launch_embedding_backward(bool bf16, EmbeddingArgs a, void* workspace, hipStream_t st);
 
-hipError_t launch_loss_labels(const LossArgs& a, hipStream_t st);   // label; with dloss grad and alpha
+hipError_t launch_loss_mean(const LossArgs& a, float* alpha, hipStream_t st);   // dloss over the rows with a target
 hipError_t launch_loss_strips(const LossArgs& a, hipStream_t st);   // raw -> part and logit
 hipError_t launch_loss_finish(const LossArgs& a, hipStream_t st);   // part -> lse and loss
 hipError_t launch_loss_total(const LossArgs& a, hipStream_t st);    // loss -> total

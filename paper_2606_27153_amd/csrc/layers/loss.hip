@@ -17,8 +17,6 @@ namespace muon {
 namespace layers {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
@@ -32,28 +30,19 @@ __device__ __forceinline__ float wave_max(float v) {
 // exp(v - m) where m is the largest; a strip of nothing but -inf has sum 0.
 __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
 
-// One block: the labels, how many there are, and what the gradients are scaled with.
-__global__ __launch_bounds__(1024) void label_kernel(LossArgs a) {
+// One block: how many rows have a target, and the factor of a mean's gradients.
+__global__ __launch_bounds__(1024) void mean_kernel(LossArgs a, float* alpha) {
   __shared__ int counts[16];
-  int count = 0;
-  for (int i = threadIdx.x; i < a.rows; i += 1024) {
-    const int64_t t = a.target_bytes == 8 ? static_cast<const int64_t*>(a.targets)[i]
-                                          : int64_t(static_cast<const int32_t*>(a.targets)[i]);
-    const bool live = t >= 0 && t < a.vocab && t != a.ignore;
-    count += live;
-    a.label[i] = live ? int(t) : -1;
-    if (a.dloss) a.grad[i] = !live ? 0.f : a.each ? a.dloss[i] : 1.f;
-  }
-  if (!a.dloss) return;
+  int n = 0;
+  for (int i = threadIdx.x; i < a.rows; i += 1024) n += label_of(a, i) >= 0;
 #pragma unroll
-  for (int d = 32; d; d >>= 1) count += __shfl_xor(count, d);
-  if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = count;
+  for (int d = 32; d; d >>= 1) n += __shfl_xor(n, d);
+  if ((threadIdx.x & 63) == 0) counts[threadIdx.x >> 6] = n;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    int n = 0;
-    for (int w = 0; w < 16; ++w) n += counts[w];
-    *a.alpha = a.each ? 1.f : a.mean ? *a.dloss / float(max(n, 1)) : *a.dloss;
-  }
+  if (threadIdx.x) return;
+  n = 0;
+  for (int w = 0; w < 16; ++w) n += counts[w];
+  *alpha = *a.dloss / float(max(n, 1));
 }
 
 // 8 logits of a row from column c of the piece on (-inf past its end).
@@ -82,8 +71,8 @@ __global__ __launch_bounds__(256) void strip_kernel(LossArgs a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = -INFINITY;
   }
-  const int at = a.label[row] - a.first - c;
-  if (a.label[row] >= 0 && at >= 0 && at < 8) {
+  const int label = label_of(a, row), at = label - a.first - c;
+  if (label >= 0 && at >= 0 && at < 8) {
     float z = v[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) z = at == e ? v[e] : z;
@@ -107,38 +96,49 @@ __global__ __launch_bounds__(256) void strip_kernel(LossArgs a) {
         make_float2(m, red[1][0] + red[1][1] + red[1][2] + red[1][3]);
 }
 
-// 64 rows of a block, whose 16 waves share the strips.
-__global__ __launch_bounds__(1024) void finish_kernel(LossArgs a) {
+// (m, s) of two sets of columns.
+__device__ __forceinline__ float2 join(float2 a, float2 b) {
+  const float top = fmaxf(a.y == 0.f ? -INFINITY : a.x, b.y == 0.f ? -INFINITY : b.x), r = reference(top);
+  return make_float2(r, (a.y == 0.f ? 0.f : a.y * __expf(a.x - r)) + (b.y == 0.f ? 0.f : b.y * __expf(b.x - r)));
+}
+
+// 2^shift rows of a block, whose 16 waves and their lanes share the strips.
+__global__ __launch_bounds__(1024) void finish_kernel(LossArgs a, int shift) {
   __shared__ float2 red[16][64];
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-  const int64_t row = int64_t(blockIdx.x) * 64 + lane;
+  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6, in = lane & ((1 << shift) - 1);
+  const int64_t row = (int64_t(blockIdx.x) << shift) + in;
+  const int lists = 1024 >> shift, list = wid * (64 >> shift) + (lane >> shift);
   float m = -INFINITY, s = 0.f;
   if (row < a.rows) {
-    const int per = (a.strips + 15) / 16, s0 = wid * per, s1 = min(a.strips, s0 + per);
-    for (int i = s0; i < s1; i += 8) {
+    for (int i = list; i < a.strips; i += 8 * lists) {
       float2 p[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) p[k] = a.part[int64_t(min(i + k, s1 - 1)) * a.rows + row];
+      for (int k = 0; k < 8; ++k) {
+        p[k] = a.part[int64_t(min(i + k * lists, a.strips - 1)) * a.rows + row];
+        if (i + k * lists >= a.strips) p[k].y = 0.f;
+      }
       float top = m;
 #pragma unroll
       for (int k = 0; k < 8; ++k) top = fmaxf(top, p[k].y == 0.f ? -INFINITY : p[k].x);
       const float r = reference(top);
       s = s == 0.f ? 0.f : s * __expf(m - r);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s += i + k < s1 && p[k].y != 0.f ? p[k].y * __expf(p[k].x - r) : 0.f;
-      m = top;
+      for (int k = 0; k < 8; ++k) s += p[k].y == 0.f ? 0.f : p[k].y * __expf(p[k].x - r);
+      m = r;
     }
   }
-  red[wid][lane] = make_float2(m, s);
+  float2 v = make_float2(m, s);
+  for (int d = 32; d >> shift; d >>= 1) {
+    const float2 o = make_float2(__shfl_xor(v.x, d), __shfl_xor(v.y, d));
+    v = lane & d ? join(o, v) : join(v, o);
+  }
+  red[wid][lane] = v;
   __syncthreads();
-  if (wid || row >= a.rows) return;
-  float top = -INFINITY, sum = 0.f;
-  for (int w = 0; w < 16; ++w) top = fmaxf(top, red[w][lane].x);
-  const float r = reference(top);
-  for (int w = 0; w < 16; ++w) sum += red[w][lane].y == 0.f ? 0.f : red[w][lane].y * __expf(red[w][lane].x - r);
-  const float lse = r + logf(sum);
+  if (wid || lane >> shift || row >= a.rows) return;
+  for (int w = 1; w < 16; ++w) v = join(v, red[w][lane]);
+  const float lse = reference(v.x) + logf(v.y);
   a.lse[row] = lse;
-  a.loss[row] = a.label[row] >= 0 ? lse - a.logit[row] : 0.f;
+  a.loss[row] = label_of(a, row) >= 0 ? lse - a.logit[row] : 0.f;
 }
 
 // One block: the sum or mean of the rows' losses.
@@ -149,7 +149,7 @@ __global__ __launch_bounds__(1024) void total_kernel(LossArgs a) {
   int n = 0;
   for (int i = threadIdx.x; i < a.rows; i += 1024) {
     s += a.loss[i];
-    n += a.label[i] >= 0;
+    n += label_of(a, i) >= 0;
   }
   s = wave_sum(s);
 #pragma unroll
@@ -176,8 +176,8 @@ __global__ __launch_bounds__(256) void grad_kernel(LossArgs a) {
   if (c >= a.cols) return;
   float v[8];
   load_logits(a, row, c, v);
-  const int label = a.label[row];
-  const float lse = a.lse[row], g = a.grad[row];
+  const int label = label_of(a, row);
+  const float lse = a.lse[row], g = a.each ? a.dloss[row] : 1.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float p = __expf(v[e] - lse) - (label - a.first - c == e ? 1.f : 0.f);
@@ -194,7 +194,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const float* part, int splits,
   if (r >= rows) return;
   const int64_t c = (i - r * chunks) * 8;
   const int n = int(min(int64_t(8), cols - c));
-  const float f = *alpha;
+  const float f = alpha ? *alpha : 1.f;
   float v[8];
   load8(part + r * cols + c, n, v);
   for (int s = 1; s < splits; ++s) {
@@ -212,8 +212,8 @@ unsigned strips_of(const LossArgs& a) { return unsigned((a.cols + kRawStrip - 1)
 
 }  // namespace
 
-hipError_t launch_loss_labels(const LossArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(label_kernel, dim3{1}, dim3{1024}, 0, st, a);
+hipError_t launch_loss_mean(const LossArgs& a, float* alpha, hipStream_t st) {
+  hipLaunchKernelGGL(mean_kernel, dim3{1}, dim3{1024}, 0, st, a, alpha);
   return hipGetLastError();
 }
 
@@ -224,7 +224,11 @@ hipError_t launch_loss_strips(const LossArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_loss_finish(const LossArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(finish_kernel, dim3{unsigned((int64_t(a.rows) + 63) / 64)}, dim3{1024}, 0, st, a);
+  // 64 rows read whole lines; fewer where there are not enough for every CU
+  int shift = 6;
+  while (shift && (a.rows >> shift) < kCUs) --shift;
+  hipLaunchKernelGGL(finish_kernel, dim3{unsigned((int64_t(a.rows) + (1 << shift) - 1) >> shift)}, dim3{1024}, 0, st, a,
+                     shift);
   return hipGetLastError();
 }
 

@@ -434,7 +434,7 @@ __device__ __forceinline__ void strip_piece(const LossArgs& a, const Work<E>& o,
     constexpr int i = decltype(it)::value;
     // the targets' places in the strip, of row `lane` of the 32
     const int row = wm + 32 * i + (lane & 31);
-    const int label = row < o.rows ? a.label[o.m0 + row] : -1;
+    const int label = row < o.rows ? label_of(a, o.m0 + row) : -1;
     const int place = label >= 0 ? label - a.first - int(o.n0) - wn : -1;
     stage_rows<C, i>(acc, to);
     if (lane < 32 && place >= 0 && place < min(C::WTN, o.cols - wn))
@@ -475,10 +475,10 @@ struct GradOf {
   __device__ __forceinline__ void rows(int i, float* region, int lane) const {
     if (lane >= 32) return;
     const int64_t row = o.m0 + min(wm + 32 * i + lane, o.rows - 1);
-    const int label = a.label[row];
+    const int label = label_of(a, row);
     const int place = label >= 0 ? label - a.first - int(o.n0) - wn : -1;
     *reinterpret_cast<f32x4*>(region + lane * Staging<C>::LD + C::WTN) =
-        f32x4{a.lse[row], a.grad[row], __builtin_bit_cast(float, place), label >= 0 ? 1.f : 0.f};
+        f32x4{a.lse[row], a.each ? a.dloss[row] : 1.f, __builtin_bit_cast(float, place), label >= 0 ? 1.f : 0.f};
   }
   template <class C>
   __device__ __forceinline__ void columns(float (&v)[8], const float* row, int c) const {
@@ -683,7 +683,7 @@ __global__ __launch_bounds__(256, (Tile<E, TM, TN, U>::RING > 80 * 1024 ? 1 : 2)
       w.cols = (w.cols + 7) & ~7;   // (dz has room for whole groups of 8)
       store_piece<C, E, E, MUON_ACT_NONE, false, false, false>(p, w.c, p.ldc, w, acc, region, wm, wn, lane, op);
     } else if constexpr (EP == EP_SCALE) {
-      store_tile<C, E, false>(p, w, acc, region, wm, wn, lane, Scaled(*extra));
+      store_tile<C, E, false>(p, w, acc, region, wm, wn, lane, Scaled(extra ? *extra : 1.f));
     } else {
       store_tile<C, E, EP == EP_LINEAR>(p, w, acc, region, wm, wn, lane);
     }

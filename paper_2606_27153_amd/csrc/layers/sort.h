@@ -31,11 +31,6 @@ inline size_t sort_bytes(int64_t n) {
   return b > 1 ? (size_t(b) + 1) * kSortBins * 4 : 0;
 }
 
-// A key that stands for its 8 bytes or 4.
-__device__ __forceinline__ int64_t id_at(const void* ids, int bytes, int64_t i) {
-  return bytes == 8 ? static_cast<const int64_t*>(ids)[i] : int64_t(static_cast<const int32_t*>(ids)[i]);
-}
-
 // Job: what is sorted.  digit(i, key) reads item i and says its digit; put(i, key,
 // digit, place) takes its place; start(digit, first) hears, once for each digit up to
 // job.bins - 1, where its items begin.

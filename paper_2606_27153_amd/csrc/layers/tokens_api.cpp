@@ -7,7 +7,7 @@ namespace {
 
 using namespace muon::layers;
 
-constexpr int64_t kMaxInner = int64_t(1) << 21;   // of the loss: 256 rows of it within 32-bit offsets
+constexpr int64_t kMaxInner = int64_t(1) << 20;   // of the loss: 256 rows of it within 32-bit offsets
 
 muon_status check_count(const char* name, int64_t v, int64_t lo, int64_t hi) {
   if (v < lo || v > hi)
@@ -84,26 +84,20 @@ struct LossLayout {
   int64_t rows = 0;    // at a time
   int64_t piece = 0;   // columns at a time
   Choice z, x, w;      // the kernels of x W, dz W^T and x^T dz (a last piece has fewer columns, and the same ones)
-  size_t label = 0, logit = 0, loss = 0, grad = 0, alpha = 0, part = 0, raw = 0, dz = 0, dx = 0, scratch = 0, total = 0;
+  size_t logit = 0, loss = 0, alpha = 0, part = 0, raw = 0, dz = 0, dx = 0, wcopy = 0, xcopy = 0, scratch = 0, total = 0;
   void take(size_t& p, size_t bytes) {
     p = total;
     total += padded(bytes);
   }
 };
 
-// What the copies for a piece of x W take.
-size_t logit_copies(const LossLayout& l, bool bf16, int64_t inner, bool w_transposed) {
-  if (l.z.kernel == Choice::SKINNY) return 0;
-  const int64_t epc = bf16 ? 8 : 4;
-  const int form = w_transposed ? FORM_RR : FORM_RT;
-  return copy_bytes(copy_of_a(form, l.rows, inner, epc), epc, 1) +
-         copy_bytes(copy_of_b(form, l.piece, inner, epc), epc, 1);
-}
-
 // The kernel of a piece of x W: few rows leave it in memory (`raw`), tiles do not.
-Choice choose_logits(bool bf16, int64_t rows, int64_t piece, int64_t inner) {
+// The latter take over from 33 rows on (128000 x 4096 in bf16, 40 rows: 210 us for 294), and
+// at once where a bf16 weight is kept by its columns, of which a wave of the other
+// kernel reads 64 bytes at a time (one row: 213 us for 310; fp32 74 for 99 the other way).
+Choice choose_logits(bool bf16, bool w_transposed, int64_t rows, int64_t piece, int64_t inner) {
   const Choice c = choose(bf16, FORM_RT, GROUP_NONE, rows, piece, inner, 0, false);
-  return c.kernel == Choice::SKINNY ? c : choose_tile(bf16, GROUP_NONE, rows, piece, inner, 0, true, 1);
+  return c.kernel == Choice::SKINNY && rows <= 32 && !(w_transposed && bf16) ? c : choose_tile(bf16, GROUP_NONE, rows, piece, inner, 0, true, 1);
 }
 // Columns of its strips: a wave has half of a tile's.
 int64_t strip_columns(const Choice& c) {
@@ -132,81 +126,96 @@ hipError_t launch_loss_tile(const Choice& c, int step, bool bf16, int form, cons
   }
 }
 
-// A product of the loss by the kernel chosen for it; the operands' copies have room
-// in ws (a partial result's comes first).
-hipError_t loss_product(const Choice& c, int step, bool bf16, int form, Product p, const LossArgs& a, Scratch ws,
+// A product of the loss by the kernel chosen for it, whose operands it can fetch.
+hipError_t loss_product(const Choice& c, int step, bool bf16, int form, Product p, const LossArgs& a, char* part,
                         hipStream_t st) {
-  Choice k = c;
-  const Table* none = nullptr;
-  Table copies;
-  hipError_t e = fit_operands(bf16, form, GROUP_NONE, p, none, copies, k, ws, st);
-  if (e != hipSuccess) return e;
   p.splits = c.splits;
-  p.part = reinterpret_cast<float*>(ws.p);
-  e = launch_loss_tile(k, step, bf16, form, p, a, st);
+  p.part = reinterpret_cast<float*>(part);
+  const hipError_t e = launch_loss_tile(c, step, bf16, form, p, a, st);
   return e == hipSuccess && c.splits > 1 ? launch_reduce(bf16, p, st) : e;
+}
+// A product left in fp32 at `sums`, as c.splits partial results, or added to what is there.
+hipError_t product_sums(const Choice& c, bool bf16, int form, Product p, float* sums, hipStream_t st) {
+  p.splits = c.splits;
+  p.raw = 1;
+  p.part = sums;
+  return launch_choice(bf16, form, GROUP_NONE, c, p, nullptr, st);
+}
+
+// Copies of x (once) and of a piece of the weight, as it is kept, for all the products
+// that read them: rows of whole chunks, zeros after the last column.
+PackOne copy_of_w(int64_t piece, int64_t inner, bool w_transposed, int64_t epc) {
+  return w_transposed ? copy_shape(piece, inner, epc) : copy_shape(inner, piece, epc);
+}
+void take_copies(LossLayout& l, int64_t rows, int64_t inner, bool w_transposed, bool bf16, bool unaligned) {
+  const int64_t epc = bf16 ? 8 : 4;
+  l.take(l.xcopy, unaligned ? copy_bytes(copy_shape(rows, inner, epc), epc, 1) : 0);
+  l.take(l.wcopy, unaligned ? copy_bytes(copy_of_w(l.piece, inner, w_transposed, epc), epc, 1) : 0);
 }
 
 LossLayout forward_layout(int64_t rows, int64_t inner, int64_t outer, bool w_transposed, bool bf16, bool unaligned) {
   LossLayout l;
   l.rows = rows < kLossRows ? rows : kLossRows;
   l.piece = even_piece(outer, unaligned ? kCopyPiece : kPiece);
-  l.z = choose_logits(bf16, l.rows, l.piece, inner);
-  l.take(l.label, size_t(rows) * 4);
+  l.z = choose_logits(bf16, w_transposed, l.rows, l.piece, inner);
   l.take(l.logit, size_t(rows) * 4);
   l.take(l.loss, size_t(rows) * 4);
   l.take(l.part, size_t(ceil_div(outer, l.piece)) * size_t(ceil_div(l.piece, strip_columns(l.z))) * size_t(l.rows) * 8);
   l.take(l.raw, raw_bytes(l));
-  l.take(l.scratch, unaligned ? logit_copies(l, bf16, inner, w_transposed) : 0);
+  if (l.z.kernel != Choice::SKINNY) take_copies(l, rows, inner, w_transposed, bf16, unaligned);
   return l;
 }
 
 LossLayout backward_layout(int64_t rows, int64_t inner, int64_t outer, bool w_transposed, bool bf16, bool unaligned) {
   LossLayout l;
-  const int64_t epc = bf16 ? 8 : 4, cap = unaligned ? kCopyPiece : kPiece;
+  const int64_t cap = unaligned ? kCopyPiece : kPiece;
   int64_t most = kGradPiece / (rows > 0 ? rows : 1) / 256 * 256;
   most = most < 2048 ? 2048 : most > cap ? cap : most;
   l.rows = rows < kLossRows ? rows : kLossRows;
   l.piece = even_piece(outer, most);
-  l.z = choose_logits(bf16, l.rows, l.piece, inner);
+  l.z = choose_logits(bf16, w_transposed, l.rows, l.piece, inner);
   l.x = choose(bf16, FORM_RT, GROUP_NONE, rows, inner, l.piece, 0, false);
   const int64_t wm = w_transposed ? l.piece : inner, wn = w_transposed ? inner : l.piece;
   l.w = choose(bf16, FORM_TT, GROUP_NONE, wm, wn, rows, 0, false);
-  l.take(l.label, size_t(rows) * 4);
-  l.take(l.grad, size_t(rows) * 4);
   l.take(l.alpha, 4);
   l.take(l.dz, size_t(rows) * size_t(ceil_div(l.piece, 8) * 8) * (bf16 ? 2 : 4));
   l.take(l.raw, raw_bytes(l));
   l.take(l.dx, size_t(l.x.splits) * size_t(rows) * size_t(inner) * 4);
-  size_t scratch = part_bytes(l.w, wm, wn);
-  if (unaligned) {
-    scratch += copy_bytes(copy_of_a(FORM_TT, inner, rows, epc), epc, 1);   // x, as either operand
-    scratch = larger(scratch, logit_copies(l, bf16, inner, w_transposed));
-    const int form = w_transposed ? FORM_RT : FORM_RR;
-    scratch = larger(scratch, copy_bytes(copy_of_b(form, inner, l.piece, epc), epc, 1));
-  }
-  l.take(l.scratch, scratch);
+  take_copies(l, rows, inner, w_transposed, bf16, unaligned);
+  l.take(l.scratch, part_bytes(l.w, wm, wn));
   return l;
 }
 
 muon_status check_loss(int64_t rows, int64_t inner, int64_t outer, int32_t dtype, int32_t reduction) {
   TRY(check_sizes(rows, inner, outer, dtype));
-  if (inner > kMaxInner) return fail(MUON_ERR_UNSUPPORTED, "inner %lld: at most 2^21", (long long)inner);
+  if (inner > kMaxInner) return fail(MUON_ERR_UNSUPPORTED, "inner %lld: at most 2^20", (long long)inner);
   if (reduction < MUON_LOSS_ROWS || reduction > MUON_LOSS_MEAN)
     return fail(MUON_ERR_INVALID_ARG, "unknown reduction %d", reduction);
   return MUON_OK;
 }
 
-// Whether the tile kernels can fetch x and w where they lie.
-bool operands_fit(const void* x, int64_t ldx, const void* w, int64_t ldw, int32_t w_transposed, int64_t inner,
-                  int64_t outer, bool bf16) {
-  const int64_t epc = bf16 ? 8 : 4;
-  return rows_fit(x, ldx, inner, epc) && rows_fit(w, ldw, w_transposed ? inner : outer, epc);
+// x or a piece of the weight as a product's operand: where it lies, or its copy.
+struct Operand {
+  const void* p;
+  int64_t ld;
+};
+bool x_fits(const Operand& x, int64_t inner, bool bf16) { return rows_fit(x.p, x.ld, inner, bf16 ? 8 : 4); }
+bool w_fits(const Operand& w, int64_t inner, int64_t outer, bool w_transposed, bool bf16) {
+  return rows_fit(w.p, w.ld, w_transposed ? inner : outer, bf16 ? 8 : 4);
 }
-
 // Columns first .. of a weight.
-const void* columns(const void* w, int64_t ldw, int32_t w_transposed, int64_t first, size_t es) {
-  return static_cast<const char*>(w) + size_t(w_transposed ? first * ldw : first) * es;
+Operand columns(const Operand& w, bool w_transposed, int64_t first, size_t es) {
+  return Operand{static_cast<const char*>(w.p) + size_t(w_transposed ? first * w.ld : first) * es, w.ld};
+}
+hipError_t copy_operand(bool bf16, Operand& o, PackOne shape, void* to, hipStream_t st) {
+  PackArgs k{};
+  k.a = shape;
+  k.a.src = o.p;
+  k.a.ld_src = o.ld;
+  k.a.dst = to;
+  static const Table none{};
+  o = Operand{to, shape.ld_dst};
+  return launch_pack(bf16, k, none, st);
 }
 
 }  // namespace
@@ -398,55 +407,59 @@ MUON_API muon_status muon_linear_cross_entropy_forward(const void* x, int64_t ld
   const size_t es = size_of(dtype);
   const bool bf16 = dtype == MUON_BF16, each = reduction == MUON_LOSS_ROWS;
   if (rows || !each) TRY(check_needed("loss", loss, 4));
-  bool unaligned = false;
+  Operand xo{x, ldx};
+  const Operand wo{w, ldw};
+  bool xf = true, wf = true;
   if (rows) {
     TRY(check_needed("lse", lse, 4));
     TRY(check_matrix("x", x, ldx, inner, es));
     TRY(check_matrix("w", w, ldw, w_transposed ? inner : outer, es));
-    unaligned = !operands_fit(x, ldx, w, ldw, w_transposed, inner, outer, bf16);
+    xf = x_fits(xo, inner, bf16);
+    wf = w_fits(wo, inner, outer, w_transposed, bf16);
   }
-  const LossLayout l = forward_layout(rows, inner, outer, w_transposed, bf16, unaligned);
+  const LossLayout l = forward_layout(rows, inner, outer, w_transposed, bf16, !(xf && wf));
   TRY(check_workspace(workspace, workspace_bytes, l.total));
   const hipStream_t st = hipStream_t(hip_stream);
   char* ws = static_cast<char*>(workspace);
-  const Scratch scratch{ws + l.scratch, l.total - l.scratch};
+  const int64_t epc = bf16 ? 8 : 4;
+  const bool few = l.z.kernel == Choice::SKINNY;
+  if (!xf && !few) TRY(done(copy_operand(bf16, xo, copy_shape(rows, inner, epc), ws + l.xcopy, st), "copy of x"));
   LossArgs a{};
   a.targets = targets; a.target_bytes = target_bytes; a.ignore = ignore;
   a.rows = int32_t(rows); a.vocab = int32_t(outer);
-  a.label = reinterpret_cast<int32_t*>(ws + l.label);
   a.logit = reinterpret_cast<float*>(ws + l.logit);
   a.loss = each ? loss : reinterpret_cast<float*>(ws + l.loss);
   a.lse = lse;
-  if (rows) TRY(done(launch_loss_labels(a, st), "loss labels"));
-  LossArgs b = a;
+  float* const raw = reinterpret_cast<float*>(ws + l.raw);
   const int form = w_transposed ? FORM_RR : FORM_RT;
   for (int64_t r = 0; r < rows; r += l.rows) {
-    const int64_t n = rows - r < l.rows ? rows - r : l.rows;
-    b.label = a.label + r;
+    LossArgs b = a;
+    b.targets = static_cast<const char*>(targets) + r * target_bytes;
     b.logit = a.logit + r;
     b.loss = a.loss + r;
     b.lse = a.lse + r;
-    b.rows = int32_t(n);
+    b.rows = int32_t(rows - r < l.rows ? rows - r : l.rows);
     b.part = reinterpret_cast<float2*>(ws + l.part);
-    b.raw = reinterpret_cast<float*>(ws + l.raw);
-    b.strip = 0;
+    b.raw = raw;
+    b.splits = l.z.splits;
     for (int64_t c = 0; c < outer; c += l.piece) {
+      const int64_t cols = outer - c < l.piece ? outer - c : l.piece;
+      Operand wc = columns(wo, w_transposed, c, es);
+      if (!wf && !few)
+        TRY(done(copy_operand(bf16, wc, copy_of_w(cols, inner, w_transposed, epc), ws + l.wcopy, st), "copy of w"));
       Product p{};
-      p.M = b.rows;
-      p.N = int32_t(outer - c < l.piece ? outer - c : l.piece);
-      p.K = int32_t(inner);
-      p.a = static_cast<const char*>(x) + size_t(r * ldx) * es; p.lda = ldx;
-      p.b = columns(w, ldw, w_transposed, c, es); p.ldb = ldw;
+      p.M = b.rows; p.N = int32_t(cols); p.K = int32_t(inner);
+      p.a = static_cast<const char*>(xo.p) + size_t(r * xo.ld) * es; p.lda = xo.ld;
+      p.b = wc.p; p.ldb = wc.ld;
       b.first = int32_t(c);
       b.cols = p.N;
-      if (l.z.kernel == Choice::SKINNY) {
-        TRY(done(product_sums(l.z, bf16, form, p, reinterpret_cast<float*>(ws + l.raw), scratch, st), "logits"));
-        b.splits = l.z.splits;
+      if (few) {
+        TRY(done(product_sums(l.z, bf16, form, p, raw, st), "logits"));
         TRY(done(launch_loss_strips(b, st), "loss strips"));
       } else {
-        TRY(done(loss_product(l.z, LOSS_STRIPS, bf16, form, p, b, scratch, st), "loss strips"));
+        TRY(done(loss_product(l.z, LOSS_STRIPS, bf16, form, p, b, nullptr, st), "loss strips"));
       }
-      b.strip += int32_t(ceil_div(p.N, strip_columns(l.z)));
+      b.strip += int32_t(ceil_div(cols, strip_columns(l.z)));
     }
     b.strips = b.strip;
     TRY(done(launch_loss_finish(b, st), "loss"));
@@ -470,44 +483,52 @@ MUON_API muon_status muon_linear_cross_entropy_backward(const float* dloss, cons
   TRY(check_ids("targets", targets, target_bytes, rows));
   const size_t es = size_of(dtype);
   const bool bf16 = dtype == MUON_BF16;
-  bool unaligned = false;
+  Operand xo{x, ldx};
+  const Operand wo{w, ldw};
+  bool xf = true, wf = true;
   if (rows) {
     TRY(check_needed("dloss", dloss, 4));
     TRY(check_needed("lse", lse, 4));
     TRY(check_matrix("x", x, ldx, inner, es));
     TRY(check_matrix("w", w, ldw, w_transposed ? inner : outer, es));
     if (dx) TRY(check_matrix("dx", dx, lddx, inner, es));
-    unaligned = !operands_fit(x, ldx, w, ldw, w_transposed, inner, outer, bf16);
+    xf = x_fits(xo, inner, bf16);
+    wf = w_fits(wo, inner, outer, w_transposed, bf16);
   }
   if (dw) TRY(check_matrix("dw", dw, lddw, w_transposed ? inner : outer, es));
-  const LossLayout l = backward_layout(rows, inner, outer, w_transposed, bf16, unaligned);
+  const LossLayout l = backward_layout(rows, inner, outer, w_transposed, bf16, !(xf && wf));
   TRY(check_workspace(workspace, workspace_bytes, l.total));
   const hipStream_t st = hipStream_t(hip_stream);
   char* ws = static_cast<char*>(workspace);
-  const Scratch scratch{ws + l.scratch, l.total - l.scratch};
+  const int64_t epc = bf16 ? 8 : 4;
+  const bool few = l.z.kernel == Choice::SKINNY;
+  if (!xf) TRY(done(copy_operand(bf16, xo, copy_shape(rows, inner, epc), ws + l.xcopy, st), "copy of x"));
   LossArgs a{};
   a.targets = targets; a.target_bytes = target_bytes; a.ignore = ignore;
   a.rows = int32_t(rows); a.vocab = int32_t(outer);
-  a.label = reinterpret_cast<int32_t*>(ws + l.label);
-  a.grad = reinterpret_cast<float*>(ws + l.grad);
-  a.alpha = reinterpret_cast<float*>(ws + l.alpha);
   a.dloss = dloss;
   a.each = reduction == MUON_LOSS_ROWS;
-  a.mean = reduction == MUON_LOSS_MEAN;
   a.lse = const_cast<float*>(lse);
   if (!rows && !dw) return done(hipSuccess, "");
-  if (rows) TRY(done(launch_loss_labels(a, st), "loss labels"));
+  if (reduction == MUON_LOSS_SUM) a.alpha = dloss;
+  if (reduction == MUON_LOSS_MEAN && rows) {
+    float* const alpha = reinterpret_cast<float*>(ws + l.alpha);
+    TRY(done(launch_loss_mean(a, alpha, st), "loss mean"));
+    a.alpha = alpha;
+  }
   const int64_t lddz = ceil_div(l.piece, 8) * 8;
-  float* raw = reinterpret_cast<float*>(ws + l.raw);
-  float* sums = reinterpret_cast<float*>(ws + l.dx);
+  float* const raw = reinterpret_cast<float*>(ws + l.raw);
+  float* const sums = reinterpret_cast<float*>(ws + l.dx);
   for (int64_t c = 0; c < outer; c += l.piece) {
     const int64_t cols = outer - c < l.piece ? outer - c : l.piece;
-    const void* wc = columns(w, ldw, w_transposed, c, es);
+    Operand wc = columns(wo, w_transposed, c, es);
+    if (!wf && !(few && l.x.kernel == Choice::SKINNY))
+      TRY(done(copy_operand(bf16, wc, copy_of_w(cols, inner, w_transposed, epc), ws + l.wcopy, st), "copy of w"));
     for (int64_t r = 0; r < rows; r += l.rows) {
       LossArgs b = a;
       b.rows = int32_t(rows - r < l.rows ? rows - r : l.rows);
-      b.label = a.label + r;
-      b.grad = a.grad + r;
+      b.targets = static_cast<const char*>(targets) + r * target_bytes;
+      b.dloss = a.each ? dloss + r : dloss;
       b.lse = a.lse + r;
       b.raw = raw;
       b.splits = l.z.splits;
@@ -517,44 +538,39 @@ MUON_API muon_status muon_linear_cross_entropy_backward(const float* dloss, cons
       b.cols = int32_t(cols);
       Product p{};
       p.M = b.rows; p.N = b.cols; p.K = int32_t(inner);
-      p.a = static_cast<const char*>(x) + size_t(r * ldx) * es; p.lda = ldx;
-      p.b = wc; p.ldb = ldw;
+      p.a = static_cast<const char*>(xo.p) + size_t(r * xo.ld) * es; p.lda = xo.ld;
+      p.b = wc.p; p.ldb = wc.ld;
       p.c = b.dz; p.ldc = lddz;
       const int form = w_transposed ? FORM_RR : FORM_RT;
-      if (l.z.kernel == Choice::SKINNY) {
-        TRY(done(product_sums(l.z, bf16, form, p, raw, scratch, st), "logits"));
+      if (few) {
+        TRY(done(product_sums(l.z, bf16, form, p, raw, st), "logits"));
         TRY(done(launch_loss_grad(bf16, b, st), "loss gradient"));
       } else {
-        TRY(done(loss_product(l.z, LOSS_GRAD, bf16, form, p, b, scratch, st), "loss gradient"));
+        TRY(done(loss_product(l.z, LOSS_GRAD, bf16, form, p, b, nullptr, st), "loss gradient"));
       }
     }
-    const int32_t pad = int32_t(ceil_div(cols, 8) * 8);
     if (dx && rows) {
       Product p{};
       p.M = int32_t(rows); p.N = int32_t(inner); p.K = int32_t(cols);
-      p.a = ws + l.dz; p.lda = lddz; p.pad_a = pad;
-      p.b = wc; p.ldb = ldw;
+      p.a = ws + l.dz; p.lda = lddz;
+      p.b = wc.p; p.ldb = wc.ld;
       p.add = c > 0;
-      TRY(done(product_sums(l.x, bf16, w_transposed ? FORM_RT : FORM_RR, p, sums, scratch, st),
-               "loss input gradient"));
+      TRY(done(product_sums(l.x, bf16, w_transposed ? FORM_RT : FORM_RR, p, sums, st), "loss input gradient"));
     }
     if (dw) {
       Product p{};
       p.K = int32_t(rows);
-      p.c = const_cast<void*>(columns(dw, lddw, w_transposed, c, es)); p.ldc = lddw;
+      p.c = const_cast<void*>(columns(Operand{dw, lddw}, w_transposed, c, es).p); p.ldc = lddw;
       if (w_transposed) {
-        p.a = ws + l.dz; p.lda = lddz; p.pad_a = pad;
-        p.b = x; p.ldb = ldx;
+        p.a = ws + l.dz; p.lda = lddz;
+        p.b = xo.p; p.ldb = xo.ld;
         p.M = int32_t(cols); p.N = int32_t(inner);
       } else {
-        p.a = x; p.lda = ldx;
-        p.b = ws + l.dz; p.ldb = lddz; p.pad_b = pad;
+        p.a = xo.p; p.lda = xo.ld;
+        p.b = ws + l.dz; p.ldb = lddz;
         p.M = int32_t(inner); p.N = int32_t(cols);
       }
-      // (without rows there is no alpha, and dw is 0)
-      TRY(done(rows ? loss_product(l.w, LOSS_WEIGHT, bf16, FORM_TT, p, a, scratch, st)
-                    : product_by(l.w, bf16, FORM_TT, GROUP_NONE, p, nullptr, scratch, st),
-               "loss weight gradient"));
+      TRY(done(loss_product(l.w, LOSS_WEIGHT, bf16, FORM_TT, p, a, ws + l.scratch, st), "loss weight gradient"));
     }
   }
   if (dx && rows)
