@@ -10,6 +10,8 @@ from __future__ import annotations
 
 import ctypes
 import math
+from array import array
+from itertools import chain, repeat
 from typing import List, Optional, Sequence, Tuple, Union
 
 import torch
@@ -59,24 +61,45 @@ def _check_state(state: State, n: int, i, device) -> int:
     return 8 if small else 32
 
 
-def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]], states: Sequence[State], *,
-               step: Union[int, Sequence[int]], lr: float, betas: Tuple[float, float] = (0.9, 0.999),
-               eps: float = 1e-8, weight_decay: float = 0.01, seed: int = 0) -> None:
-    """One AdamW step of params (fp32 or bf16, contiguous, any shapes) in place, with
-    their gradients (fp32 or bf16; None: the tensor is left as it is) and states
-    (``new_state``; all of 32 bits or all of 8), which move on too.  ``step`` counts
-    from 1 and is one number or one for each tensor; ``seed`` varies the rounding of 8-bit
-    states.  All tensors are on one GPU and do not overlap."""
-    n = len(params)
-    if len(grads) != n or len(states) != n:
-        raise ValueError(f"{n} params, {len(grads)} grads and {len(states)} states")
-    if not n:
-        return
-    steps = [int(step)] * n if not isinstance(step, (list, tuple)) else [int(s) for s in step]
-    if len(steps) != n:
-        raise ValueError(f"{len(steps)} steps for {n} params")
+_CODES = {(p, g): pc | gc << 32 for p, pc in _DTYPES.items() for g, gc in _DTYPES.items()}
+_contiguous, _numel, _device, _pointer = (getattr(torch.Tensor, f) for f in ("is_contiguous", "numel", "get_device",
+                                                                            "data_ptr"))
+
+
+def _all_alike(params, grads, states, steps):
+    """(the library's words of the tensors, the device's index, bits) where every
+    check passes; None where one may not, which ``_one_by_one`` then names.  A step
+    over many small tensors is bound by these checks: taken list by list they cost 1 us a
+    tensor, one by one 2."""
+    try:
+        small = len(states[0]) == 3
+        if small:
+            m, v, b = zip(*states)
+        else:
+            m, v = zip(*states)
+            b = ()
+        every = [*params, *grads, *m, *v, *b]
+        devices = set(map(_device, every))
+        n = [*map(_numel, params)]
+        if len(devices) != 1 or -1 in devices or not all(map(_contiguous, every)) or n != [*map(_numel, m)] or \
+                n != [*map(_numel, v)] or [p.shape for p in params] != [g.shape for g in grads] or \
+                {t.dtype for t in m + v} != {torch.uint8 if small else torch.float32}:
+            return None
+        if small and ({t.dtype for t in b} != {torch.int16} or
+                      [t.shape for t in b] != [(-(-k // AL.MUON_ADAMW_BLOCK), 2) for k in n]):
+            return None
+        codes = [_CODES[p.dtype, g.dtype] for p, g in zip(params, grads)]
+        at = [map(_pointer, t) for t in (params, grads, m, v)]
+        return array("q", chain.from_iterable(zip(*at, map(_pointer, b) if small else repeat(0), n, steps, codes))), \
+            devices.pop(), 8 if small else 32
+    except (TypeError, ValueError, KeyError, AttributeError, RuntimeError):
+        return None
+
+
+def _one_by_one(params, grads, states, steps):
+    """The same, with an exception for the first tensor that does not fit."""
     device, bits, words = None, None, []
-    for i in range(n):
+    for i in range(len(params)):
         p, g, s = params[i], grads[i], states[i]
         if not isinstance(p, torch.Tensor):
             raise TypeError(f"param {i} must be a tensor, not {type(p).__name__}")
@@ -110,16 +133,36 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Te
             raise ValueError(f"grad {i} is on {g.device}, expected {device}")
         words += (p.data_ptr(), g.data_ptr(), s[0].data_ptr(), s[1].data_ptr(), s[2].data_ptr() if b == 8 else 0,
                   p.numel(), steps[i], pc | gc << 32)
+    return array("q", words), device.index, bits
+
+
+def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]], states: Sequence[State], *,
+               step: Union[int, Sequence[int]], lr: float, betas: Tuple[float, float] = (0.9, 0.999),
+               eps: float = 1e-8, weight_decay: float = 0.01, seed: int = 0) -> None:
+    """One AdamW step of params (fp32 or bf16, contiguous, any shapes) in place, with
+    their gradients (fp32 or bf16; None: the tensor is left as it is) and states
+    (``new_state``; all of 32 bits or all of 8), which move on too.  ``step`` counts
+    from 1 and is one number or one for each tensor; ``seed`` varies the rounding of 8-bit
+    states.  All tensors are on one GPU and do not overlap."""
+    n = len(params)
+    if len(grads) != n or len(states) != n:
+        raise ValueError(f"{n} params, {len(grads)} grads and {len(states)} states")
+    if not n:
+        return
+    steps = [int(step)] * n if not isinstance(step, (list, tuple)) else [int(s) for s in step]
+    if len(steps) != n:
+        raise ValueError(f"{len(steps)} steps for {n} params")
+    found = _all_alike(params, grads, states, steps) or _one_by_one(params, grads, states, steps)
+    words, index, bits = found
     opts = AL.muon_adamw_opts(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), bits,
                               int(seed) & 0xFFFFFFFF)
     lib = AL.load()
-    arr = (ctypes.c_int64 * len(words))(*words)
-    index = device.index
+    at = words.buffer_info()[0]
     if index == torch._C._cuda_getDevice():
-        AL.check(lib.muon_adamw_step(arr, n, ctypes.byref(opts), torch._C._cuda_getCurrentRawStream(index)))
+        AL.check(lib.muon_adamw_step(at, n, ctypes.byref(opts), torch._C._cuda_getCurrentRawStream(index)))
     else:
         with torch.cuda.device(index):
-            AL.check(lib.muon_adamw_step(arr, n, ctypes.byref(opts), torch._C._cuda_getCurrentRawStream(index)))
+            AL.check(lib.muon_adamw_step(at, n, ctypes.byref(opts), torch._C._cuda_getCurrentRawStream(index)))
 
 
 def state_values(state: State) -> Tuple[torch.Tensor, torch.Tensor]:

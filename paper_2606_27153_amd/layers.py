@@ -698,9 +698,9 @@ def sort_by_expert(experts: torch.Tensor, count: int) -> Routing:
         if n < 1 or n > LL.MUON_GROUPED_MAX_EXPERTS:
             raise ValueError(f"{name} {n}; 1 to {LL.MUON_GROUPED_MAX_EXPERTS} are supported")
     stream = _stream(experts)
-    n = tokens * top
-    new = lambda *s: torch.empty(s, dtype=torch.int32, device=experts.device)
-    routing = Routing(new(count + 1), new(tokens, top), new(n))
+    i32 = torch.int32
+    routing = Routing(experts.new_empty((count + 1,), dtype=i32), experts.new_empty((tokens, top), dtype=i32),
+                      experts.new_empty((tokens * top,), dtype=i32))
     need = _bytes("muon_sort_by_expert_workspace_bytes", tokens, top)
     ws = _workspace(need, experts)
     LL.check(lib.muon_sort_by_expert(ip, size, tokens, top, count, routing.offsets.data_ptr(),
