@@ -1,16 +1,16 @@
 """Trains one transformer feed-forward block on synthetic data with this
-library's layer operators and its Muon step, then serves single tokens.
+library's layer operators, its Muon step and its AdamW step, then serves single tokens.
 
     python examples/train_block.py --block mlp
     python examples/train_block.py --block moe --experts 8 --top 2 --steps 50
 
 The block is pre-norm: ``x + down(act(up(norm(x))))``, either one MLP (bias and
 GELU fused into the first product, bias and the residual into the second) or a
-bank of experts (rows sorted by expert, gate and up projections, SiLU gating, the
-experts' outputs weighted and added back).  It learns to imitate a block of the
-same kind with other weights.  ``Muon`` steps the 2-D weights, whose gradients
-the backward passes leave in the layout the step reads; the norm's and the biases'
-vectors take plain SGD.
+bank of experts (the router's choices sorted by expert, tokens dispatched to their
+experts, gate and up projections, SiLU gating, the experts' outputs weighted and
+combined with the residual).  It learns to imitate a block of the same kind with
+other weights.  ``Muon`` steps the 2-D weights, whose gradients the backward passes
+leave in the layout the step reads; ``AdamW`` the norm's and the biases' vectors.
 """
 import argparse
 import math
@@ -21,7 +21,7 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
-from paper_2606_27153_amd import Muon, layers  # noqa: E402
+from paper_2606_27153_amd import AdamW, Muon, layers  # noqa: E402
 
 
 class Mlp(torch.nn.Module):
@@ -53,26 +53,18 @@ class Experts(torch.nn.Module):
         self.router = par(width, experts, std=width ** -0.5)
         self.gate, self.up, self.down = bank(width, hidden), bank(width, hidden), bank(hidden, width)
 
-    def route(self, h):
-        """Rows sorted by expert, entirely on the GPU: (row of each slot, weight
-        of each slot, offsets of the experts)."""
-        score = torch.softmax(layers.linear(h, self.router).float(), dim=-1)
-        weight, expert = torch.topk(score, self.top, dim=-1)
-        order = torch.argsort(expert.flatten(), stable=True)
-        edges = torch.arange(len(self.gate) + 1, device=h.device)
-        offsets = torch.searchsorted(expert.flatten()[order], edges).to(torch.int32)
-        return order // self.top, weight.flatten()[order], offsets
-
     def forward(self, x):
         h = layers.layer_norm(x, self.norm_w, self.norm_b)
-        rows, weight, offsets = self.route(h)
-        slots = h[rows]
-        g = layers.grouped_linear(slots, list(self.gate), offsets)
-        u = layers.grouped_linear(slots, list(self.up), offsets)
+        score = torch.softmax(layers.linear(h, self.router).float(), dim=-1)
+        weight, expert = torch.topk(score, self.top, dim=-1)
+        # entirely on the GPU: the host never sees which expert has how many rows
+        routing = layers.sort_by_expert(expert, len(self.gate))
+        rows = layers.dispatch(h, routing)
+        g = layers.grouped_linear(rows, list(self.gate), routing.offsets)
+        u = layers.grouped_linear(rows, list(self.up), routing.offsets)
         a = (torch.nn.functional.silu(g.float()) * u.float()).to(x.dtype)
-        y = layers.grouped_linear(a, list(self.down), offsets)
-        out = torch.zeros(x.shape, dtype=torch.float32, device=x.device)
-        return (x.float() + out.index_add(0, rows, y.float() * weight[:, None])).to(x.dtype)
+        y = layers.grouped_linear(a, list(self.down), routing.offsets)
+        return layers.combine(y, weight, routing, residual=x)
 
 
 def make(args, device):
@@ -92,7 +84,7 @@ def train(args, log=print):
     matrices = [p for n, p in block.named_parameters() if p.ndim == 2 and n != "router"]
     vectors = [p for p in block.parameters() if p.ndim == 1]
     opt = Muon(matrices, lr=args.lr, momentum=0.95, weight_decay=0.0)
-    sgd = torch.optim.SGD(vectors, lr=args.lr)
+    adamw = AdamW(vectors, lr=0.1 * args.lr, weight_decay=0.0)
     losses = []
     for step in range(args.steps):
         x = torch.randn(args.tokens, args.width, device=device).to(block.norm_w.dtype if args.dtype == "f32"
@@ -102,14 +94,13 @@ def train(args, log=print):
         # the residual is the same on both sides
         loss = ((block(x).float() - want) ** 2).mean()
         opt.zero_grad()
-        sgd.zero_grad()
+        adamw.zero_grad()
         loss.backward()
         scale = 0.5 * (1 + math.cos(math.pi * step / args.steps))
-        for o in (opt, sgd):
+        for o, lr in ((opt, args.lr), (adamw, 0.1 * args.lr)):
             for g in o.param_groups:
-                g["lr"] = args.lr * scale
-        opt.step()
-        sgd.step()
+                g["lr"] = lr * scale
+            o.step()
         losses.append(loss.detach())
         if step % max(1, args.steps // 10) == 0 or step == args.steps - 1:
             log(f"step {step:4d}  loss {float(losses[-1]):.5f}")

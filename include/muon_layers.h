@@ -238,8 +238,8 @@ MUON_API muon_status muon_linear_cross_entropy_backward(const float* dloss, cons
                                                         void* hip_stream);
 
 /* Workspace bytes of either pass (flags: MUON_LAYERS_BACKWARD,
- * MUON_LAYERS_UNALIGNED -- which these passes need where x or w are off 16-byte
- * chunks). */
+ * MUON_LAYERS_UNALIGNED -- which these passes need where rows of x or w are not
+ * whole, aligned 16-byte chunks, or lie 2^23 bytes or more apart). */
 MUON_API muon_status muon_linear_cross_entropy_workspace_bytes(int64_t rows, int64_t inner, int64_t outer,
                                                                int32_t dtype, int32_t flags, size_t* bytes);
 

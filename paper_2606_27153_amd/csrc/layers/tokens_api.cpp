@@ -64,9 +64,10 @@ RouteArgs route_args(int64_t tokens, int64_t top, int64_t cols, const int32_t* p
 
 // -------------------------------------------------------------------- loss
 
-// Rows of a forward pass at a time: its strips' sums take 8 bytes a row and 128
-// columns or so.
+// Rows at a time, fewer in a forward pass over a very large vocabulary: its strips'
+// sums take 8 bytes a row and 128 columns or so, 1 GB in all.
 constexpr int64_t kLossRows = 32768;
+constexpr int64_t kLossSums = int64_t(1) << 27;
 // Columns of a piece: as many as one grid has tiles for; where the weight has to
 // be copied, fewer, so that the copy stays small; of a gradient piece, 2^29 elements at most
 // (and 2048 columns at least).
@@ -155,7 +156,9 @@ void take_copies(LossLayout& l, int64_t rows, int64_t inner, bool w_transposed, 
 
 LossLayout forward_layout(int64_t rows, int64_t inner, int64_t outer, bool w_transposed, bool bf16, bool unaligned) {
   LossLayout l;
-  l.rows = rows < kLossRows ? rows : kLossRows;
+  int64_t most = kLossSums / ceil_div(outer, 128);
+  most = most < 256 ? 256 : most > kLossRows ? kLossRows : most;
+  l.rows = rows < most ? rows : most;
   l.piece = even_piece(outer, unaligned ? kCopyPiece : kPiece);
   l.z = choose_logits(bf16, w_transposed, l.rows, l.piece, inner);
   l.take(l.logit, size_t(rows) * 4);

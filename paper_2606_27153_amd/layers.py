@@ -871,6 +871,13 @@ def _reduction(name: str) -> int:
     return code
 
 
+def _loss_flags(backward: int, x: torch.Tensor, outer: int, xp: int, ldx: int, wp: int, ldw: int) -> int:
+    """_flags, and room for the copies that rows far apart need too."""
+    size = x.element_size()
+    far = 2 if max(ldx, ldw) * size >= 1 << 23 else 0
+    return _flags(backward, x, outer, xp, ldx * size, wp, ldw * size) | far
+
+
 @_on_device
 def linear_cross_entropy_forward(x: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, *,
                                  reduction: str = "mean", ignore_index: int = -100):
@@ -894,9 +901,8 @@ def linear_cross_entropy_forward(x: torch.Tensor, weight: torch.Tensor, targets:
     stream = _stream(x)
     lse = x.new_empty((rows,), dtype=torch.float32)
     loss = x.new_empty((rows,) if red == 0 else (), dtype=torch.float32)
-    size = x.element_size()
     need = _bytes("muon_linear_cross_entropy_workspace_bytes", rows, inner, outer, code,
-                  _flags(0, x, outer, xp, ldx * size, wp, ldw * size))
+                  _loss_flags(0, x, outer, xp, ldx, wp, ldw))
     ws = _workspace(need, x)
     LL.check(lib.muon_linear_cross_entropy_forward(xp, ldx, wp, ldw, wt, tp, tsize, ignore, red, loss.data_ptr(),
                                                    lse.data_ptr(), rows, inner, outer, code,
@@ -931,9 +937,8 @@ def linear_cross_entropy_backward(dloss: torch.Tensor, x: torch.Tensor, weight: 
     stream = _stream(x)
     dx = x.new_empty((rows, inner)) if input_grad else None
     dw = _like_weight(weight, wt) if weight_grad else None
-    size = x.element_size()
     need = _bytes("muon_linear_cross_entropy_workspace_bytes", rows, inner, outer, code,
-                  _flags(1, x, outer, xp, ldx * size, wp, ldw * size))
+                  _loss_flags(1, x, outer, xp, ldx, wp, ldw))
     ws = _workspace(need, x)
     LL.check(lib.muon_linear_cross_entropy_backward(dloss.data_ptr(), xp, ldx, wp, ldw, wt, tp, tsize, ignore, red,
                                                     lse.data_ptr(), None if dx is None else dx.data_ptr(), inner,
