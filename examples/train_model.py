@@ -72,7 +72,7 @@ def train(args, log=print):
             o.step()
         losses.append(loss.detach())
         if step % max(1, args.steps // 10) == 0 or step == args.steps - 1:
-            log(f"step {step:4d}  loss {float(loss):.5f}")
+            log(f"step {step:4d}  loss {float(losses[-1]):.5f}")
     return [float(v) for v in losses], model
 
 
