@@ -48,7 +48,7 @@ typedef struct muon_adamw_tensor {
   void* exp_avg;       /* n fp32, or n codes */
   void* exp_avg_sq;    /* n fp32, or n codes */
   int16_t* bases;      /* 8 bits: the bases of exp_avg and exp_avg_sq, a pair for each block */
-  int64_t n;           /* elements, 0 to 2^40 */
+  int64_t n;           /* elements, 0 to 2^35 */
   int64_t step;        /* from 1 on */
   int32_t param_dtype; /* MUON_F32 or MUON_BF16 */
   int32_t grad_dtype;

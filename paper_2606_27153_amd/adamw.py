@@ -89,7 +89,9 @@ def _all_alike(params, grads, states, steps):
                       [t.shape for t in b] != [(-(-k // AL.MUON_ADAMW_BLOCK), 2) for k in n]):
             return None
         codes = [_CODES[p.dtype, g.dtype] for p, g in zip(params, grads)]
-        at = [map(_pointer, t) for t in (params, grads, m, v)]
+        at = [[*map(_pointer, params)], *(map(_pointer, t) for t in (grads, m, v))]
+        if len({*at[0]}) != len(n):     # (the same tensor twice, or several without elements)
+            return None
         return array("q", chain.from_iterable(zip(*at, map(_pointer, b) if small else repeat(0), n, steps, codes))), \
             devices.pop(), 8 if small else 32
     except (TypeError, ValueError, KeyError, AttributeError, RuntimeError):
@@ -98,7 +100,7 @@ def _all_alike(params, grads, states, steps):
 
 def _one_by_one(params, grads, states, steps):
     """The same, with an exception for the first tensor that does not fit."""
-    device, bits, words = None, None, []
+    device, bits, words, seen = None, None, [], {}
     for i in range(len(params)):
         p, g, s = params[i], grads[i], states[i]
         if not isinstance(p, torch.Tensor):
@@ -114,6 +116,8 @@ def _one_by_one(params, grads, states, steps):
             raise ValueError(f"param {i} is on {p.device}, expected {device}")
         if not p.is_contiguous():
             raise ValueError(f"param {i} is not contiguous (stride {p.stride()})")
+        if p.numel() and seen.setdefault(p.data_ptr(), i) != i:
+            raise ValueError(f"param {i} is param {seen[p.data_ptr()]} again")
         b = _check_state(s, p.numel(), i, device)
         if bits is None:
             bits = b

@@ -31,8 +31,8 @@ muon_status done(hipError_t e, const char* what) {
     if (try_st != MUON_OK) return try_st; \
   } while (0)
 
-constexpr int64_t kMaxElements = int64_t(1) << 40;
-constexpr int64_t kMaxBlocks = (int64_t(1) << 31) - 1;
+constexpr int64_t kMaxElements = int64_t(1) << 35;
+constexpr int64_t kMaxBlocks = (int64_t(1) << 24) - 1;   // of 256 threads that one grid holds
 
 muon_status check_pointer(const char* name, int32_t i, const void* p, size_t align) {
   if (!p) return fail(MUON_ERR_INVALID_ARG, "tensor %d: %s is NULL", i, name);
@@ -46,7 +46,7 @@ bool known(int32_t dtype) { return dtype == MUON_F32 || dtype == MUON_BF16; }
 
 muon_status check_tensor(const muon_adamw_tensor& t, int32_t i, int32_t bits) {
   if (t.n < 0 || t.n > kMaxElements)
-    return fail(MUON_ERR_INVALID_ARG, "tensor %d: n %lld out of [0, 2^40]", i, (long long)t.n);
+    return fail(MUON_ERR_INVALID_ARG, "tensor %d: n %lld out of [0, 2^35]", i, (long long)t.n);
   if (!known(t.param_dtype) || !known(t.grad_dtype))
     return fail(MUON_ERR_UNSUPPORTED, "tensor %d: dtypes %d and %d: MUON_F32 or MUON_BF16", i, t.param_dtype,
                 t.grad_dtype);
@@ -131,7 +131,7 @@ MUON_API muon_status muon_adamw_step(const muon_adamw_tensor* tensors, int32_t c
 
 MUON_API muon_status muon_adamw_state_values(const void* exp_avg, const void* exp_avg_sq, const int16_t* bases,
                                              int64_t n, void* exp_avg_out, void* exp_avg_sq_out, void* hip_stream) {
-  if (n < 0 || n > kMaxElements) return fail(MUON_ERR_INVALID_ARG, "n %lld out of [0, 2^40]", (long long)n);
+  if (n < 0 || n > kMaxElements) return fail(MUON_ERR_INVALID_ARG, "n %lld out of [0, 2^35]", (long long)n);
   if (!n || (!exp_avg_out && !exp_avg_sq_out)) return done(hipSuccess, "");
   TRY(check_pointer("bases", 0, bases, 2));
   if (exp_avg_out) {

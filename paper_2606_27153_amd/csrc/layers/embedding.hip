@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256) void table_grad_kernel(EmbeddingArgs a) {
 template <typename E, bool WHOLE>
 hipError_t forward(const EmbeddingArgs& a, hipStream_t st) {
   const int64_t blocks = (int64_t(a.rows) * ((a.cols + 7) / 8) + 255) / 256;
-  if (blocks >= (int64_t(1) << 31)) return hipErrorInvalidConfiguration;
+  if (blocks >= kMaxGrid) return hipErrorInvalidConfiguration;
   if (blocks) hipLaunchKernelGGL((lookup_kernel<E, WHOLE>), dim3{unsigned(blocks)}, dim3{256}, 0, st, a);
   return hipGetLastError();
 }
@@ -172,6 +172,9 @@ hipError_t forward(const EmbeddingArgs& a, hipStream_t st) {
 template <typename E, bool WHOLE>
 hipError_t backward(EmbeddingArgs a, int32_t* const (&keys)[2], int32_t* const (&index)[2], int32_t* counts,
                     hipStream_t st) {
+  const int64_t groups = a.rows / kRun, starts = (int64_t(a.vocab) + 256) / 256;
+  const int64_t blocks = ((int64_t(a.vocab) + kRows - 1) / kRows * ((a.cols + 7) / 8) + 255) / 256;
+  if (blocks >= kMaxGrid || groups >= kMaxGrid) return hipErrorInvalidConfiguration;
   int at = 0;
   for (int shift = 0; a.rows && (shift == 0 || (a.vocab >> shift)); shift += kSortBits, at ^= 1) {
     TokenJob job{};
@@ -192,12 +195,9 @@ hipError_t backward(EmbeddingArgs a, int32_t* const (&keys)[2], int32_t* const (
   a.keys = keys[at ^ 1];
   a.index = index[at ^ 1];
   if (a.rows) {
-    const int64_t groups = a.rows / kRun, starts = (int64_t(a.vocab) + 256) / 256;
     const dim3 g{unsigned(groups > starts ? groups : starts), unsigned((a.cols + 2047) / 2048 + 1)};
     hipLaunchKernelGGL((group_kernel<E, WHOLE>), g, dim3{256}, 0, st, a, int(groups));
   }
-  const int64_t blocks = ((int64_t(a.vocab) + kRows - 1) / kRows * ((a.cols + 7) / 8) + 255) / 256;
-  if (blocks >= (int64_t(1) << 31)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((table_grad_kernel<E, WHOLE>), dim3{unsigned(blocks)}, dim3{256}, 0, st, a);
   return hipGetLastError();
 }

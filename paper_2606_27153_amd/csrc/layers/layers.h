@@ -25,6 +25,7 @@ enum Form {
 };
 
 constexpr int kCUs = 256;   // of an MI355X
+constexpr int64_t kMaxGrid = int64_t(1) << 24;   // blocks of 256 threads that one grid holds
 
 enum Group {
   GROUP_NONE = 0,
@@ -167,9 +168,9 @@ hipError_t launch_loss_strips(const LossArgs& a, hipStream_t st);   // raw -> pa
 hipError_t launch_loss_finish(const LossArgs& a, hipStream_t st);   // part -> lse and loss
 hipError_t launch_loss_total(const LossArgs& a, hipStream_t st);    // loss -> total
 hipError_t launch_loss_grad(bool bf16, const LossArgs& a, hipStream_t st);   // raw -> dz
-// y = *alpha times the sum of `splits` partial results of rows x cols
-hipError_t launch_loss_sum(bool bf16, const float* part, int splits, const float* alpha, void* y, int64_t ldy,
-                           int64_t rows, int64_t cols, hipStream_t st);
+// y: alpha times the sum of `splits` partial results of a.rows x cols, 0 in rows without a target
+hipError_t launch_loss_sum(bool bf16, const LossArgs& a, const float* part, int splits, void* y, int64_t ldy,
+                           int64_t cols, hipStream_t st);
 
 hipError_t launch_simple(bool bf16, int form, int group, const Product& p, const Table* t, hipStream_t st);
 

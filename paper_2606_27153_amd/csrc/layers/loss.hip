@@ -187,24 +187,27 @@ __global__ __launch_bounds__(256) void grad_kernel(LossArgs a) {
   store8(static_cast<E*>(a.dz) + row * a.lddz + c, 8, v);
 }
 
+// The input's gradient: the partial results added up, times alpha; 0 in rows without a target
+// (also where a weight that is not finite or an infinite alpha would leave NaN).
 template <typename E>
-__global__ __launch_bounds__(256) void sum_kernel(const float* part, int splits, const float* alpha, E* y, int64_t ldy,
-                                                  int64_t rows, int64_t cols) {
+__global__ __launch_bounds__(256) void sum_kernel(LossArgs a, const float* part, int splits, E* y, int64_t ldy,
+                                                  int64_t cols) {
   const int64_t chunks = (cols + 7) / 8, i = int64_t(blockIdx.x) * 256 + threadIdx.x, r = i / chunks;
-  if (r >= rows) return;
+  if (r >= a.rows) return;
   const int64_t c = (i - r * chunks) * 8;
   const int n = int(min(int64_t(8), cols - c));
-  const float f = alpha ? *alpha : 1.f;
+  const float f = a.alpha ? *a.alpha : 1.f;
+  const bool live = label_of(a, r) >= 0;
   float v[8];
   load8(part + r * cols + c, n, v);
   for (int s = 1; s < splits; ++s) {
     float x[8];
-    load8(part + (s * rows + r) * cols + c, n, x);
+    load8(part + (int64_t(s) * a.rows + r) * cols + c, n, x);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += x[e];
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] *= f;
+  for (int e = 0; e < 8; ++e) v[e] = live ? v[e] * f : 0.f;
   store8(y + r * ldy + c, n, v);
 }
 
@@ -247,17 +250,15 @@ hipError_t launch_loss_grad(bool bf16, const LossArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_loss_sum(bool bf16, const float* part, int splits, const float* alpha, void* y, int64_t ldy,
-                           int64_t rows, int64_t cols, hipStream_t st) {
-  const int64_t blocks = (rows * ((cols + 7) / 8) + 255) / 256;
-  if (blocks >= (int64_t(1) << 31)) return hipErrorInvalidConfiguration;
-  const dim3 g{unsigned(blocks)};
+hipError_t launch_loss_sum(bool bf16, const LossArgs& a, const float* part, int splits, void* y, int64_t ldy,
+                           int64_t cols, hipStream_t st) {
+  const int64_t blocks = (a.rows * ((cols + 7) / 8) + 255) / 256;
+  if (blocks >= kMaxGrid) return hipErrorInvalidConfiguration;
+  const dim3 g{unsigned(blocks)}, b{256};
   if (bf16)
-    hipLaunchKernelGGL((sum_kernel<__bf16>), g, dim3{256}, 0, st, part, splits, alpha, static_cast<__bf16*>(y), ldy,
-                       rows, cols);
+    hipLaunchKernelGGL((sum_kernel<__bf16>), g, b, 0, st, a, part, splits, static_cast<__bf16*>(y), ldy, cols);
   else
-    hipLaunchKernelGGL((sum_kernel<float>), g, dim3{256}, 0, st, part, splits, alpha, static_cast<float*>(y), ldy,
-                       rows, cols);
+    hipLaunchKernelGGL((sum_kernel<float>), g, b, 0, st, a, part, splits, static_cast<float*>(y), ldy, cols);
   return hipGetLastError();
 }
 

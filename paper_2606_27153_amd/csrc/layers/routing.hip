@@ -173,7 +173,7 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(RouteArgs a) {
 
 bool grid_of(int64_t blocks, dim3& g) {
   g = dim3{unsigned(blocks)};
-  return blocks < (int64_t(1) << 31);
+  return blocks < kMaxGrid;
 }
 
 template <typename E, bool WHOLE>

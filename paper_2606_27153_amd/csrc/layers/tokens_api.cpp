@@ -577,7 +577,7 @@ MUON_API muon_status muon_linear_cross_entropy_backward(const float* dloss, cons
     }
   }
   if (dx && rows)
-    TRY(done(launch_loss_sum(bf16, sums, l.x.splits, a.alpha, dx, lddx, rows, inner, st), "loss input gradient"));
+    TRY(done(launch_loss_sum(bf16, a, sums, l.x.splits, dx, lddx, inner, st), "loss input gradient"));
   return done(hipSuccess, "");
 }
 

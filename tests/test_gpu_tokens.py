@@ -255,6 +255,14 @@ def test_loss_without_targets_and_with_extreme_logits(dtype):
         assert torch.isfinite(loss)
         dx, dw = layers.linear_cross_entropy_backward(torch.ones((), device=DEV), nan, w, t, lse)
         assert (dx[2] == 0).all() and torch.isfinite(dx).all()
+        # an infinite gradient and a weight that is not finite leave such rows' gradients alone too
+        inf = torch.full((), float("inf"), device=DEV)
+        w9 = w.clone()
+        w9[3, 7] = float("nan")
+        for weight, d in ((w, inf), (w9, inf / inf)):
+            dx, _ = layers.linear_cross_entropy_backward(d, x, weight, t, lse.nan_to_num())
+            live = (t >= 0) & (t < vocab)
+            assert (dx[~live] == 0).all() and not torch.isfinite(dx[live]).all(1).any()
         # -inf columns (a vocabulary masked through its weight) have probability 0
         x1 = torch.cat([x.abs(), torch.ones(rows, 8, device=DEV, dtype=dtype)], 1)
         w1 = torch.cat([w, torch.zeros(8, vocab, device=DEV, dtype=dtype)])

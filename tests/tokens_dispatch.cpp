@@ -134,9 +134,9 @@ hipError_t launch_loss_grad(bool bf16, const LossArgs& a, hipStream_t) {
   g_words += std::string(" dz/rows/") + (bf16 ? "bf16" : "f32");
   return hipSuccess;
 }
-hipError_t launch_loss_sum(bool, const float* part, int splits, const float*, void*, int64_t, int64_t rows,
-                           int64_t cols, hipStream_t) {
-  span("sums", part, size_t(splits) * rows * cols * 4);
+hipError_t launch_loss_sum(bool, const LossArgs& a, const float* part, int splits, void*, int64_t, int64_t cols,
+                           hipStream_t) {
+  span("sums", part, size_t(splits) * a.rows * cols * 4);
   return hipSuccess;
 }
 hipError_t launch_simple(bool, int, int, const Product&, const Table*, hipStream_t) { return hipErrorInvalidValue; }
