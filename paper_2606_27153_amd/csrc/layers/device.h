@@ -150,6 +150,22 @@ template <bool WHOLE, typename E>
 __device__ __forceinline__ void load_8(const E* p, int n, float (&v)[8]) {
   load8(p, WHOLE ? 8 : n, v);
 }
+// Of data that is read once: past the caches' order of use, which leaves them to what is
+// read again.
+template <bool WHOLE, typename E>
+__device__ __forceinline__ void load_8_once(const E* p, int n, float (&v)[8]) {
+  typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
+  if constexpr (WHOLE) {
+    Words w[sizeof(E) / 2];
+#pragma unroll
+    for (int i = 0; i < int(sizeof(E) / 2); ++i) w[i] = __builtin_nontemporal_load(reinterpret_cast<const Words*>(p) + i);
+    const Packed8<E> x = __builtin_bit_cast(Packed8<E>, w);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = float(x.v[e]);
+  } else {
+    load8(p, n, v);
+  }
+}
 template <bool WHOLE, typename E>
 __device__ __forceinline__ void store_8(E* p, int n, const float (&v)[8]) {
   store8(p, WHOLE ? 8 : n, v);

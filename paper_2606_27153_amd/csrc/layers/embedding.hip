@@ -60,8 +60,10 @@ __global__ __launch_bounds__(256) void lookup_kernel(EmbeddingArgs a) {
 constexpr int kRun = 16;    // places of a group
 constexpr int kRows = 16;   // table rows of a block
 
-// v[0..7] += the gradients of places lo .. hi - 1, in order, 4 in flight.
-template <typename E, bool WHOLE>
+// v[0..7] += the gradients of places lo .. hi - 1, in order, 4 in flight.  ONCE: past the
+// caches' order of use (the groups' 25 us for 41; rows of a few places, next to the
+// table's stores, lose 3%).
+template <typename E, bool WHOLE, bool ONCE>
 __device__ __forceinline__ void add_run(const EmbeddingArgs& a, int lo, int hi, int c, int n, float (&v)[8]) {
   const E* dy = static_cast<const E*>(a.dy) + c;
   for (int p = lo; p < hi; p += 4) {
@@ -70,7 +72,12 @@ __device__ __forceinline__ void add_run(const EmbeddingArgs& a, int lo, int hi, 
 #pragma unroll
     for (int k = 0; k < 4; ++k) row[k] = a.index[min(p + k, hi - 1)];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) load_8<WHOLE>(dy + row[k] * a.lddy, n, x[k]);
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (ONCE)
+        load_8_once<WHOLE>(dy + row[k] * a.lddy, n, x[k]);
+      else
+        load_8<WHOLE>(dy + row[k] * a.lddy, n, x[k]);
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -117,7 +124,7 @@ __global__ __launch_bounds__(256) void group_kernel(EmbeddingArgs a, int groups)
   const int c = ((blockIdx.y - 1) * 256 + threadIdx.x) * 8, n = min(8, a.cols - c);
   if (n <= 0) return;
   float v[8] = {};
-  add_run<E, WHOLE>(a, first, first + kRun, c, n, v);
+  add_run<E, WHOLE, true>(a, first, first + kRun, c, n, v);
   store_8<WHOLE>(a.part + int64_t(blockIdx.x) * a.cols + c, n, v);
 }
 
@@ -149,11 +156,11 @@ __global__ __launch_bounds__(256) void table_grad_kernel(EmbeddingArgs a) {
     float v[8] = {};
     const int g0 = (lo + kRun - 1) / kRun, g1 = hi / kRun;
     if (g0 < g1) {
-      add_run<E, WHOLE>(a, lo, g0 * kRun, c, n, v);
+      add_run<E, WHOLE, false>(a, lo, g0 * kRun, c, n, v);
       add_groups<WHOLE>(a, g0, g1, c, n, v);
-      add_run<E, WHOLE>(a, g1 * kRun, hi, c, n, v);
+      add_run<E, WHOLE, false>(a, g1 * kRun, hi, c, n, v);
     } else {
-      add_run<E, WHOLE>(a, lo, hi, c, n, v);
+      add_run<E, WHOLE, false>(a, lo, hi, c, n, v);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= a.scale;

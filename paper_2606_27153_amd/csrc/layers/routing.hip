@@ -87,7 +87,8 @@ __global__ __launch_bounds__(256) void dispatch_kernel(RouteArgs a) {
 }
 // y[t] = r[t] + sum_j w[t, j] rows[position[t, j]]; without weights, the gradient of
 // dispatch.  K choices' loads are in flight together.  16384 x 2048 tokens of 6 choices
-// 136 us with a residual and 107 without (3.9 and 4.4 TB/s): whole rows of 4 KB from 64 places.
+// 101 us with a residual and 88 without (5.3 TB/s), past the caches' order of use; as
+// ordinary loads 135 and 106.
 template <typename E, int K, bool WHOLE>
 __global__ __launch_bounds__(256) void gather_kernel(RouteArgs a) {
   int64_t t;
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(256) void gather_kernel(RouteArgs a) {
   const int64_t all = int64_t(a.tokens) * a.top;
   const E* rows = static_cast<const E*>(a.rows) + c;
   float v[8] = {};
-  if (a.res) load_8<WHOLE>(static_cast<const E*>(a.res) + t * a.ldres + c, n, v);
+  if (a.res) load_8_once<WHOLE>(static_cast<const E*>(a.res) + t * a.ldres + c, n, v);
   for (int j = 0; j < a.top; j += K) {
     float x[K][8], w[K];
     int p[K];
@@ -108,7 +109,7 @@ __global__ __launch_bounds__(256) void gather_kernel(RouteArgs a) {
       w[k] = weight_of<E>(a, slot);
     }
 #pragma unroll
-    for (int k = 0; k < K; ++k) load_8<WHOLE>(rows + max(p[k], 0) * a.ldr, n, x[k]);
+    for (int k = 0; k < K; ++k) load_8_once<WHOLE>(rows + max(p[k], 0) * a.ldr, n, x[k]);
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
@@ -120,8 +121,8 @@ __global__ __launch_bounds__(256) void gather_kernel(RouteArgs a) {
 // A wave per row: its gradient, and the product of both rows for the weight's.  A row
 // behind the last expert's stands for a choice of no expert: both are 0.  Two chunks of
 // 512 columns are in flight; both large streams go through memory in order, the tokens'
-// gradients come from the cache: 174 us at 16384 x 2048 and 6 choices, 5.0 TB/s (by
-// token, with its gradient in registers, 281).
+// gradients come from the cache: 191 us at 16384 x 2048 and 6 choices, 4.6 TB/s (the
+// rows as ordinary loads 203; by token, with its gradient in registers, 281).
 template <typename E, bool WHOLE>
 __global__ __launch_bounds__(256) void combine_grad_kernel(RouteArgs a) {
   const int lane = threadIdx.x & 63;
@@ -141,9 +142,9 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(RouteArgs a) {
     float g[2][8], x[2][8];
     const int c2 = two ? c + 512 : c;
     load_8<WHOLE>(dy + c, n, g[0]);
-    load_8<WHOLE>(h + c, n, x[0]);
+    load_8_once<WHOLE>(h + c, n, x[0]);
     load_8<WHOLE>(dy + c2, two ? n2 : n, g[1]);
-    load_8<WHOLE>(h + c2, two ? n2 : n, x[1]);
+    load_8_once<WHOLE>(h + c2, two ? n2 : n, x[1]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       dot = fmaf(g[0][e], x[0][e], dot);
