@@ -1,6 +1,7 @@
 """ctypes binding of libmuon_adamw.so (the C ABI declared in
-include/muon_adamw.h).  Argument marshalling only; ``load()`` raises if the
-library has not been built -- there is no fallback path."""
+include/muon_adamw.h), and of the extension that reads its tensors.  Argument
+marshalling only; ``load()`` and ``tensors()`` raise if their library has not been
+built -- there is no fallback path."""
 from __future__ import annotations
 
 import ctypes
@@ -29,7 +30,6 @@ class muon_adamw_opts(ctypes.Structure):
 
 # name -> (restype, argtypes); every function declared in include/muon_adamw.h
 SIGNATURES = {
-    # (the tensors come as one array of 64-bit words, 8 for each)
     "muon_adamw_step": (_ST, [_P, _I32, ctypes.POINTER(muon_adamw_opts), _P]),
     "muon_adamw_state_values": (_ST, [_P, _P, _P, _I64, _P, _P, _P]),
     "muon_adamw_last_error": (ctypes.c_char_p, []),
@@ -37,6 +37,7 @@ SIGNATURES = {
 
 _lock = threading.Lock()
 _lib = None
+_tensors = None
 
 
 def load(path: str = LIB_PATH):
@@ -58,6 +59,20 @@ def load(path: str = LIB_PATH):
             fn.argtypes = args
         _lib = lib
         return lib
+
+
+def tensors():
+    """adamw_tensors(params, grads, states, steps) of csrc/adamw/binding.cpp."""
+    global _tensors
+    if _tensors is None:
+        import torch  # noqa: F401  (whose libraries the extension is linked to)
+        try:
+            from ._adamw_binding import adamw_tensors
+        except ImportError as e:
+            raise RuntimeError(f"_adamw_binding.so cannot be loaded ({e}); build it first with "
+                               f"`python -m paper_2606_27153_amd.build` (there is no fallback path)") from e
+        _tensors = adamw_tensors
+    return _tensors
 
 
 def check(status: int) -> None:

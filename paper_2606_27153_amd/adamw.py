@@ -10,8 +10,6 @@ from __future__ import annotations
 
 import ctypes
 import math
-from array import array
-from itertools import chain, repeat
 from typing import List, Optional, Sequence, Tuple, Union
 
 import torch
@@ -61,46 +59,10 @@ def _check_state(state: State, n: int, i, device) -> int:
     return 8 if small else 32
 
 
-_CODES = {(p, g): pc | gc << 32 for p, pc in _DTYPES.items() for g, gc in _DTYPES.items()}
-_contiguous, _numel, _device, _pointer = (getattr(torch.Tensor, f) for f in ("is_contiguous", "numel", "get_device",
-                                                                            "data_ptr"))
-
-
-def _all_alike(params, grads, states, steps):
-    """(the library's words of the tensors, the device's index, bits) where every
-    check passes; None where one may not, which ``_one_by_one`` then names.  A step
-    over many small tensors is bound by these checks: taken list by list they cost 1 us a
-    tensor, one by one 2."""
-    try:
-        small = len(states[0]) == 3
-        if small:
-            m, v, b = zip(*states)
-        else:
-            m, v = zip(*states)
-            b = ()
-        every = [*params, *grads, *m, *v, *b]
-        devices = set(map(_device, every))
-        n = [*map(_numel, params)]
-        if len(devices) != 1 or -1 in devices or not all(map(_contiguous, every)) or n != [*map(_numel, m)] or \
-                n != [*map(_numel, v)] or [p.shape for p in params] != [g.shape for g in grads] or \
-                {t.dtype for t in m + v} != {torch.uint8 if small else torch.float32}:
-            return None
-        if small and ({t.dtype for t in b} != {torch.int16} or
-                      [t.shape for t in b] != [(-(-k // AL.MUON_ADAMW_BLOCK), 2) for k in n]):
-            return None
-        codes = [_CODES[p.dtype, g.dtype] for p, g in zip(params, grads)]
-        at = [[*map(_pointer, params)], *(map(_pointer, t) for t in (grads, m, v))]
-        if len({*at[0]}) != len(n):     # (the same tensor twice, or several without elements)
-            return None
-        return array("q", chain.from_iterable(zip(*at, map(_pointer, b) if small else repeat(0), n, steps, codes))), \
-            devices.pop(), 8 if small else 32
-    except (TypeError, ValueError, KeyError, AttributeError, RuntimeError):
-        return None
-
-
 def _one_by_one(params, grads, states, steps):
-    """The same, with an exception for the first tensor that does not fit."""
-    device, bits, words, seen = None, None, [], {}
+    """(the library's array of tensors as bytes, the device's index, the states' bits) with
+    an exception for the first tensor that does not fit; gradients may be None."""
+    device, bits, found, seen = None, None, [], {}
     for i in range(len(params)):
         p, g, s = params[i], grads[i], states[i]
         if not isinstance(p, torch.Tensor):
@@ -124,7 +86,7 @@ def _one_by_one(params, grads, states, steps):
         elif b != bits:
             raise ValueError(f"state {i} has {b} bits, the ones before {bits}")
         if g is None:
-            words += (p.data_ptr(), 0, 0, 0, 0, 0, 1, pc | pc << 32)
+            found.append(AL.muon_adamw_tensor(param_dtype=pc, grad_dtype=pc))
             continue
         if not isinstance(g, torch.Tensor):
             raise TypeError(f"grad {i} must be a tensor or None, not {type(g).__name__}")
@@ -135,9 +97,9 @@ def _one_by_one(params, grads, states, steps):
             raise ValueError(f"grad {i} must be contiguous and of param {i}'s shape {tuple(p.shape)}")
         if g.device != device:
             raise ValueError(f"grad {i} is on {g.device}, expected {device}")
-        words += (p.data_ptr(), g.data_ptr(), s[0].data_ptr(), s[1].data_ptr(), s[2].data_ptr() if b == 8 else 0,
-                  p.numel(), steps[i], pc | gc << 32)
-    return array("q", words), device.index, bits
+        found.append(AL.muon_adamw_tensor(p.data_ptr(), g.data_ptr(), s[0].data_ptr(), s[1].data_ptr(),
+                                          s[2].data_ptr() if b == 8 else None, p.numel(), steps[i], pc, gc))
+    return b"".join(map(bytes, found)), device.index, bits
 
 
 def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]], states: Sequence[State], *,
@@ -156,17 +118,15 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Te
     steps = [int(step)] * n if not isinstance(step, (list, tuple)) else [int(s) for s in step]
     if len(steps) != n:
         raise ValueError(f"{len(steps)} steps for {n} params")
-    found = _all_alike(params, grads, states, steps) or _one_by_one(params, grads, states, steps)
-    words, index, bits = found
+    tensors, index, bits = AL.tensors()(params, grads, states, steps) or _one_by_one(params, grads, states, steps)
     opts = AL.muon_adamw_opts(float(lr), float(betas[0]), float(betas[1]), float(eps), float(weight_decay), bits,
                               int(seed) & 0xFFFFFFFF)
     lib = AL.load()
-    at = words.buffer_info()[0]
     if index == torch._C._cuda_getDevice():
-        AL.check(lib.muon_adamw_step(at, n, ctypes.byref(opts), torch._C._cuda_getCurrentRawStream(index)))
+        AL.check(lib.muon_adamw_step(tensors, n, ctypes.byref(opts), torch._C._cuda_getCurrentRawStream(index)))
     else:
         with torch.cuda.device(index):
-            AL.check(lib.muon_adamw_step(at, n, ctypes.byref(opts), torch._C._cuda_getCurrentRawStream(index)))
+            AL.check(lib.muon_adamw_step(tensors, n, ctypes.byref(opts), torch._C._cuda_getCurrentRawStream(index)))
 
 
 def state_values(state: State) -> Tuple[torch.Tensor, torch.Tensor]:

@@ -1,5 +1,5 @@
 """Builds libmuon_mi355x.so (the optimizer), libmuon_layers.so (the layer
-operators), libmuon_adamw.so (the AdamW step) and libmuon_diag.so (a matrix-core
+operators), libmuon_adamw.so (the AdamW step) with its tensors' binding, and libmuon_diag.so (a matrix-core
 ceiling probe the bench reports as context) for gfx950 with hipcc, in-tree, no JIT
 cache.
 
@@ -35,6 +35,9 @@ LAYER_SOURCES = ["layers/layers_api.cpp", "layers/mm_simple.hip", "layers/mm_til
                  "layers/mm_loss_64_bf16.hip", "layers/mm_loss_128_f32.hip", "layers/mm_loss_64_f32.hip"]
 ADAMW_SOURCES = ["adamw/adamw_api.cpp", "adamw/adamw.hip"]
 ADAMW_LIB_PATH = os.path.join(PKG, "libmuon_adamw.so")
+# a CPython extension that reads torch's tensors (host code, g++)
+BINDING_SOURCE = "adamw/binding.cpp"
+BINDING_PATH = os.path.join(PKG, "_adamw_binding.so")
 LAYER_LIB_PATH = os.path.join(PKG, "libmuon_layers.so")
 DIAG_SOURCES = ["diag/mfma_ceiling.hip"]
 DIAG_LIB_PATH = os.path.join(PKG, "libmuon_diag.so")
@@ -79,13 +82,35 @@ def _link(objs, path: str, verbose: bool) -> None:
     os.replace(tmp, path)
 
 
+def _binding(verbose: bool) -> None:
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = BINDING_PATH + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-D__HIP_PLATFORM_AMD__",
+           "-I" + os.path.join(ROOT, "include"), *("-isystem" + d for d in cpp_extension.include_paths()),
+           "-isystem" + sysconfig.get_paths()["include"], os.path.join(CSRC, BINDING_SOURCE), "-o", tmp, "-L" + lib,
+           "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath," + lib]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"building {BINDING_SOURCE} failed:\n{r.stdout}{r.stderr}")
+    os.replace(tmp, BINDING_PATH)
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     parts = ((SOURCES, LIB_PATH), (LAYER_SOURCES, LAYER_LIB_PATH), (ADAMW_SOURCES, ADAMW_LIB_PATH),
              (DIAG_SOURCES, DIAG_LIB_PATH))
     srcs = [s for sources, _ in parts for s in sources]
     with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 4)) as ex:
+        binding = ex.submit(_binding, verbose)
         objs = dict(zip(srcs, ex.map(lambda s: _compile(s, verbose), srcs)))
+        binding.result()
     for sources, path in parts:
         _link([objs[s] for s in sources], path, verbose)
     return LIB_PATH

@@ -112,6 +112,16 @@ def test_python_refusals():
             AdamW([torch.nn.Parameter(torch.zeros(2))], **kw)
 
 
+def test_binding_gives_nothing_for_tensors_that_do_not_fit():
+    """What it answers with None is then named by the checks one by one."""
+    f, p = AL.tensors(), torch.zeros(3)
+    for args in (([p], [p], [(p, p)], [1]), (1, 2, 3, 4), ([None], [None], [None], [1]), ([p], [], [(p, p)], [1]),
+                 ([p], [p], [p], [1]), ([p.to_sparse()], [p], [(p, p)], [1])):
+        assert f(*args) is None
+    with pytest.raises(TypeError):
+        f([p])
+
+
 def test_states_keep_their_types_through_a_state_dict():
     p, q = torch.nn.Parameter(torch.zeros(300, dtype=torch.bfloat16)), torch.nn.Parameter(torch.zeros(5))
     for bits in (32, 8):
