@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import math
-from typing import List, Optional, Sequence, Tuple, Union
+from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -188,23 +188,26 @@ class AdamW(torch.optim.Optimizer):
             with torch.enable_grad():
                 loss = closure()
         for index, group in enumerate(self.param_groups):
-            per_device = {}
+            per_device: Dict[int, Tuple[List, ...]] = {}
             for p in group["params"]:
-                if p.grad is None:
+                grad = p.grad
+                if grad is None:
                     continue
                 st = self.state[p]
                 if not st:
                     st["step"] = 0
                     st.update(zip(("exp_avg", "exp_avg_sq", "bases"), new_state(p, group["state_bits"])))
-                st["step"] += 1
-                lists: Tuple[List, List, List, List] = per_device.setdefault(p.device, ([], [], [], []))
-                state = (st["exp_avg"], st["exp_avg_sq"], st["bases"]) if "bases" in st else \
-                    (st["exp_avg"], st["exp_avg_sq"])
-                grad = p.grad if p.grad.layout != torch.strided else p.grad.contiguous()
-                for to, v in zip(lists, (p.data, grad, state, st["step"])):
-                    to.append(v)
-            for params, grads, states, steps in per_device.values():
+                params, grads, states, steps, held = per_device.setdefault(p.get_device(), ([], [], [], [], []))
+                params.append(p)
+                grads.append(grad if grad.layout != torch.strided else grad.contiguous())
+                states.append((st["exp_avg"], st["exp_avg_sq"], st["bases"]) if "bases" in st else
+                              (st["exp_avg"], st["exp_avg_sq"]))
+                steps.append(st["step"] + 1)
+                held.append(st)
+            for params, grads, states, steps, held in per_device.values():
                 # (groups differ in their rounding)
                 adamw_step(params, grads, states, step=steps, lr=group["lr"], betas=group["betas"], eps=group["eps"],
                            weight_decay=group["weight_decay"], seed=group["seed"] + index * 0x632BE5AB)
+                for st in held:     # (a step that was refused does not count)
+                    st["step"] += 1
         return loss

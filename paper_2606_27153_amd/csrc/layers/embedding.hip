@@ -10,7 +10,12 @@
 // it: the sum of its run, or zeros (most of a large table).  A frequent token's run
 // can be a good part of the list: groups of 16 places that lie inside one run are
 // summed first, by blocks of their own, and the row adds up the groups.
-// Bound by memory: dy read once, dW written once.
+// Bound by memory: dy read once, dW written once.  32768 tokens (their frequency
+// falling with their rank) of a table of 128000 x 4096 in bf16: forward 98 us (5.4
+// TB/s); backward 300 us, of which the sort takes 31 in four launches, the groups 25 and
+// the table's rows 243 (1.05 GB written).  With groups of 64, the block of the most
+// frequent token ended last, and each block searching its own rows' runs waited for
+// that: 522 us for the table's rows.
 #include "sort.h"
 
 namespace muon {

@@ -8,6 +8,11 @@
 // z computed again and lse.  Everything is fp32 until dz is rounded to the operands' type.
 // A row without a target has loss 0 and a gradient of 0, whatever its logits hold.
 //
+// The products are all that counts (the tile kernels', whose epilogues are the strips
+// and the gradient: mm_tile.h): 16384 rows x 4096 over 128000 columns in bf16 take 54.6
+// ms both ways: four products of 17.2 TFLOP at 1200 to 1360 TFLOP/s; one row
+// reads the weight at 6.2 TB/s.  The kernels of this file take 5 to 25 us each.
+//
 // An upstream gradient that is one number is no factor of dz but of the products
 // that read it (alpha): rounding g (p - 1) to bf16 would give all rows the same
 // relative error, up to 2^-9, where those of p - 1 and p are independent.

@@ -8,8 +8,9 @@
 // The counts of the waves, of the digits and (count_kernel) of the blocks before are then
 // added up.  4096 keys are one launch, more are two: the counts of each block,
 // then every block adds up those before its own; beyond 32 blocks a third in
-// between does that once.  Latency is all that it costs (a chain of about 100 LDS
-// and cross-lane steps; 4 bytes a key from the L2).
+// between does that once.  Latency is all that it costs: a chain of about 100 LDS
+// and cross-lane steps, 4 to 5 us for up to 4096 keys, 14 us for 98304 choices among 64
+// experts, 15 us for each digit of 32768 tokens.
 #ifndef MUON_LAYERS_SORT_H
 #define MUON_LAYERS_SORT_H
 

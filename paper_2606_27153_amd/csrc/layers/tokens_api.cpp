@@ -93,9 +93,9 @@ struct LossLayout {
 };
 
 // The kernel of a piece of x W: few rows leave it in memory (`raw`), tiles do not.
-// The latter take over from 33 rows on (128000 x 4096 in bf16, 40 rows: 210 us for 294), and
+// The latter take over from 33 rows on (128000 x 4096 in bf16, 40 rows: 223 us for 294), and
 // at once where a bf16 weight is kept by its columns, of which a wave of the other
-// kernel reads 64 bytes at a time (one row: 213 us for 310; fp32 74 for 99 the other way).
+// kernel reads 64 bytes at a time (one row: 182 us for 270; in fp32, 32000 x 2048, 92 for 69).
 Choice choose_logits(bool bf16, bool w_transposed, int64_t rows, int64_t piece, int64_t inner) {
   const Choice c = choose(bf16, FORM_RT, GROUP_NONE, rows, piece, inner, 0, false);
   return c.kernel == Choice::SKINNY && rows <= 32 && !(w_transposed && bf16) ? c : choose_tile(bf16, GROUP_NONE, rows, piece, inner, 0, true, 1);

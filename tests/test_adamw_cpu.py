@@ -138,3 +138,13 @@ def test_states_keep_their_types_through_a_state_dict():
                 got = fresh.state[t][k]
                 assert got == v if k == "step" else got.dtype == v.dtype and torch.equal(got, v), k
                 assert k == "step" or got.data_ptr() != v.data_ptr()
+
+
+def test_a_refused_step_does_not_count():
+    p = torch.nn.Parameter(torch.zeros(8))
+    p.grad = torch.zeros(8)
+    opt = AdamW([p])
+    for _ in range(2):
+        with pytest.raises(ValueError, match="GPU"):
+            opt.step()
+    assert opt.state[p]["step"] == 0
