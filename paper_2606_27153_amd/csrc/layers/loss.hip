@@ -203,13 +203,15 @@ __global__ __launch_bounds__(256) void sum_kernel(LossArgs a, const float* part,
   const int n = int(min(int64_t(8), cols - c));
   const float f = a.alpha ? *a.alpha : 1.f;
   const bool live = label_of(a, r) >= 0;
-  float v[8];
-  load8(part + r * cols + c, n, v);
-  for (int s = 1; s < splits; ++s) {
-    float x[8];
-    load8(part + (int64_t(s) * a.rows + r) * cols + c, n, x);
+  float v[8] = {};
+  for (int s = 0; s < splits; s += 4) {   // in order, 4 in flight
+    float x[4][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += x[e];
+    for (int k = 0; k < 4; ++k) load8(part + (int64_t(min(s + k, splits - 1)) * a.rows + r) * cols + c, n, x[k]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += s + k < splits ? x[k][e] : 0.f;
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = live ? v[e] * f : 0.f;
