@@ -78,9 +78,11 @@ def _one_by_one(params, grads, states, steps):
             raise ValueError(f"param {i} is on {p.device}, expected {device}")
         if not p.is_contiguous():
             raise ValueError(f"param {i} is not contiguous (stride {p.stride()})")
-        if p.numel() and seen.setdefault(p.data_ptr(), i) != i:
-            raise ValueError(f"param {i} is param {seen[p.data_ptr()]} again")
         b = _check_state(s, p.numel(), i, device)
+        for name, t in zip(("param", "exp_avg", "exp_avg_sq", "bases"), (p, *s)):
+            first = seen.setdefault(t.data_ptr(), f"{name} {i}") if p.numel() else ""
+            if first and first != f"{name} {i}":
+                raise ValueError(f"{name} {i} is {first} again")
         if bits is None:
             bits = b
         elif b != bits:
@@ -109,7 +111,8 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Te
     their gradients (fp32 or bf16; None: the tensor is left as it is) and states
     (``new_state``; all of 32 bits or all of 8), which move on too.  ``step`` counts
     from 1 and is one number or one for each tensor; ``seed`` varies the rounding of 8-bit
-    states.  All tensors are on one GPU and do not overlap."""
+    states.  All tensors are on one GPU and do not overlap.  A step captured into a graph is
+    replayed with the numbers it was captured with."""
     n = len(params)
     if len(grads) != n or len(states) != n:
         raise ValueError(f"{n} params, {len(grads)} grads and {len(states)} states")

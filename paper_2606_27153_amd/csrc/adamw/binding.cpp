@@ -4,7 +4,6 @@
 // small tensors is not bound by the host.
 #include <torch/csrc/autograd/python_variable.h>
 
-#include <algorithm>
 #include <cstdint>
 #include <vector>
 
@@ -34,14 +33,34 @@ int dtype_code(const at::Tensor& t) {
   return t.scalar_type() == at::kFloat ? MUON_F32 : t.scalar_type() == at::kBFloat16 ? MUON_BF16 : -1;
 }
 
+// The addresses that a step writes to: a table with a quarter of its places taken at most.
+class Written {
+ public:
+  explicit Written(size_t count) {
+    size_t places = 16;
+    while (places < 4 * count) places *= 2;
+    at_.resize(places);
+  }
+  // Whether p is new.
+  bool add(const void* p) {
+    size_t i = size_t(reinterpret_cast<uintptr_t>(p) * 0x9E3779B97F4A7C15u >> 20) & (at_.size() - 1);
+    for (; at_[i]; i = (i + 1) & (at_.size() - 1))
+      if (at_[i] == p) return false;
+    at_[i] = p;
+    return true;
+  }
+
+ private:
+  std::vector<const void*> at_;
+};
+
 // Whether every tensor fits; fills `out`, the device and the states' bits.
 bool collect(const Items& params, const Items& grads, const Items& states, const Items& steps,
              std::vector<muon_adamw_tensor>& out, int64_t& device, int& bits) {
   const Py_ssize_t n = params.size();
   if (grads.size() != n || states.size() != n || steps.size() != n) return false;
   out.resize(size_t(n));
-  std::vector<void*> seen;
-  seen.reserve(size_t(n));
+  Written written(4 * size_t(n));
   device = -1;
   bits = 0;
   for (Py_ssize_t i = 0; i < n; ++i) {
@@ -81,10 +100,11 @@ bool collect(const Items& params, const Items& grads, const Items& states, const
     t.n = elements;
     t.step = PyLong_AsLongLong(steps[i]);
     if (t.step == -1 && PyErr_Occurred()) return false;
-    if (elements) seen.push_back(t.param);
+    if (elements && !(written.add(t.param) && written.add(t.exp_avg) && written.add(t.exp_avg_sq) &&
+                      (!t.bases || written.add(t.bases))))
+      return false;
   }
-  std::sort(seen.begin(), seen.end());
-  return std::adjacent_find(seen.begin(), seen.end()) == seen.end();
+  return true;
 }
 
 // adamw_tensors(params, grads, states, steps) -> (bytes, device index, bits), the bytes an

@@ -261,3 +261,18 @@ def test_bad_tensors_are_refused():
             call([p], [d], [st], **kw)
     with pytest.raises(ValueError, match="steps"):
         call([p], [d], [st], step=[1, 2])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_state_in_two_places_is_refused(bits):
+    g = gen(31)
+    p, d, st = make(g, (600,), BF16, BF16, bits)
+    q, e, other = make(g, (600,), BF16, BF16, bits)
+    before = [t.clone() for t in (p, q, *st, *other)]
+    for k in range(len(st)):
+        shared = (*other[:k], st[k], *other[k + 1:])
+        with pytest.raises(ValueError, match="again"):
+            adamw.adamw_step([p, q], [d, e], [st, shared], step=1, lr=1e-3)
+    with pytest.raises(ValueError, match="again"):
+        adamw.adamw_step([p], [d], [(st[0], st[0], *st[2:])], step=1, lr=1e-3)
+    assert all(torch.equal(a, b) for a, b in zip(before, (p, q, *st, *other)))
