@@ -60,6 +60,7 @@ SIGNATURES = {
 
 _lock = threading.Lock()
 _lib = None
+_binding = None
 
 
 def load(path: str = LIB_PATH):
@@ -81,6 +82,21 @@ def load(path: str = LIB_PATH):
             fn.argtypes = args
         _lib = lib
         return lib
+
+
+def binding():
+    """The functions of csrc/layers/binding.cpp."""
+    global _binding
+    if _binding is None:
+        import torch  # noqa: F401  (whose libraries the extension is linked to)
+        load()
+        try:
+            from . import _layers_binding
+        except ImportError as e:
+            raise RuntimeError(f"_layers_binding.so cannot be loaded ({e}); build it first with "
+                               f"`python -m paper_2606_27153_amd.build` (there is no fallback path)") from e
+        _binding = _layers_binding
+    return _binding
 
 
 def check(status: int) -> None:

@@ -1,7 +1,8 @@
 """Builds libmuon_mi355x.so (the optimizer), libmuon_layers.so (the layer
-operators), libmuon_adamw.so (the AdamW step) with its tensors' binding, and libmuon_diag.so (a matrix-core
-ceiling probe the bench reports as context) for gfx950 with hipcc, in-tree, no JIT
-cache.
+operators), libmuon_adamw.so (the AdamW step), and libmuon_diag.so (a matrix-core
+ceiling probe the bench reports as context) for gfx950 with hipcc, and the extensions
+that read torch's tensors for the layer operators and AdamW with the host's compiler;
+in-tree, no JIT cache.
 
 Usage: python -m paper_2606_27153_amd.build [-v]
 """
@@ -35,10 +36,10 @@ LAYER_SOURCES = ["layers/layers_api.cpp", "layers/mm_simple.hip", "layers/mm_til
                  "layers/mm_loss_64_bf16.hip", "layers/mm_loss_128_f32.hip", "layers/mm_loss_64_f32.hip"]
 ADAMW_SOURCES = ["adamw/adamw_api.cpp", "adamw/adamw.hip"]
 ADAMW_LIB_PATH = os.path.join(PKG, "libmuon_adamw.so")
-# a CPython extension that reads torch's tensors (host code, g++)
-BINDING_SOURCE = "adamw/binding.cpp"
-BINDING_PATH = os.path.join(PKG, "_adamw_binding.so")
 LAYER_LIB_PATH = os.path.join(PKG, "libmuon_layers.so")
+# CPython extensions that read torch's tensors (host code): source, path, and the library they call
+BINDINGS = [("adamw/binding.cpp", os.path.join(PKG, "_adamw_binding.so"), None),
+            ("layers/binding.cpp", os.path.join(PKG, "_layers_binding.so"), "muon_layers")]
 DIAG_SOURCES = ["diag/mfma_ceiling.hip"]
 DIAG_LIB_PATH = os.path.join(PKG, "libmuon_diag.so")
 
@@ -82,24 +83,34 @@ def _link(objs, path: str, verbose: bool) -> None:
     os.replace(tmp, path)
 
 
-def _binding(verbose: bool) -> None:
-    import sysconfig
-
-    import torch
-    from torch.utils import cpp_extension
-    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
-    tmp = BINDING_PATH + ".tmp"
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-D__HIP_PLATFORM_AMD__",
-           "-I" + os.path.join(ROOT, "include"), *("-isystem" + d for d in cpp_extension.include_paths()),
-           "-isystem" + sysconfig.get_paths()["include"], os.path.join(CSRC, BINDING_SOURCE), "-o", tmp, "-L" + lib,
-           "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath," + lib]
+def _run(cmd, what: str, verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError(f"building {BINDING_SOURCE} failed:\n{r.stdout}{r.stderr}")
-    os.replace(tmp, BINDING_PATH)
+        raise RuntimeError(f"building {what} failed:\n{r.stdout}{r.stderr}")
+
+
+def _compile_binding(src: str, verbose: bool) -> str:
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    obj = os.path.join(BUILD, src.replace("/", "_") + ".o")
+    _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall",
+          f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-D__HIP_PLATFORM_AMD__",
+          "-I" + os.path.join(ROOT, "include"), *("-isystem" + d for d in cpp_extension.include_paths()),
+          "-isystem" + sysconfig.get_paths()["include"], "-c", os.path.join(CSRC, src), "-o", obj], src, verbose)
+    return obj
+
+
+def _link_binding(obj: str, path: str, library, verbose: bool) -> None:
+    import torch
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    own = [f"-L{PKG}", f"-l{library}", "-Wl,-rpath,$ORIGIN"] if library else []
+    _run([os.environ.get("CXX", "g++"), "-shared", obj, "-o", path + ".tmp", *own, "-L" + lib, "-ltorch_python",
+          "-ltorch_cpu", "-lc10", "-Wl,-rpath," + lib], path, verbose)
+    os.replace(path + ".tmp", path)
 
 
 def build(verbose: bool = False) -> str:
@@ -108,11 +119,13 @@ def build(verbose: bool = False) -> str:
              (DIAG_SOURCES, DIAG_LIB_PATH))
     srcs = [s for sources, _ in parts for s in sources]
     with cf.ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 4)) as ex:
-        binding = ex.submit(_binding, verbose)
+        bindings = [ex.submit(_compile_binding, src, verbose) for src, _, _ in BINDINGS]
         objs = dict(zip(srcs, ex.map(lambda s: _compile(s, verbose), srcs)))
-        binding.result()
+        bindings = [b.result() for b in bindings]
     for sources, path in parts:
         _link([objs[s] for s in sources], path, verbose)
+    for obj, (_, path, library) in zip(bindings, BINDINGS):
+        _link_binding(obj, path, library, verbose)
     return LIB_PATH
 
 

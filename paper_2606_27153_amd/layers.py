@@ -43,6 +43,12 @@ def _load():
     return _lib
 
 
+def _compiled():
+    """The operators of few bytes, called by compiled code; each returns None where an
+    argument does not fit, and the function below of that name says which."""
+    return LL._binding or LL.binding()
+
+
 def _tensor(t, name: str) -> None:
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a tensor, not {type(t).__name__}")
@@ -604,10 +610,16 @@ def _numbers(t: torch.Tensor, name: str, shape=None, like: Optional[torch.Tensor
 
 # ---------------------------------------------------------------- embedding
 
-@_on_device
 def embedding_forward(ids: torch.Tensor, weight: torch.Tensor, *, scale: float = 1.0) -> torch.Tensor:
     """``scale * weight[ids]`` for ids of any shape and a table [vocab, cols]; a
     number outside [0, vocab) gets a row of 0."""
+    scale = float(scale)
+    y = _compiled().embedding_forward(ids, weight, scale)
+    return _embedding_forward(ids, weight, scale) if y is None else y
+
+
+@_on_device
+def _embedding_forward(ids: torch.Tensor, weight: torch.Tensor, scale: float) -> torch.Tensor:
     lib = _load()
     ip, size = _numbers(ids, "ids")
     _input(weight, "weight")
@@ -617,7 +629,6 @@ def embedding_forward(ids: torch.Tensor, weight: torch.Tensor, *, scale: float =
         raise ValueError("weight has no rows")
     _numbers(ids, "ids", None, weight)
     wp, ldw = _rows(weight, "weight", weight, vocab, cols)
-    scale = float(scale)
     stream = _stream(weight)
     y = weight.new_empty((*ids.shape, cols))
     LL.check(lib.muon_embedding_forward(ip, size, wp, ldw, y.data_ptr(), cols, ids.numel(), vocab, cols, scale, code,
@@ -625,10 +636,16 @@ def embedding_forward(ids: torch.Tensor, weight: torch.Tensor, *, scale: float =
     return y
 
 
-@_on_device
 def embedding_backward(dy: torch.Tensor, ids: torch.Tensor, vocab: int, *, scale: float = 1.0) -> torch.Tensor:
     """The table's gradient [vocab, cols] for the output gradient dy [*ids.shape,
     cols]: ``scale`` times the sum of each token's rows, taken in their order."""
+    scale = float(scale)
+    dw = _compiled().embedding_backward(dy, ids, vocab, scale)
+    return _embedding_backward(dy, ids, vocab, scale) if dw is None else dw
+
+
+@_on_device
+def _embedding_backward(dy: torch.Tensor, ids: torch.Tensor, vocab: int, scale: float) -> torch.Tensor:
     lib = _load()
     _tensor(dy, "dy")
     ip, size = _numbers(ids, "ids")
@@ -640,7 +657,7 @@ def embedding_backward(dy: torch.Tensor, ids: torch.Tensor, vocab: int, *, scale
     rows, cols = dy.shape
     _numbers(ids, "ids", None, dy)
     gp, ldg = _rows(dy, "dy", dy, rows, cols)
-    vocab, scale = int(vocab), float(scale)
+    vocab = int(vocab)
     if vocab < 1:
         raise ValueError(f"vocab {vocab}: a table has at least one row")
     stream = _stream(dy)
@@ -684,10 +701,15 @@ class Routing(NamedTuple):
     source: torch.Tensor     # int32 [tokens * top]: each row's choice t * top + j; behind the last, ~ those of no expert
 
 
-@_on_device
 def sort_by_expert(experts: torch.Tensor, count: int) -> Routing:
     """The choices experts [tokens, top] of ``count`` experts sorted by expert, in
     their own order within each.  One outside [0, count) goes to no expert."""
+    found = _compiled().sort_by_expert(experts, count)
+    return _sort_by_expert(experts, count) if found is None else Routing(*found)
+
+
+@_on_device
+def _sort_by_expert(experts: torch.Tensor, count: int) -> Routing:
     lib = _load()
     ip, size = _numbers(experts, "experts")
     if experts.dim() != 2:
@@ -739,10 +761,15 @@ def _router_weights(weights: torch.Tensor, x: torch.Tensor, tokens: int, top: in
     return weights.data_ptr(), _DTYPES[weights.dtype]
 
 
-@_on_device
 def dispatch_forward(x: torch.Tensor, routing: Routing) -> torch.Tensor:
     """Every token's row x[t] at its choices' rows [tokens * top, cols], sorted by
     expert; rows behind the last expert's get 0."""
+    rows = _compiled().dispatch_forward(x, routing)
+    return _dispatch_forward(x, routing) if rows is None else rows
+
+
+@_on_device
+def _dispatch_forward(x: torch.Tensor, routing: Routing) -> torch.Tensor:
     lib = _load()
     _input(x)
     code = _dtype_code(x)
@@ -755,9 +782,14 @@ def dispatch_forward(x: torch.Tensor, routing: Routing) -> torch.Tensor:
     return rows
 
 
-@_on_device
 def dispatch_backward(drows: torch.Tensor, routing: Routing) -> torch.Tensor:
     """dx [tokens, cols]: the sum of each token's choices' rows."""
+    dx = _compiled().dispatch_backward(drows, routing)
+    return _dispatch_backward(drows, routing) if dx is None else dx
+
+
+@_on_device
+def _dispatch_backward(drows: torch.Tensor, routing: Routing) -> torch.Tensor:
     lib = _load()
     _input(drows, "drows")
     code = _dtype_code(drows)
@@ -770,11 +802,17 @@ def dispatch_backward(drows: torch.Tensor, routing: Routing) -> torch.Tensor:
     return dx
 
 
-@_on_device
 def combine_forward(rows: torch.Tensor, weights: torch.Tensor, routing: Routing, *,
                     residual: Optional[torch.Tensor] = None) -> torch.Tensor:
     """``y[t] = residual[t] + sum of weights[t, j] * rows[position[t, j]]`` over the
     token's choices; weights [tokens, top] are fp32 or of the rows' dtype."""
+    y = _compiled().combine_forward(rows, weights, routing, residual)
+    return _combine_forward(rows, weights, routing, residual) if y is None else y
+
+
+@_on_device
+def _combine_forward(rows: torch.Tensor, weights: torch.Tensor, routing: Routing,
+                     residual: Optional[torch.Tensor]) -> torch.Tensor:
     lib = _load()
     _input(rows, "rows")
     code = _dtype_code(rows)
@@ -790,11 +828,17 @@ def combine_forward(rows: torch.Tensor, weights: torch.Tensor, routing: Routing,
     return y
 
 
-@_on_device
 def combine_backward(dy: torch.Tensor, rows: torch.Tensor, weights: torch.Tensor, routing: Routing, *,
                      rows_grad: bool = True, weights_grad: bool = True):
     """Gradients ``(drows, dweights)`` of ``combine_forward`` (the residual's is dy);
     those not asked for are None.  Rows behind the last expert's get 0."""
+    found = _compiled().combine_backward(dy, rows, weights, routing, rows_grad, weights_grad)
+    return _combine_backward(dy, rows, weights, routing, rows_grad, weights_grad) if found is None else found
+
+
+@_on_device
+def _combine_backward(dy: torch.Tensor, rows: torch.Tensor, weights: torch.Tensor, routing: Routing, rows_grad: bool,
+                      weights_grad: bool):
     lib = _load()
     _input(dy, "dy")
     code = _dtype_code(dy)

@@ -557,3 +557,75 @@ def test_bad_arguments_are_refused():
         layers.embedding_forward(t, x, scale=float("nan"))
     with pytest.raises(MuonError, match="2\\^20"):
         f(torch.zeros(1, (1 << 20) + 8, device=DEV), torch.zeros((1 << 20) + 8, 8, device=DEV), t[:1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids_of)
+@pytest.mark.parametrize("tokens,top,cols,experts", [(1, 1, 1, 1), (3, 2, 72, 5), (700, 6, 40, 64)])
+def test_compiled_calls_and_those_in_python_are_the_same(dtype, tokens, top, cols, experts):
+    """On another stream than the default one, rows of wider ones."""
+    g = gen(tokens)
+    fast = layers._compiled()
+    wide = lambda n: torch.randn(n, cols + 3, generator=g, device=DEV).to(dtype)[:, :cols]
+    choice = torch.randint(-1, experts + 1, (tokens, top), generator=g, device=DEV)
+    x, h, r = wide(tokens), wide(tokens * top), wide(tokens)
+    w = torch.rand(tokens, top, generator=g, device=DEV)
+    ids = torch.randint(-1, tokens + 1, (2, 3), generator=g, device=DEV, dtype=torch.int32)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        route = layers._sort_by_expert(choice, experts)
+        pairs = [(fast.sort_by_expert(choice, experts), route),
+                 (fast.dispatch_forward(x, route), layers._dispatch_forward(x, route)),
+                 (fast.dispatch_backward(h, route), layers._dispatch_backward(h, route)),
+                 (fast.embedding_forward(ids, x, 1.5), layers._embedding_forward(ids, x, 1.5))]
+        dy = x.new_ones(2, 3, cols) / 3
+        pairs.append((fast.embedding_backward(dy, ids, tokens, 1.5), layers._embedding_backward(dy, ids, tokens, 1.5)))
+        for res in (None, r):
+            pairs.append((fast.combine_forward(h, w, route, res), layers._combine_forward(h, w, route, res)))
+        for weights in (w, w.to(dtype)):
+            for rg, wg in ((True, True), (True, False), (False, True), (False, False)):
+                pairs.append((fast.combine_backward(x, h, weights, route, rg, wg),
+                              layers._combine_backward(x, h, weights, route, rg, wg)))
+    stream.synchronize()
+    for a, b in pairs:
+        a, b = (v if isinstance(v, tuple) else (v,) for v in (a, b))
+        assert len(a) == len(b)
+        for s, t in zip(a, b):
+            assert (s is None) == (t is None)
+            assert s is None or (s.dtype == t.dtype and s.shape == t.shape and s.stride() == t.stride()
+                                 and torch.equal(s, t))
+
+
+def test_compiled_calls_leave_what_does_not_fit_to_python():
+    """(Each of these either is refused there or has nothing to do.)"""
+    fast = layers._compiled()
+    x, h = torch.zeros(4, 8, device=DEV), torch.zeros(8, 8, device=DEV)
+    w, choice = torch.zeros(4, 2, device=DEV), torch.zeros(4, 2, device=DEV, dtype=torch.int64)
+    ids = torch.zeros(3, device=DEV, dtype=torch.int64)
+    r = layers.sort_by_expert(choice, 4)
+    torch.cuda.synchronize()
+    none = [fast.sort_by_expert(*a) for a in ((choice, 0), (choice, 1 << 20), (choice, 1 << 80), (choice, 2.0), (choice,),
+                                              (choice.float(), 4), (choice.t(), 4), (choice.cpu(), 4), (choice[0], 4),
+                                              (choice[:0], 4), (3, 4), (None, 4))]
+    for a in ((x.half(), r), (x.t(), r), (x[:3], r), (x[:, ::2], r), (x.cpu(), r), (x[0], r), (x, r[:2]), (x, None), (7, r),
+              (x, (r[0], r[1].long(), r[2])), (x, (r[0], r[1], r[2][:7])), (x, (r[0], r[1].cpu(), r[2])),
+              (x[:, :0], r), (x[:1].expand(4, 8), r)):
+        none += [fast.dispatch_forward(*a)]
+    none += [fast.dispatch_backward(x, r), fast.dispatch_backward(h.t()[:7], r)]
+    for a in ((h, w, r, x[:3]), (h, w, r, x.bfloat16()), (h, w.double(), r, None), (h, w.bfloat16(), r, None),
+              (h, w.t(), r, None), (h[:7], w, r, None), (h, w, r), (h, w[:3], r, None), (h, None, r, None)):
+        none += [fast.combine_forward(*a)]
+    for a in ((x, h, w, r, 1, True), (x[:3], h, w, r, True, True), (x, h[:7], w, r, True, True),
+              (x, h.bfloat16(), w, r, True, True)):
+        none += [fast.combine_backward(*a)]
+    for a in ((ids, x, 1), (ids.float(), x, 1.0), (ids, x[:0], 1.0), (ids[:0], x, 1.0), (ids[::2], x, 1.0),
+              (ids.cpu(), x, 1.0), (ids, x.half(), 1.0), (ids, x, float("nan")), (ids, x, float("inf"))):
+        none += [fast.embedding_forward(*a)]
+    dy = x[:3]
+    for a in ((dy, ids, 1.0, 1.0), (dy, ids, 0, 1.0), (dy[:2], ids, 4, 1.0), (dy.half(), ids, 4, 1.0), (dy, ids.cpu(), 4, 1.0),
+              (x[:3, 1:], ids, 4, 1.0), (dy, ids, 4, float("inf")), (dy[:0], ids[:0], 4, 1.0), (dy[:, :0], ids, 4, 1.0),
+              (dy, ids[0], 4, 1.0), (dy[0, 0], ids, 4, 1.0)):
+        none += [fast.embedding_backward(*a)]
+    assert all(v is None for v in none)
+    with pytest.raises(MuonError, match="scale"):
+        layers.embedding_forward(ids, x, scale=float("nan"))
