@@ -228,8 +228,8 @@ MUON_API muon_status muon_linear_cross_entropy_forward(const void* x, int64_t ld
 
 /* Its gradients for dloss (rows fp32, or one): z is computed again piece by piece.
  * dz is rounded to dtype before the products that read it.  dx and dw may be NULL;
- * dw is kept like w.  Rows without a target have dx = 0 and add 0 times their x to
- * dw (which has to be finite). */
+ * dw is kept like w.  Rows without a target have dx = 0 and add nothing to dw,
+ * whatever they hold. */
 MUON_API muon_status muon_linear_cross_entropy_backward(const float* dloss, const void* x, int64_t ldx, const void* w,
                                                         int64_t ldw, int32_t w_transposed, const void* targets,
                                                         int32_t target_bytes, int64_t ignore, int32_t reduction,

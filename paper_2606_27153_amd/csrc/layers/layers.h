@@ -168,6 +168,9 @@ hipError_t launch_loss_strips(const LossArgs& a, hipStream_t st);   // raw -> pa
 hipError_t launch_loss_finish(const LossArgs& a, hipStream_t st);   // part -> lse and loss
 hipError_t launch_loss_total(const LossArgs& a, hipStream_t st);    // loss -> total
 hipError_t launch_loss_grad(bool bf16, const LossArgs& a, hipStream_t st);   // raw -> dz
+// y (rows of ldy): x, with zeros in rows without a target and behind the columns
+hipError_t launch_loss_rows(bool bf16, const LossArgs& a, const void* x, int64_t ldx, void* y, int64_t ldy,
+                            int64_t cols, hipStream_t st);
 // y: alpha times the sum of `splits` partial results of a.rows x cols, 0 in rows without a target
 hipError_t launch_loss_sum(bool bf16, const LossArgs& a, const float* part, int splits, void* y, int64_t ldy,
                            int64_t cols, hipStream_t st);

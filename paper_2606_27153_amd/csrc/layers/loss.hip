@@ -192,6 +192,23 @@ __global__ __launch_bounds__(256) void grad_kernel(LossArgs a) {
   store8(static_cast<E*>(a.dz) + row * a.lddz + c, 8, v);
 }
 
+// x with zeros in the rows without a target (and behind its columns), for the weight's
+// gradient: whatever they hold, their 0 of dz must not make NaN of it.  16384 x 4096 in
+// bf16 take 55 us of a step's 54500.
+template <typename E, bool WHOLE>
+__global__ __launch_bounds__(256) void rows_kernel(LossArgs a, const E* x, int64_t ldx, E* y, int64_t ldy,
+                                                   int64_t cols) {
+  const int64_t chunks = (ldy + 7) / 8, i = int64_t(blockIdx.x) * 256 + threadIdx.x, r = i / chunks;
+  if (r >= a.rows) return;
+  const int64_t c = (i - r * chunks) * 8;
+  const bool live = label_of(a, r) >= 0;
+  float v[8];
+  load_8<WHOLE>(x + r * ldx + c, int(min(int64_t(8), cols - c)), v);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = live ? v[e] : 0.f;
+  store_8<WHOLE>(y + r * ldy + c, int(min(int64_t(8), ldy - c)), v);
+}
+
 // The input's gradient: the partial results added up, times alpha; 0 in rows without a target
 // (also where a weight that is not finite or an infinite alpha would leave NaN).
 template <typename E>
@@ -254,6 +271,22 @@ hipError_t launch_loss_grad(bool bf16, const LossArgs& a, hipStream_t st) {
     hipLaunchKernelGGL((grad_kernel<__bf16>), g, dim3{256}, 0, st, a);
   else
     hipLaunchKernelGGL((grad_kernel<float>), g, dim3{256}, 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_rows(bool bf16, const LossArgs& a, const void* x, int64_t ldx, void* y, int64_t ldy,
+                            int64_t cols, hipStream_t st) {
+  const int64_t blocks = (a.rows * ((ldy + 7) / 8) + 255) / 256;
+  if (blocks >= kMaxGrid) return hipErrorInvalidConfiguration;
+  const dim3 g{unsigned(blocks)}, b{256};
+  auto run = [&](auto kernel, auto one) {
+    typedef decltype(one) E;
+    hipLaunchKernelGGL(kernel, g, b, 0, st, a, static_cast<const E*>(x), ldx, static_cast<E*>(y), ldy, cols);
+  };
+  if (cols % 8)
+    bf16 ? run(rows_kernel<__bf16, false>, __bf16()) : run(rows_kernel<float, false>, float());
+  else
+    bf16 ? run(rows_kernel<__bf16, true>, __bf16()) : run(rows_kernel<float, true>, float());
   return hipGetLastError();
 }
 

@@ -143,14 +143,15 @@ hipError_t product_sums(const Choice& c, bool bf16, int form, Product p, float* 
   return launch_choice(bf16, form, GROUP_NONE, c, p, nullptr, st);
 }
 
-// Copies of x (once) and of a piece of the weight, as it is kept, for all the products
-// that read them: rows of whole chunks, zeros after the last column.
+// Copies of x (once; in the backward pass always, without what rows of no target hold) and of
+// a piece of the weight, as it is kept, for all the products that read them: rows of
+// whole chunks, zeros after the last column.
 PackOne copy_of_w(int64_t piece, int64_t inner, bool w_transposed, int64_t epc) {
   return w_transposed ? copy_shape(piece, inner, epc) : copy_shape(inner, piece, epc);
 }
-void take_copies(LossLayout& l, int64_t rows, int64_t inner, bool w_transposed, bool bf16, bool unaligned) {
+void take_copies(LossLayout& l, int64_t rows, int64_t inner, bool w_transposed, bool bf16, bool unaligned, bool backward) {
   const int64_t epc = bf16 ? 8 : 4;
-  l.take(l.xcopy, unaligned ? copy_bytes(copy_shape(rows, inner, epc), epc, 1) : 0);
+  l.take(l.xcopy, unaligned || backward ? copy_bytes(copy_shape(rows, inner, epc), epc, 1) : 0);
   l.take(l.wcopy, unaligned ? copy_bytes(copy_of_w(l.piece, inner, w_transposed, epc), epc, 1) : 0);
 }
 
@@ -165,7 +166,7 @@ LossLayout forward_layout(int64_t rows, int64_t inner, int64_t outer, bool w_tra
   l.take(l.loss, size_t(rows) * 4);
   l.take(l.part, size_t(ceil_div(outer, l.piece)) * size_t(ceil_div(l.piece, strip_columns(l.z))) * size_t(l.rows) * 8);
   l.take(l.raw, raw_bytes(l));
-  if (l.z.kernel != Choice::SKINNY) take_copies(l, rows, inner, w_transposed, bf16, unaligned);
+  if (l.z.kernel != Choice::SKINNY) take_copies(l, rows, inner, w_transposed, bf16, unaligned, false);
   return l;
 }
 
@@ -184,7 +185,7 @@ LossLayout backward_layout(int64_t rows, int64_t inner, int64_t outer, bool w_tr
   l.take(l.dz, size_t(rows) * size_t(ceil_div(l.piece, 8) * 8) * (bf16 ? 2 : 4));
   l.take(l.raw, raw_bytes(l));
   l.take(l.dx, size_t(l.x.splits) * size_t(rows) * size_t(inner) * 4);
-  take_copies(l, rows, inner, w_transposed, bf16, unaligned);
+  take_copies(l, rows, inner, w_transposed, bf16, unaligned, true);
   l.take(l.scratch, part_bytes(l.w, wm, wn));
   return l;
 }
@@ -505,7 +506,6 @@ MUON_API muon_status muon_linear_cross_entropy_backward(const float* dloss, cons
   char* ws = static_cast<char*>(workspace);
   const int64_t epc = bf16 ? 8 : 4;
   const bool few = l.z.kernel == Choice::SKINNY;
-  if (!xf) TRY(done(copy_operand(bf16, xo, copy_shape(rows, inner, epc), ws + l.xcopy, st), "copy of x"));
   LossArgs a{};
   a.targets = targets; a.target_bytes = target_bytes; a.ignore = ignore;
   a.rows = int32_t(rows); a.vocab = int32_t(outer);
@@ -513,6 +513,11 @@ MUON_API muon_status muon_linear_cross_entropy_backward(const float* dloss, cons
   a.each = reduction == MUON_LOSS_ROWS;
   a.lse = const_cast<float*>(lse);
   if (!rows && !dw) return done(hipSuccess, "");
+  if (rows && (dw || !xf)) {
+    const int64_t ld = copy_shape(rows, inner, epc).ld_dst;
+    TRY(done(launch_loss_rows(bf16, a, xo.p, xo.ld, ws + l.xcopy, ld, inner, st), "copy of x"));
+    xo = Operand{ws + l.xcopy, ld};
+  }
   if (reduction == MUON_LOSS_SUM) a.alpha = dloss;
   if (reduction == MUON_LOSS_MEAN && rows) {
     float* const alpha = reinterpret_cast<float*>(ws + l.alpha);

@@ -321,6 +321,32 @@ def test_loss_rows_far_apart():
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids_of)
+@pytest.mark.parametrize("shape", [(1, 8, 9), (5, 24, 40), (40, 33, 257), (300, 264, 1000)], ids=ids_of)
+def test_loss_rows_without_a_target_may_hold_anything(shape, dtype):
+    """(As the rows of a padded batch do: results are those of zeros in their place.)"""
+    rows, inner, vocab = shape
+    g = gen(rows)
+    for transposed in (False, True):
+        x, w, t = loss_case(g, rows, inner, vocab, dtype, transposed)
+        t[::3] = -100
+        t[1::5] = vocab + 3
+        dead = (t < 0) | (t >= vocab)
+        zeros, bad = x.clone(), x.clone()
+        zeros[dead] = 0
+        bad[dead] = torch.tensor([float("nan"), float("inf"), -float("inf"), 1e38], device=DEV).to(dtype).repeat(inner)[:inner]
+        for reduction in ("mean", "sum", "none"):
+            out = []
+            for v in (zeros, bad):
+                loss, lse = layers.linear_cross_entropy_forward(v, w, t, reduction=reduction)
+                d = torch.full_like(loss, 0.7)
+                if reduction == "none":
+                    d[dead] = float("nan")
+                out.append((loss, *layers.linear_cross_entropy_backward(d, v, w, t, lse, reduction=reduction)))
+            for a, b in zip(*out):
+                assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
 # ----------------------------------------------------- autograd and together
 
 def _directional(f, inputs, grads, g):

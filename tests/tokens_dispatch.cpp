@@ -134,6 +134,12 @@ hipError_t launch_loss_grad(bool bf16, const LossArgs& a, hipStream_t) {
   g_words += std::string(" dz/rows/") + (bf16 ? "bf16" : "f32");
   return hipSuccess;
 }
+hipError_t launch_loss_rows(bool bf16, const LossArgs& a, const void*, int64_t, void* y, int64_t ldy, int64_t cols,
+                            hipStream_t) {
+  if (ldy < cols) g_failed += " xcopy's rows overlap;";
+  span("xcopy", y, size_t(a.rows) * ldy * (bf16 ? 2 : 4));
+  return hipSuccess;
+}
 hipError_t launch_loss_sum(bool, const LossArgs& a, const float* part, int splits, void*, int64_t, int64_t cols,
                            hipStream_t) {
   span("sums", part, size_t(splits) * a.rows * cols * 4);
