@@ -171,6 +171,25 @@ __device__ __forceinline__ void store_8(E* p, int n, const float (&v)[8]) {
   store8(p, WHOLE ? 8 : n, v);
 }
 
+// Past the caches' order of use as well, which leaves them to what is read.
+template <bool WHOLE, typename E>
+__device__ __forceinline__ void store_8_once(E* p, int n, const float (&v)[8]) {
+  typedef uint32_t Words __attribute__((ext_vector_type(4), aligned(2)));
+  if constexpr (WHOLE) {
+    Packed8<E> x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x.v[e] = E(v[e]);
+    struct Both {
+      Words w[sizeof(E) / 2];
+    };
+    const Both b = __builtin_bit_cast(Both, x);
+#pragma unroll
+    for (int i = 0; i < int(sizeof(E) / 2); ++i) __builtin_nontemporal_store(b.w[i], reinterpret_cast<Words*>(p) + i);
+  } else {
+    store8(p, n, v);
+  }
+}
+
 // Number i of a list of int64 or int32.
 __device__ __forceinline__ int64_t id_at(const void* ids, int bytes, int64_t i) {
   return bytes == 8 ? static_cast<const int64_t*>(ids)[i] : int64_t(static_cast<const int32_t*>(ids)[i]);

@@ -11,9 +11,10 @@
 // can be a good part of the list: groups of 16 places that lie inside one run are
 // summed first, by blocks of their own, and the row adds up the groups.
 // Bound by memory: dy read once, dW written once.  32768 tokens (their frequency
-// falling with their rank) of a table of 128000 x 4096 in bf16: forward 98 us (5.4
-// TB/s); backward 300 us, of which the sort takes 31 in four launches, the groups 25 and
-// the table's rows 243 (1.05 GB written).  With groups of 64, the block of the most
+// falling with their rank) of a table of 128000 x 4096 in bf16: forward 85 us (6.3
+// TB/s); backward 280 us, of which the sort takes 31 in four launches, the groups 25 and
+// the table's rows 222 (1.05 GB written, past the caches' order of use: 243 as ordinary
+// stores, and 98 for the lookup after them).  With groups of 64, the block of the most
 // frequent token ended last, and each block searching its own rows' runs waited for
 // that: 522 us for the table's rows.
 #include "sort.h"
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(256) void table_grad_kernel(EmbeddingArgs a) {
     if (start[r] < start[r + 1])
       met |= 1u << r;
     else if (v0 + r < a.vocab)
-      store_8<WHOLE>(to + r * a.lddw, n, zero);
+      store_8_once<WHOLE>(to + r * a.lddw, n, zero);
   }
   while (met) {
     const int r = __builtin_ctz(met);
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(256) void table_grad_kernel(EmbeddingArgs a) {
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= a.scale;
-    store_8<WHOLE>(to + r * a.lddw, n, v);
+    store_8_once<WHOLE>(to + r * a.lddw, n, v);
   }
 }
 

@@ -9,6 +9,9 @@
 //
 // Bound by memory.  What is read or added up once for a token goes by token, what
 // is read and written for each choice by row.  A thread has 8 columns (16 bytes of bf16) at a time.
+// Results are stored past the caches' order of use: combine's gradient 187 -> 170 us at the
+// sizes below, the sums by token 95 -> 84, and a product over the experts that reads
+// them next is not slower for it, be they 3 MB or 400.
 #include "sort.h"
 
 namespace muon {
@@ -56,8 +59,8 @@ __device__ __forceinline__ bool row_chunk(const RouteArgs& a, int64_t rows, int6
 
 // By token: its row is read once and stored at its choices' rows; the rows behind the
 // last expert's are cleared by the threads of the tokens that their numbers fall to.
-// 16384 x 2048 tokens of 6 choices in bf16 take 75 us, 6.3 TB/s, most of it stores (by
-// row, each reading its token from the cache, 122).
+// 16384 x 2048 tokens of 6 choices in bf16 take 74 to 77 us, 6.2 TB/s, most of it stores
+// (by row, each reading its token from the cache, 122).
 constexpr int kStores = 6;   // choices whose places are looked up together
 template <typename E, bool WHOLE>
 __global__ __launch_bounds__(256) void dispatch_kernel(RouteArgs a) {
@@ -80,15 +83,15 @@ __global__ __launch_bounds__(256) void dispatch_kernel(RouteArgs a) {
 #pragma unroll
     for (int k = 0; k < kStores; ++k) {
       if (j + k >= a.top) continue;
-      if (p[k] >= 0) store_8<WHOLE>(rows + p[k] * a.ldr, n, v);
-      if (s[k] < 0) store_8<WHOLE>(rows + (t * a.top + j + k) * a.ldr, n, zero);
+      if (p[k] >= 0) store_8_once<WHOLE>(rows + p[k] * a.ldr, n, v);
+      if (s[k] < 0) store_8_once<WHOLE>(rows + (t * a.top + j + k) * a.ldr, n, zero);
     }
   }
 }
 // y[t] = r[t] + sum_j w[t, j] rows[position[t, j]]; without weights, the gradient of
 // dispatch.  K choices' loads are in flight together.  16384 x 2048 tokens of 6 choices
-// 101 us with a residual and 88 without (5.3 TB/s), past the caches' order of use; as
-// ordinary loads 135 and 106.
+// 84 us on average with a residual and without (6.0 TB/s), loads past the caches' order of
+// use; with ordinary loads and stores 135 and 106.
 template <typename E, int K, bool WHOLE>
 __global__ __launch_bounds__(256) void gather_kernel(RouteArgs a) {
   int64_t t;
@@ -115,14 +118,14 @@ __global__ __launch_bounds__(256) void gather_kernel(RouteArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = p[k] >= 0 ? fmaf(w[k], x[k][e], v[e]) : v[e];
   }
-  store_8<WHOLE>(static_cast<E*>(a.y) + t * a.ldy + c, n, v);
+  store_8_once<WHOLE>(static_cast<E*>(a.y) + t * a.ldy + c, n, v);
 }
 
 // A wave per row: its gradient, and the product of both rows for the weight's.  A row
 // behind the last expert's stands for a choice of no expert: both are 0.  Two chunks of
 // 512 columns are in flight; both large streams go through memory in order, the tokens'
-// gradients come from the cache: 191 us at 16384 x 2048 and 6 choices, 4.6 TB/s (the
-// rows as ordinary loads 203; by token, with its gradient in registers, 281).
+// gradients come from the cache: 170 us at 16384 x 2048 and 6 choices, 5.1 TB/s (by token,
+// with its gradient in registers, half as slow again).
 template <typename E, bool WHOLE>
 __global__ __launch_bounds__(256) void combine_grad_kernel(RouteArgs a) {
   const int lane = threadIdx.x & 63;
@@ -150,14 +153,14 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(RouteArgs a) {
       dot = fmaf(g[0][e], x[0][e], dot);
       g[0][e] = live ? g[0][e] * w : 0.f;
     }
-    if (dh) store_8<WHOLE>(dh + c, n, g[0]);
+    if (dh) store_8_once<WHOLE>(dh + c, n, g[0]);
     if (two) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         dot = fmaf(g[1][e], x[1][e], dot);
         g[1][e] = live ? g[1][e] * w : 0.f;
       }
-      if (dh) store_8<WHOLE>(dh + c2, n2, g[1]);
+      if (dh) store_8_once<WHOLE>(dh + c2, n2, g[1]);
     }
   }
   if (!a.dweights || !named) return;
