@@ -11,10 +11,10 @@
 // can be a good part of the list: groups of 16 places that lie inside one run are
 // summed first, by blocks of their own, and the row adds up the groups.
 // Bound by memory: dy read once, dW written once.  32768 tokens (their frequency
-// falling with their rank) of a table of 128000 x 4096 in bf16: forward 85 us (6.3
-// TB/s); backward 280 us, of which the sort takes 31 in four launches, the groups 25 and
+// falling with their rank) of a table of 128000 x 4096 in bf16: forward 73 us (7.3
+// TB/s, with what the caches have of frequent rows); backward 280 us, of which the sort takes 31 in four launches, the groups 25 and
 // the table's rows 222 (1.05 GB written, past the caches' order of use: 243 as ordinary
-// stores, and 98 for the lookup after them).  With groups of 64, the block of the most
+// stores).  With groups of 64, the block of the most
 // frequent token ended last, and each block searching its own rows' runs waited for
 // that: 522 us for the table's rows.
 #include "sort.h"
@@ -48,7 +48,11 @@ struct TokenJob {
   }
 };
 
-template <typename E, bool WHOLE>
+// FAR: stored past the caches' order of use.  32768 x 4096 in bf16 then take 73 us for 92,
+// and 194 for 203 with the norm that reads them; of 32 MB the norm finds most in the caches
+// (9 for 11, and 27 for 25).  At 64 MB both are alike.
+constexpr int64_t kFar = int64_t(1) << 26;   // bytes beyond which the output is stored so
+template <typename E, bool WHOLE, bool FAR>
 __global__ __launch_bounds__(256) void lookup_kernel(EmbeddingArgs a) {
   const int chunks = (a.cols + 7) / 8;
   const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, r = i / chunks;
@@ -60,7 +64,11 @@ __global__ __launch_bounds__(256) void lookup_kernel(EmbeddingArgs a) {
   load_8<WHOLE>(static_cast<const E*>(a.w) + (live ? id : 0) * a.ldw + c, n, v);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = live ? v[e] * a.scale : 0.f;
-  store_8<WHOLE>(static_cast<E*>(a.y) + r * a.ldy + c, n, v);
+  E* to = static_cast<E*>(a.y) + r * a.ldy + c;
+  if constexpr (FAR)
+    store_8_once<WHOLE>(to, n, v);
+  else
+    store_8<WHOLE>(to, n, v);
 }
 
 constexpr int kRun = 16;    // places of a group
@@ -178,7 +186,11 @@ template <typename E, bool WHOLE>
 hipError_t forward(const EmbeddingArgs& a, hipStream_t st) {
   const int64_t blocks = (int64_t(a.rows) * ((a.cols + 7) / 8) + 255) / 256;
   if (blocks >= kMaxGrid) return hipErrorInvalidConfiguration;
-  if (blocks) hipLaunchKernelGGL((lookup_kernel<E, WHOLE>), dim3{unsigned(blocks)}, dim3{256}, 0, st, a);
+  const dim3 g{unsigned(blocks)}, b{256};
+  if (int64_t(a.rows) * a.cols * int64_t(sizeof(E)) > kFar)
+    hipLaunchKernelGGL((lookup_kernel<E, WHOLE, true>), g, b, 0, st, a);
+  else if (blocks)
+    hipLaunchKernelGGL((lookup_kernel<E, WHOLE, false>), g, b, 0, st, a);
   return hipGetLastError();
 }
 

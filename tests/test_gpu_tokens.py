@@ -322,6 +322,19 @@ def test_loss_rows_far_apart():
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=ids_of)
+@pytest.mark.parametrize("cols", [1023, 1024])
+def test_lookups_of_many_bytes(cols, dtype):
+    """Outputs of more than 64 MB are stored by another kernel: exact, row by row."""
+    g = gen(cols)
+    rows = (1 << 26) // (cols * dtype.itemsize) + 2
+    w = rand(g, 50, cols, dtype=dtype)
+    ids = numbers(g, 50, rows, outside=0.1)
+    y = layers.embedding_forward(ids, w, scale=0.5)
+    live = (ids >= 0) & (ids < 50)
+    assert torch.equal(y, torch.where(live[:, None], w[ids.clamp(0, 49)] * 0.5, torch.zeros_like(y)))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids_of)
 @pytest.mark.parametrize("shape", [(1, 8, 9), (5, 24, 40), (40, 33, 257), (300, 264, 1000)], ids=ids_of)
 def test_loss_rows_without_a_target_may_hold_anything(shape, dtype):
     """(As the rows of a padded batch do: results are those of zeros in their place.)"""
