@@ -11,12 +11,12 @@
 // can be a good part of the list: groups of 16 places that lie inside one run are
 // summed first, by blocks of their own, and the row adds up the groups.
 // Bound by memory: dy read once, dW written once.  32768 tokens (their frequency
-// falling with their rank) of a table of 128000 x 4096 in bf16: forward 73 us (7.3
-// TB/s, with what the caches have of frequent rows); backward 280 us, of which the sort takes 31 in four launches, the groups 25 and
-// the table's rows 222 (1.05 GB written, past the caches' order of use: 243 as ordinary
-// stores).  With groups of 64, the block of the most
-// frequent token ended last, and each block searching its own rows' runs waited for
-// that: 522 us for the table's rows.
+// falling with their rank) of a table of 128000 x 4096 in bf16: forward 73 us, 86
+// after a backward pass (6.2 TB/s, with what the caches have of frequent rows); backward
+// 275 us, of which the sort takes 30 in four launches, the groups 24 and the table's
+// rows 222 (1.05 GB written, past the caches' order of use: 243 as ordinary stores).
+// With groups of 64, the block of the most frequent token ended last, and each block
+// searching its own rows' runs waited for that: 522 us for the table's rows.
 #include "sort.h"
 
 namespace muon {
