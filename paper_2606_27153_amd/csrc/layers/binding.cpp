@@ -119,6 +119,18 @@ at::Tensor empty_like(const Matrix& x, at::IntArrayRef sizes) {
 
 void called(muon_status s) { need(s == MUON_OK); }
 
+// Other threads run Python meanwhile: an allocation or a launch may wait.
+class NoGil {
+ public:
+  NoGil() : state_(PyEval_SaveThread()) {}
+  ~NoGil() { PyEval_RestoreThread(state_); }
+  NoGil(const NoGil&) = delete;
+  NoGil& operator=(const NoGil&) = delete;
+
+ private:
+  PyThreadState* state_;
+};
+
 // sort_by_expert(experts, count) -> (offsets, position, source)
 PyObject* sort_by_expert(PyObject* const* args, Py_ssize_t n) {
   need(n == 2);
@@ -130,14 +142,19 @@ PyObject* sort_by_expert(PyObject* const* args, Py_ssize_t n) {
   const int64_t tokens = e.t.size(0);
   const int32_t top = int32_t(e.t.size(1));
   void* const stream = stream_of(device);
-  size_t bytes = 0;
-  called(muon_sort_by_expert_workspace_bytes(tokens, top, &bytes));
-  at::Tensor offsets = empty({count + 1}, device, at::kInt), position = empty({tokens, top}, device, at::kInt),
-             source = empty({tokens * top}, device, at::kInt), ws;
-  if (bytes) ws = empty({int64_t(bytes)}, device, at::kByte);
-  called(muon_sort_by_expert(e.p, e.bytes, tokens, top, int32_t(count), static_cast<int32_t*>(offsets.data_ptr()),
-                             static_cast<int32_t*>(position.data_ptr()), static_cast<int32_t*>(source.data_ptr()),
-                             bytes ? ws.data_ptr() : nullptr, bytes, stream));
+  at::Tensor offsets, position, source, ws;
+  {
+    const NoGil run;
+    size_t bytes = 0;
+    called(muon_sort_by_expert_workspace_bytes(tokens, top, &bytes));
+    offsets = empty({count + 1}, device, at::kInt);
+    position = empty({tokens, top}, device, at::kInt);
+    source = empty({tokens * top}, device, at::kInt);
+    if (bytes) ws = empty({int64_t(bytes)}, device, at::kByte);
+    called(muon_sort_by_expert(e.p, e.bytes, tokens, top, int32_t(count), static_cast<int32_t*>(offsets.data_ptr()),
+                               static_cast<int32_t*>(position.data_ptr()), static_cast<int32_t*>(source.data_ptr()),
+                               bytes ? ws.data_ptr() : nullptr, bytes, stream));
+  }
   return Py_BuildValue("NNN", THPVariable_Wrap(offsets), THPVariable_Wrap(position), THPVariable_Wrap(source));
 }
 
@@ -148,9 +165,13 @@ PyObject* dispatch_forward(PyObject* const* args, Py_ssize_t n) {
   const Routing r(args[1], x.device);
   need(x.rows == r.tokens);
   void* const stream = stream_of(x.device);
-  at::Tensor rows = empty_like(x, {r.tokens * r.top, x.cols});
-  called(muon_dispatch_forward(x.p, x.ld, r.position, r.source, rows.data_ptr(), x.cols, r.tokens, r.top, x.cols,
-                               x.dtype, stream));
+  at::Tensor rows;
+  {
+    const NoGil run;
+    rows = empty_like(x, {r.tokens * r.top, x.cols});
+    called(muon_dispatch_forward(x.p, x.ld, r.position, r.source, rows.data_ptr(), x.cols, r.tokens, r.top, x.cols,
+                                 x.dtype, stream));
+  }
   return THPVariable_Wrap(rows);
 }
 
@@ -161,9 +182,13 @@ PyObject* dispatch_backward(PyObject* const* args, Py_ssize_t n) {
   const Routing r(args[1], g.device);
   need(g.rows == r.tokens * r.top);
   void* const stream = stream_of(g.device);
-  at::Tensor dx = empty_like(g, {r.tokens, g.cols});
-  called(muon_dispatch_backward(g.p, g.ld, r.position, dx.data_ptr(), g.cols, r.tokens, r.top, g.cols, g.dtype,
-                                stream));
+  at::Tensor dx;
+  {
+    const NoGil run;
+    dx = empty_like(g, {r.tokens, g.cols});
+    called(muon_dispatch_backward(g.p, g.ld, r.position, dx.data_ptr(), g.cols, r.tokens, r.top, g.cols, g.dtype,
+                                  stream));
+  }
   return THPVariable_Wrap(dx);
 }
 
@@ -183,9 +208,13 @@ PyObject* combine_forward(PyObject* const* args, Py_ssize_t n) {
     ldres = m.ld;
   }
   void* const stream = stream_of(h.device);
-  at::Tensor y = empty_like(h, {r.tokens, h.cols});
-  called(muon_combine_forward(h.p, h.ld, w.p, w.dtype, r.position, res, ldres, y.data_ptr(), h.cols, r.tokens, r.top,
-                              h.cols, h.dtype, stream));
+  at::Tensor y;
+  {
+    const NoGil run;
+    y = empty_like(h, {r.tokens, h.cols});
+    called(muon_combine_forward(h.p, h.ld, w.p, w.dtype, r.position, res, ldres, y.data_ptr(), h.cols, r.tokens, r.top,
+                                h.cols, h.dtype, stream));
+  }
   return THPVariable_Wrap(y);
 }
 
@@ -200,11 +229,15 @@ PyObject* combine_backward(PyObject* const* args, Py_ssize_t n) {
   h.like(g, r.tokens * r.top);
   void* const stream = stream_of(g.device);
   at::Tensor dh, dw;
-  if (args[4] == Py_True) dh = empty_like(g, {h.rows, g.cols});
-  if (args[5] == Py_True) dw = empty({r.tokens, r.top}, g.device, w.dtype == MUON_F32 ? at::kFloat : at::kBFloat16);
-  called(muon_combine_backward(g.p, g.ld, h.p, h.ld, w.p, w.dtype, r.source, dh.defined() ? dh.data_ptr() : nullptr,
-                               g.cols, dw.defined() ? dw.data_ptr() : nullptr, r.tokens, r.top, g.cols, g.dtype,
-                               stream));
+  const bool rows_grad = args[4] == Py_True, weights_grad = args[5] == Py_True;
+  {
+    const NoGil run;
+    if (rows_grad) dh = empty_like(g, {h.rows, g.cols});
+    if (weights_grad) dw = empty({r.tokens, r.top}, g.device, w.dtype == MUON_F32 ? at::kFloat : at::kBFloat16);
+    called(muon_combine_backward(g.p, g.ld, h.p, h.ld, w.p, w.dtype, r.source, dh.defined() ? dh.data_ptr() : nullptr,
+                                 g.cols, dw.defined() ? dw.data_ptr() : nullptr, r.tokens, r.top, g.cols, g.dtype,
+                                 stream));
+  }
   return Py_BuildValue("NN", THPVariable_Wrap(dh), THPVariable_Wrap(dw));   // (None for one that is not there)
 }
 
@@ -217,9 +250,14 @@ PyObject* embedding_forward(PyObject* const* args, Py_ssize_t n) {
   void* const stream = stream_of(w.device);
   c10::SmallVector<int64_t, 5> sizes(ids.t.sizes().begin(), ids.t.sizes().end());
   sizes.push_back(w.cols);
-  at::Tensor y = empty_like(w, sizes);
-  called(muon_embedding_forward(ids.p, ids.bytes, w.p, w.ld, y.data_ptr(), w.cols, ids.t.numel(), w.rows, w.cols,
-                                float(PyFloat_AS_DOUBLE(args[2])), w.dtype, stream));
+  const float scale = float(PyFloat_AS_DOUBLE(args[2]));
+  at::Tensor y;
+  {
+    const NoGil run;
+    y = empty_like(w, sizes);
+    called(muon_embedding_forward(ids.p, ids.bytes, w.p, w.ld, y.data_ptr(), w.cols, ids.t.numel(), w.rows, w.cols,
+                                  scale, w.dtype, stream));
+  }
   return THPVariable_Wrap(y);
 }
 
@@ -235,11 +273,17 @@ PyObject* embedding_backward(PyObject* const* args, Py_ssize_t n) {
   need(dy.sizes().slice(0, ids.t.dim()).equals(ids.t.sizes()) && ids.t.get_device() == device && rows > 0 &&
        cols > 0 && vocab > 0);
   void* const stream = stream_of(device);
-  size_t bytes = 0;
-  called(muon_embedding_workspace_bytes(rows, vocab, cols, &bytes));
-  at::Tensor dw = empty({vocab, cols}, device, dy.scalar_type()), ws = empty({int64_t(bytes)}, device, at::kByte);
-  called(muon_embedding_backward(dy.const_data_ptr(), cols, ids.p, ids.bytes, dw.data_ptr(), cols, rows, vocab, cols,
-                                 float(PyFloat_AS_DOUBLE(args[3])), dtype, ws.data_ptr(), bytes, stream));
+  const float scale = float(PyFloat_AS_DOUBLE(args[3]));
+  at::Tensor dw;
+  {
+    const NoGil run;
+    size_t bytes = 0;
+    called(muon_embedding_workspace_bytes(rows, vocab, cols, &bytes));
+    dw = empty({vocab, cols}, device, dy.scalar_type());
+    const at::Tensor ws = empty({int64_t(bytes)}, device, at::kByte);
+    called(muon_embedding_backward(dy.const_data_ptr(), cols, ids.p, ids.bytes, dw.data_ptr(), cols, rows, vocab, cols,
+                                   scale, dtype, ws.data_ptr(), bytes, stream));
+  }
   return THPVariable_Wrap(dw);
 }
 
@@ -266,7 +310,8 @@ PyMethodDef methods[] = {method<sort_by_expert>("sort_by_expert"),
                          method<embedding_forward>("embedding_forward"),
                          method<embedding_backward>("embedding_backward"),
                          {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module = {PyModuleDef_HEAD_INIT, "_layers_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_layers_binding", nullptr, -1, methods, nullptr, nullptr, nullptr,
+                      nullptr};
 
 }  // namespace
 

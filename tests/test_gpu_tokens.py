@@ -668,3 +668,40 @@ def test_compiled_calls_leave_what_does_not_fit_to_python():
     assert all(v is None for v in none)
     with pytest.raises(MuonError, match="scale"):
         layers.embedding_forward(ids, x, scale=float("nan"))
+
+
+def test_calls_of_two_threads_at_once():
+    """Each on its own stream, with its own sizes and one refusal among its calls."""
+    import threading
+    bad = []
+
+    def work(seed, tokens, experts, cols):
+        g = gen(seed)
+        x, w = rand(g, tokens, cols), torch.rand(tokens, 2, generator=g, device=DEV)
+        choice, ids = numbers(g, experts, tokens, 2), numbers(g, tokens, 40)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(torch.cuda.Stream()):
+            first = None
+            for i in range(200):
+                r = layers.sort_by_expert(choice, experts)
+                h = layers.dispatch_forward(x, r)
+                y = layers.combine_forward(h, w, r, residual=x)
+                dh, dw = layers.combine_backward(y, h, w, r)
+                e = layers.embedding_forward(ids, y)
+                de = layers.embedding_backward(e, ids, tokens)
+                out = (*r, h, y, dh, dw, e, de)
+                if i == 50:
+                    with pytest.raises(ValueError):
+                        layers.dispatch_forward(x[1:], r)
+                first = first or out
+                torch.cuda.current_stream().synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(out, first)):
+                    bad.append((seed, i))
+                    return
+
+    threads = [threading.Thread(target=work, args=a) for a in ((1, 300, 9, 64), (2, 41, 64, 130))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
