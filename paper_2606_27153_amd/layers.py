@@ -929,9 +929,8 @@ def linear_cross_entropy_forward(x: torch.Tensor, weight: torch.Tensor, targets:
     in], weight [in, vocab], targets [rows], and the rows' log of the sum of
     exponentials, which the backward pass reads.  The logits are never kept: the
     vocabulary is gone through in pieces.  A row whose target is ignore_index or
-    outside [0, vocab) has loss 0 and no gradients, whatever it holds, and does not count in
-    the mean.  Both are fp32;
-    loss is one number unless the reduction is "none"."""
+    outside [0, vocab) has loss 0 and no gradients, whatever it holds, and does not
+    count in the mean.  Both are fp32; loss is one number unless the reduction is "none"."""
     lib = _load()
     _input(x)
     red = _reduction(reduction)
