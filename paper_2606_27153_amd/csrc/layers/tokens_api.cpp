@@ -513,7 +513,9 @@ MUON_API muon_status muon_linear_cross_entropy_backward(const float* dloss, cons
   a.each = reduction == MUON_LOSS_ROWS;
   a.lse = const_cast<float*>(lse);
   if (!rows && !dw) return done(hipSuccess, "");
-  if (rows && (dw || !xf)) {
+  // few rows: the weight's gradient reads x as it lies
+  const bool outer_product = rows && rows <= outer_rows(bf16);
+  if (rows && ((dw && !outer_product) || (!xf && !few))) {
     const int64_t ld = copy_shape(rows, inner, epc).ld_dst;
     TRY(done(launch_loss_rows(bf16, a, xo.p, xo.ld, ws + l.xcopy, ld, inner, st), "copy of x"));
     xo = Operand{ws + l.xcopy, ld};
@@ -565,7 +567,15 @@ MUON_API muon_status muon_linear_cross_entropy_backward(const float* dloss, cons
       p.add = c > 0;
       TRY(done(product_sums(l.x, bf16, w_transposed ? FORM_RT : FORM_RR, p, sums, st), "loss input gradient"));
     }
-    if (dw) {
+    if (dw && outer_product) {
+      LossArgs b = a;
+      b.dz = ws + l.dz;
+      b.lddz = lddz;
+      b.cols = int32_t(cols);
+      TRY(done(launch_loss_outer(bf16, !w_transposed, b, xo.p, xo.ld, inner,
+                                 const_cast<void*>(columns(Operand{dw, lddw}, w_transposed, c, es).p), lddw, st),
+               "loss weight gradient"));
+    } else if (dw) {
       Product p{};
       p.K = int32_t(rows);
       p.c = const_cast<void*>(columns(Operand{dw, lddw}, w_transposed, c, es).p); p.ldc = lddw;

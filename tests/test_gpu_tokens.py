@@ -169,7 +169,7 @@ def test_combine_in_place_of_the_residual_and_strided_rows():
 # rows x inner x vocab: one element, odd ones, few rows, one past tiles and strips
 LOSSES = [(1, 1, 1), (3, 7, 13), (2, 40, 3), (5, 64, 300), (1, 4096, 1000), (16, 200, 65), (33, 72, 4100), (64, 128, 5003),
           (65, 256, 768), (129, 200, 2049), (300, 1000, 129), (257, 72, 4100), (700, 136, 1031), (100, 65, 7),
-          (1030, 264, 2056), (0, 16, 40)]
+          (1030, 264, 2056), (18, 824, 4184), (0, 16, 40)]
 
 
 def loss_case(g, rows, inner, vocab, dtype, transposed, outside=0.1, ignore=-100):
@@ -303,6 +303,20 @@ def test_loss_large(case):
     x, w, t = loss_case(g, rows, inner, vocab, dtype, transposed)
     check_loss(x, w, t, "mean", g)
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids_of)
+@pytest.mark.parametrize("rows", [1, 3, 4, 5, 8, 9, 16, 17, 32, 33])
+def test_loss_of_few_rows(rows, dtype):
+    """Whose weight gradient is an outer product: every number of rows that a kernel is made for."""
+    g = gen(rows + 70)
+    for i, (inner, vocab, pad) in enumerate(((37, 1031, 0), (264, 40, 0), (1, 3, 0), (2056, 7, 0), (40, 2056, 3), (33, 31, 1))):
+        x = rand(g, rows, inner + pad, dtype=dtype)[:, :inner]
+        for transposed in (False, True):
+            a, b = (vocab, inner) if transposed else (inner, vocab)
+            w = rand(g, a, b + pad, dtype=dtype, scale=0.1)[:, :b]
+            w = w.t() if transposed else w
+            check_loss(x, w, numbers(g, vocab, rows, outside=0.2), ("mean", "none", "sum")[i % 3], g, ignore=vocab // 2)
 
 
 def test_loss_rows_far_apart():

@@ -140,6 +140,14 @@ hipError_t launch_loss_rows(bool bf16, const LossArgs& a, const void*, int64_t, 
   span("xcopy", y, size_t(a.rows) * ldy * (bf16 ? 2 : 4));
   return hipSuccess;
 }
+hipError_t launch_loss_outer(bool bf16, bool x_down, const LossArgs& a, const void*, int64_t ldx, int64_t inner, void*,
+                             int64_t ldo, hipStream_t) {
+  span("dz", a.dz, block(a.rows, a.lddz, a.cols, bf16 ? 2 : 4));
+  if (a.rows > outer_rows(bf16)) g_failed += " too many rows;";
+  if (ldx < inner || ldo < (x_down ? a.cols : inner)) g_failed += " rows overlap;";
+  g_words += std::string(" weight/outer/") + (bf16 ? "bf16" : "f32");
+  return hipSuccess;
+}
 hipError_t launch_loss_sum(bool, const LossArgs& a, const float* part, int splits, void*, int64_t, int64_t cols,
                            hipStream_t) {
   span("sums", part, size_t(splits) * a.rows * cols * 4);
