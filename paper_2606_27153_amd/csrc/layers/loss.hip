@@ -372,7 +372,7 @@ hipError_t launch_loss_outer(bool bf16, bool x_down, const LossArgs& a, const vo
                              void* out, int64_t ldo, hipStream_t st) {
   const int64_t down = x_down ? inner : a.cols, across = x_down ? a.cols : inner, wide = 256 * (bf16 ? 8 : 4);
   const dim3 g{unsigned((across + wide - 1) / wide), unsigned((down + kOuterRows - 1) / kOuterRows)}, b{256};
-  if (a.rows > outer_rows(bf16) || int64_t(g.x) * 256 >= int64_t(1) << 32 || g.y > 65535) return hipErrorInvalidConfiguration;
+  if (a.rows > outer_rows(bf16) || g.x >= kMaxGrid || g.y > 65535) return hipErrorInvalidConfiguration;
   auto run = [&](auto kernel, auto one) {
     typedef decltype(one) E;
     hipLaunchKernelGGL(kernel, g, b, 0, st, a, static_cast<const E*>(x), ldx, inner, static_cast<E*>(out), ldo);

@@ -149,7 +149,8 @@ hipError_t product_sums(const Choice& c, bool bf16, int form, Product p, float* 
 PackOne copy_of_w(int64_t piece, int64_t inner, bool w_transposed, int64_t epc) {
   return w_transposed ? copy_shape(piece, inner, epc) : copy_shape(inner, piece, epc);
 }
-void take_copies(LossLayout& l, int64_t rows, int64_t inner, bool w_transposed, bool bf16, bool unaligned, bool backward) {
+void take_copies(LossLayout& l, int64_t rows, int64_t inner, bool w_transposed, bool bf16, bool unaligned,
+                 bool backward) {
   const int64_t epc = bf16 ? 8 : 4;
   l.take(l.xcopy, unaligned || backward ? copy_bytes(copy_shape(rows, inner, epc), epc, 1) : 0);
   l.take(l.wcopy, unaligned ? copy_bytes(copy_of_w(l.piece, inner, w_transposed, epc), epc, 1) : 0);
