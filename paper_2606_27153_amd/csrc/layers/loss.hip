@@ -216,16 +216,18 @@ __global__ __launch_bounds__(256) void rows_kernel(LossArgs a, const E* x, int64
 // bytes.  Bound by the stores and, towards the most rows, as much by the M multiply-adds an
 // element: 4096 x 128000 of 8 rows 200 us in bf16 (5.2 TB/s) and 380 in fp32 (5.5), of 20 rows
 // in fp32 450.  The tile kernels, which have one slab of K to do and wait for their
-// stores, take 310 and 590 of any few rows.  X_DOWN: a is x, else b is.
+// stores, take 310 and 590 of any few rows.  Where `out` is narrow, a block's threads are
+// 2^shift columns' by as many rows as there are.  X_DOWN: a is x, else b is.
 constexpr int kOuterRows = 32;
 template <typename E, int M, bool X_DOWN>
 __global__ __launch_bounds__(256) void outer_kernel(LossArgs l, const E* x, int64_t ldx, int64_t inner, E* out,
-                                                    int64_t ldo) {
+                                                    int64_t ldo, int shift) {
   constexpr int N = 16 / sizeof(E);
   __shared__ __attribute__((aligned(16))) float down[kOuterRows][M];
   const E* const dz = static_cast<const E*>(l.dz);
   const int64_t rows = X_DOWN ? inner : l.cols, cols = X_DOWN ? l.cols : inner;
-  const int64_t r0 = int64_t(blockIdx.y) * kOuterRows, c = (int64_t(blockIdx.x) * 256 + threadIdx.x) * N;
+  const int64_t r0 = int64_t(blockIdx.y) * kOuterRows;
+  const int64_t c = ((int64_t(blockIdx.x) << shift) + (threadIdx.x & ((1 << shift) - 1))) * N;
   const int n = int(min(int64_t(N), cols - c)), deep = int(min(int64_t(kOuterRows), rows - r0));
   for (int i = threadIdx.x; i < kOuterRows * M; i += 256) {
     const int m = i / kOuterRows, r = i % kOuterRows;
@@ -259,8 +261,8 @@ __global__ __launch_bounds__(256) void outer_kernel(LossArgs l, const E* x, int6
   const float f = l.alpha ? *l.alpha : 1.f;
   __syncthreads();
   if (n <= 0) return;
-  E* to = out + r0 * ldo + c;
-  for (int r = 0; r < deep; ++r, to += ldo) {
+  for (int r = threadIdx.x >> shift; r < deep; r += 256 >> shift) {
+    E* const to = out + (r0 + r) * ldo + c;
     float v[N] = {};
 #pragma unroll
     for (int m = 0; m < M; m += 4) {
@@ -370,12 +372,16 @@ hipError_t launch_loss_rows(bool bf16, const LossArgs& a, const void* x, int64_t
 
 hipError_t launch_loss_outer(bool bf16, bool x_down, const LossArgs& a, const void* x, int64_t ldx, int64_t inner,
                              void* out, int64_t ldo, hipStream_t st) {
-  const int64_t down = x_down ? inner : a.cols, across = x_down ? a.cols : inner, wide = 256 * (bf16 ? 8 : 4);
+  const int64_t down = x_down ? inner : a.cols, across = x_down ? a.cols : inner, lane = bf16 ? 8 : 4;
+  int shift = 8;
+  while (shift > 3 && across <= lane << (shift - 1)) --shift;
+  const int64_t wide = lane << shift;
   const dim3 g{unsigned((across + wide - 1) / wide), unsigned((down + kOuterRows - 1) / kOuterRows)}, b{256};
   if (a.rows > outer_rows(bf16) || g.x >= kMaxGrid || g.y > 65535) return hipErrorInvalidConfiguration;
   auto run = [&](auto kernel, auto one) {
     typedef decltype(one) E;
-    hipLaunchKernelGGL(kernel, g, b, 0, st, a, static_cast<const E*>(x), ldx, inner, static_cast<E*>(out), ldo);
+    hipLaunchKernelGGL(kernel, g, b, 0, st, a, static_cast<const E*>(x), ldx, inner, static_cast<E*>(out), ldo,
+                       shift);
   };
   auto rows = [&](auto one) {
     typedef decltype(one) E;
