@@ -38,6 +38,7 @@ SIGNATURES = {
 _lock = threading.Lock()
 _lib = None
 _tensors = None
+_written = None
 
 
 def load(path: str = LIB_PATH):
@@ -63,16 +64,24 @@ def load(path: str = LIB_PATH):
 
 def tensors():
     """adamw_tensors(params, grads, states, steps) of csrc/adamw/binding.cpp."""
-    global _tensors
+    global _tensors, _written
     if _tensors is None:
         import torch  # noqa: F401  (whose libraries the extension is linked to)
         try:
-            from ._adamw_binding import adamw_tensors
+            from ._adamw_binding import adamw_tensors, adamw_written
         except ImportError as e:
             raise RuntimeError(f"_adamw_binding.so cannot be loaded ({e}); build it first with "
                                f"`python -m paper_2606_27153_amd.build` (there is no fallback path)") from e
+        _written = adamw_written
         _tensors = adamw_tensors
     return _tensors
+
+
+def written(params, grads, states) -> None:
+    """adamw_written of csrc/adamw/binding.cpp."""
+    if _written is None:
+        tensors()
+    _written(params, grads, states)
 
 
 def check(status: int) -> None:

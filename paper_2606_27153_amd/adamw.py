@@ -111,7 +111,8 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Te
     their gradients (fp32 or bf16; None: the tensor is left as it is) and states
     (``new_state``; all of 32 bits or all of 8), which move on too.  ``step`` counts
     from 1 and is one number or one for each tensor; ``seed`` varies the rounding of 8-bit
-    states.  All tensors are on one GPU and do not overlap.  A step captured into a graph is
+    states.  All tensors are on one GPU and do not overlap.  As any write in place, a step makes
+    autograd refuse a backward pass that would read a param as it was.  A step captured into a graph is
     replayed with the numbers it was captured with."""
     n = len(params)
     if len(grads) != n or len(states) != n:
@@ -130,6 +131,7 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Te
     else:
         with torch.cuda.device(index):
             AL.check(lib.muon_adamw_step(tensors, n, ctypes.byref(opts), torch._C._cuda_getCurrentRawStream(index)))
+    AL.written(params, grads, states)
 
 
 def state_values(state: State) -> Tuple[torch.Tensor, torch.Tensor]:

@@ -131,9 +131,36 @@ PyObject* adamw_tensors(PyObject*, PyObject* const* args, Py_ssize_t count) {
   Py_RETURN_NONE;
 }
 
+// adamw_written(params, grads, states): raises the versions of the tensors that a step
+// with these gradients wrote to (through their addresses, unseen by torch), so that
+// autograd refuses a backward pass that would read one saved before.
+PyObject* adamw_written(PyObject*, PyObject* const* args, Py_ssize_t count) {
+  if (count != 3) {
+    PyErr_SetString(PyExc_TypeError, "adamw_written takes params, grads and states");
+    return nullptr;
+  }
+  const auto written = [](PyObject* o) {
+    if (!THPVariable_Check(o)) return;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.defined() && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();   // (an inference tensor has none)
+  };
+  const Items params(args[0]), grads(args[1]), states(args[2]);
+  if (!params.ok() || !grads.ok() || !states.ok()) return nullptr;
+  for (Py_ssize_t i = 0; i < params.size() && i < grads.size() && i < states.size(); ++i) {
+    if (grads[i] == Py_None) continue;
+    written(params[i]);
+    const Items state(states[i]);
+    if (!state.ok()) return nullptr;
+    for (Py_ssize_t k = 0; k < state.size(); ++k) written(state[k]);
+  }
+  Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
     {"adamw_tensors", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(adamw_tensors)), METH_FASTCALL,
      "The tensors of an AdamW step as the library takes them, or None."},
+    {"adamw_written", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(adamw_written)), METH_FASTCALL,
+     "Raises the versions of the tensors that an AdamW step wrote to."},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_adamw_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -148,3 +148,16 @@ def test_a_refused_step_does_not_count():
         with pytest.raises(ValueError, match="GPU"):
             opt.step()
     assert opt.state[p]["step"] == 0
+
+
+def test_written_tensors_get_another_version():
+    p, q, m, v = (torch.zeros(3) for _ in range(4))
+    with torch.inference_mode():
+        inside = torch.zeros(3)     # (without a version)
+    AL.written([p, q, inside], (p, None, p), [(m, v), [q, q], [inside, inside]])
+    assert p._version > 0 and m._version > 0 and v._version > 0 and q._version == 0
+    AL.written([], [], [])
+    with pytest.raises(TypeError):
+        AL.written(1, 2, 3)
+    with pytest.raises(TypeError):
+        AL.written([p], [p], [4])

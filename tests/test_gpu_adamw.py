@@ -276,3 +276,43 @@ def test_a_state_in_two_places_is_refused(bits):
     with pytest.raises(ValueError, match="again"):
         adamw.adamw_step([p], [d], [(st[0], st[0], *st[2:])], step=1, lr=1e-3)
     assert all(torch.equal(a, b) for a, b in zip(before, (p, q, *st, *other)))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_backward_passes_over_stepped_parameters_are_refused(bits):
+    """A step writes in place: what autograd saved of a parameter before it is gone."""
+    g = gen(40)
+    ps = [torch.nn.Parameter(torch.randn(300, generator=g, device=DEV).to(d)) for d in (F32, BF16)]
+    idle = torch.nn.Parameter(torch.randn(300, generator=g, device=DEV))
+    losses = [(p * p).sum() for p in (*ps, idle)]
+    opt = AdamW([*ps, idle], state_bits=bits)
+    for p in ps:
+        p.grad = torch.ones_like(p)
+    opt.step()
+    for loss in losses[:2]:
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    losses[2].backward()      # (no gradient, no step)
+    assert torch.equal(idle.grad, 2 * idle.detach())
+    # by the function: params of any kind, states too; a refused step writes nothing
+    p, d, st = make(g, (40,), F32, F32, bits)
+    with torch.inference_mode():
+        q, e, other = make(g, (40,), F32, F32, bits)
+    kept = [t._version for t in (p, d, *st)]
+    with pytest.raises(MuonError):
+        adamw.adamw_step([p], [d], [st], step=0, lr=1e-3)
+    assert [t._version for t in (p, d, *st)] == kept
+    adamw.adamw_step([p, q], (d, e), [st, list(other)], step=1, lr=1e-3)
+    assert d._version == kept[1]
+    assert all(t._version > k for t, k in zip((p, *st), [kept[0], *kept[2:]]))
+
+
+def test_the_versions_of_parameters_by_one_check_after_the_other():
+    """The same where the tensors are not read by compiled code (a gradient is None)."""
+    g = gen(41)
+    p, d, st = make(g, (40,), F32, F32, 32)
+    q, _, other = make(g, (40,), F32, F32, 32)
+    kept = [t._version for t in (p, *st, q, *other)]
+    adamw.adamw_step([p, q], [d, None], [st, other], step=1, lr=1e-3)
+    now = [t._version for t in (p, *st, q, *other)]
+    assert all(a > b for a, b in zip(now[:3], kept[:3])) and now[3:] == kept[3:]
