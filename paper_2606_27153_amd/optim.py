@@ -307,7 +307,9 @@ class Muon(_optimizer_base()):
     gradient is passed to the library as a skipped matrix (its param and
     momentum stay as they are), so a changing set of routed MoE experts
     reuses the same plan.  The plans of all groups share one workspace per
-    device, sized to the largest.  ``ns_coefficients`` is None (the quintic
+    device, sized to the largest.  As any write in place, a step makes autograd
+    refuse a backward pass that would read a parameter as it was.
+    ``ns_coefficients`` is None (the quintic
     (3.4445, -4.7750, 2.0315) at every step), one (a, b, c), or one triple
     per NS step.
     """
@@ -396,4 +398,6 @@ class Muon(_optimizer_base()):
             plan.step(params, grads, moms, lr=group["lr"], momentum=group["momentum"],
                       weight_decay=group["weight_decay"], ns_steps=group["ns_steps"],
                       nesterov=group["nesterov"], workspace=ws)
+            # (written through their addresses: autograd refuses backward passes over what was saved of them before)
+            torch.autograd.graph.increment_version([t for p, m in zip(ps, moms) if p.grad is not None for t in (p, m)])
         return loss

@@ -527,3 +527,23 @@ def test_bench_times_the_schedule_a_caller_gets(capsys):
     assert line["steps"] == 30 and line["value"] == line["ms_per_step"]
     assert line["value"] < 0.7 * line["split_ms_per_step"]
     assert {k["kind"] for k in line["kernels"]} >= {"momentum", "finalize", "gram", "poly", "bx"}
+
+
+def test_backward_passes_over_stepped_parameters_are_refused():
+    """A step writes in place: what autograd saved of a parameter before it is gone."""
+    g = torch.Generator(device="cuda:0").manual_seed(40)
+    ps = [torch.nn.Parameter(torch.randn(64, 96, generator=g, device="cuda:0").to(d))
+          for d in (torch.float32, torch.bfloat16)]
+    idle = torch.nn.Parameter(torch.randn(64, 96, generator=g, device="cuda:0"))
+    opt = Muon([*ps, idle])
+    for step in range(2):
+        losses = [(p * p).sum() for p in (*ps, idle)]
+        for p in ps:
+            p.grad = torch.randn(64, 96, generator=g, device="cuda:0").to(p.dtype)
+        idle.grad = None
+        opt.step()
+        for loss in losses[:2]:
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                loss.backward()
+        losses[2].backward()      # (no gradient, no step)
+        assert torch.equal(idle.grad, 2 * idle.detach())
