@@ -65,7 +65,7 @@ RouteArgs route_args(int64_t tokens, int64_t top, int64_t cols, const int32_t* p
 // -------------------------------------------------------------------- loss
 
 // Rows at a time, fewer in a forward pass over a very large vocabulary: its strips'
-// sums take 8 bytes a row and 128 columns or so, 1 GB in all.
+// sums take 8 bytes a row and strip, 1 GB in all.
 constexpr int64_t kLossRows = 32768;
 constexpr int64_t kLossSums = int64_t(1) << 27;
 // Columns of a piece: as many as one grid has tiles for; where the weight has to
@@ -158,11 +158,16 @@ void take_copies(LossLayout& l, int64_t rows, int64_t inner, bool w_transposed, 
 
 LossLayout forward_layout(int64_t rows, int64_t inner, int64_t outer, bool w_transposed, bool bf16, bool unaligned) {
   LossLayout l;
-  int64_t most = kLossSums / ceil_div(outer, 128);
-  most = most < 256 ? 256 : most > kLossRows ? kLossRows : most;
-  l.rows = rows < most ? rows : most;
   l.piece = even_piece(outer, unaligned ? kCopyPiece : kPiece);
-  l.z = choose_logits(bf16, w_transposed, l.rows, l.piece, inner);
+  // as many rows as the strips of the kernel chosen for them allow: 256 at least (2^24
+  // columns by 32)
+  for (int64_t strip = 128;;) {
+    const int64_t sums = kLossSums / ceil_div(outer, strip), most = sums < kLossRows ? sums : kLossRows;
+    l.rows = rows < most ? rows : most;
+    l.z = choose_logits(bf16, w_transposed, l.rows, l.piece, inner);
+    if (strip_columns(l.z) >= strip) break;
+    strip = strip_columns(l.z);
+  }
   l.take(l.logit, size_t(rows) * 4);
   l.take(l.loss, size_t(rows) * 4);
   l.take(l.part, size_t(ceil_div(outer, l.piece)) * size_t(ceil_div(l.piece, strip_columns(l.z))) * size_t(l.rows) * 8);

@@ -155,3 +155,16 @@ def test_python_refusals_without_a_gpu():
                  lambda: layers.combine(x, None, None)):
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("outer", [131072, 524288, 1 << 20, 3000001, 1 << 24])
+def test_the_losss_sums_over_a_very_large_vocabulary_stay_in_1_gb(lay, outer, dtype):
+    """The forward pass's workspace: 2^27 sums of 8 bytes at most (their places are counted
+    piece by piece, so up to 64 columns' worth more for each of the pieces), and two
+    numbers a row."""
+    n = ctypes.c_size_t()
+    for rows in (33, 64, 300, 5000, 20000, 32768, 1 << 20):
+        for inner in (64, 256):
+            assert lay.muon_linear_cross_entropy_workspace_bytes(rows, inner, outer, dtype, 0, ctypes.byref(n)) == L.MUON_OK
+            assert n.value <= (1 << 30) + (64 * 32768 * 8) + 8 * rows + 1024, (rows, n.value)

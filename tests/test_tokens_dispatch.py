@@ -75,3 +75,10 @@ def test_every_reachable_kernel_has_a_gpu_case(passes):
     assert not missing, missing
     for w in ("strips/tile256/bf16/RT/0", "dz/tile256/bf16/RR/0", "weight/tile64/f32/TT/1", "dz/rows/bf16"):
         assert w in covered
+
+
+def test_very_large_vocabularies_are_taken_in_fewer_rows_at_a_time(passes):
+    """(The buffers in bounds and apart, as above, where rows and columns both come in pieces.)"""
+    words = passes([f"{bf16} {t} {rows} 16 {vocab} {off} 2" for bf16 in (0, 1) for t in (0, 1)
+                    for rows in (300, 5000, 40000) for vocab in (524288, 3000001, 1 << 24) for off in (0, 1)])
+    assert all(w for w in words)
