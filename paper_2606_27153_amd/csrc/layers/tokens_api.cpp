@@ -76,7 +76,11 @@ constexpr int64_t kGradPiece = int64_t(1) << 29;
 
 int64_t even_piece(int64_t outer, int64_t most) {
   const int64_t pieces = ceil_div(outer, most);
-  const int64_t p = ceil_div(ceil_div(outer, pieces), 256) * 256;
+  int64_t p = ceil_div(ceil_div(outer, pieces), 256) * 256;
+  // of many pieces the last can be short: not below the 16 bytes of columns that the kernel of
+  // few rows needs (their pieces are never smaller than these: two steps down are enough for
+  // all of the 2^24 columns)
+  while (most >= kCopyPiece && p > 256 && p < outer && outer % p && outer % p < 8) p -= 256;
   return p < outer ? p : outer;
 }
 size_t larger(size_t a, size_t b) { return a > b ? a : b; }

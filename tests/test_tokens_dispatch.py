@@ -82,3 +82,11 @@ def test_very_large_vocabularies_are_taken_in_fewer_rows_at_a_time(passes):
     words = passes([f"{bf16} {t} {rows} 16 {vocab} {off} 2" for bf16 in (0, 1) for t in (0, 1)
                     for rows in (300, 5000, 40000) for vocab in (524288, 3000001, 1 << 24) for off in (0, 1)])
     assert all(w for w in words)
+
+
+def test_last_pieces_of_few_rows_have_columns_enough(passes):
+    """Columns that 32768 at a time would leave 1 to 7 of: the kernel of few rows reads 16
+    bytes of them."""
+    vocabs = [v for v in range(32768 * 127 + 1, 1 << 24, 32768) for v in (v, v + 2, v + 6)][::13]
+    words = passes([f"{bf16} 0 {rows} 8 {v} 1 2" for bf16 in (0, 1) for rows in (1, 20) for v in vocabs])
+    assert all(any(w.startswith("logits/skinny") for w in line) for line in words)
