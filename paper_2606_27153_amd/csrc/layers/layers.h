@@ -172,7 +172,8 @@ hipError_t launch_loss_grad(bool bf16, const LossArgs& a, hipStream_t st);   // 
 hipError_t launch_loss_rows(bool bf16, const LossArgs& a, const void* x, int64_t ldx, void* y, int64_t ldy,
                             int64_t cols, hipStream_t st);
 // The weight's gradient (a piece: a.cols columns; x_down: kept as [inner, cols], else
-// [cols, inner]) of at most outer_rows rows, from x as it lies and dz.
+// [cols, inner]) of at most outer_rows rows, from x as it lies and dz (which sizes take
+// it: outer_product_wins).
 constexpr int outer_rows(bool bf16) { return bf16 ? 16 : 32; }
 hipError_t launch_loss_outer(bool bf16, bool x_down, const LossArgs& a, const void* x, int64_t ldx, int64_t inner,
                              void* out, int64_t ldo, hipStream_t st);

@@ -719,3 +719,15 @@ def test_calls_of_two_threads_at_once():
     for t in threads:
         t.join()
     assert not bad
+
+
+@pytest.mark.parametrize("case", [(9, 1344, 66001, torch.bfloat16), (16, 1329, 66048, torch.bfloat16),
+                                  (17, 680, 66001, torch.float32), (32, 669, 66048, torch.float32)], ids=ids_of)
+def test_large_weight_gradients_of_few_rows(case):
+    """Of more than 160 MB: the outer products of the most rows."""
+    rows, inner, vocab, dtype = case
+    g = gen(rows + 170)
+    for transposed in (False, True):
+        x, w, t = loss_case(g, rows, inner, vocab, dtype, transposed, outside=0.2)
+        check_loss(x, w, t, "none" if transposed else "sum", g)
+        torch.cuda.empty_cache()

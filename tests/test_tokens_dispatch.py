@@ -90,3 +90,21 @@ def test_last_pieces_of_few_rows_have_columns_enough(passes):
     vocabs = [v for v in range(32768 * 127 + 1, 1 << 24, 32768) for v in (v, v + 2, v + 6)][::13]
     words = passes([f"{bf16} 0 {rows} 8 {v} 1 2" for bf16 in (0, 1) for rows in (1, 20) for v in vocabs])
     assert all(any(w.startswith("logits/skinny") for w in line) for line in words)
+
+
+def test_weight_gradients_of_few_rows_by_size(passes):
+    """The outer product where its streamed stores count, the tiles where the gradient is small."""
+    cases = [  # rows, inner, vocab, transposed, dtype, outer product
+        (1, 64, 1000, False, torch.bfloat16, True), (4, 256, 16384, True, torch.bfloat16, True),
+        (8, 200, 10727, False, torch.float32, True), (8, 4096, 128000, False, torch.bfloat16, True),
+        (8, 200, 10727, True, torch.bfloat16, True), (8, 200, 10727, False, torch.bfloat16, False),
+        (8, 4096, 2000, True, torch.bfloat16, False), (6, 512, 32000, False, torch.bfloat16, True),
+        (16, 200, 10727, True, torch.float32, True), (16, 256, 16384, False, torch.float32, False),
+        (10, 200, 10727, True, torch.bfloat16, False), (16, 1024, 65536, True, torch.bfloat16, False),
+        (16, 2048, 65536, True, torch.bfloat16, True), (9, 4096, 128000, False, torch.bfloat16, True),
+        (32, 256, 32000, True, torch.float32, False), (20, 1408, 32000, False, torch.float32, True),
+        (17, 4096, 128000, False, torch.bfloat16, False), (33, 4096, 128000, False, torch.float32, False)]
+    words = passes([_line(dtype, t, rows, inner, vocab) for rows, inner, vocab, t, dtype, _ in cases])
+    for line, case in zip(words, cases):
+        assert any(w.startswith("weight/outer") for w in line) == case[-1], (case, line)
+        assert sum(w.startswith("weight") for w in line) == 1, line
