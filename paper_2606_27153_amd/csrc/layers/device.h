@@ -190,6 +190,25 @@ __device__ __forceinline__ void store_8_once(E* p, int n, const float (&v)[8]) {
   }
 }
 
+// The same where what is past the caches has to be whole lines: in 16 bits, of which a
+// wave's instruction has one run of bytes.  In 32 bits each of a thread's two has half of every
+// 32 bytes, which the caches put together: 16384 x 2048 tokens at 6 choices' rows 211 us for 358
+// past them, a table's gradient of 128000 x 4096 600 for 915.
+template <bool WHOLE, typename E>
+__device__ __forceinline__ void load_8_run(const E* p, int n, float (&v)[8]) {
+  if constexpr (sizeof(E) == 2)
+    load_8_once<WHOLE>(p, n, v);
+  else
+    load_8<WHOLE>(p, n, v);
+}
+template <bool WHOLE, typename E>
+__device__ __forceinline__ void store_8_run(E* p, int n, const float (&v)[8]) {
+  if constexpr (sizeof(E) == 2)
+    store_8_once<WHOLE>(p, n, v);
+  else
+    store_8<WHOLE>(p, n, v);
+}
+
 // Number i of a list of int64 or int32.
 __device__ __forceinline__ int64_t id_at(const void* ids, int bytes, int64_t i) {
   return bytes == 8 ? static_cast<const int64_t*>(ids)[i] : int64_t(static_cast<const int32_t*>(ids)[i]);

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(256) void table_grad_kernel(EmbeddingArgs a) {
     if (start[r] < start[r + 1])
       met |= 1u << r;
     else if (v0 + r < a.vocab)
-      store_8_once<WHOLE>(to + r * a.lddw, n, zero);
+      store_8_run<WHOLE>(to + r * a.lddw, n, zero);
   }
   while (met) {
     const int r = __builtin_ctz(met);
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(256) void table_grad_kernel(EmbeddingArgs a) {
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= a.scale;
-    store_8_once<WHOLE>(to + r * a.lddw, n, v);
+    store_8_run<WHOLE>(to + r * a.lddw, n, v);
   }
 }
 

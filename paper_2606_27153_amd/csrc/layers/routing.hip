@@ -9,7 +9,7 @@
 //
 // Bound by memory.  What is read or added up once for a token goes by token, what
 // is read and written for each choice by row.  A thread has 8 columns (16 bytes of bf16) at a time.
-// Results are stored past the caches' order of use: combine's gradient 187 -> 170 us at the
+// Results in bf16 are stored past the caches' order of use: combine's gradient 187 -> 170 us at the
 // sizes below, the sums by token 95 -> 84, and a product over the experts that reads
 // them next is not slower for it, be they 3 MB or 400.
 #include "sort.h"
@@ -83,15 +83,16 @@ __global__ __launch_bounds__(256) void dispatch_kernel(RouteArgs a) {
 #pragma unroll
     for (int k = 0; k < kStores; ++k) {
       if (j + k >= a.top) continue;
-      if (p[k] >= 0) store_8_once<WHOLE>(rows + p[k] * a.ldr, n, v);
-      if (s[k] < 0) store_8_once<WHOLE>(rows + (t * a.top + j + k) * a.ldr, n, zero);
+      if (p[k] >= 0) store_8_run<WHOLE>(rows + p[k] * a.ldr, n, v);
+      if (s[k] < 0) store_8_run<WHOLE>(rows + (t * a.top + j + k) * a.ldr, n, zero);
     }
   }
 }
 // y[t] = r[t] + sum_j w[t, j] rows[position[t, j]]; without weights, the gradient of
 // dispatch.  K choices' loads are in flight together.  16384 x 2048 tokens of 6 choices
 // 84 us on average with a residual and without (6.0 TB/s), loads past the caches' order of
-// use; with ordinary loads and stores 135 and 106.
+// use; with ordinary loads and stores 135 and 106.  In fp32 176 and 202 with ordinary ones (past the
+// caches 191 and 212; 4096 x 1024 18 and 20, 25 and 26).
 template <typename E, int K, bool WHOLE>
 __global__ __launch_bounds__(256) void gather_kernel(RouteArgs a) {
   int64_t t;
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(256) void gather_kernel(RouteArgs a) {
   const int64_t all = int64_t(a.tokens) * a.top;
   const E* rows = static_cast<const E*>(a.rows) + c;
   float v[8] = {};
-  if (a.res) load_8_once<WHOLE>(static_cast<const E*>(a.res) + t * a.ldres + c, n, v);
+  if (a.res) load_8_run<WHOLE>(static_cast<const E*>(a.res) + t * a.ldres + c, n, v);
   for (int j = 0; j < a.top; j += K) {
     float x[K][8], w[K];
     int p[K];
@@ -112,13 +113,13 @@ __global__ __launch_bounds__(256) void gather_kernel(RouteArgs a) {
       w[k] = weight_of<E>(a, slot);
     }
 #pragma unroll
-    for (int k = 0; k < K; ++k) load_8_once<WHOLE>(rows + max(p[k], 0) * a.ldr, n, x[k]);
+    for (int k = 0; k < K; ++k) load_8_run<WHOLE>(rows + max(p[k], 0) * a.ldr, n, x[k]);
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = p[k] >= 0 ? fmaf(w[k], x[k][e], v[e]) : v[e];
   }
-  store_8_once<WHOLE>(static_cast<E*>(a.y) + t * a.ldy + c, n, v);
+  store_8_run<WHOLE>(static_cast<E*>(a.y) + t * a.ldy + c, n, v);
 }
 
 // A wave per row: its gradient, and the product of both rows for the weight's.  A row
