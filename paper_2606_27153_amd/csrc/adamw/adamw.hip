@@ -27,10 +27,10 @@ template <typename A, typename B>
 struct Pick<false, A, B> {
   typedef B T;
 };
-template <bool WHOLE, typename E, int N>
+template <bool WHOLE, bool ONCE = true, typename E, int N>
 __device__ __forceinline__ void load(const E* p, int64_t n, float (&v)[N]) {
   if (WHOLE || n >= N) {
-    // past the caches' order of use: everything is read once (977 us for 1009 of 8-bit states)
+    // ONCE: past the caches' order of use, as everything is read once (977 us for 1009 of 8-bit states)
     typedef uint32_t Words __attribute__((ext_vector_type(2), aligned(2)));
     typedef uint32_t Words4 __attribute__((ext_vector_type(4), aligned(2)));
     constexpr bool FOUR = N * sizeof(E) % 16 == 0;
@@ -38,7 +38,7 @@ __device__ __forceinline__ void load(const E* p, int64_t n, float (&v)[N]) {
     W w[N * sizeof(E) / sizeof(W)];
 #pragma unroll
     for (int i = 0; i < int(N * sizeof(E) / sizeof(W)); ++i)
-      w[i] = __builtin_nontemporal_load(reinterpret_cast<const W*>(p) + i);
+      w[i] = ONCE ? __builtin_nontemporal_load(reinterpret_cast<const W*>(p) + i) : reinterpret_cast<const W*>(p)[i];
     const Packed<E, N> x = __builtin_bit_cast(Packed<E, N>, w);
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] = float(x.v[e]);
@@ -49,7 +49,7 @@ __device__ __forceinline__ void load(const E* p, int64_t n, float (&v)[N]) {
 }
 // Past them as well: 131 million elements with 32-bit states 496 us for 529, 525 million with
 // 8-bit ones and the values read out 1428 for 1535.
-template <bool WHOLE, typename E, int N>
+template <bool WHOLE, bool ONCE = true, typename E, int N>
 __device__ __forceinline__ void store(E* p, int64_t n, const float (&v)[N]) {
   if (WHOLE || n >= N) {
     Packed<E, N> x;
@@ -64,7 +64,12 @@ __device__ __forceinline__ void store(E* p, int64_t n, const float (&v)[N]) {
     };
     const All b = __builtin_bit_cast(All, x);
 #pragma unroll
-    for (int i = 0; i < int(N * sizeof(E) / sizeof(W)); ++i) __builtin_nontemporal_store(b.w[i], reinterpret_cast<W*>(p) + i);
+    for (int i = 0; i < int(N * sizeof(E) / sizeof(W)); ++i) {
+      if constexpr (ONCE)
+        __builtin_nontemporal_store(b.w[i], reinterpret_cast<W*>(p) + i);
+      else
+        reinterpret_cast<W*>(p)[i] = b.w[i];
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < N; ++e)
@@ -210,14 +215,18 @@ __device__ __forceinline__ void step8(const Args& a, const Tensor& t, int64_t st
   uint32_t key = t.key;
   if (start >> 32) key = mix(key + uint32_t(start >> 32));   // (a chunk does not cross a multiple of 2^32)
   constexpr int U = kChunk / 2048;
+  // 8 fp32 neighbours are two halves of every 32 bytes of a wave's run, which the caches have to
+  // put together (134 million parameters with gradients in fp32 385 us for 465, in bf16 338
+  // for 405; their gradients alone, with bf16 parameters, lose 5%)
+  constexpr bool ONCE = sizeof(P) == 2;
   float w[U][8], d[U][8];
   Codes om[U], ov[U];
   int obm[U], obv[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int64_t i = start + u * 2048 + threadIdx.x * 8, n = max(t.n - i, int64_t(0));
-    load<WHOLE>(static_cast<const P*>(t.p) + i, n, w[u]);
-    load<WHOLE>(static_cast<const G*>(t.g) + i, n, d[u]);
+    load<WHOLE, ONCE>(static_cast<const P*>(t.p) + i, n, w[u]);
+    load<WHOLE, ONCE || sizeof(G) == 2>(static_cast<const G*>(t.g) + i, n, d[u]);
     om[u] = load_codes<WHOLE, true>(static_cast<const uint8_t*>(t.m) + i, n);
     ov[u] = load_codes<WHOLE, true>(static_cast<const uint8_t*>(t.v) + i, n);
     const int16_t* base = t.bases + i / kBlock * 2;
@@ -238,7 +247,7 @@ __device__ __forceinline__ void step8(const Args& a, const Tensor& t, int64_t st
       top_m = max(top_m, __builtin_bit_cast(uint32_t, m[e]) & 0x7fffffffu);
       top_v = max(top_v, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
     }
-    store<WHOLE>(static_cast<P*>(t.p) + i, n, w[u]);
+    store<WHOLE, ONCE>(static_cast<P*>(t.p) + i, n, w[u]);
     const int bm = base_of<true>(block_max(top_m)), bv = base_of<false>(block_max(top_v));
     Codes cm{}, cv{};
     uint32_t at = uint32_t(i) * 0x9E3779B1u;
