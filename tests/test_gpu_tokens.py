@@ -731,3 +731,54 @@ def test_large_weight_gradients_of_few_rows(case):
         x, w, t = loss_case(g, rows, inner, vocab, dtype, transposed, outside=0.2)
         check_loss(x, w, t, "none" if transposed else "sum", g)
         torch.cuda.empty_cache()
+
+
+def test_calls_of_two_threads_give_what_one_gives():
+    """Threads on streams of their own, with refusals among their calls: every output is that
+    of the same calls made before by one thread, and what a thread raises is raised here."""
+    from concurrent.futures import ThreadPoolExecutor
+    from paper_2606_27153_amd import adamw
+    rounds = 200
+
+    def inputs(seed, tokens, experts, cols):
+        g = gen(seed)
+        return dict(x=rand(g, tokens, cols), w=torch.rand(tokens, 2, generator=g, device=DEV), experts=experts,
+                    choice=numbers(g, experts, tokens, 2), ids=numbers(g, tokens, 40), t=numbers(g, tokens, tokens),
+                    p=rand(g, tokens, cols), state=adamw.new_state(torch.empty(tokens, cols, device=DEV), 8))
+
+    def calls(a):
+        r = layers.sort_by_expert(a["choice"], a["experts"])
+        h = layers.dispatch_forward(a["x"], r)
+        y = layers.combine_forward(h, a["w"], r, residual=a["x"])
+        dx = layers.dispatch_backward(h, r)
+        dh, dw = layers.combine_backward(y, h, a["w"], r)
+        e = layers.embedding_forward(a["ids"], y)
+        de = layers.embedding_backward(e, a["ids"], len(a["x"]))
+        loss, lse = layers.linear_cross_entropy_forward(a["x"], y.t(), a["t"], reduction="sum")
+        grads = layers.linear_cross_entropy_backward(torch.ones_like(loss), a["x"], y.t(), a["t"], lse, reduction="sum")
+        p, state = a["p"].clone(), [s.clone() for s in a["state"]]
+        adamw.adamw_step([p], [dx], [state], step=1, lr=1e-3)
+        return (*r, h, y, dx, dh, dw, e, de, loss, lse, *grads, p, *state)
+
+    cases = [inputs(1, 300, 9, 64), inputs(2, 41, 64, 130)]
+    want = [calls(a) for a in cases]
+    torch.cuda.synchronize()
+
+    def work(k):
+        a, done = cases[k], 0
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for i in range(rounds):
+                got = calls(a)
+                if i % 50 == 7:
+                    with pytest.raises(ValueError):
+                        layers.dispatch_forward(a["x"][1:], got[:3])
+                    with pytest.raises(MuonError):
+                        layers.embedding_forward(a["ids"], a["x"], scale=float("inf"))
+                torch.cuda.current_stream().synchronize()
+                for j, (v, w) in enumerate(zip(got, want[k])):
+                    assert torch.equal(v, w), (k, i, j)
+                done += 1
+        return done
+
+    with ThreadPoolExecutor(2) as pool:
+        assert [f.result() for f in [pool.submit(work, k) for k in (0, 1)]] == [rounds, rounds]
