@@ -782,3 +782,24 @@ def test_calls_of_two_threads_give_what_one_gives():
 
     with ThreadPoolExecutor(2) as pool:
         assert [f.result() for f in [pool.submit(work, k) for k in (0, 1)]] == [rounds, rounds]
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ids_of)
+@pytest.mark.parametrize("tokens,top,cols,pad", [(1, 1, 1, 0), (40, 3, 50, 11), (300, 6, 264, 0), (65, 9, 136, 24),
+                                                 (33, 17, 77, 3)])
+def test_combine_writes_over_its_residual(tokens, top, cols, pad, dtype):
+    """y in the residual's own buffer (same ld), as the C ABI allows: bit by bit what another
+    buffer gets, and nothing beside its rows."""
+    g = gen(tokens + 60)
+    lib = layers._load()
+    routing = layers.sort_by_expert(numbers(g, 19, tokens, top, outside=0.2), 19)
+    h, w = rand(g, tokens * top, cols, dtype=dtype), torch.rand(tokens, top, generator=g, device=DEV)
+    wide = rand(g, tokens + 2, cols + pad, dtype=dtype)
+    y = wide[1:-1, pad // 2:pad // 2 + cols]
+    want = wide.clone()
+    want[1:-1, pad // 2:pad // 2 + cols] = layers.combine_forward(h, w, routing, residual=y)
+    code = layers._DTYPES[dtype]
+    layers.LL.check(lib.muon_combine_forward(
+        h.data_ptr(), cols, w.data_ptr(), layers.MUON_F32, routing.position.data_ptr(), y.data_ptr(), cols + pad,
+        y.data_ptr(), cols + pad, tokens, top, cols, code, torch.cuda.current_stream().cuda_stream))
+    assert torch.equal(wide, want)
