@@ -915,6 +915,13 @@ def _reduction(name: str) -> int:
     return code
 
 
+def _ignore(index) -> int:
+    index = int(index)
+    if not -1 << 63 <= index < 1 << 63:
+        raise ValueError(f"ignore_index {index} does not fit in 64 bits")
+    return index
+
+
 def _loss_flags(backward: int, x: torch.Tensor, outer: int, xp: int, ldx: int, wp: int, ldw: int) -> int:
     """_flags, and room for the copies that rows far apart need too."""
     size = x.element_size()
@@ -941,7 +948,7 @@ def linear_cross_entropy_forward(x: torch.Tensor, weight: torch.Tensor, targets:
     if outer == 0:
         raise ValueError("weight has no output features")
     tp, tsize = _numbers(targets, "targets", (rows,), x)
-    ignore = int(ignore_index)
+    ignore = _ignore(ignore_index)
     stream = _stream(x)
     lse = x.new_empty((rows,), dtype=torch.float32)
     loss = x.new_empty((rows,) if red == 0 else (), dtype=torch.float32)
@@ -977,7 +984,7 @@ def linear_cross_entropy_backward(dloss: torch.Tensor, x: torch.Tensor, weight: 
             raise ValueError(f"{name} must be a contiguous float32 tensor of shape {shape}")
         if t.device != x.device:
             raise ValueError(f"{name} is on {t.device}, expected {x.device}")
-    ignore = int(ignore_index)
+    ignore = _ignore(ignore_index)
     stream = _stream(x)
     dx = x.new_empty((rows, inner)) if input_grad else None
     dw = _like_weight(weight, wt) if weight_grad else None

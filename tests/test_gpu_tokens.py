@@ -803,3 +803,17 @@ def test_combine_writes_over_its_residual(tokens, top, cols, pad, dtype):
         h.data_ptr(), cols, w.data_ptr(), layers.MUON_F32, routing.position.data_ptr(), y.data_ptr(), cols + pad,
         y.data_ptr(), cols + pad, tokens, top, cols, code, torch.cuda.current_stream().cuda_stream))
     assert torch.equal(wide, want)
+
+
+def test_an_ignore_index_of_more_than_64_bits_is_refused():
+    """(Cut to 64 bits it would be a token's.)"""
+    x, w = torch.ones(2, 8, device=DEV), torch.ones(8, 6, device=DEV)
+    t = torch.tensor([5, 1], device=DEV)
+    loss, lse = layers.linear_cross_entropy_forward(x, w, t, ignore_index=-1 << 63)
+    for index in ((1 << 64) + 5, 1 << 63, -(1 << 63) - 1):
+        with pytest.raises(ValueError, match="64 bits"):
+            layers.linear_cross_entropy_forward(x, w, t, ignore_index=index)
+        with pytest.raises(ValueError, match="64 bits"):
+            layers.linear_cross_entropy_backward(loss, x, w, t, lse, ignore_index=index)
+        with pytest.raises(ValueError, match="64 bits"):
+            layers.linear_cross_entropy(x, w, t, ignore_index=index)
