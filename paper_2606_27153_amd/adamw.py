@@ -99,6 +99,8 @@ def _one_by_one(params, grads, states, steps):
             raise ValueError(f"grad {i} must be contiguous and of param {i}'s shape {tuple(p.shape)}")
         if g.device != device:
             raise ValueError(f"grad {i} is on {g.device}, expected {device}")
+        if not -1 << 63 <= steps[i] < 1 << 63:
+            raise ValueError(f"step {steps[i]} of param {i} does not fit in 64 bits")
         found.append(AL.muon_adamw_tensor(p.data_ptr(), g.data_ptr(), s[0].data_ptr(), s[1].data_ptr(),
                                           s[2].data_ptr() if b == 8 else None, p.numel(), steps[i], pc, gc))
     return b"".join(map(bytes, found)), device.index, bits

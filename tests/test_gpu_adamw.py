@@ -316,3 +316,15 @@ def test_the_versions_of_parameters_by_one_check_after_the_other():
     adamw.adamw_step([p, q], [d, None], [st, other], step=1, lr=1e-3)
     now = [t._version for t in (p, *st, q, *other)]
     assert all(a > b for a, b in zip(now[:3], kept[:3])) and now[3:] == kept[3:]
+
+
+def test_steps_of_more_than_64_bits_are_refused():
+    """(Cut to 64 bits they would be others.)"""
+    g = gen(42)
+    p, d, st = make(g, (40,), F32, F32, 32)
+    q, e, other = make(g, (40,), F32, F32, 32)
+    before = [t.clone() for t in (p, q, *st, *other)]
+    for step in ((1 << 64) + 1, [1, 1 << 63], [-(1 << 63) - 1, 1]):
+        with pytest.raises(ValueError, match="64 bits"):
+            adamw.adamw_step([p, q], [d, e], [st, other], step=step, lr=1e-3)
+    assert all(torch.equal(a, b) for a, b in zip(before, (p, q, *st, *other)))
