@@ -202,8 +202,7 @@ class AdamW(torch.optim.Optimizer):
                     continue
                 st = self.state[p]
                 if not st:
-                    st["step"] = 0
-                    st.update(zip(("exp_avg", "exp_avg_sq", "bases"), new_state(p, group["state_bits"])))
+                    st.update(zip(("exp_avg", "exp_avg_sq", "bases"), new_state(p, group["state_bits"])), step=0)
                 params, grads, states, steps, held = per_device.setdefault(p.get_device(), ([], [], [], [], []))
                 params.append(p)
                 grads.append(grad if grad.layout != torch.strided else grad.contiguous())

@@ -161,3 +161,14 @@ def test_written_tensors_get_another_version():
         AL.written(1, 2, 3)
     with pytest.raises(TypeError):
         AL.written([p], [p], [4])
+
+
+def test_a_state_that_cannot_be_made_leaves_none():
+    """A group's own options are read at the step: what is wrong with them is said every time."""
+    p = torch.nn.Parameter(torch.zeros(8))
+    p.grad = torch.zeros(8)
+    opt = AdamW([dict(params=[p], state_bits=4)])
+    for _ in range(2):
+        with pytest.raises(ValueError, match="4 bits"):
+            opt.step()
+        assert not opt.state[p]
