@@ -115,23 +115,25 @@ int64_t strip_columns(const Choice& c) {
   }
 }
 // Whether the weight's gradient [down, across], as it is kept, is made by the outer product of
-// few rows: its stores are streamed, but each 16 bytes wait for up to 4 loads and 32 to 256
-// multiply-adds, and a block walks down 32 rows, so a small gradient leaves most CUs idle. The
-// tile kernels, one launch more, leave up to about 150 MB in the caches, beyond that
-// at half the memory's rate. us of a backward pass without dx, outer product and tile:
+// few rows.  Its stores are streamed at the memory's rate, but a thread walks down 32 rows of it with
+// a multiply-add for each element and row of x (4, 8, 16 or 32 of these): time that small gradients,
+// whose blocks do not fill the CUs, cannot hide.  The tile kernels, one launch more, leave up
+// to about 150 MB in the caches, and store beyond that at half the memory's rate.  us of a backward
+// pass without dx, outer product and tile:
 //   up to 4 rows (fp32 8): 16384 x 200 in bf16 17 and 21, 65536 x 2048 101 and 159
-//   up to 8 (fp32 16), down 32 rows at most 128 lanes wide: 32000 x 256 in bf16 20 and 20, in fp32
+//   up to 8 (fp32 16), where a row has at most 128 lanes of 16 bytes: 32000 x 256 in bf16 20 and 20, in fp32
 //     25 and 30; wider, of 12 MB 25 and 23, 21 MB 32 and 31, 33 MB 29 and 29 (fp32 29 and 29),
 //     90 MB 45 and 52, 268 MB 104 and 160
-//   up to 16 (fp32 32): 16 MB 32 and 20, 66 MB 48 and 37 (fp32 55 and 49), 134 MB 80 and 63, 151 MB
-//     88 and 91 or, tied, 102 and 80, 185 MB 101 and 118 or 108 and 108 (fp32 97 and 122), 268 MB 121 and 160
+//   up to 16 (fp32 32): in bf16 of 16 MB 32 and 20, 66 MB 48 and 37, 134 MB 80 and 63, 151 MB 88 and 91 or,
+//     tied, 102 and 80, 185 MB 101 and 118 or 108 and 108, 268 MB 134 and 175; in fp32 of 33 MB 40 and 33,
+//     66 MB 47 and 48 or, tied, 55 and 49, 131 MB 78 and 82 or 82 and 83, 180 MB 97 and 122
 bool outer_product_wins(bool bf16, bool w_transposed, int64_t rows, int64_t inner, int64_t outer) {
-  constexpr int64_t kWide = int64_t(24) << 20, kMost = int64_t(160) << 20;
+  constexpr int64_t kWide = int64_t(24) << 20;
   if (!rows || rows > outer_rows(bf16)) return false;
   const int64_t es = bf16 ? 2 : 4, bytes = inner * outer * es, across = w_transposed ? inner : outer;
   if (rows <= 8 / (bf16 ? 2 : 1)) return true;
   if (rows <= 16 / (bf16 ? 2 : 1)) return bytes >= kWide || across * es <= 128 * 16;
-  return bytes >= kMost;
+  return bytes >= int64_t(bf16 ? 160 : 96) << 20;
 }
 size_t raw_bytes(const LossLayout& l) {
   return l.z.kernel == Choice::SKINNY ? size_t(l.z.splits) * size_t(l.rows) * size_t(l.piece) * 4 : 0;

@@ -103,6 +103,7 @@ def test_weight_gradients_of_few_rows_by_size(passes):
         (10, 200, 10727, True, torch.bfloat16, False), (16, 1024, 65536, True, torch.bfloat16, False),
         (16, 2048, 65536, True, torch.bfloat16, True), (9, 4096, 128000, False, torch.bfloat16, True),
         (32, 256, 32000, True, torch.float32, False), (20, 1408, 32000, False, torch.float32, True),
+        (32, 1024, 32000, True, torch.float32, True), (16, 2048, 32000, True, torch.bfloat16, False),
         (17, 4096, 128000, False, torch.bfloat16, False), (33, 4096, 128000, False, torch.float32, False)]
     words = passes([_line(dtype, t, rows, inner, vocab) for rows, inner, vocab, t, dtype, _ in cases])
     for line, case in zip(words, cases):
