@@ -157,8 +157,8 @@ def state_values(state: State) -> Tuple[torch.Tensor, torch.Tensor]:
 
 
 class AdamW(torch.optim.Optimizer):
-    """torch.optim-style AdamW over fp32 or bf16 parameters of any shape, for those
-    that ``Muon`` does not step.  Per-parameter state: ``step``, ``exp_avg``,
+    """torch.optim-style AdamW over fp32 or bf16 parameters of any shape (contiguous
+    ones), for those that ``Muon`` does not step.  Per-parameter state: ``step``, ``exp_avg``,
     ``exp_avg_sq`` and, with ``state_bits=8``, ``bases``.  A parameter without a
     gradient is left as it is."""
 

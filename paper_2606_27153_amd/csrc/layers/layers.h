@@ -136,7 +136,7 @@ struct LossArgs {
   const void* targets;
   const float* dloss;     // a number for every row (each), or one
   const float* alpha;     // factor of all gradients, or NULL (1)
-  float2* part;           // strips x rows: the largest logit and the sum of the others relative to it
+  float2* part;           // strips x rows: the largest logit and the sum of exponentials relative to it
   float* logit;           // the target's
   float* loss;            // of every row
   float* lse;
@@ -184,8 +184,7 @@ hipError_t launch_loss_sum(bool bf16, const LossArgs& a, const float* part, int 
 hipError_t launch_simple(bool bf16, int form, int group, const Product& p, const Table* t, hipStream_t st);
 
 // Matrix-core kernels on tiles of 256 x 256 and 128 x 256 (bf16 only), 128 x 128
-// and 64 x 64;
-// the operands must suit them (tile_fits in layers_api.cpp).
+// and 64 x 64; the operands must suit them (tile_fits in host.h).
 hipError_t launch_tile256_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st);
 hipError_t launch_tile128x256_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st);
 hipError_t launch_tile128_bf16(int form, int group, const Product& p, const Table* t, hipStream_t st);
