@@ -61,7 +61,7 @@ __device__ __forceinline__ bool row_chunk(const RouteArgs& a, int64_t rows, int6
 // last expert's are cleared by the threads of the tokens that their numbers fall to.
 // 16384 x 2048 tokens of 6 choices in bf16 take 74 to 77 us, 6.2 TB/s, most of it stores
 // (by row, each reading its token from the cache, 122).
-// Choices whose places are looked up together: most routers' in one round.  6, or kernels of their
+// Choices whose places are looked up together: all of most routers at once.  6, or kernels of their
 // own for 2, 4, 6 and 8, take as long (1 to 16 choices; those kernels 23 us for 21 of one choice).
 constexpr int kStores = 8;
 template <typename E, bool WHOLE>
